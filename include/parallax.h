@@ -220,6 +220,44 @@ plx_status parallax_decode_combine(const plx_decode_args *args, void *hip_stream
 plx_status parallax_decode_fused(const plx_decode_args *args, void *hip_stream);
 
 /*
+ * Decode with a sliding window and a few first tokens that stay visible (sinks): a row at position pos sees key j iff
+ * j <= pos and (j > pos - window or j < sinks). Everything else as parallax_decode: one row or the last Tq positions,
+ * contiguous or paged cache (pages between the sinks and the window may have been freed: their table entries
+ * are clamped and what is read there reaches no output), bf16 and fp32, workspace rules and split counts.
+ *   sinks   0 .. any; > 0 needs window > 0 (PLX_ERR_SHAPE). prep must be all zero (PLX_ERR_SHAPE).
+ * Results depend on what a row sees only: rows behind seq_lens, freed pages and keys outside a row's set may hold
+ * anything, infinities and NaN included. parallax_decode_sinks_call_splits: as parallax_decode_call_splits.
+ */
+int32_t parallax_decode_sinks_call_splits(const plx_decode_args *args, int32_t sinks);
+plx_status parallax_decode_sinks(const plx_decode_args *args, int32_t sinks, void *hip_stream);
+
+/*
+ * Verification of drafted tokens that form a tree: the Tq rows of a sequence are nodes, whose keys and values are the last
+ * n_b = min(draft_lens[b], Tq, L_b) of its L_b cached tokens (node m at position L_b - n_b + m of the cache). Node t
+ * sees every committed key (the L_b - n_b before them) and the drafted key m iff bit m % 64 of word m / 64 of its mask is
+ * set: its ancestors and itself, in whatever order the nodes lie (bits from n_b on are ignored). Rows t >= n_b,
+ * and rows that see nothing, return zeros. The rest is parallax_decode over Tq rows: q, r, o [B, Hq, Tq, d], the cache
+ * contiguous or paged and read once for up to 32 (head of a group, node) pairs, bf16 and fp32, workspace and
+ * split counts. A key that a node does not see does not reach it, whatever its row holds.
+ *   tree_mask   [mask_batch][Tq][ceil(Tq / 64)] on the device, 8-byte aligned; mask_batch 1 (one tree for all) or B
+ *   draft_lens  [B] int32 on the device, or NULL = Tq
+ *   window, sinks  (decode.window, sinks; 0 = none) apply to the committed keys: node t sits at position L_b - n_b +
+ *               (number of its set bits) - 1 and sees those behind that position - window, and the first `sinks`
+ * Tq <= PLX_MAX_TREE_NODES; decode.prep all zero (PLX_ERR_SHAPE).
+ */
+#define PLX_MAX_TREE_NODES 256
+typedef struct {
+    plx_decode_args decode;
+    const uint64_t *tree_mask;
+    const int32_t *draft_lens;
+    int32_t mask_batch;
+    int32_t sinks;
+} plx_decode_tree_args;
+
+int32_t parallax_decode_tree_call_splits(const plx_decode_tree_args *args);
+plx_status parallax_decode_tree(const plx_decode_tree_args *args, void *hip_stream);
+
+/*
  * Prefill forward over T query rows and Tkv keys per sequence (Algorithm 1, Sec. 3.3; forward
  * equation Sec. 3.1). Tkv = 0 means Tkv = T (the paper's square case).
  * causal != 0: the query rows are the LAST T positions of the Tkv-long sequence (a prefill

@@ -1,0 +1,83 @@
+"""Which cached keys the rows of a decode call see -- CPU ORACLE in numpy (test infrastructure, not product): plain
+loops over the definitions, for oracle/masked.py to sum over.
+
+`chain`: the rows are the last Tq positions of a sequence of L cached tokens; a row at position pos sees the keys
+j <= pos with j > pos - window or j < sinks (window 0: all).
+`tree`: the last n = min(drafted, Tq, L) cached tokens are drafted nodes behind base = L - n committed ones; node t < n
+sees the committed keys (window > 0: j > base + (number of its bits) - 1 - window, or j < sinks) and the drafted key
+base + m iff bits[t][m]; node t >= n nothing.
+"""
+from __future__ import annotations
+
+import numpy as np
+
+
+def chain(L, Tq, cap, window=0, sinks=0):
+    see = np.zeros((Tq, cap), dtype=bool)
+    for t in range(Tq):
+        pos = L - Tq + t
+        for j in range(max(pos + 1, 0)):
+            see[t, j] = window == 0 or j > pos - window or j < sinks
+    return see
+
+
+def tree(L, Tq, cap, bits, drafted=None, window=0, sinks=0):
+    n = min(Tq if drafted is None else max(drafted, 0), Tq, L)
+    base = L - n
+    see = np.zeros((Tq, cap), dtype=bool)
+    for t in range(n):
+        pos = base + max(int(sum(bits[t][:n])) - 1, 0)
+        for j in range(base):
+            see[t, j] = window == 0 or j > pos - window or j < sinks
+        for m in range(n):
+            see[t, base + m] = bits[t][m]
+    return see
+
+
+def words(bits):
+    """bits [.., Tq, Tq] -> int64 words [.., Tq, ceil(Tq / 64)]"""
+    bits = np.asarray(bits, dtype=bool)
+    Tq = bits.shape[-1]
+    out = np.zeros(bits.shape[:-1] + (-(-Tq // 64),), dtype=np.uint64)
+    for m in range(Tq):
+        out[..., m // 64] |= bits[..., m].astype(np.uint64) << np.uint64(m % 64)
+    return out.view(np.int64)
+
+
+def random_tree(Tq, rng, reach=6):
+    """Ancestor bits [Tq, Tq] of a random tree (several roots, parents up to `reach` nodes back)."""
+    bits = np.zeros((Tq, Tq), dtype=bool)
+    for t in range(Tq):
+        parent = int(rng.integers(max(-1, t - reach - 1), t)) if t else -1
+        if parent >= 0:
+            bits[t] = bits[parent]
+        bits[t, t] = True
+    return bits
+
+
+def bf16_bound(q, r, k, v, scale, mask):
+    """Element-wise bound on a bf16 kernel's error that rounds P1 = p, P2 = p u and the output to bf16 (half a step is 2^-8 of
+    a value) and keeps everything else in fp32: O1 and d1 hold the same rounded P1, O2 and d2 the same rounded P2, so
+    with o = O1 / d1 (1 + d2 / d1) - O2 / d1
+        |err| <= 2^-8 (|o| + 2 |1 + ubar| sum p |v| + sum p |u| |v| + 3 (sum p |u|) sum p |v|) + second order
+    (each quotient by d1 moves by at most 2^-8 of itself); 1.02 covers the second order and the fp32 sums."""
+    q, r, k, v = (np.asarray(x, dtype=np.float64) for x in (q, r, k, v))
+    B, Hq, Tq, d = q.shape
+    G = Hq // k.shape[1]
+    mask = np.broadcast_to(np.asarray(mask, dtype=bool), (B, Hq, Tq, k.shape[2]))
+    bound = np.zeros_like(q)
+    for b in range(B):
+        for h in range(Hq):
+            K, V, M = k[b, h // G], v[b, h // G], mask[b, h]
+            V = np.where(M.any(axis=0)[:, None], V, 0.0)
+            K = np.where(M.any(axis=0)[:, None], K, 0.0)
+            A = np.where(M, scale * (q[b, h] @ K.T), -np.inf)
+            amax = A.max(axis=1, keepdims=True)
+            W = np.where(M, np.exp(A - np.where(np.isfinite(amax), amax, 0.0)), 0.0)
+            P = W / np.maximum(W.sum(axis=1, keepdims=True), 1e-300)
+            U = r[b, h] @ K.T
+            ubar, ua = (P * U).sum(axis=1, keepdims=True), (P * np.abs(U)).sum(axis=1, keepdims=True)
+            o = (P * (1 + ubar - U)) @ V
+            pv = P @ np.abs(V)
+            bound[b, h] = 1.02 * 2.0 ** -8 * (np.abs(o) + 2 * np.abs(1 + ubar) * pv + (P * np.abs(U)) @ np.abs(V) + 3 * ua * pv)
+    return bound

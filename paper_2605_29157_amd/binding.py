@@ -26,6 +26,7 @@ EXPORTED_SYMBOLS = (
     "parallax_decode_workspace_bytes", "parallax_decode_num_splits", "parallax_decode_call_splits", "parallax_decode",
     "parallax_decode_partials", "parallax_decode_combine", "parallax_decode_fused",
     "parallax_decode_static", "parallax_decode_static_scratch_bytes",
+    "parallax_decode_sinks", "parallax_decode_sinks_call_splits", "parallax_decode_tree", "parallax_decode_tree_call_splits",
     "parallax_decode_mla", "parallax_decode_mla_workspace_bytes", "parallax_decode_mla_num_splits",
     "parallax_prefill", "parallax_prefill_split", "parallax_prefill_workspace_bytes", "parallax_prefill_form", "parallax_prefill_backward", "parallax_prefill_backward_form",
     "parallax_prefill_backward_workspace_bytes",
@@ -63,6 +64,11 @@ class plx_decode_args(ctypes.Structure):
         ("split_counters", ctypes.c_void_p),
         ("prep", plx_qr_prep),
     ]
+
+
+class plx_decode_tree_args(ctypes.Structure):
+    _fields_ = [("decode", plx_decode_args), ("tree_mask", ctypes.c_void_p), ("draft_lens", ctypes.c_void_p),
+                ("mask_batch", ctypes.c_int32), ("sinks", ctypes.c_int32)]
 
 
 class plx_prefill_args(ctypes.Structure):
@@ -208,6 +214,14 @@ def load_library() -> ctypes.CDLL:
                      "parallax_decode_static"):
             getattr(lib, name).argtypes = [ctypes.POINTER(plx_decode_args), ctypes.c_void_p]
             getattr(lib, name).restype = ctypes.c_int
+        lib.parallax_decode_sinks.argtypes = [ctypes.POINTER(plx_decode_args), ctypes.c_int32, ctypes.c_void_p]
+        lib.parallax_decode_sinks.restype = ctypes.c_int
+        lib.parallax_decode_sinks_call_splits.argtypes = [ctypes.POINTER(plx_decode_args), ctypes.c_int32]
+        lib.parallax_decode_sinks_call_splits.restype = ctypes.c_int32
+        lib.parallax_decode_tree.argtypes = [ctypes.POINTER(plx_decode_tree_args), ctypes.c_void_p]
+        lib.parallax_decode_tree.restype = ctypes.c_int
+        lib.parallax_decode_tree_call_splits.argtypes = [ctypes.POINTER(plx_decode_tree_args)]
+        lib.parallax_decode_tree_call_splits.restype = ctypes.c_int32
         lib.parallax_prefill.argtypes = [ctypes.POINTER(plx_prefill_args), ctypes.c_void_p]
         lib.parallax_prefill.restype = ctypes.c_int
         lib.parallax_prefill_workspace_bytes.argtypes = [ctypes.POINTER(plx_prefill_args)]
@@ -393,11 +407,17 @@ def decode_args(q, r, k, v, out, scale, seq_lens=None, use_r=True, num_splits=0,
 
 def parallax_decode(q, r, k, v, scale, seq_lens=None, use_r=True, num_splits=0, workspace=None,
                     out=None, stream=None, block_table=None, max_len=None, split_counters=None,
-                    window=0, prep=None):
+                    window=0, prep=None, sinks=0):
     """Single-step Parallax decode. Allocates `out` / `workspace` with torch when not given
     (allocation only; all arithmetic is in the library). With `split_counters` (zeroed int32
     device tensor, >= B * Hkv entries) the call goes to parallax_decode_fused: one launch, the
-    last split of every group to arrive merges inside the kernel."""
+    last split of every group to arrive merges inside the kernel. With `sinks` > 0 the first tokens stay visible
+    behind the sliding window (parallax_decode_sinks; no split_counters, no prep)."""
+    if sinks:
+        if split_counters is not None or prep is not None:
+            raise ValueError("sinks go with neither split_counters nor prep")
+        return _decode_rows(q, r, k, v, scale, seq_lens, use_r, num_splits, workspace, out, stream, block_table,
+                            max_len, window, _i32(sinks))
     if not (q.is_cuda and k.is_cuda and v.is_cuda and (r is None or r.is_cuda)):
         raise ValueError("parallax_decode needs device tensors")
     if q.stride(-1) != 1 or k.stride(-1) != 1 or v.stride(-1) != 1 or not q.is_contiguous() or (
@@ -436,6 +456,100 @@ def parallax_decode(q, r, k, v, scale, seq_lens=None, use_r=True, num_splits=0, 
     if st != PLX_OK:
         raise ParallaxError(st, entry)
     return out
+
+
+def _decode_rows(q, r, k, v, scale, seq_lens, use_r, num_splits, workspace, out, stream, block_table, max_len, window,
+                 sinks, tree_mask=None, draft_lens=None):
+    """parallax_decode_sinks, or parallax_decode_tree with a tree_mask."""
+    where = "parallax_decode_sinks" if tree_mask is None else "parallax_decode_tree"
+    for t in (q, r, k, v, out, seq_lens, block_table, tree_mask, draft_lens, workspace):
+        if t is not None and (not t.is_cuda or t.device != q.device):
+            raise ValueError("%s needs device tensors of one device" % where)
+    if q.dim() not in (3, 4) or k.dim() != 4 or v.shape != k.shape or k.shape[3] != q.shape[-1]:
+        raise ValueError("q [B, Hq, (Tq,) d], k and v of one shape [.., Hkv, .., d]")
+    if use_r and r is None:
+        raise ValueError("r is needed unless use_r=False")
+    for t in (r, out):
+        if t is not None and t.shape != q.shape:
+            raise ValueError("r and out have the shape of q")
+    for t in (r, k, v, out):
+        if t is not None and t.dtype != q.dtype:
+            raise TypeError("q, r, k, v and out have one dtype")
+    if k.stride(-1) != 1 or v.stride(-1) != 1 or not all(t is None or t.is_contiguous() for t in (q, r, out)):
+        raise ValueError("q, r, out must be contiguous and k, v contiguous in the last dimension")
+    B, Hq, d = q.shape[0], q.shape[1], q.shape[-1]
+    Tq = q.shape[2] if q.dim() == 4 else 1
+    for name, t in (("seq_lens", seq_lens), ("draft_lens", draft_lens)):
+        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (B,) or not t.is_contiguous()):
+            raise TypeError("%s must be a contiguous int32 tensor [B]" % name)
+    if block_table is not None:
+        if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.stride(1) != 1:
+            raise TypeError("block_table must be an int32 device tensor [B, pages per sequence]")
+        if block_table.shape[0] != B:
+            raise ValueError("block_table needs one row per sequence")
+    elif k.shape[0] != B:
+        raise ValueError("k and v need one cache per sequence")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    if out is None:
+        out = _result_maker(stream, torch.empty_like)(q)
+    a = decode_args(q, r, k, v, out, scale, seq_lens, use_r, num_splits, workspace, block_table, max_len, window)
+    lib = load_library()
+    if tree_mask is None:
+        splits, call, head = lib.parallax_decode_sinks_call_splits, lib.parallax_decode_sinks, (ctypes.byref(a), sinks)
+    else:
+        words = -(-Tq // 64)
+        if tree_mask.dtype != torch.int64 or not tree_mask.is_contiguous():
+            raise TypeError("tree_mask must be a contiguous int64 tensor of 64-bit words")
+        shape = tuple(tree_mask.shape)
+        if words == 1 and shape in ((Tq,), (1, Tq), (B, Tq)):
+            shape += (1,)
+        if len(shape) == 2:
+            shape = (1,) + shape
+        if shape not in ((1, Tq, words), (B, Tq, words)):
+            raise ValueError("tree_mask must be [(1 or B,) Tq, ceil(Tq/64)]")
+        tree = plx_decode_tree_args()
+        tree.decode, tree.tree_mask, tree.mask_batch = a, tree_mask.data_ptr(), shape[0]
+        tree.draft_lens, tree.sinks = _ptr(draft_lens), sinks
+        a = tree.decode  # (the copy inside)
+        splits, call, head = lib.parallax_decode_tree_call_splits, lib.parallax_decode_tree, (ctypes.byref(tree),)
+    if workspace is None and num_splits != 1:
+        S = splits(*head)  # (0: refused below)
+        if S > 1:
+            workspace = _scratch(stream, B * Hq * Tq * S * (2 * d + 4), q.device)
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), _bytes(workspace)
+    st = call(*head, _stream_ptr(stream))
+    if st != PLX_OK:
+        raise ParallaxError(st, where)
+    return out
+
+
+def parallax_decode_tree(q, r, k, v, scale, tree_mask, seq_lens=None, draft_lens=None, use_r=True, num_splits=0,
+                         workspace=None, out=None, stream=None, block_table=None, max_len=None, window=0, sinks=0):
+    """Attention of drafted tokens that form a tree. q, r [B, Hq, Tq, d]: the nodes, whose keys and values are the last
+    draft_lens[b] (default Tq) of the seq_lens[b] cached tokens. tree_mask int64 [Tq], [Tq, W], [1 or B, Tq] or
+    [1 or B, Tq, W], W = ceil(Tq / 64) (tree_mask_words makes one): bit m of node t's words: it sees drafted key m. Every node sees
+    the committed keys (with window: its window's and the first `sinks`). Rows from draft_lens[b] on return zeros."""
+    if q.dim() != 4:
+        raise ValueError("q [B, Hq, Tq, d]")
+    return _decode_rows(q, r, k, v, scale, seq_lens, use_r, num_splits, workspace, out, stream, block_table, max_len,
+                        window, _i32(sinks), tree_mask, draft_lens)
+
+
+def tree_mask_words(parents):
+    """Parents [.., Tq] (integers; the parent of node t lies before it, negative: a root) -> the mask words [.., Tq,
+    ceil(Tq / 64)] (int64) of parallax_decode_tree: every node sees its ancestors and itself. Index bookkeeping only."""
+    Tq = parents.shape[-1]
+    sees = torch.eye(Tq, dtype=torch.bool, device=parents.device).expand(*parents.shape, Tq).clone()
+    for t in range(1, Tq):
+        up = parents[..., t].long()
+        if bool((up >= t).any()):
+            raise ValueError("the parent of a node lies before it")
+        row = sees.gather(-2, up.clamp(min=0)[..., None, None].expand(*up.shape, 1, Tq))[..., 0, :]
+        sees[..., t, :] |= row & (up >= 0)[..., None]
+    words = -(-Tq // 64)
+    sees = torch.nn.functional.pad(sees, (0, 64 * words - Tq)).reshape(*parents.shape, words, 64)
+    return (sees.long() << torch.arange(64, device=parents.device)).sum(-1)
 
 
 def parallax_decode_static_scratch_bytes() -> int:

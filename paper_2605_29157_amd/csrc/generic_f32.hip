@@ -56,6 +56,12 @@ struct F32Forward {
     int32_t page_size, table_stride, num_pages;
     float *ws;                // S > 1: split records [b][hq][t][s] of (2 d + 4) floats
     float *vbar, *row_stats;  // row cache of the backward pass, or NULL
+    // VIS: first tokens that stay visible behind a window, and drafted nodes (see DecodeRowsParams)
+    int32_t sinks;
+    const uint64_t *mask;
+    int64_t mask_stride_b;
+    int32_t mask_words;
+    const int32_t *draft_lens;
 };
 
 // 16 rows (columns of the matrix tiles) in LDS: [16][DP + 4] floats, the padding makes 16 rows at one
@@ -203,8 +209,9 @@ union F32ForwardLds {
     f32x4 merge[2 * 2 * (DP / 16) * 64];  // the accumulators of two waves
 };
 
-// FULL: d == DP, nothing to pad
-template <int DP, bool PAGED, bool USE_R, bool FULL>
+// FULL: d == DP, nothing to pad. VIS: rows whose key sets are not one range (sinks, drafted nodes): the blocks
+// walked are those of the sinks, then those from the first key any window reaches.
+template <int DP, bool PAGED, bool USE_R, bool FULL, bool VIS = false>
 __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_forward_kernel(F32Forward p) {
     __shared__ F32ForwardLds<DP> lds;
     __shared__ float sm[3][kF32Waves][16];
@@ -224,16 +231,42 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_forward_ke
 
     // columns of this workgroup: key range [lo, end) of each, their union and intersection
     const int len = p.seq_lens ? min(max(p.seq_lens[b], 0), p.Lk) : p.Lk;
+    const bool tree = VIS && p.mask != nullptr;
+    // drafted nodes: the last n of the cached tokens, behind `base` committed ones
+    const int n = !tree ? 0 : min(p.draft_lens ? min(max(p.draft_lens[b], 0), p.Tq) : p.Tq, len), base = len - n;
     auto row_end = [&](int t) { return max(p.tail ? len - (p.Tq - 1 - t) : len, 0); };
     auto row_lo = [&](int t) { return p.window > 0 ? max(row_end(t) - p.window, 0) : 0; };
     const int x_last = min(16 * blk + 15, p.n_cols - 1);
     const int t0 = 16 * blk / p.gcols, t1 = x_last / p.gcols;
     const int x = min(16 * blk + c, x_last);
     const int t = x / p.gcols, head = hgrp * p.gcols + x % p.gcols;
-    const int my_end = row_end(t), my_lo = row_lo(t);
-    const int all_lo = row_lo(t1), all_end = row_end(t0);  // every column sees [all_lo, all_end)
+    int my_end = row_end(t), my_lo = row_lo(t);
+    int all_lo = row_lo(t1), all_end = row_end(t0);  // every column sees [all_lo, all_end)
     int lo = row_lo(t0) / 16, hi = (row_end(t1) + 15) / 16;  // 16-key blocks of the union
-    const int last_key = row_end(t1) - 1;
+    int last_key = row_end(t1) - 1;
+    const uint64_t *words = nullptr;
+    int sinks = 0, n_sink_blocks = 0, skip = 0;  // VIS: block i of the walk is key block i, or i + skip behind the sinks'
+    if constexpr (VIS) {
+        if (tree) {
+            words = p.mask + (int64_t)b * p.mask_stride_b + (int64_t)t * p.mask_words;
+            my_end = t < n ? len : 0, my_lo = 0;
+            all_lo = 0, all_end = base, lo = 0;
+            hi = t0 < n ? (len + 15) / 16 : 0, last_key = len - 1;
+            if (p.window > 0) {
+                int ancestors = 0;  // set bits among the n drafted nodes: the node's depth, itself included
+                for (int i = 0; i < p.mask_words && 64 * i < n; ++i)
+                    ancestors += __popcll(words[i] & (n - 64 * i >= 64 ? ~0ull : (1ull << (n - 64 * i)) - 1));
+                my_lo = min(max(base + max(ancestors - 1, 0) - p.window + 1, 0), base);
+                all_lo = min(max(base + n - p.window, 0), base);
+                lo = min(max(base + 1 - p.window, 0), base) / 16;
+            }
+        }
+        sinks = p.window > 0 ? p.sinks : 0;
+        n_sink_blocks = min((sinks + 15) / 16, hi);
+        skip = max(lo - n_sink_blocks, 0);
+        lo = 0, hi = max(hi - skip, 0);
+    }
+    auto block_of = [&](int i) { return VIS ? (i < n_sink_blocks ? i : i + skip) : i; };
     if (p.S > 1) {
         const int per = (hi - lo + p.S - 1) / p.S;
         lo += split * per;
@@ -293,18 +326,21 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_forward_ke
     for (int n = 0; n < NA; ++n) o1[n] = o2[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     int kblk = lo + w;
-    if (kblk < hi) load_k(kblk), load_v(kblk);
+    if (kblk < hi) load_k(block_of(kblk)), load_v(block_of(kblk));
     __syncthreads();
     for (; kblk < hi; kblk += kF32Waves) {
-        const int key0 = 16 * kblk, next = kblk + kF32Waves;
+        const int key0 = 16 * block_of(kblk), next = kblk + kF32Waves;
         f32x4 s1 = f32_scores<DP>(kf, lds.rows[0], d, c, g);
         f32x4 s2 = {0.f, 0.f, 0.f, 0.f};
         if constexpr (USE_R) s2 = f32_scores<DP>(kf, lds.rows[1], d, c, g);
         // the next block's K rows travel under the exponentials and the V product, its V rows (below)
         // under its scores: each register set is refilled as soon as it has been used
-        if (next < hi) load_k(next);
+        if (next < hi) load_k(block_of(next));
 
-        const bool whole = key0 >= all_lo && key0 + 16 <= all_end;  // uniform
+        const bool whole = (key0 >= all_lo || (VIS && key0 + 16 <= sinks)) && key0 + 16 <= all_end;  // uniform
+        uint32_t bits = 0xffffffffu;  // (of the block's keys, from key0 on)
+        if constexpr (VIS)
+            if (tree && key0 + 16 > base) bits = tree_bits(words, p.mask_words, key0 - base);
         unsigned seen = 15u;
         float tmax = kNegInf;
 #pragma unroll
@@ -312,7 +348,7 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_forward_ke
             s1[r] *= scale_log2;
             if (!whole) {
                 const int key = key0 + 4 * g + r;
-                const bool ok = key >= my_lo && key < my_end;
+                const bool ok = (key >= my_lo || (VIS && key < sinks)) && key < my_end && (!VIS || ((bits >> (4 * g + r)) & 1u));
                 if (!ok) s1[r] = kNegInf, s2[r] = 0.f, seen &= ~(1u << r);
             }
             tmax = fmaxf(tmax, s1[r]);
@@ -344,7 +380,7 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_forward_ke
         }
         f32_outputs<DP>(vf, p1, d, o1);
         if constexpr (USE_R) f32_outputs<DP>(vf, p2, d, o2);
-        if (next < hi) load_v(next);
+        if (next < hi) load_v(block_of(next));
     }
 
     // ---- the four waves' states on one reference, summed into wave 0 ------------------------
@@ -365,10 +401,18 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_forward_ke
     for (int n = 0; n < NA; ++n) o1[n] *= wt, o2[n] *= wt;
     f32_sum_waves<NA>(o1, o2, lds.merge, w, lane, hi - lo);
     if (w != 0 || 16 * blk + c >= p.n_cols) return;
+    if constexpr (VIS)  // a node behind the sequence's drafted ones sees nothing, also where the others see everything
+        if (my_end == 0) {
+            m_all = kNegInf, d1 = d2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < NA; ++i) o1[i] = o2[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
 
     // lane (c, g): dimensions 64 m + 16 g + 4 rr .. + 3 of column c, float4 by float4
-    const float inv = d1 > 0.f ? 1.f / d1 : 0.f;
+    const bool any = VIS ? d1 != 0.f : d1 > 0.f;  // (VIS: NaN where the column sees one, not the zeros of an empty key set)
+    const float inv = any ? 1.f / d1 : 0.f;
     if (p.S > 1) {
+        if (VIS && d1 != d1) m_all = 3.0e38f, d1 = -kNegInf;  // the merge takes this record alone
         float *rec = p.ws + ((((int64_t)b * p.Hq + head) * p.Tq + t) * p.S + split) * (2 * d + 4);
         if (g == 0) *(f32x4 *)rec = f32x4{m_all, d1, d2, 0.f};
 #pragma unroll
@@ -390,7 +434,7 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_forward_ke
             const int dim = 64 * m + 16 * g + 4 * rr;
             if (dim >= d) continue;
             f32x4 out = {0.f, 0.f, 0.f, 0.f}, mean = out;  // empty key set: zeros
-            if (d1 > 0.f)
+            if (any)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     mean[i] = o1[4 * m + i][rr] * inv;
@@ -467,27 +511,28 @@ __global__ __launch_bounds__(256) void f32_combine_kernel(F32Forward p) {
 static hipError_t launch_forward(F32Forward &g, hipStream_t stream) {
     g.n_blocks = (g.n_cols + 15) / 16;
     const dim3 grid = f32_grid((int64_t)g.n_blocks * g.B * g.heads * g.S), block(kF32Threads);
-    auto pick = [&](auto paged, auto use_r) {
-        constexpr bool P = decltype(paged)::value, R = decltype(use_r)::value;
+    auto pick = [&](auto paged, auto use_r, auto vis) {
+        constexpr bool P = decltype(paged)::value, R = decltype(use_r)::value, V = decltype(vis)::value;
         if (g.d == 64)
-            hipLaunchKernelGGL((f32_forward_kernel<64, P, R, true>), grid, block, 0, stream, g);
+            hipLaunchKernelGGL((f32_forward_kernel<64, P, R, true, V>), grid, block, 0, stream, g);
         else if (g.d < 64)
-            hipLaunchKernelGGL((f32_forward_kernel<64, P, R, false>), grid, block, 0, stream, g);
+            hipLaunchKernelGGL((f32_forward_kernel<64, P, R, false, V>), grid, block, 0, stream, g);
         else if (g.d == 128)
-            hipLaunchKernelGGL((f32_forward_kernel<128, P, R, true>), grid, block, 0, stream, g);
+            hipLaunchKernelGGL((f32_forward_kernel<128, P, R, true, V>), grid, block, 0, stream, g);
         else if (g.d < 128)
-            hipLaunchKernelGGL((f32_forward_kernel<128, P, R, false>), grid, block, 0, stream, g);
+            hipLaunchKernelGGL((f32_forward_kernel<128, P, R, false, V>), grid, block, 0, stream, g);
         else if (g.d == 256)
-            hipLaunchKernelGGL((f32_forward_kernel<256, P, R, true>), grid, block, 0, stream, g);
+            hipLaunchKernelGGL((f32_forward_kernel<256, P, R, true, V>), grid, block, 0, stream, g);
         else
-            hipLaunchKernelGGL((f32_forward_kernel<256, P, R, false>), grid, block, 0, stream, g);
+            hipLaunchKernelGGL((f32_forward_kernel<256, P, R, false, V>), grid, block, 0, stream, g);
     };
     const std::true_type yes;
     const std::false_type no;
+    const bool vis = g.mask != nullptr || g.sinks > 0;
     if (g.block_table)
-        g.use_r ? pick(yes, yes) : pick(yes, no);
+        g.use_r ? (vis ? pick(yes, yes, yes) : pick(yes, yes, no)) : (vis ? pick(yes, no, yes) : pick(yes, no, no));
     else
-        g.use_r ? pick(no, yes) : pick(no, no);
+        g.use_r ? (vis ? pick(no, yes, yes) : pick(no, yes, no)) : (vis ? pick(no, no, yes) : pick(no, no, no));
     if (hipError_t err = hipGetLastError()) return err;
     if (g.S > 1) {
         hipLaunchKernelGGL(f32_combine_kernel, f32_grid((int64_t)g.B * g.Hq * g.Tq), dim3(256), 0, stream, g);
@@ -496,7 +541,7 @@ static hipError_t launch_forward(F32Forward &g, hipStream_t stream) {
     return hipSuccess;
 }
 
-hipError_t launch_decode_f32(const DecodeParams &p, hipStream_t stream) {
+static F32Forward decode_forward(const DecodeParams &p) {
     F32Forward g{};
     g.q = (const float *)p.q, g.r = (const float *)p.r, g.k = (const float *)p.k, g.v = (const float *)p.v;
     g.o = (float *)p.o;
@@ -512,6 +557,18 @@ hipError_t launch_decode_f32(const DecodeParams &p, hipStream_t stream) {
     g.block_table = p.block_table;
     g.page_size = p.page_size, g.table_stride = p.table_stride, g.num_pages = p.num_pages;
     g.S = p.S, g.ws = p.ws;
+    return g;
+}
+
+hipError_t launch_decode_f32(const DecodeParams &p, hipStream_t stream) {
+    F32Forward g = decode_forward(p);
+    return launch_forward(g, stream);
+}
+
+hipError_t launch_decode_rows_f32(const DecodeRowsParams &p, hipStream_t stream) {
+    F32Forward g = decode_forward(p.d);
+    g.sinks = p.sinks;
+    g.mask = p.mask, g.mask_stride_b = p.mask_stride_b, g.mask_words = p.mask_words, g.draft_lens = p.draft_lens;
     return launch_forward(g, stream);
 }
 

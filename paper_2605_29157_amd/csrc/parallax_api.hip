@@ -275,12 +275,12 @@ int32_t pick_splits_f32(const plx_decode_args *a, int32_t Tq) {
 }
 
 // ... and no more than the caller's workspace has room for.
-int32_t splits_with_room_f32(const plx_decode_args *a, int32_t Tq) {
+int32_t room_f32(const plx_decode_args *a, int32_t Tq) {
     const int64_t room =
         a->workspace && aligned16(a->workspace) ? (int64_t)(a->workspace_bytes / ws_bytes(a->B, (int64_t)a->Hq * Tq, 1, a->d)) : 0;
-    const int64_t s = pick_splits_f32(a, Tq);
-    return s > room ? (room < 1 ? 1 : (int32_t)room) : (int32_t)s;
+    return (int32_t)std::max<int64_t>(std::min<int64_t>(room, PLX_MAX_SPLITS), 1);
 }
+int32_t splits_with_room_f32(const plx_decode_args *a, int32_t Tq) { return std::min(pick_splits_f32(a, Tq), room_f32(a, Tq)); }
 
 plx_status attach_workspace(const plx_decode_args *a, int32_t S, plx::DecodeParams *p) {
     if (!a->workspace || !aligned16(a->workspace)) return PLX_ERR_WORKSPACE;
@@ -408,6 +408,91 @@ plx_status parallax_decode_combine(const plx_decode_args *a, void *hip_stream) {
     return plx::launch_decode_combine(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess
                ? PLX_OK
                : PLX_ERR_LAUNCH;
+}
+
+namespace {
+
+// Rows whose key sets differ: sinks behind a window, drafted nodes (tree != nullptr).
+plx_status prepare_decode_rows(const plx_decode_args *a, const plx_decode_tree_args *tree, int32_t sinks, bool need_out,
+                               plx::DecodeRowsParams *out) {
+    plx::DecodeRowsParams p{};
+    const plx_status st = prepare_decode(a, true, need_out, &p.d);
+    if (st != PLX_OK) return st;
+    if (p.d.prep.gamma_q != nullptr) return PLX_ERR_SHAPE;  // (rows prepared beforehand only)
+    if (sinks < 0 || (sinks > 0 && a->window == 0)) return PLX_ERR_SHAPE;
+    p.sinks = sinks;
+    if (tree) {
+        if (!tree->tree_mask) return PLX_ERR_NULL;
+        if ((reinterpret_cast<uintptr_t>(tree->tree_mask) & 7u) || (reinterpret_cast<uintptr_t>(tree->draft_lens) & 3u))
+            return PLX_ERR_ALIGN;
+        if (p.d.Tq > PLX_MAX_TREE_NODES || (tree->mask_batch != 1 && tree->mask_batch != a->B)) return PLX_ERR_SHAPE;
+        p.mask = tree->tree_mask, p.mask_words = (p.d.Tq + 63) / 64;
+        p.mask_stride_b = tree->mask_batch == 1 ? 0 : (int64_t)p.d.Tq * p.mask_words;
+        p.draft_lens = tree->draft_lens;
+    }
+    *out = p;
+    return PLX_OK;
+}
+
+// Split count of such a call: that of a plain one over as many keys, a pair of workgroup columns for every
+// group of columns
+int32_t pick_splits_rows(const plx_decode_args *a, const plx::DecodeRowsParams &p) {
+    if (a->num_splits > 0) return a->num_splits;
+    const int64_t in_window = (int64_t)a->window + p.d.Tq - 1 + p.sinks;
+    const int32_t keys = a->window > 0 && in_window < a->Lmax ? (int32_t)in_window : a->Lmax;
+    if (a->dtype == PLX_F32) {
+        plx_decode_args plain = *a;
+        plain.Lmax = keys, plain.window = 0;
+        return pick_splits_f32(&plain, p.d.Tq);
+    }
+    const int32_t cols = p.d.G * p.d.Tq, per = plx::decode_rows_columns(cols);
+    return parallax_decode_num_splits(a->B, a->Hq, a->Hkv * ((cols + per - 1) / per), keys, a->d, 0);
+}
+
+int32_t decode_rows_splits(const plx_decode_args *a, const plx_decode_tree_args *tree, int32_t sinks) {
+    plx::DecodeRowsParams p{};
+    return prepare_decode_rows(a, tree, sinks, false, &p) == PLX_OK ? pick_splits_rows(a, p) : 0;
+}
+
+plx_status decode_rows(const plx_decode_args *a, const plx_decode_tree_args *tree, int32_t sinks, void *hip_stream) {
+    plx::DecodeRowsParams p{};
+    plx_status st = prepare_decode_rows(a, tree, sinks, true, &p);
+    if (st != PLX_OK) return st;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    int32_t S = pick_splits_rows(a, p);
+    if (a->dtype == PLX_F32) {
+        p.d.S = std::min(S, room_f32(a, p.d.Tq));
+        p.d.ws = static_cast<float *>(a->workspace), p.d.r = a->r;
+        return plx::launch_decode_rows_f32(p, stream) == hipSuccess ? PLX_OK : PLX_ERR_LAUNCH;
+    }
+    p.d.S = S, p.d.direct_out = S == 1;
+    const int32_t cols = p.d.G * p.d.Tq, per = plx::decode_rows_columns(cols);
+    if ((int64_t)S * a->Hkv * a->B > (0x7fffffffLL - 8) / ((cols + per - 1) / per)) return PLX_ERR_SHAPE;  // (the grid)
+    if (S > 1) {
+        st = attach_workspace(a, S, &p.d);
+        if (st != PLX_OK) return st;
+    }
+    if (plx::launch_decode_rows_bf16(p, stream) != hipSuccess) return PLX_ERR_LAUNCH;
+    if (S > 1 && plx::launch_decode_combine(p.d, stream) != hipSuccess) return PLX_ERR_LAUNCH;
+    return PLX_OK;
+}
+
+}  // namespace
+
+int32_t parallax_decode_sinks_call_splits(const plx_decode_args *a, int32_t sinks) {
+    return decode_rows_splits(a, nullptr, sinks);
+}
+
+plx_status parallax_decode_sinks(const plx_decode_args *a, int32_t sinks, void *hip_stream) {
+    return decode_rows(a, nullptr, sinks, hip_stream);
+}
+
+int32_t parallax_decode_tree_call_splits(const plx_decode_tree_args *a) {
+    return a ? decode_rows_splits(&a->decode, a, a->sinks) : 0;
+}
+
+plx_status parallax_decode_tree(const plx_decode_tree_args *a, void *hip_stream) {
+    return a ? decode_rows(&a->decode, a, a->sinks, hip_stream) : PLX_ERR_NULL;
 }
 
 namespace {

@@ -40,6 +40,19 @@ struct DecodeParams {
     QrPrep prep;
 };
 
+// Decode of rows whose key sets differ (decode_rows_bf16.hip; fp32: generic_f32.hip): d.window with `sinks` first tokens that
+// stay visible, and / or drafted nodes (mask != nullptr): the last n_b = min(draft_lens[b], Tq, L_b) cached tokens of a
+// sequence, node t seeing the committed keys and key L_b - n_b + j iff bit j of its mask words is set.
+struct DecodeRowsParams {
+    DecodeParams d;
+    int32_t sinks;
+    const uint64_t *mask;  // [batch][Tq][mask_words]
+    int64_t mask_stride_b;  // words per sequence, 0: one tree for all
+    int32_t mask_words;
+    const int32_t *draft_lens;  // [B] or nullptr: Tq
+    int32_t col_groups;  // set by the launcher
+};
+
 struct PrefillParams {
     const void *q, *r, *k, *v;
     void *o;
@@ -137,6 +150,9 @@ struct NormRopeParams {
 
 // Each returns hipSuccess or the launch error. No allocation, no synchronisation.
 hipError_t launch_decode_bf16(const DecodeParams &p, hipStream_t stream);
+hipError_t launch_decode_rows_bf16(const DecodeRowsParams &p, hipStream_t stream);  // the split kernel only
+int decode_rows_columns(int n_cols);  // columns of a workgroup of it, of n_cols = heads of a group x rows
+hipError_t launch_decode_rows_f32(const DecodeRowsParams &p, hipStream_t stream);
 hipError_t launch_decode_combine(const DecodeParams &p, hipStream_t stream);
 hipError_t launch_prefill_bf16(const PrefillParams &p, hipStream_t stream);
 // Plans a call: p.rows for a launch without a workspace and, with_ranges, p.split_tiles > 0 where key ranges are
