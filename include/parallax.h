@@ -258,6 +258,83 @@ int32_t parallax_decode_tree_call_splits(const plx_decode_tree_args *args);
 plx_status parallax_decode_tree(const plx_decode_tree_args *args, void *hip_stream);
 
 /*
+ * The pages of a paged cache, kept on the device so that the calls can be enqueued (and captured) between the steps that use
+ * them; the block table and lengths are those that the decode entry points read. All arrays are the caller's.
+ *   block_table   [sequences, block_table_stride], pages_per_sequence <= block_table_stride of them used; entry i of a
+ *                 sequence is the page of its tokens i * page_size .., -1 = none
+ *   seq_lens      [sequences] cached tokens
+ *   page_refs     [num_pages] table entries that name the page
+ *   free_pages    [num_pages]; the first *free_count (a device int32) are the pages nobody names, the next one taken is the
+ *                 last of them. To begin with: block_table all -1, seq_lens and page_refs 0, every page on the list.
+ * Lists of sequences are int32 on the device; entries outside [0, sequences) are passed over, so a list may be padded
+ * with -1. n = 0 is allowed and does nothing. The state after a call does not depend on the order its threads ran in.
+ */
+typedef struct {
+    int32_t *block_table, *seq_lens, *page_refs, *free_pages, *free_count;
+    int32_t sequences, pages_per_sequence, block_table_stride, num_pages, page_size;
+} plx_page_table;
+
+/* Pools of pages [num_pages, heads, page_size, d]: element strides {page, head, row}, last dimension contiguous, base and
+ * strides 16-byte aligned. v may be NULL (one pool: a latent cache, heads = 1, d = 576). */
+typedef struct {
+    void *k, *v;
+    int32_t num_pages, heads, page_size, d;
+    int64_t k_stride[3], v_stride[3];
+    plx_dtype dtype;
+} plx_cache_pools;
+
+#define PLX_MAX_EXTEND 1024 /* sequences per parallax_cache_extend */
+
+/* children[i] becomes a copy of parents[i]: the same pages, each named once more, and the same length. No row is copied: a
+ * last page that is shared is replaced when one of its sequences grows (parallax_cache_extend). A pair is passed
+ * over if the child is not empty (seq_lens 0), is listed earlier in children, or is listed in parents. n <= 65535. */
+plx_status parallax_cache_fork(const plx_page_table *pages, const int32_t *parents, const int32_t *children, int32_t n,
+                               void *hip_stream);
+/*
+ * Room for new_lens[i] tokens in sequence seqs[i] (not less than it has, no more than pages_per_sequence * page_size; listed
+ * twice, the first time counts): free pages, in the order of the list, for the entries behind its last page that hold
+ * none. A last page that is partly filled and that others name too when the sequence's turn comes is
+ * replaced by a fresh one: src[i], dst[i], rows[i] then say what parallax_cache_copy has to move, in every
+ * layer's pools, before the sequence is used (-1, -1, 0 otherwise). seq_lens[s] becomes new_lens[i]; the new rows hold
+ * whatever was there. missing (one int32): 0, or how many pages were lacking, and then nothing was changed.
+ * src, dst, rows: [n] on the device, written. n <= PLX_MAX_EXTEND.
+ */
+plx_status parallax_cache_extend(const plx_page_table *pages, const int32_t *seqs, const int32_t *new_lens, int32_t n,
+                                 int32_t *src, int32_t *dst, int32_t *rows, int32_t *missing, void *hip_stream);
+/*
+ * Sequence seqs[i] gives back the pages that lie in its tokens first[i] .. last[i] - 1 as a whole (first NULL: from 0, last
+ * NULL: to the end; a last[i] at or behind its length takes the partial last page along, and the length becomes
+ * first[i] if that is less). first 0, last NULL ends a sequence; first = the tokens to keep drops its end; first = the
+ * sinks, last = length - window drops what parallax_decode_sinks does not look at. Pages that nobody names any
+ * more go on top of the free list in ascending order. n <= 65535.
+ */
+plx_status parallax_cache_free(const plx_page_table *pages, const int32_t *seqs, const int32_t *first, const int32_t *last,
+                               int32_t n, void *hip_stream);
+/* Page src[i] -> page dst[i] of every pool, its first rows[i] rows (NULL: all). Pairs with a page outside the pool are passed
+ * over. No dst may be another pair's src or dst (their rows would be a mixture). */
+plx_status parallax_cache_copy(const plx_cache_pools *pools, const int32_t *src, const int32_t *dst, const int32_t *rows,
+                               int32_t n, void *hip_stream);
+/*
+ * After the verification of drafted nodes (parallax_decode_tree): the rows of the accepted ones, numbers accepted[b][0 ..
+ * n_accepted[b]) in ascending order, move together behind the committed rows: row base + accepted[b][i] to base +
+ * i, base = L_b - n_b, n_b = min(draft_lens[b], max_draft, L_b). new_lens[b] = base + n_accepted[b] (at most n_b of them).
+ * What lies behind is left as it was; parallax_cache_free gives its pages back. Numbers are clamped to [i, n_b);
+ * a list that does not ascend moves the wrong rows. pools as above; without a block table [B, heads, capacity, d] with
+ * the sequence's stride first and page_size = capacity, num_pages = B. The pages of the drafted rows must not be shared.
+ * new_lens must not be seq_lens. max_accepted <= max_draft <= PLX_MAX_TREE_NODES.
+ */
+typedef struct {
+    plx_cache_pools pools;
+    const int32_t *block_table; /* NULL = contiguous cache */
+    const int32_t *seq_lens, *draft_lens; /* draft_lens NULL = max_draft */
+    const int32_t *accepted, *n_accepted; /* [B, max_accepted], [B] */
+    int32_t *new_lens;
+    int32_t B, block_table_stride, max_draft, max_accepted;
+} plx_cache_compact_args;
+
+plx_status parallax_cache_compact(const plx_cache_compact_args *args, void *hip_stream);
+
+/*
  * Prefill forward over T query rows and Tkv keys per sequence (Algorithm 1, Sec. 3.3; forward
  * equation Sec. 3.1). Tkv = 0 means Tkv = T (the paper's square case).
  * causal != 0: the query rows are the LAST T positions of the Tkv-long sequence (a prefill

@@ -30,6 +30,7 @@ EXPORTED_SYMBOLS = (
     "parallax_decode_mla", "parallax_decode_mla_workspace_bytes", "parallax_decode_mla_num_splits",
     "parallax_prefill", "parallax_prefill_split", "parallax_prefill_workspace_bytes", "parallax_prefill_form", "parallax_prefill_backward", "parallax_prefill_backward_form",
     "parallax_prefill_backward_workspace_bytes",
+    "parallax_cache_fork", "parallax_cache_extend", "parallax_cache_free", "parallax_cache_copy", "parallax_cache_compact",
     "parallax_block_lists", "parallax_norm_rope", "parallax_rope_table", "parallax_util_copy", "parallax_util_read",
     "parallax_util_read_grid", "parallax_util_read_sink_slots", "parallax_util_mfma", "parallax_strerror", "parallax_version",
 )
@@ -140,6 +141,26 @@ class plx_block_list_args(ctypes.Structure):
                 ("tile_idx", ctypes.c_void_p), ("col_ptr", ctypes.c_void_p), ("col_idx", ctypes.c_void_p)]
 
 
+class plx_page_table(ctypes.Structure):
+    _fields_ = [("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("page_refs", ctypes.c_void_p),
+                ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p), ("sequences", ctypes.c_int32),
+                ("pages_per_sequence", ctypes.c_int32), ("block_table_stride", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32)]
+
+
+class plx_cache_pools(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("d", ctypes.c_int32), ("k_stride", ctypes.c_int64 * 3),
+                ("v_stride", ctypes.c_int64 * 3), ("dtype", ctypes.c_int)]
+
+
+class plx_cache_compact_args(ctypes.Structure):
+    _fields_ = [("pools", plx_cache_pools), ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+                ("draft_lens", ctypes.c_void_p), ("accepted", ctypes.c_void_p), ("n_accepted", ctypes.c_void_p),
+                ("new_lens", ctypes.c_void_p), ("B", ctypes.c_int32), ("block_table_stride", ctypes.c_int32),
+                ("max_draft", ctypes.c_int32), ("max_accepted", ctypes.c_int32)]
+
+
 class plx_norm_rope_tensor(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("gamma", ctypes.c_void_p),
                 ("H", ctypes.c_int32), ("rope", ctypes.c_int32)]
@@ -162,6 +183,9 @@ _PACK = {
     plx_decode_mla_args: struct.Struct("@5P3i3i2qfiPNP3i2i0P"),
     plx_norm_rope_args: struct.Struct("@" + 3 * "3P2i" + "4iP2fiPi0P"),
     plx_block_list_args: struct.Struct("@P3i5P"),
+    plx_page_table: struct.Struct("@5P5i0P"),
+    plx_cache_pools: struct.Struct("@2P4i6qi0P"),
+    plx_cache_compact_args: struct.Struct("@2P4i6qi0P6P4i0P"),
 }
 for _args, _format in _PACK.items():
     assert _format.size == ctypes.sizeof(_args), _args
@@ -239,6 +263,15 @@ def load_library() -> ctypes.CDLL:
         lib.parallax_prefill_backward_workspace_bytes.restype = ctypes.c_size_t
         lib.parallax_block_lists.argtypes = [ctypes.POINTER(plx_block_list_args), ctypes.c_void_p]
         lib.parallax_block_lists.restype = ctypes.c_int
+        _list = ctypes.c_void_p
+        lib.parallax_cache_fork.argtypes = [ctypes.POINTER(plx_page_table), _list, _list, ctypes.c_int32, ctypes.c_void_p]
+        lib.parallax_cache_extend.argtypes = [ctypes.POINTER(plx_page_table), _list, _list, ctypes.c_int32, _list, _list, _list,
+                                              _list, ctypes.c_void_p]
+        lib.parallax_cache_free.argtypes = [ctypes.POINTER(plx_page_table), _list, _list, _list, ctypes.c_int32, ctypes.c_void_p]
+        lib.parallax_cache_copy.argtypes = [ctypes.POINTER(plx_cache_pools), _list, _list, _list, ctypes.c_int32, ctypes.c_void_p]
+        lib.parallax_cache_compact.argtypes = [ctypes.POINTER(plx_cache_compact_args), ctypes.c_void_p]
+        for name in ("fork", "extend", "free", "copy", "compact"):
+            getattr(lib, "parallax_cache_" + name).restype = ctypes.c_int
         lib.parallax_norm_rope.argtypes = [ctypes.POINTER(plx_norm_rope_args), ctypes.c_void_p]
         lib.parallax_norm_rope.restype = ctypes.c_int
         lib.parallax_rope_table.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_float,
@@ -876,6 +909,156 @@ def parallax_decode_mla(q, r, ckv, scale, seq_lens=None, num_splits=0, out=None,
     if st != PLX_OK:
         raise ParallaxError(st, "parallax_decode_mla")
     return out
+
+
+def _int_list(where, name, t, n=None, device=None):
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
+        raise TypeError("%s: %s must be a contiguous int32 device tensor" % (where, name))
+    if n is not None and t.numel() != n:
+        raise ValueError("%s: %s must have %d entries" % (where, name, n))
+    if device is not None and t.device != device:
+        raise ValueError("%s: %s is on another device" % (where, name))
+    return t.data_ptr()
+
+
+class PageTable:
+    """Which pages the sequences of a paged cache hold, on the device: block_table [sequences, pages per sequence], seq_lens
+    [sequences], page_refs [num_pages], free_pages [num_pages], free_count [1], all int32 (see plx_page_table). The
+    tensors are the caller's and are what parallax_decode and the others take as block_table and seq_lens; `empty` makes
+    those of a cache nobody uses yet."""
+
+    __slots__ = ("block_table", "seq_lens", "page_refs", "free_pages", "free_count", "page_size", "_args")
+
+    def __init__(self, block_table, seq_lens, page_refs, free_pages, free_count, page_size):
+        if block_table.dtype != torch.int32 or not block_table.is_cuda or block_table.dim() != 2 or block_table.stride(1) != 1:
+            raise TypeError("block_table must be an int32 device tensor [sequences, pages per sequence]")
+        device, (sequences, width), pages = block_table.device, block_table.shape, page_refs.numel()
+        ptrs = [_int_list("PageTable", name, t, n, device) for name, t, n in (
+            ("seq_lens", seq_lens, sequences), ("page_refs", page_refs, pages), ("free_pages", free_pages, pages),
+            ("free_count", free_count, 1))]
+        self.block_table, self.seq_lens, self.page_refs = block_table, seq_lens, page_refs
+        self.free_pages, self.free_count, self.page_size = free_pages, free_count, int(page_size)
+        self._args = _filled(plx_page_table, block_table.data_ptr(), *ptrs, sequences, width,
+                             block_table.stride(0) if sequences > 1 else width, pages, _i32(page_size))
+
+    @classmethod
+    def empty(cls, sequences, pages_per_sequence, num_pages, page_size, device="cuda:0"):
+        opts = dict(dtype=torch.int32, device=device)
+        return cls(torch.full((sequences, pages_per_sequence), -1, **opts), torch.zeros(sequences, **opts),
+                   torch.zeros(num_pages, **opts), torch.arange(num_pages - 1, -1, -1, **opts),
+                   torch.full((1,), num_pages, **opts), page_size)
+
+
+def _pools(where, k, v):
+    """The fields of a plx_cache_pools: [pages, heads, rows, d], or [pages, rows, d] for one head."""
+    if k.dim() == 3:
+        k = k.unsqueeze(1)
+    if k.dim() != 4 or not k.is_cuda or k.stride(-1) != 1:
+        raise ValueError("%s needs device pools [num_pages, (heads,) page_size, d], contiguous in the last dimension" % where)
+    vs = (0, 0, 0)
+    if v is not None:
+        if v.dim() == 3:
+            v = v.unsqueeze(1)
+        if v.shape != k.shape or v.dtype != k.dtype or v.device != k.device or v.stride(-1) != 1:
+            raise ValueError("%s: k and v are pools of one shape and type" % where)
+        vs = v.stride()[:3]
+    pages, heads, rows, d = k.shape
+    return (k.data_ptr(), _ptr(v), pages, heads, rows, d, *k.stride()[:3], *vs, _dtype_code(k))
+
+
+def parallax_cache_fork(pages, parents, children, stream=None):
+    """Sequence children[i] (empty) becomes a copy of parents[i] that shares its pages; see parallax_cache_fork in the header."""
+    where, device = "parallax_cache_fork", pages.block_table.device
+    n = parents.numel()
+    ptrs = _int_list(where, "parents", parents, None, device), _int_list(where, "children", children, n, device)
+    st = load_library().parallax_cache_fork(ctypes.byref(pages._args), *ptrs, n, _stream_ptr(stream))
+    if st != PLX_OK:
+        raise ParallaxError(st, where)
+
+
+def parallax_cache_extend(pages, seqs, new_lens, *pools, stream=None):
+    """Room for new_lens[i] tokens in sequence seqs[i]. pools: k, v (, k, v ...) of the layers that the table serves; shared
+    last pages that are replaced are copied in all of them. Returns `missing` (int32 [1] on the device: 0, or how many
+    pages were lacking, and then nothing was changed). Without pools (missing, src, dst, rows) is returned, and
+    parallax_cache_copy(k, v, src, dst, rows) is the caller's to call for every layer."""
+    where, device = "parallax_cache_extend", pages.block_table.device
+    n = seqs.numel()
+    ptrs = _int_list(where, "seqs", seqs, None, device), _int_list(where, "new_lens", new_lens, n, device)
+    if len(pools) % 2:
+        raise ValueError("pools come as k, v (v None: a single pool)")
+    for k in pools[::2]:
+        if k.shape[0] != pages.page_refs.numel() or k.shape[-2] != pages.page_size:
+            raise ValueError("the pools have the pages of the table")
+    buf = _result_maker(stream, torch.empty)(3 * n + 1, dtype=torch.int32, device=device)
+    at = buf.data_ptr()
+    src, dst, rows, missing = at, at + 4 * n, at + 8 * n, at + 12 * n
+    lib, where_to = load_library(), _stream_ptr(stream)
+    st = lib.parallax_cache_extend(ctypes.byref(pages._args), *ptrs, n, src, dst, rows, missing, where_to)
+    if st != PLX_OK:
+        raise ParallaxError(st, where)
+    for i in range(0, len(pools), 2):
+        a = _filled(plx_cache_pools, *_pools(where, pools[i], pools[i + 1]))
+        st = lib.parallax_cache_copy(ctypes.byref(a), src, dst, rows, n, where_to)
+        if st != PLX_OK:
+            raise ParallaxError(st, "parallax_cache_copy")
+    return buf[3 * n:] if pools else (buf[3 * n:], buf[:n], buf[n:2 * n], buf[2 * n:3 * n])
+
+
+def parallax_cache_free(pages, seqs, first=None, last=None, stream=None):
+    """Sequence seqs[i] gives back the whole pages in its tokens first[i] .. last[i] - 1 (default: all of them; a last[i] at or
+    behind its length takes the partial last page along and shortens the sequence to first[i])."""
+    where, device = "parallax_cache_free", pages.block_table.device
+    n = seqs.numel()
+    ptrs = [_int_list(where, "seqs", seqs, None, device)]
+    ptrs += [0 if t is None else _int_list(where, name, t, n, device) for name, t in (("first", first), ("last", last))]
+    st = load_library().parallax_cache_free(ctypes.byref(pages._args), *ptrs, n, _stream_ptr(stream))
+    if st != PLX_OK:
+        raise ParallaxError(st, where)
+
+
+def parallax_cache_copy(k, v, src, dst, rows=None, stream=None):
+    """Page src[i] -> page dst[i] of the pools k and v (None: k only), its first rows[i] rows (default: all)."""
+    where = "parallax_cache_copy"
+    a = _filled(plx_cache_pools, *_pools(where, k, v))
+    n = src.numel()
+    ptrs = [_int_list(where, "src", src, None, k.device), _int_list(where, "dst", dst, n, k.device)]
+    ptrs.append(0 if rows is None else _int_list(where, "rows", rows, n, k.device))
+    st = load_library().parallax_cache_copy(ctypes.byref(a), *ptrs, n, _stream_ptr(stream))
+    if st != PLX_OK:
+        raise ParallaxError(st, where)
+
+
+def parallax_cache_compact(k, v, seq_lens, draft_lens, accepted, n_accepted, block_table=None, new_lens=None, max_draft=None,
+                           stream=None):
+    """The rows of the accepted nodes (numbers accepted[b][: n_accepted[b]], ascending) among the last draft_lens[b] cached ones
+    (None: max_draft) move together behind the committed rows. k, v: pools with a block_table, else [B, Hkv, capacity, d];
+    v None: k only. Returns new_lens [B] = committed + accepted; seq_lens stays as it is."""
+    where = "parallax_cache_compact"
+    pools = _pools(where, k, v)
+    if accepted.dim() != 2:
+        raise ValueError("accepted [B, most]")
+    B, most = accepted.shape
+    if max_draft is None:
+        if draft_lens is None:
+            raise ValueError("draft_lens or max_draft is needed")
+        max_draft = 256
+    if new_lens is None:
+        new_lens = _result_maker(stream, torch.empty)(B, dtype=torch.int32, device=k.device)
+    ptrs = [0 if t is None else _int_list(where, name, t, m, k.device) for name, t, m in (
+        ("seq_lens", seq_lens, B), ("draft_lens", draft_lens, B), ("accepted", accepted, B * most),
+        ("n_accepted", n_accepted, B), ("new_lens", new_lens, B))]
+    table, stride = 0, 0
+    if block_table is not None:
+        if block_table.dtype != torch.int32 or block_table.device != k.device or block_table.stride(1) != 1:
+            raise TypeError("block_table must be an int32 device tensor [B, pages per sequence]")
+        if block_table.shape[0] != B:
+            raise ValueError("block_table needs one row per sequence")
+        table, stride = block_table.data_ptr(), block_table.stride(0) if B > 1 else block_table.shape[1]
+    a = _filled(plx_cache_compact_args, *pools, table, *ptrs, B, stride, _i32(max_draft), most)
+    st = load_library().parallax_cache_compact(ctypes.byref(a), _stream_ptr(stream))
+    if st != PLX_OK:
+        raise ParallaxError(st, where)
+    return new_lens
 
 
 def parallax_util_copy(dst, src, stream=None):

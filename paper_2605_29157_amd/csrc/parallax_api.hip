@@ -837,6 +837,126 @@ int32_t parallax_prefill_backward_form(const plx_prefill_bwd_args *a) {
     return a->dtype == PLX_F32 ? plx::backward_form_f32(p) : plx::backward_form_bf16(p, query_num_cus());
 }
 
+namespace {
+
+plx_status take_page_table(const plx_page_table *a, plx::PageTable *out) {
+    if (!a || !a->block_table || !a->seq_lens || !a->page_refs || !a->free_pages || !a->free_count) return PLX_ERR_NULL;
+    for (const int32_t *ptr : {a->block_table, a->seq_lens, a->page_refs, a->free_pages, a->free_count})
+        if (reinterpret_cast<uintptr_t>(ptr) & 3u) return PLX_ERR_ALIGN;
+    if (a->sequences < 1 || a->pages_per_sequence < 1 || a->num_pages < 1 || a->page_size < 1) return PLX_ERR_SHAPE;
+    if (a->block_table_stride < a->pages_per_sequence) return PLX_ERR_SHAPE;
+    if ((int64_t)a->pages_per_sequence * a->page_size > 0x7fffffffLL) return PLX_ERR_SHAPE;  // (lengths are int32)
+    *out = plx::PageTable{a->block_table, a->seq_lens, a->page_refs, a->free_pages, a->free_count,
+                          a->sequences, a->pages_per_sequence, a->num_pages, a->page_size, a->block_table_stride};
+    return PLX_OK;
+}
+
+// A list of n int32 on the device
+plx_status check_list(const int32_t *list, bool needed) {
+    if (needed && !list) return PLX_ERR_NULL;
+    return (reinterpret_cast<uintptr_t>(list) & 3u) ? PLX_ERR_ALIGN : PLX_OK;
+}
+
+plx_status take_pools(const plx_cache_pools &a, plx::CachePools *out) {
+    if (!a.k) return PLX_ERR_NULL;
+    if (a.dtype != PLX_BF16 && a.dtype != PLX_F32) return PLX_ERR_DTYPE;
+    if (a.num_pages < 1 || a.heads < 1 || a.page_size < 1 || a.d < 1 || a.d > (1 << 16) || a.heads > (1 << 16)) return PLX_ERR_SHAPE;
+    if (!aligned16(a.k) || !aligned16(a.v) || !stride_aligned(a.d, a.dtype)) return PLX_ERR_ALIGN;
+    const int size = elem_size(a.dtype);
+    plx::CachePools c{};
+    c.k = static_cast<char *>(a.k), c.v = static_cast<char *>(a.v);
+    c.num_pages = a.num_pages, c.heads = a.heads, c.page_size = a.page_size, c.row_chunks = a.d * size / 16;
+    for (int i = 0; i < 3; ++i) {
+        if (a.k_stride[i] < 0 || (a.v && a.v_stride[i] < 0)) return PLX_ERR_SHAPE;
+        if (!stride_aligned(a.k_stride[i], a.dtype) || (a.v && !stride_aligned(a.v_stride[i], a.dtype))) return PLX_ERR_ALIGN;
+        c.ks[i] = a.k_stride[i] * size, c.vs[i] = a.v ? a.v_stride[i] * size : 0;
+    }
+    if (a.k_stride[2] < a.d || (a.v && a.v_stride[2] < a.d)) return PLX_ERR_SHAPE;
+    // (a page's chunks are counted in 32 bits)
+    if ((int64_t)a.heads * a.page_size * c.row_chunks > 0x3fffffffLL) return PLX_ERR_SHAPE;
+    *out = c;
+    return PLX_OK;
+}
+
+plx_status launched(hipError_t err) { return err == hipSuccess ? PLX_OK : PLX_ERR_LAUNCH; }
+
+}  // namespace
+
+plx_status parallax_cache_fork(const plx_page_table *pages, const int32_t *parents, const int32_t *children, int32_t n,
+                               void *hip_stream) {
+    plx::PageTable t{};
+    plx_status st = take_page_table(pages, &t);
+    if (st != PLX_OK) return st;
+    if (n < 0 || n > 65535) return PLX_ERR_SHAPE;
+    for (const int32_t *list : {parents, children})
+        if ((st = check_list(list, n > 0)) != PLX_OK) return st;
+    return n == 0 ? PLX_OK : launched(plx::launch_cache_fork(t, parents, children, n, static_cast<hipStream_t>(hip_stream)));
+}
+
+plx_status parallax_cache_extend(const plx_page_table *pages, const int32_t *seqs, const int32_t *new_lens, int32_t n,
+                                 int32_t *src, int32_t *dst, int32_t *rows, int32_t *missing, void *hip_stream) {
+    plx::PageTable t{};
+    plx_status st = take_page_table(pages, &t);
+    if (st != PLX_OK) return st;
+    if (n < 0 || n > PLX_MAX_EXTEND) return PLX_ERR_SHAPE;
+    for (const int32_t *list : {seqs, new_lens, (const int32_t *)src, (const int32_t *)dst, (const int32_t *)rows})
+        if ((st = check_list(list, n > 0)) != PLX_OK) return st;
+    if ((st = check_list(missing, true)) != PLX_OK) return st;
+    // (an empty list is launched too: it says that nothing is missing)
+    return launched(plx::launch_cache_extend(t, seqs, new_lens, n, src, dst, rows, missing, static_cast<hipStream_t>(hip_stream)));
+}
+
+plx_status parallax_cache_free(const plx_page_table *pages, const int32_t *seqs, const int32_t *first, const int32_t *last,
+                               int32_t n, void *hip_stream) {
+    plx::PageTable t{};
+    plx_status st = take_page_table(pages, &t);
+    if (st != PLX_OK) return st;
+    if (n < 0 || n > 65535) return PLX_ERR_SHAPE;
+    if ((st = check_list(seqs, n > 0)) != PLX_OK) return st;
+    for (const int32_t *list : {first, last})
+        if ((st = check_list(list, false)) != PLX_OK) return st;
+    return n == 0 ? PLX_OK : launched(plx::launch_cache_free(t, seqs, first, last, n, static_cast<hipStream_t>(hip_stream)));
+}
+
+plx_status parallax_cache_copy(const plx_cache_pools *pools, const int32_t *src, const int32_t *dst, const int32_t *rows,
+                               int32_t n, void *hip_stream) {
+    if (!pools) return PLX_ERR_NULL;
+    plx::CachePools c{};
+    plx_status st = take_pools(*pools, &c);
+    if (st != PLX_OK) return st;
+    if (n < 0) return PLX_ERR_SHAPE;
+    for (const int32_t *list : {src, dst})
+        if ((st = check_list(list, n > 0)) != PLX_OK) return st;
+    if ((st = check_list(rows, false)) != PLX_OK) return st;
+    return n == 0 ? PLX_OK : launched(plx::launch_cache_copy(c, src, dst, rows, n, static_cast<hipStream_t>(hip_stream)));
+}
+
+plx_status parallax_cache_compact(const plx_cache_compact_args *a, void *hip_stream) {
+    if (!a) return PLX_ERR_NULL;
+    plx::CacheCompact p{};
+    plx_status st = take_pools(a->pools, &p.pools);
+    if (st != PLX_OK) return st;
+    if (a->B < 1 || a->max_draft < 1 || a->max_draft > PLX_MAX_TREE_NODES || a->max_accepted < 1 || a->max_accepted > a->max_draft)
+        return PLX_ERR_SHAPE;
+    for (const int32_t *list : {a->seq_lens, a->accepted, a->n_accepted, (const int32_t *)a->new_lens})
+        if ((st = check_list(list, true)) != PLX_OK) return st;
+    for (const int32_t *list : {a->draft_lens, a->block_table})
+        if ((st = check_list(list, false)) != PLX_OK) return st;
+    if (a->new_lens == a->seq_lens) return PLX_ERR_SHAPE;
+    int64_t capacity = a->pools.page_size;
+    if (a->block_table) {
+        if (a->block_table_stride < 1) return PLX_ERR_SHAPE;
+        capacity *= a->block_table_stride;
+    } else if (a->pools.num_pages != a->B) {
+        return PLX_ERR_SHAPE;
+    }
+    p.block_table = a->block_table, p.table_stride = a->block_table_stride;
+    p.seq_lens = a->seq_lens, p.draft_lens = a->draft_lens, p.accepted = a->accepted, p.n_accepted = a->n_accepted;
+    p.new_lens = a->new_lens, p.B = a->B, p.max_draft = a->max_draft, p.max_accepted = a->max_accepted;
+    p.capacity = (int32_t)std::min<int64_t>(capacity, 0x7fffffff);
+    return launched(plx::launch_cache_compact(p, static_cast<hipStream_t>(hip_stream)));
+}
+
 plx_status parallax_norm_rope(const plx_norm_rope_args *a, void *hip_stream) {
     if (!a) return PLX_ERR_NULL;
     if (a->dtype != PLX_BF16 && a->dtype != PLX_F32) return PLX_ERR_DTYPE;

@@ -130,6 +130,28 @@ struct BlockListParams {
     int32_t *counts, *row_ptr, *tile_idx, *col_ptr, *col_idx;
 };
 
+// Which pages a paged cache's sequences hold (cache_pages.hip); all arrays on the device
+struct PageTable {
+    int32_t *block_table, *seq_lens, *page_refs, *free_pages, *free_count;
+    int32_t sequences, pages_per_sequence, num_pages, page_size;
+    int64_t stride;  // of block_table
+};
+// Pools [num_pages][heads][page_size][row] (v nullptr: one pool); strides in bytes, rows in 16-byte chunks
+struct CachePools {
+    char *k, *v;
+    int32_t num_pages, heads, page_size, row_chunks;
+    int64_t ks[3], vs[3];
+};
+// Accepted nodes (ascending) of the last n_b drafted rows of every sequence, moved behind the committed rows
+struct CacheCompact {
+    CachePools pools;  // (no block table: [B][heads][capacity][row], the first stride a sequence's)
+    const int32_t *block_table;
+    int64_t table_stride;
+    const int32_t *seq_lens, *draft_lens, *accepted, *n_accepted;
+    int32_t *new_lens;
+    int32_t B, capacity, max_draft, max_accepted;
+};
+
 // RMSNorm + RoPE on up to three contiguous [B, H, T, d] tensors of one (B, T, d).
 struct NormRopeTensor {
     const void *x;
@@ -168,6 +190,12 @@ hipError_t launch_prefill_bwd_f32(const PrefillBwdParams &p, hipStream_t stream)
 hipError_t launch_decode_f32(const DecodeParams &p, hipStream_t stream);
 hipError_t launch_prefill_f32(const PrefillParams &p, hipStream_t stream);
 hipError_t launch_block_lists(const BlockListParams &p, hipStream_t stream);
+hipError_t launch_cache_fork(const PageTable &t, const int32_t *parents, const int32_t *children, int n, hipStream_t stream);
+hipError_t launch_cache_extend(const PageTable &t, const int32_t *seqs, const int32_t *new_lens, int n, int32_t *src, int32_t *dst,
+                               int32_t *rows, int32_t *missing, hipStream_t stream);
+hipError_t launch_cache_free(const PageTable &t, const int32_t *seqs, const int32_t *first, const int32_t *last, int n, hipStream_t stream);
+hipError_t launch_cache_copy(const CachePools &c, const int32_t *src, const int32_t *dst, const int32_t *rows, int n, hipStream_t stream);
+hipError_t launch_cache_compact(const CacheCompact &a, hipStream_t stream);
 hipError_t launch_norm_rope(const NormRopeParams &p, bool f32, hipStream_t stream);
 hipError_t launch_rope_table(float *table, int n_pos, int d, float theta, hipStream_t stream);
 hipError_t launch_decode_mla(const MlaDecodeParams &p, hipStream_t stream);
