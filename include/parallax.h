@@ -390,6 +390,13 @@ typedef struct {
 plx_status parallax_prefill(const plx_prefill_args *args, void *hip_stream);
 
 /*
+ * parallax_prefill with a sliding window and a few first tokens that stay visible: row i sees key j iff j <= pos and
+ * (j > pos - window or j < sinks), pos = i + (Tkv - T). The row cache may be asked for; causal and window > 0 are
+ * needed for sinks > 0, block lists do not combine (PLX_ERR_SHAPE). sinks = 0 is parallax_prefill.
+ */
+plx_status parallax_prefill_sinks(const plx_prefill_args *args, int32_t sinks, void *hip_stream);
+
+/*
  * parallax_prefill for launches that leave compute units idle (a short prompt, a few hundred rows
  * behind a long cache): row blocks with many keys are cut into key ranges, one workgroup each, whose
  * unnormalised fp32 records go to the workspace and are merged by a second kernel (App. C). bf16,
@@ -520,6 +527,11 @@ typedef struct {
 
 size_t parallax_prefill_backward_workspace_bytes(int32_t B, int32_t Hq, int32_t T);
 plx_status parallax_prefill_backward(const plx_prefill_bwd_args *args, void *hip_stream);
+/* The backward of parallax_prefill_sinks (row cache from a forward with the same window and sinks). The workspace is larger:
+ * the gradients of the sinks' keys, which every row sees, are summed over parts of the rows. 0 bytes: not valid (the
+ * workspace of args is not looked at there). */
+size_t parallax_prefill_backward_sinks_workspace_bytes(const plx_prefill_bwd_args *args, int32_t sinks);
+plx_status parallax_prefill_backward_sinks(const plx_prefill_bwd_args *args, int32_t sinks, void *hip_stream);
 /* How a call runs: keys per workgroup of the pass for dk and dv (64 or 128; fp32: 32 in bf16 thirds, else 0), plus 256 *
  * query rows per workgroup of the pass for dq and dr (likewise); 0: fp32 and neither in thirds, or not valid. As in the forward the form is the quickest for the launch and depends on B
  * and the heads; two launches of the same form give a sequence the same bits. Plus 65536: block lists, and what share

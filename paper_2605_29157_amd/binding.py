@@ -30,6 +30,7 @@ EXPORTED_SYMBOLS = (
     "parallax_decode_mla", "parallax_decode_mla_workspace_bytes", "parallax_decode_mla_num_splits",
     "parallax_prefill", "parallax_prefill_split", "parallax_prefill_workspace_bytes", "parallax_prefill_form", "parallax_prefill_backward", "parallax_prefill_backward_form",
     "parallax_prefill_backward_workspace_bytes",
+    "parallax_prefill_sinks", "parallax_prefill_backward_sinks", "parallax_prefill_backward_sinks_workspace_bytes",
     "parallax_cache_fork", "parallax_cache_extend", "parallax_cache_free", "parallax_cache_copy", "parallax_cache_compact",
     "parallax_block_lists", "parallax_norm_rope", "parallax_rope_table", "parallax_util_copy", "parallax_util_read",
     "parallax_util_read_grid", "parallax_util_read_sink_slots", "parallax_util_mfma", "parallax_strerror", "parallax_version",
@@ -263,6 +264,12 @@ def load_library() -> ctypes.CDLL:
         lib.parallax_prefill_backward_workspace_bytes.restype = ctypes.c_size_t
         lib.parallax_block_lists.argtypes = [ctypes.POINTER(plx_block_list_args), ctypes.c_void_p]
         lib.parallax_block_lists.restype = ctypes.c_int
+        lib.parallax_prefill_sinks.argtypes = [ctypes.POINTER(plx_prefill_args), ctypes.c_int32, ctypes.c_void_p]
+        lib.parallax_prefill_sinks.restype = ctypes.c_int
+        lib.parallax_prefill_backward_sinks.argtypes = [ctypes.POINTER(plx_prefill_bwd_args), ctypes.c_int32, ctypes.c_void_p]
+        lib.parallax_prefill_backward_sinks.restype = ctypes.c_int
+        lib.parallax_prefill_backward_sinks_workspace_bytes.argtypes = [ctypes.POINTER(plx_prefill_bwd_args), ctypes.c_int32]
+        lib.parallax_prefill_backward_sinks_workspace_bytes.restype = ctypes.c_size_t
         _list = ctypes.c_void_p
         lib.parallax_cache_fork.argtypes = [ctypes.POINTER(plx_page_table), _list, _list, ctypes.c_int32, ctypes.c_void_p]
         lib.parallax_cache_extend.argtypes = [ctypes.POINTER(plx_page_table), _list, _list, ctypes.c_int32, _list, _list, _list,
@@ -737,10 +744,13 @@ def attach_block_lists(a, block_mask, device, stream=None, columns=False):
 
 
 def parallax_prefill(q, r, k, v, scale, causal=True, use_r=True, out=None, stream=None, window=0,
-                     save_for_backward=False, block_mask=None, prep=None):
+                     save_for_backward=False, block_mask=None, prep=None, sinks=0):
     """Parallax prefill forward over T query rows and Tkv keys (causal: the rows are the last
     T positions of the Tkv-long sequence). With save_for_backward the kernel also writes the row
-    cache of the backward pass and (out, vbar, row_stats) is returned."""
+    cache of the backward pass and (out, vbar, row_stats) is returned. With sinks > 0 the first tokens stay visible
+    behind the sliding window (no block_mask, no prep)."""
+    if sinks and (block_mask is not None or prep is not None):
+        raise ValueError("sinks go with neither block_mask nor prep")
     for t in (q, k, v) + ((r,) if r is not None else ()):
         if not t.is_cuda:
             raise ValueError("parallax_prefill needs device tensors")
@@ -766,14 +776,16 @@ def parallax_prefill(q, r, k, v, scale, causal=True, use_r=True, out=None, strea
         row_stats = _result_maker(stream, torch.empty)(B, Hq, T, 2, dtype=torch.float32, device=q.device)
         _ROW_CACHE.pack_into(a, plx_prefill_args.vbar.offset, vbar.data_ptr(), row_stats.data_ptr())
     lib, where = load_library(), _stream_ptr(stream)
-    split_bytes = lib.parallax_prefill_workspace_bytes(ctypes.byref(a))
-    if split_bytes:  # few row blocks, many keys: split over key ranges
+    split_bytes = 0 if sinks else lib.parallax_prefill_workspace_bytes(ctypes.byref(a))
+    if sinks:
+        st = lib.parallax_prefill_sinks(ctypes.byref(a), _i32(sinks), where)
+    elif split_bytes:  # few row blocks, many keys: split over key ranges
         workspace = _scratch(stream, split_bytes // 4, q.device)
         st = lib.parallax_prefill_split(ctypes.byref(a), workspace.data_ptr(), split_bytes, where)
     else:
         st = lib.parallax_prefill(ctypes.byref(a), where)
     if st != PLX_OK:
-        raise ParallaxError(st, "parallax_prefill")
+        raise ParallaxError(st, "parallax_prefill_sinks" if sinks else "parallax_prefill")
     return (out, vbar, row_stats) if save_for_backward else out
 
 
@@ -800,14 +812,29 @@ def prefill_bwd_args(q, r, k, v, o, vbar, row_stats, d_o, dq, dr, dk, dv, scale,
 
 
 def parallax_prefill_backward(q, r, k, v, o, vbar, row_stats, d_o, scale, causal=True, stream=None,
-                              workspace=None, window=0, block_mask=None):
+                              workspace=None, window=0, block_mask=None, sinks=0):
     """Gradients (dq, dr, dk, dv) of parallax_prefill for the upstream gradient d_o, from the
-    forward's output and row cache (save_for_backward=True, same causal / window / block_mask)."""
+    forward's output and row cache (save_for_backward=True, same causal / window / block_mask / sinks)."""
+    if sinks and block_mask is not None:
+        raise ValueError("sinks do not go with a block_mask")
     like = _result_maker(stream, torch.empty_like)
     dq, dr, dk, dv = like(q), like(q), like(k), like(k)
-    if workspace is None:
+    own_scratch = workspace is None
+    if own_scratch and not sinks:
         workspace = _scratch(stream, q.shape[0] * q.shape[1] * q.shape[2] * 4, q.device)
-    a = prefill_bwd_args(q, r, k, v, o, vbar, row_stats, d_o, dq, dr, dk, dv, scale, causal, workspace, window)
+    # (with sinks the library says how much; row_stats in the place of the workspace until then)
+    a = prefill_bwd_args(q, r, k, v, o, vbar, row_stats, d_o, dq, dr, dk, dv, scale, causal,
+                         row_stats if workspace is None else workspace, window)
+    if sinks:
+        lib = load_library()
+        if own_scratch:
+            need = lib.parallax_prefill_backward_sinks_workspace_bytes(ctypes.byref(a), _i32(sinks))  # (0: refused below)
+            workspace = _scratch(stream, (need + 3) // 4, q.device)
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), need
+        st = lib.parallax_prefill_backward_sinks(ctypes.byref(a), _i32(sinks), _stream_ptr(stream))
+        if st != PLX_OK:
+            raise ParallaxError(st, "parallax_prefill_backward_sinks")
+        return dq, dr, dk, dv
     if block_mask is not None:
         nrb, nkt = -(-q.shape[2] // BLOCK_ROWS), -(-k.shape[2] // BLOCK_KEYS)
         if tuple(block_mask.shape[-2:]) != (nrb, nkt):

@@ -573,6 +573,7 @@ hipError_t launch_decode_rows_f32(const DecodeRowsParams &p, hipStream_t stream)
 }
 
 int32_t prefill_form_f32(const PrefillParams &p) {
+    if (p.sinks > 0) return 0;
     return f32_thirds_pay(p.d, p.T, p.Tk, p.causal, p.window, f32_thirds_blocks(p.T, p.B, p.Hq)) ? kF32ThirdsColumns : 0;
 }
 
@@ -587,6 +588,7 @@ hipError_t launch_prefill_f32(const PrefillParams &p, hipStream_t stream) {
         g.qs[a] = p.qs[a], g.rs[a] = p.rs[a], g.ks[a] = p.ks[a], g.vs[a] = p.vs[a], g.os[a] = p.os[a];
     g.scale = p.scale, g.use_r = p.use_r, g.tail = p.causal, g.window = p.window;
     g.vbar = (float *)p.vbar, g.row_stats = p.row_stats;
+    g.sinks = p.sinks;
     g.S = 1;
     return launch_forward(g, stream);
 }
@@ -603,7 +605,8 @@ struct F32RowsLds {
     };
 };
 
-template <int DP, bool FULL>
+// SINKS: the first p.sinks keys stay visible behind the window (the blocks are walked as in the forward).
+template <int DP, bool FULL, bool SINKS = false>
 __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_bwd_rows_kernel(PrefillBwdParams p) {
     __shared__ F32RowsLds<DP> lds;
     __shared__ f32x4 scalars[16];
@@ -650,8 +653,11 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_bwd_rows_k
     const int my_lo = p.window > 0 ? max(my_end - p.window, 0) : 0;
     const int last = min(i0 + 15, p.T - 1);
     const int end = p.causal ? min(last + 1 + off, p.Tk) : p.Tk, first_end = p.causal ? min(i0 + 1 + off, p.Tk) : p.Tk;
-    const int lo = p.window > 0 ? max(first_end - p.window, 0) / 16 : 0;
     const int all_lo = p.window > 0 ? max(end - p.window, 0) : 0;
+    int lo = p.window > 0 ? max(first_end - p.window, 0) / 16 : 0, hi = (end + 15) / 16;
+    const int n_sink_blocks = SINKS ? min((p.sinks + 15) / 16, hi) : 0, skip = SINKS ? max(lo - n_sink_blocks, 0) : 0;
+    if constexpr (SINKS) lo = 0, hi -= skip;
+    auto block_of = [&](int i) { return SINKS && i >= n_sink_blocks ? i + skip : i; };
     const float *k = (const float *)p.k + khead * d, *v = (const float *)p.v + khead * d;
     f32x4 kf[NA], vf[NA];
     auto load = [&](f32x4(&x)[NA], const float *base, int kblk) {
@@ -661,21 +667,20 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_bwd_rows_k
 #pragma unroll
     for (int n = 0; n < NA; ++n) dq[n] = dr[n] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float scale_log2 = p.scale * kLog2e;
-    const int hi = (end + 15) / 16;
     int kblk = lo + w;
-    if (kblk < hi) load(kf, k, kblk), load(vf, v, kblk);
+    if (kblk < hi) load(kf, k, block_of(kblk)), load(vf, v, block_of(kblk));
     __syncthreads();
     const f32x4 sc = scalars[c];
     for (; kblk < hi; kblk += kF32Waves) {
-        const int key0 = 16 * kblk, next = kblk + kF32Waves;
+        const int key0 = 16 * block_of(kblk), next = kblk + kF32Waves;
         const f32x4 a = f32_scores<DP>(vf, lds.rows[2], d, c, g);
-        if (next < hi) load(vf, v, next);
+        if (next < hi) load(vf, v, block_of(next));
         const f32x4 s1 = f32_scores<DP>(kf, lds.rows[0], d, c, g);
         const f32x4 s2 = f32_scores<DP>(kf, lds.rows[1], d, c, g);
         f32x4 kt[4][DP / 64];
         f32_turn<DP>(kf, lds.tile[w], kt, c, g);
-        if (next < hi) load(kf, k, next);
-        const bool whole = key0 >= all_lo && key0 + 16 <= first_end;
+        if (next < hi) load(kf, k, block_of(next));
+        const bool whole = (key0 >= all_lo || (SINKS && key0 + 16 <= p.sinks)) && key0 + 16 <= first_end;
         unsigned seen = 15u;
         f32x4 g1, g2;
 #pragma unroll
@@ -686,7 +691,7 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_bwd_rows_k
             g2[r] = -pr * dlt;
             if (!whole) {
                 const int key = key0 + 4 * g + r;
-                if (!(key >= my_lo && key < my_end)) g1[r] = g2[r] = 0.f, seen &= ~(1u << r);
+                if (!((key >= my_lo || (SINKS && key < p.sinks)) && key < my_end)) g1[r] = g2[r] = 0.f, seen &= ~(1u << r);
             }
         }
         if (__builtin_expect(!whole && f32_not_finite<DP>(kt), 0)) f32_take_out_not_finite<DP, 2>(kt, {&g1, &g2}, seen, {&dq, &dr});
@@ -720,7 +725,7 @@ struct F32ColsLds {
     };
 };
 
-template <int DP, bool FULL>
+template <int DP, bool FULL, bool SINKS = false>
 __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_bwd_cols_kernel(PrefillBwdParams p) {
     __shared__ F32ColsLds<DP> lds;
     constexpr int NA = DP / 16;
@@ -748,9 +753,11 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_bwd_cols_k
     auto key_lo = [&](int j) { return p.causal ? max(j - off, 0) : 0; };
     auto key_end = [&](int j) { return p.window > 0 ? min(p.T, max(j - off + p.window, 0)) : p.T; };
     const int j_last = min(j0 + 15, p.Tk - 1), j = min(j0 + c, j_last);
-    const int my_lo = key_lo(j), my_end = key_end(j);
-    const int lo = key_lo(j0) / 16, end = key_end(j_last);  // union (both bounds grow with the key)
-    const int all_lo = key_lo(j_last), all_end = key_end(j0);
+    const int my_lo = key_lo(j), my_end = SINKS && j < p.sinks ? p.T : key_end(j);
+    const int lo = key_lo(j0) / 16, end = SINKS && j0 < p.sinks ? p.T : key_end(j_last);  // union (both bounds grow with the key)
+    // (sinks: the first key behind them drops out first)
+    const int first_out = SINKS ? max(j0, p.sinks) : j0;
+    const int all_lo = key_lo(j_last), all_end = SINKS && first_out > j_last ? p.T : key_end(first_out);
     const int per_head = max((end + 15) / 16 - lo, 0), n_items = per_head * p.G;
 
     f32x4 xq[NA], xr[NA], xg[NA];
@@ -817,6 +824,7 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_bwd_cols_k
 }
 
 int32_t backward_form_f32(const PrefillBwdParams &p) {
+    if (p.sinks > 0) return 0;
     // (each pass by itself: with several query heads to a key head there are fewer key blocks)
     auto pay = [&](int n, int heads) { return f32_thirds_pay(p.d, p.T, p.Tk, p.causal, p.window, f32_thirds_blocks(n, p.B, heads)); };
     return (pay(p.Tk, p.Hkv) ? kF32ThirdsColumns : 0) + 256 * (pay(p.T, p.Hq) ? kF32ThirdsColumns : 0);
@@ -826,6 +834,12 @@ template <int DP, bool FULL>
 static hipError_t launch_backward(const PrefillBwdParams &p, hipStream_t stream) {
     const int32_t form = backward_form_f32(p);
     const int64_t row_blocks = (p.T + 15) / 16, key_blocks = (p.Tk + 15) / 16;
+    if (p.sinks > 0) {
+        hipLaunchKernelGGL((f32_bwd_rows_kernel<DP, FULL, true>), f32_grid(row_blocks * p.B * p.Hq), dim3(kF32Threads), 0, stream, p);
+        if (hipError_t err = hipGetLastError()) return err;
+        hipLaunchKernelGGL((f32_bwd_cols_kernel<DP, FULL, true>), f32_grid(key_blocks * p.B * p.Hkv), dim3(kF32Threads), 0, stream, p);
+        return hipGetLastError();
+    }
     if (form / 256) {
         if (hipError_t err = launch_bwd_rows_thirds(p, stream)) return err;
     } else {

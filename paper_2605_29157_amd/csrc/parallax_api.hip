@@ -597,6 +597,34 @@ plx_status parallax_prefill_split(const plx_prefill_args *a, void *workspace, si
     return plx::launch_prefill_bf16(p, stream) == hipSuccess ? PLX_OK : PLX_ERR_LAUNCH;
 }
 
+namespace {
+
+// Window and sinks of a prefill or backward call whose window has been taken (0: none, or one that hides nothing): with
+// sinks that reach its first key nothing is hidden from any row either.
+plx_status take_sinks(int32_t given_window, int32_t given_sinks, bool lists, int32_t keys, int32_t *window, int32_t *sinks) {
+    if (given_sinks < 0 || (given_sinks > 0 && (given_window <= 0 || lists))) return PLX_ERR_SHAPE;
+    if (*window > 0 && given_sinks > 0) {
+        if ((int64_t)*window + given_sinks >= keys)
+            *window = 0;
+        else
+            *sinks = given_sinks;
+    }
+    return PLX_OK;
+}
+
+}  // namespace
+
+plx_status parallax_prefill_sinks(const plx_prefill_args *a, int32_t sinks, void *hip_stream) {
+    plx::PrefillParams p{};
+    plx_status st = prepare_prefill(a, &p);
+    if (st == PLX_OK) st = take_sinks(a->window, sinks, a->sparse_row_ptr != nullptr, p.Tk, &p.window, &p.sinks);
+    if (st != PLX_OK) return st;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (a->dtype == PLX_F32) return plx::launch_prefill_f32(p, stream) == hipSuccess ? PLX_OK : PLX_ERR_LAUNCH;
+    plx::plan_prefill_bf16(p, query_num_cus(), false);
+    return plx::launch_prefill_bf16(p, stream) == hipSuccess ? PLX_OK : PLX_ERR_LAUNCH;
+}
+
 size_t parallax_decode_mla_workspace_bytes(int32_t B, int32_t Hq) {
     if (B <= 0 || Hq <= 0) return 0;
     return (size_t)B * Hq * PLX_MAX_SPLITS * (2 * 512 + 4) * sizeof(float);
@@ -824,6 +852,48 @@ plx_status prepare_prefill_backward(const plx_prefill_bwd_args *a, plx::PrefillB
 plx_status parallax_prefill_backward(const plx_prefill_bwd_args *a, void *hip_stream) {
     plx::PrefillBwdParams p{};
     const plx_status st = prepare_prefill_backward(a, &p);
+    if (st != PLX_OK) return st;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const hipError_t err = a->dtype == PLX_F32 ? plx::launch_prefill_bwd_f32(p, stream)
+                                               : plx::launch_prefill_bwd_bf16(p, query_num_cus(), stream);
+    return err == hipSuccess ? PLX_OK : PLX_ERR_LAUNCH;
+}
+
+namespace {
+
+plx_status prepare_backward_sinks(const plx_prefill_bwd_args *a, int32_t sinks, bool need_workspace, plx::PrefillBwdParams *out,
+                                  size_t *bytes) {
+    if (!a) return PLX_ERR_NULL;
+    plx_prefill_bwd_args b = *a;
+    alignas(16) static const char anywhere[16] = {};
+    if (!need_workspace) b.workspace = const_cast<char *>(anywhere), b.workspace_bytes = (size_t)-1;  // (not looked at)
+    plx::PrefillBwdParams p{};
+    plx_status st = prepare_prefill_backward(&b, &p);
+    if (st == PLX_OK) st = take_sinks(a->window, sinks, a->sparse_row_ptr != nullptr, p.Tk, &p.window, &p.sinks);
+    if (st != PLX_OK) return st;
+    const size_t rows = parallax_prefill_backward_workspace_bytes(a->B, a->Hq, a->T);
+    *bytes = rows;
+    if (p.sinks > 0 && a->dtype == PLX_BF16) {
+        *bytes += plx::backward_sinks_bytes_bf16(p, query_num_cus());
+        p.sink_sums = reinterpret_cast<float *>(static_cast<char *>(b.workspace) + rows);
+    }
+    if (need_workspace && a->workspace_bytes < *bytes) return PLX_ERR_WORKSPACE;
+    *out = p;
+    return PLX_OK;
+}
+
+}  // namespace
+
+size_t parallax_prefill_backward_sinks_workspace_bytes(const plx_prefill_bwd_args *a, int32_t sinks) {
+    plx::PrefillBwdParams p{};
+    size_t bytes = 0;
+    return prepare_backward_sinks(a, sinks, false, &p, &bytes) == PLX_OK ? bytes : 0;
+}
+
+plx_status parallax_prefill_backward_sinks(const plx_prefill_bwd_args *a, int32_t sinks, void *hip_stream) {
+    plx::PrefillBwdParams p{};
+    size_t bytes = 0;
+    const plx_status st = prepare_backward_sinks(a, sinks, true, &p, &bytes);
     if (st != PLX_OK) return st;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const hipError_t err = a->dtype == PLX_F32 ? plx::launch_prefill_bwd_f32(p, stream)

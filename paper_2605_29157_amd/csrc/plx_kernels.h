@@ -76,6 +76,7 @@ struct PrefillParams {
     // (ws != nullptr: take them)
     float *ws;
     int32_t rows, split_tiles, items_per_head;
+    int32_t sinks;  // > 0 (window > 0): the first `sinks` keys stay visible
 };
 
 // Decode over an MLA-style latent cache: one row [latent 512 | rope 64] per token shared by all
@@ -119,6 +120,11 @@ struct PrefillBwdParams {
     // > 0 (set by the launcher): both forms are launched, that of 64 keys per workgroup runs if the row lists hold at most
     // this many entries, the other one if they hold more
     int32_t list_limit;
+    int32_t sinks;  // > 0 (window > 0): the first `sinks` keys stay visible
+    // bf16: the key blocks with sinks (sink_blocks per head) are cut into sink_parts parts of sink_part_tiles 64-row tiles (set by
+    // the launcher), whose sums are in sink_sums
+    int32_t sink_part_tiles, sink_parts, sink_blocks;
+    float *sink_sums;
 };
 
 // Block mask [lists, n_row_blocks, n_tiles] (bytes, nonzero = listed) -> the lists of PrefillParams and,
@@ -182,6 +188,7 @@ hipError_t launch_prefill_bf16(const PrefillParams &p, hipStream_t stream);
 size_t plan_prefill_bf16(PrefillParams &p, int num_cus, bool with_ranges);
 // keys per workgroup of the column pass, plus 256 * rows per workgroup of the row pass, plus 65536 where the lists decide
 int32_t backward_form_bf16(const PrefillBwdParams &p, int num_cus);
+size_t backward_sinks_bytes_bf16(const PrefillBwdParams &p, int num_cus);  // of sink_sums
 hipError_t launch_prefill_bwd_bf16(const PrefillBwdParams &p, int num_cus, hipStream_t stream);
 // 32 for a pass in bf16 thirds (prefill_f32.hip), 0 on the fp32 instruction; the backward as backward_form_bf16
 int32_t prefill_form_f32(const PrefillParams &p);

@@ -79,8 +79,11 @@ __device__ __forceinline__ void keep_blocks(const f32x16 &a, const f32x16 &b) { 
 // norm_rope.hip, the rotation taken from a table of (cos, sin) per position and pair).
 // PAIR: 64 rows per workgroup. Waves w and w ^ 2 share 32 rows, each takes one 32-key half of every tile, and they add
 // their sums up at the end: half the chain for twice the workgroups, for launches that wait for their longest one.
+// SINKS: with a window, the first p.sinks keys stay visible. The tiles walked are those of the sinks, then those from the first
+// key any window of the workgroup reaches; a tile that holds both is walked twice, once for its keys below p.sinks and
+// once for the others, so that a tile's keys are one range for every row and the masks stay two bounds.
 template <int D, bool USE_R, bool CAUSAL, bool WINDOW, bool STATS = false, bool SPARSE = false, bool PREP = false,
-          bool SPLIT = false, bool PAIR = false>
+          bool SPLIT = false, bool PAIR = false, bool SINKS = false>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(PrefillParams p) {
     static_assert(!PREP || (USE_R && !WINDOW && !STATS && !SPARSE), "q / rho preparation: dense forward only");
     static_assert(!SPLIT || (!WINDOW && !SPARSE && !PREP), "key ranges: dense forward only");
@@ -90,6 +93,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
     static_assert(CAUSAL || !WINDOW, "a sliding window needs the rows' positions");
     static_assert(!STATS || USE_R, "the row cache is written for the backward pass only");
     static_assert(!SPARSE || !WINDOW, "block-sparse: its own tile iterator, no window");
+    static_assert(!SINKS || WINDOW, "sinks: what a window leaves visible");
     constexpr int CPR = D / 8;            // 16-byte chunks per row
     constexpr int KSTEPS = D / 16;        // k-steps of the score contraction
     constexpr int NDB = D / 32;           // 32-wide blocks of output dimensions
@@ -168,7 +172,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
     // the first key of the workgroup's first row are skipped by moving the K / V base; from
     // here on key positions, Tk and off are relative to that first tile.
     // (SPLIT skips the tiles before its key range the same way.)
-    const int kt_skip = WINDOW  ? max(rb * kBR + (p.Tk - T) - p.window + 1, 0) / kBC
+    const int kt_skip = SINKS   ? 0
+                        : WINDOW  ? max(rb * kBR + (p.Tk - T) - p.window + 1, 0) / kBC
                         : SPLIT ? range * range_tiles
                                 : 0;
     const int Tk = p.Tk - kt_skip * kBC;  // keys
@@ -278,15 +283,22 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
     const int vis_end = CAUSAL ? min(rb * kBR + off + 1, Tk) : Tk;
     const int n_list_full = SPARSE ? list_count(vis_end - kBC + 1) : 0;
     if constexpr (SPARSE) n_list = list_count(key_end);
+    // SINKS: n_sink tiles of sinks, then the tiles from first_tile on (keys below n_sink_keys belong to the former)
+    const int n_sink_keys = SINKS ? min(p.sinks, key_end) : 0, n_sink = (n_sink_keys + kBC - 1) / kBC;
+    const int first_tile = SINKS ? max(max(rb * kBR + off - p.window + 1, 0) / kBC, n_sink_keys / kBC) : 0;
     // a row block that lists nothing runs one tile with every key masked: sums of zero, zeros out
     const bool no_tiles = SPARSE && n_list == 0;
     auto tile_at = [&](int i) __attribute__((always_inline)) {
         if constexpr (SPARSE)
             return no_tiles ? 0 : min(max(tile_list[min(i, n_list - 1)], 0), (Tk - 1) / kBC);
+        else if constexpr (SINKS)
+            return i < n_sink ? i : i - n_sink + first_tile;
         else
             return i;
     };
-    int n_tiles_ = SPARSE ? max(n_list, 1) : (key_end + kBC - 1) / kBC;
+    int n_tiles_ = SPARSE  ? max(n_list, 1)
+                   : SINKS ? n_sink + (n_sink_keys < key_end ? (key_end + kBC - 1) / kBC - first_tile : 0)
+                           : (key_end + kBC - 1) / kBC;
     // (block-sparse: the count is handed over as an opaque value. Knowing it is at least 1, the
     // compiler merges the pipeline prologue into the first loop iteration, and that one long
     // region needs more registers than the file holds.)
@@ -297,12 +309,15 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
     // (block-sparse: leading list entries; the entry prefetched two ahead is then not the last
     // one, the only one that may be the partial tile)
     const int n_full = SPARSE ? max(0, min(n_list_full, n_list - kDist))
-                              : max(0, min(CAUSAL ? min((rb * kBR + off + 1) / kBC, Tv / kBC) : Tv / kBC, Tk / kBC - kDist));
+                              : max(0, min(CAUSAL ? min((rb * kBR + off + 1) / kBC, Tv / kBC) : Tv / kBC, Tk / kBC - kDist) +
+                                           (SINKS ? n_sink - first_tile : 0));
     // sliding window: first key this lane's row sees, and the leading tiles that hold a key
     // some row of the workgroup does not see (its last row starts latest)
     int row_lo;
     row_lo = WINDOW ? my_row + off - p.window + 1 : 0;
-    const int n_left = WINDOW ? min(n_tiles, max(rb * kBR + kBR + off - p.window + kBC - 1, 0) / kBC) : 0;
+    if constexpr (SINKS) row_lo = max(row_lo, n_sink_keys);
+    const int left_tiles = WINDOW ? max(rb * kBR + kBR + off - p.window + kBC - 1, 0) / kBC : 0;
+    const int n_left = SINKS ? min(n_tiles, n_sink + max(max(left_tiles, n_sink) - first_tile, 0)) : min(n_tiles, left_tiles);
 
     // ---- global -> LDS tile loads (no staging registers, no LDS write instructions) --------
     // Load instruction i of wave w fills LDS chunks [64*(w + 4i), +64) of a tile; lane l owns
@@ -398,9 +413,11 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
     };
 
     // accumulator register r of an S^T block <-> key key_base + 8*(r/4) + 4*h + r%4
-    auto key_ok = [&](int key_base, int r) __attribute__((always_inline)) {
+    // (sink: in one of the tiles of the sinks)
+    auto key_ok = [&](int key_base, int r, bool sink = false) __attribute__((always_inline)) {
         const int key = key_base + 8 * (r >> 2) + 4 * h + (r & 3);
-        return key < Tv && (!CAUSAL || key <= my_row + off) && (!WINDOW || key >= row_lo) && !no_tiles;
+        const bool in_window = !WINDOW || (SINKS && sink ? key < n_sink_keys : key >= row_lo);
+        return key < Tv && (!CAUSAL || key <= my_row + off) && in_window && !no_tiles;
     };
 
     // d1 / d2 are accumulated by MFMAs as well: Ones(32 x 16 keys) x P^T gives a block whose
@@ -445,14 +462,14 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
 
     // P1 = exp2(S1*scale - m_ref), P2 = P1*S2 for one key block, left as packed bf16 MFMA
     // operands (two groups of 16 keys).
-    auto probs = [&](auto masked_tag, int key_base, f32x16 &s1, f32x16 &s2, u32x4(&pb1)[2],
+    auto probs = [&](auto masked_tag, int key_base, bool sink, f32x16 &s1, f32x16 &s2, u32x4(&pb1)[2],
                      u32x4(&pb2)[2]) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked_tag)::value;
         const float neg_m = m_ref == kNegInf ? 0.f : -m_ref;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             float p1 = fast_exp2(fmaf(s1[r], row_scale, neg_m));
-            if constexpr (MASKED) p1 = key_ok(key_base, r) ? p1 : 0.f;
+            if constexpr (MASKED) p1 = key_ok(key_base, r, sink) ? p1 : 0.f;
             s1[r] = p1;
             // s2 is finite (rows past the last key re-read it) and P1 = 0 where masked
             if constexpr (USE_R) s2[r] = p1 * s2[r];
@@ -518,9 +535,9 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
     };
 
     // does this wave see any key of the block starting at key_base?
-    auto block_visible = [&](int key_base) __attribute__((always_inline)) {
+    auto block_visible = [&](int key_base, bool sink) __attribute__((always_inline)) {
         return key_base < Tv && (!CAUSAL || key_base <= row0 + WROWS - 1 + off) &&
-               (!WINDOW || key_base + kKB > row0 + off - p.window + 1);
+               (!WINDOW || (SINKS && sink) || key_base + kKB > row0 + off - p.window + 1);
     };
 
     u32x4 pb1[2], pb2[2];
@@ -609,15 +626,25 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
         return u32x4{pack_bf16(s[8 * j + 0], s[8 * j + 1]), pack_bf16(s[8 * j + 2], s[8 * j + 3]),
                      pack_bf16(s[8 * j + 4], s[8 * j + 5]), pack_bf16(s[8 * j + 6], s[8 * j + 7])};
     };
-    auto pipeline_step = [&](auto masked_tag, auto dma_tag, int key_base_cur, int key_base_next, const u32x4 *tk_next,
+    // bounds of this lane's keys in a block, as offsets; sink: the block is in one of the tiles of the sinks
+    auto key_bounds = [&](int key_base, bool sink, int &lim, int &lo) __attribute__((always_inline)) {
+        lim = (SINKS && sink ? min(row_lim, n_sink_keys - 1) : row_lim) - key_base - 4 * h;
+        lo = (SINKS && sink ? 0 : row_lo) - key_base - 4 * h;
+    };
+    auto pipeline_step = [&](auto masked_tag, auto dma_tag, int key_base_cur, int key_base_next, bool sink_cur, bool sink_next, const u32x4 *tk_next,
                              const unsigned short *tv_cur, const u32x4 *tk_after, f32x16 &sc1,
                              f32x16 &sc2, f32x16 &sn1, f32x16 &sn2) __attribute__((always_inline)) {
         int lim_cur, lim_next, lo_cur, lo_next;  // current block, next block
         float neg_m;
-        lim_cur = row_lim - key_base_cur - 4 * h;
-        lim_next = row_lim - key_base_next - 4 * h;
-        lo_cur = row_lo - key_base_cur - 4 * h;
-        lo_next = row_lo - key_base_next - 4 * h;
+        if constexpr (SINKS) {
+            key_bounds(key_base_cur, sink_cur, lim_cur, lo_cur);
+            key_bounds(key_base_next, sink_next, lim_next, lo_next);
+        } else {
+            lim_cur = row_lim - key_base_cur - 4 * h;
+            lim_next = row_lim - key_base_next - 4 * h;
+            lo_cur = row_lo - key_base_cur - 4 * h;
+            lo_next = row_lo - key_base_next - 4 * h;
+        }
         neg_m = -m_ref;
         constexpr int SLOTS1 = 2 * KSTEPS;               // phase 1: one slot per score MFMA
         constexpr bool DMA = decltype(dma_tag)::value;  // this step also fetches tile (dma_tk, dma_tv)
@@ -751,6 +778,13 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
         if constexpr (SPARSE) {  // (the clamping form only: it needs no per-lane offsets kept alive)
 #pragma unroll
             for (int t = 0; t < kDist; ++t) dma_tile(tile_at(t), t);
+        } else if constexpr (SINKS) {  // (the second tile may be the last one, or one behind the keys)
+#pragma unroll
+            for (int t = 0; t < kDist; ++t)
+                if ((tile_at(t) + 1) * kBC <= Tk)  // workgroup-uniform
+                    dma_full_tile(tile_at(t), t);
+                else
+                    dma_tile(tile_at(t), t);
         } else if (Tk >= kDist * kBC) {  // workgroup-uniform
 #pragma unroll
             for (int t = 0; t < kDist; ++t) dma_full_tile(t, t);
@@ -867,7 +901,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
 #pragma unroll
             for (int ks = 0; ks < KSTEPS; ++ks) s0 = mfma32(k_block_ptr(0, 0)[2 * ks], qf[ks], s0);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, key_ok(0, r) ? s0[r] : kNegInf);
+            for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, key_ok(0, r, true) ? s0[r] : kNegInf);
             if constexpr (WINDOW) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) tall = fmaxf(tall, s0[r]);
@@ -889,7 +923,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
             }
         } else {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, key_ok(kb0, r) ? sa1[r] : kNegInf);
+            for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, key_ok(kb0, r, true) ? sa1[r] : kNegInf);
         }
         tmax = halves_max(tmax);
         if constexpr (WINDOW || SPARSE) {
@@ -904,8 +938,12 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
         }
         m_ref = tmax * row_scale;
         neg_m = -m_ref;
-        lim0 = row_lim - kb0 - half * kKB - 4 * h;
-        lo0 = row_lo - kb0 - half * kKB - 4 * h;
+        if constexpr (SINKS) {
+            key_bounds(kb0 + half * kKB, true, lim0, lo0);
+        } else {
+            lim0 = row_lim - kb0 - half * kKB - 4 * h;
+            lo0 = row_lo - kb0 - half * kKB - 4 * h;
+        }
 #pragma unroll
         for (int sl = 0; sl < 12; ++sl)
             exp_stages(std::true_type{}, std::false_type{}, sa1, sa2, 0, sl, 0, 12, neg_m, lim0, lo0, msum1, msum2);
@@ -913,22 +951,23 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
         if constexpr (USE_R) pb2[0] = pack_group(sa2, 0);
     }
     // kt: key tile in `stage`, kt_next: key tile in `next_stage` (kt + 1 unless block-sparse)
-    auto tile_steps = [&](auto masked_tag, auto dma_tag, int kt, int kt_next, int stage, int next_stage, f32x16 &sa1,
+    // sink, sink_next: SINKS, whether they are tiles of the sinks
+    auto tile_steps = [&](auto masked_tag, auto dma_tag, int kt, int kt_next, bool sink, bool sink_next, int stage, int next_stage, f32x16 &sa1,
                           f32x16 &sa2, f32x16 &sb1, f32x16 &sb2) __attribute__((always_inline)) {
         if constexpr (PAIR) {
             // block (kt, half) -> P, PV; scores of (kt_next, half), whose first fragments are read now
             const u32x4 *tk_next = k_block_ptr(next_stage, half);
 #pragma unroll
             for (int f = 0; f < kLookAhead; ++f) load_kfrag(tk_next, f);
-            pipeline_step(masked_tag, dma_tag, kt * kBC + half * kKB, kt_next * kBC + half * kKB, tk_next,
+            pipeline_step(masked_tag, dma_tag, kt * kBC + half * kKB, kt_next * kBC + half * kKB, sink, sink_next, tk_next,
                           v_block_ptr(stage, half), nullptr, sa1, sa2, sb1, sb2);
             return;
         }
         // block (kt,0) -> P, PV; scores of (kt,1); K fragments of (kt_next,0); loads of the tile after
-        pipeline_step(masked_tag, dma_tag, kt * kBC, kt * kBC + kKB, k_block_ptr(stage, 1),
+        pipeline_step(masked_tag, dma_tag, kt * kBC, kt * kBC + kKB, sink, sink, k_block_ptr(stage, 1),
                       v_block_ptr(stage, 0), k_block_ptr(next_stage, 0), sa1, sa2, sb1, sb2);
         // block (kt,1) -> P, PV; scores of (kt_next,0); K fragments of (kt_next,1)
-        pipeline_step(masked_tag, std::false_type{}, kt * kBC + kKB, kt_next * kBC, k_block_ptr(next_stage, 0),
+        pipeline_step(masked_tag, std::false_type{}, kt * kBC + kKB, kt_next * kBC, sink, sink_next, k_block_ptr(next_stage, 0),
                       v_block_ptr(stage, 1), k_block_ptr(next_stage, 1), sb1, sb2, sa1, sa2);
     };
     // One tile of the pipeline with per-lane key masks. Blocks a wave cannot see at all
@@ -945,7 +984,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
             else
                 dma_tile(k2, free_stage);
         }
-        tile_steps(std::true_type{}, std::false_type{}, tile_at(kt), tile_at(kt + 1), stage, next_stage, sa1, sa2, sb1, sb2);
+        tile_steps(std::true_type{}, std::false_type{}, tile_at(kt), tile_at(kt + 1), kt < n_sink, kt + 1 < n_sink, stage, next_stage, sa1, sa2, sb1, sb2);
         stage = next_stage;
     };
     // PAIR: tiles go by twos, as a step hands its score registers over to the next one in the other set; the
@@ -965,8 +1004,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
     if constexpr (WINDOW) masked_tiles(kt, PAIR ? min((n_left + 1) & ~1, n_tiles & ~1) : n_left);
     // Tiles whose keys -- and those of the tile after -- are visible to every row: no masks, a
     // branch-free body. (A step also prepares the lower half of the NEXT block, hence the -1.)
-    dma_tk = (const char *)kbase + (kt + kDist) * k_tile_bytes;
-    dma_tv = (const char *)vbase + (kt + kDist) * v_tile_bytes;
+    dma_tk = (const char *)kbase + (SINKS ? tile_at(kt + kDist) : kt + kDist) * k_tile_bytes;
+    dma_tv = (const char *)vbase + (SINKS ? tile_at(kt + kDist) : kt + kDist) * v_tile_bytes;
     auto full_tile = [&](int kt, f32x16 &sa1, f32x16 &sa2, f32x16 &sb1, f32x16 &sb2)
                          __attribute__((always_inline)) {
         const int next_stage = stage == STAGES - 1 ? 0 : stage + 1;
@@ -981,7 +1020,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
             dma_tk = (const char *)kbase + k2 * k_tile_bytes;
             dma_tv = (const char *)vbase + k2 * v_tile_bytes;
         }
-        tile_steps(std::false_type{}, std::true_type{}, tile_at(kt), tile_at(kt + 1), stage, next_stage, sa1, sa2, sb1, sb2);
+        tile_steps(std::false_type{}, std::true_type{}, tile_at(kt), tile_at(kt + 1), false, false, stage, next_stage, sa1, sa2, sb1, sb2);
         if constexpr (!SPARSE) {
             dma_tk += k_tile_bytes;
             dma_tv += v_tile_bytes;
@@ -1157,12 +1196,13 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
             for (int kb = 0; kb < kBC / kKB; ++kb) {
                 if (PAIR && kb != half) continue;
                 const int key_base = tile_at(t) * kBC + kb * kKB;
-                if (!block_visible(key_base)) continue;
+                const bool sink = t < n_sink;
+                if (!block_visible(key_base, sink)) continue;
                 scores(stage, kb, sa1, sa2);
                 float tmax = kNegInf;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    tmax = fmaxf(tmax, key_ok(key_base, r) ? sa1[r] * row_scale : kNegInf);
+                    tmax = fmaxf(tmax, key_ok(key_base, r, sink) ? sa1[r] * row_scale : kNegInf);
                 tmax = halves_max(tmax);
                 const float m_new = fmaxf(m_ref, tmax);
                 const float m_use = m_new == kNegInf ? 0.f : m_new;
@@ -1182,7 +1222,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prefill_bf16_kernel(Pref
                         if constexpr (USE_R) o2[n][r] *= alpha;
                     }
                 }
-                probs(std::true_type{}, key_base, sa1, sa2, pb1, pb2);
+                probs(std::true_type{}, key_base, sink, sa1, sa2, pb1, pb2);
                 accumulate(stage, kb, pb1, pb2);
             }
             stage = next_stage;
@@ -1415,7 +1455,7 @@ static double launch_us(const LaunchCosts &c, int resident, int num_cus, double 
 // A launch without key ranges, `rows` query rows per workgroup
 static double unsplit_us(const PrefillParams &p, int num_cus, int rows, const LaunchCosts &c, int resident) {
     const double heads = (double)p.B * p.Hq, blocks = (p.T + rows - 1) / rows, all = (p.Tk + kBC - 1) / kBC;
-    const double span = p.window > 0 ? (p.window + rows - 1.0) / kBC + 1 : 1e30;
+    const double span = p.window > 0 ? (p.window + rows - 1.0) / kBC + 1 + (p.sinks + kBC - 1) / kBC : 1e30;
     // row block j (from 1) sees `before` + j * `step` tiles under a causal mask
     const double before = (p.Tk - p.T + kBC - 1) / kBC, step = rows / kBC, longest = std::min(all, span);
     double sum = blocks * longest;
@@ -1577,7 +1617,11 @@ static hipError_t launch_prefill_pair(const PrefillParams &p, hipStream_t stream
     const long long total = (long long)((p.T + 63) / 64) * p.Hq * p.B;
     if (total > 0x7fffffffLL) return hipErrorInvalidValue;
     const dim3 grid((unsigned)total), block(256);
-    if (p.prep.gamma_q != nullptr)
+    if (p.sinks > 0 && p.row_stats != nullptr)
+        hipLaunchKernelGGL((prefill_bf16_kernel<D, true, true, true, true, false, false, false, true, true>), grid, block, 0, stream, p);
+    else if (p.sinks > 0)
+        hipLaunchKernelGGL((prefill_bf16_kernel<D, true, true, true, false, false, false, false, true, true>), grid, block, 0, stream, p);
+    else if (p.prep.gamma_q != nullptr)
         hipLaunchKernelGGL((prefill_bf16_kernel<D, true, true, false, false, false, true, false, true>), grid, block, 0, stream, p);
     else if (p.row_stats != nullptr && p.window > 0)
         hipLaunchKernelGGL((prefill_bf16_kernel<D, true, true, true, true, false, false, false, true>), grid, block, 0, stream, p);
@@ -1602,6 +1646,15 @@ static hipError_t launch_prefill_dense(const PrefillParams &p, hipStream_t strea
             hipLaunchKernelGGL((prefill_bf16_kernel<D, true, true, false, false, false, true>), grid, block, 0, stream, p);
         else
             hipLaunchKernelGGL((prefill_bf16_kernel<D, true, false, false, false, false, true>), grid, block, 0, stream, p);
+        return hipGetLastError();
+    }
+    if (p.sinks > 0) {  // window and sinks (causal)
+        if (p.row_stats != nullptr)
+            hipLaunchKernelGGL((prefill_bf16_kernel<D, true, true, true, true, false, false, false, false, true>), grid, block, 0, stream, p);
+        else if (p.use_r)
+            hipLaunchKernelGGL((prefill_bf16_kernel<D, true, true, true, false, false, false, false, false, true>), grid, block, 0, stream, p);
+        else
+            hipLaunchKernelGGL((prefill_bf16_kernel<D, false, true, true, false, false, false, false, false, true>), grid, block, 0, stream, p);
         return hipGetLastError();
     }
     if (p.row_stats != nullptr && p.window > 0) {  // row cache + sliding window (causal, use_r)

@@ -272,8 +272,10 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float sc
 // WINDOW (sliding window, causal only): the key tiles before the window of the block's first row
 // are skipped by moving the key origin; the leading tiles that some row sees only in part take
 // the masked form of the pipeline, like the diagonal ones.
+// SINKS: the first p.sinks keys stay visible behind the window; the tiles are walked as in the forward (those of the
+// sinks, then those of the windows; a tile that holds both twice, once for its keys below p.sinks).
 // PAIR: see bwd_passes_kernel.
-template <int D, bool CAUSAL, bool WINDOW, bool SPARSE, bool PAIR>
+template <int D, bool CAUSAL, bool WINDOW, bool SPARSE, bool PAIR, bool SINKS>
 __device__ __forceinline__ void bwd_dq_dr(const PrefillBwdParams &p, const int id, u32x4 *lds) {
     static_assert(CAUSAL || !WINDOW, "a sliding window is causal");
     static_assert(!(SPARSE && WINDOW), "block lists and a sliding window do not combine");
@@ -317,7 +319,7 @@ __device__ __forceinline__ void bwd_dq_dr(const PrefillBwdParams &p, const int i
     }
     const int rb = CAUSAL ? nrb - 1 - rbi : rbi;  // heavy row blocks first
     // key tiles no row of this block sees (all keys before the window of its first row)
-    const int kt_skip = WINDOW ? max(rb * ROWS + (p.Tk - T) - p.window + 1, 0) / kTileRows : 0;
+    const int kt_skip = WINDOW && !SINKS ? max(rb * ROWS + (p.Tk - T) - p.window + 1, 0) / kTileRows : 0;
     const int Tk = p.Tk - kt_skip * kTileRows, off = Tk - T;  // keys from the first tile read on
     const int hk = hq / p.G;
     const int row0 = rb * ROWS + wr * 32, my_row = row0 + col;
@@ -412,13 +414,19 @@ __device__ __forceinline__ void bwd_dq_dr(const PrefillBwdParams &p, const int i
         }
         n_list = lo_i;
     }
+    const int n_sink_keys = SINKS ? min(p.sinks, key_end) : 0, n_sink = (n_sink_keys + kTileRows - 1) / kTileRows;
+    const int first_tile = SINKS ? max(max(rb * ROWS + off - p.window + 1, 0) / kTileRows, n_sink_keys / kTileRows) : 0;
     auto tile_at = [&](int i) __attribute__((always_inline)) {
         if constexpr (SPARSE)
             return min(max(tile_list[min(i, n_list - 1)], 0), (Tk - 1) / kTileRows);
+        else if constexpr (SINKS)
+            return i < n_sink ? i : i - n_sink + first_tile;
         else
             return i;
     };
-    const int n_tiles = SPARSE ? n_list : (key_end + kTileRows - 1) / kTileRows;
+    const int n_tiles = SPARSE  ? n_list
+                        : SINKS ? n_sink + (n_sink_keys < key_end ? (key_end + kTileRows - 1) / kTileRows - first_tile : 0)
+                                : (key_end + kTileRows - 1) / kTileRows;
     const int lim_row = CAUSAL ? min(my_row + off, Tk - 1) : Tk - 1;  // last key this lane's row sees
     if constexpr (SPARSE) {
         if (n_tiles == 0) {  // (workgroup-uniform) a row block that lists nothing: zero gradients
@@ -462,10 +470,11 @@ __device__ __forceinline__ void bwd_dq_dr(const PrefillBwdParams &p, const int i
     // consecutive slots so that a slot holds independent instructions only; the results replace
     // the scores: g1 in aa, g2 in s2. Register r holds key offset 8*(r/4) + r%4 (+ 4h, already
     // taken off lim). With a window a key counts iff 0 <= lim - offset < window: one unsigned compare.
-    const unsigned wspan = WINDOW ? (unsigned)p.window : 0u;
+    // (SINKS: the keys of this lane's window that are no sinks; in a tile of the sinks every key up to lim)
+    const unsigned wspan = SINKS ? (unsigned)max(min(p.window, lim_row + 1 - n_sink_keys), 0) : WINDOW ? (unsigned)p.window : 0u;
     float dl[8];
     auto elem_stages = [&](auto masked_tag, f32x16 &s1, f32x16 &s2, f32x16 &aa, int r0, int slot, int slot0,
-                           int n_slots, int lim) __attribute__((always_inline)) {
+                           int n_slots, int lim, unsigned span) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked_tag)::value;
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
@@ -483,7 +492,7 @@ __device__ __forceinline__ void bwd_dq_dr(const PrefillBwdParams &p, const int i
             if constexpr (MASKED)
                 if (slot == first + 2) {
                     if constexpr (WINDOW)
-                        s1[r] = ((unsigned)(lim - (8 * (r >> 2) + (r & 3))) < wspan) ? s1[r] : 0.f;
+                        s1[r] = ((unsigned)(lim - (8 * (r >> 2) + (r & 3))) < span) ? s1[r] : 0.f;
                     else
                         s1[r] = (8 * (r >> 2) + (r & 3) <= lim) ? s1[r] : 0.f;
                 }
@@ -499,9 +508,14 @@ __device__ __forceinline__ void bwd_dq_dr(const PrefillBwdParams &p, const int i
     // one out). Each brings two wait states for its operands; the first vector read of a block
     // comes in slot 1 of phase 2, behind two more MFMAs: by then the block's last MFMA retired.
     u32x4 pg1[2], pg2[2];
-    auto pipeline_step = [&](auto masked_tag, auto dma_tag, int key_base_cur, int key_base_next, const u32x4 *next_blk, const u32x4 *cur_blk, const u32x4 *after_blk,
+    // last key of this lane's row in the tiles of the sinks or in the others
+    auto limit = [&](bool sink) __attribute__((always_inline)) { return SINKS && sink ? min(lim_row, n_sink_keys - 1) : lim_row; };
+    auto span_of = [&](bool sink) __attribute__((always_inline)) { return SINKS && sink ? 0x7fffffffu : wspan; };
+    // (sink_cur, sink_next: SINKS, the block is in one of the tiles of the sinks)
+    auto pipeline_step = [&](auto masked_tag, auto dma_tag, int key_base_cur, int key_base_next, bool sink_cur, bool sink_next, const u32x4 *next_blk, const u32x4 *cur_blk, const u32x4 *after_blk,
                              f32x16 &c1, f32x16 &c2, f32x16 &ca, f32x16 &n1, f32x16 &n2, f32x16 &na) __attribute__((always_inline)) {
-        const int lim_cur = lim_row - key_base_cur - 4 * h, lim_next = lim_row - key_base_next - 4 * h;
+        const int lim_cur = limit(sink_cur) - key_base_cur - 4 * h, lim_next = limit(sink_next) - key_base_next - 4 * h;
+        const unsigned span_cur = span_of(sink_cur), span_next = span_of(sink_next);
         constexpr int SLOTS1 = 3 * KSTEPS, SLOTS2 = 4 * NDB;
         constexpr bool DMA = decltype(dma_tag)::value;  // this step also fetches tile (dma_k, dma_v)
         static_assert(2 * TL::NDMA <= SLOTS1, "one tile load per slot");
@@ -522,7 +536,7 @@ __device__ __forceinline__ void bwd_dq_dr(const PrefillBwdParams &p, const int i
                 else mfma32_scores<true, kAccB<D>>(na, f1[2 * ks + 1], gf[ks]);
                 prefetch(2 * ks + 1, next_blk, cur_blk, after_blk);
             }
-            elem_stages(masked_tag, c1, c2, ca, 8, sl, 0, SLOTS1, lim_cur);
+            elem_stages(masked_tag, c1, c2, ca, 8, sl, 0, SLOTS1, lim_cur, span_cur);
             if (sl == SLOTS1 - 2) pg1[1] = pack_group(ca, 1);
             if (sl == SLOTS1 - 1) pg2[1] = pack_group(c2, 1);
             __builtin_amdgcn_sched_barrier(0);
@@ -537,7 +551,7 @@ __device__ __forceinline__ void bwd_dq_dr(const PrefillBwdParams &p, const int i
             } else {
                 dr[n] = mfma32(f2[f], pg2[j], dr[n]);
             }
-            elem_stages(masked_tag, n1, n2, na, 0, sl, 1, SLOTS2, lim_next);
+            elem_stages(masked_tag, n1, n2, na, 0, sl, 1, SLOTS2, lim_next, span_next);
             if (sl == SLOTS2 - 2) nb1 = pack_group(na, 0);
             if (sl == SLOTS2 - 1) nb2 = pack_group(n2, 0);
             __builtin_amdgcn_sched_barrier(0);
@@ -570,7 +584,7 @@ __device__ __forceinline__ void bwd_dq_dr(const PrefillBwdParams &p, const int i
 #pragma unroll
         for (int sl = 0; sl < 12; ++sl)
             elem_stages(std::true_type{}, a1, a2, a3, 0, sl, 0, 12,
-                        lim_row - tile_at(0) * kTileRows - half * kBlk - 4 * h);
+                        limit(true) - tile_at(0) * kTileRows - half * kBlk - 4 * h, span_of(true));
         pg1[0] = pack_group(a3, 0);
         pg2[0] = pack_group(a2, 0);
         if constexpr (!PAIR)
@@ -594,16 +608,16 @@ __device__ __forceinline__ void bwd_dq_dr(const PrefillBwdParams &p, const int i
             const u32x4 *next_blk = k_block(next_stage, half);
 #pragma unroll
             for (int f = 0; f < LA; ++f) load_f1(next_blk, f);
-            pipeline_step(masked_tag, dma_tag, key_base + half * kBlk, key_base_after + half * kBlk, next_blk,
+            pipeline_step(masked_tag, dma_tag, key_base + half * kBlk, key_base_after + half * kBlk, t < n_sink, t + 1 < n_sink, next_blk,
                           k_block(stage, half), nullptr, a1, a2, a3, b1, b2, b3);
             stage = next_stage;
             return;
         }
         // block (t, 0) -> g, dQ / dR; scores of (t, 1); fragments of (t + 1, 0)
-        pipeline_step(masked_tag, dma_tag, key_base, key_base + kBlk, k_block(stage, 1), k_block(stage, 0),
+        pipeline_step(masked_tag, dma_tag, key_base, key_base + kBlk, t < n_sink, t < n_sink, k_block(stage, 1), k_block(stage, 0),
                       k_block(next_stage, 0), a1, a2, a3, b1, b2, b3);
         // block (t, 1) -> g, dQ / dR; scores of (t + 1, 0); fragments of (t + 1, 1)
-        pipeline_step(masked_tag, std::false_type{}, key_base + kBlk, key_base_after, k_block(next_stage, 0),
+        pipeline_step(masked_tag, std::false_type{}, key_base + kBlk, key_base_after, t < n_sink, t + 1 < n_sink, k_block(next_stage, 0),
                       k_block(stage, 1), k_block(next_stage, 1), b1, b2, b3, a1, a2, a3);
         stage = next_stage;
     };
@@ -625,15 +639,17 @@ __device__ __forceinline__ void bwd_dq_dr(const PrefillBwdParams &p, const int i
     // next block) -- every row of the workgroup sees: no masks; then the diagonal / tail tiles.
     // The unmasked loop also stops two short of the last complete tile, so that the tile it
     // fetches exists completely.
-    const int n_full = SPARSE ? 0 : min(CAUSAL ? (rb * ROWS + off + 1) / kTileRows : Tk / kTileRows, Tk / kTileRows - 1);
+    const int n_full = SPARSE ? 0 : min(CAUSAL ? (rb * ROWS + off + 1) / kTileRows : Tk / kTileRows, Tk / kTileRows - 1) +
+                                        (SINKS ? n_sink - first_tile : 0);
     int t = 0;
     if constexpr (WINDOW) {
         // leading tiles that hold a key before the window of the block's last row
-        const int n_left = min(n_tiles, max(rb * ROWS + ROWS + off - p.window + kTileRows - 1, 0) / kTileRows);
+        const int left_tiles = max(rb * ROWS + ROWS + off - p.window + kTileRows - 1, 0) / kTileRows;
+        const int n_left = min(n_tiles, SINKS ? n_sink + max(max(left_tiles, n_sink) - first_tile, 0) : left_tiles);
         run_tiles(std::true_type{}, std::false_type{}, t, n_left, [] {});
     }
-    dma_k = (const char *)kbase + (t + 2) * k_tile_bytes;
-    dma_v = (const char *)vbase + (t + 2) * v_tile_bytes;
+    dma_k = (const char *)kbase + (SINKS ? tile_at(t + 2) : t + 2) * k_tile_bytes;
+    dma_v = (const char *)vbase + (SINKS ? tile_at(t + 2) : t + 2) * v_tile_bytes;
     // (PAIR: in pairs of tiles, an odd one is left to the masked form)
     run_tiles(std::false_type{}, std::true_type{}, t, PAIR ? t + (max(n_full - 1 - t, 0) & ~1) : n_full - 1, [&] {
         dma_k += k_tile_bytes;
@@ -687,6 +703,13 @@ struct ColumnList {
     }
 };
 
+// SINKS: where the sums of one part of a key block that holds sinks are, in float4 from p.sink_sums on: [32 keys][dK | dV]
+// [accumulator block n][q4][lane]
+template <int D, int KEYS>
+__device__ __forceinline__ int64_t sink_record(const PrefillBwdParams &p, int pair, int cb, int part) {
+    return (((int64_t)pair * p.sink_blocks + cb) * p.sink_parts + part) * (KEYS * D / 2);
+}
+
 // ---- column pass: dK, dV ----------------------------------------------------------------------
 // The same software pipeline over 32-row blocks of the streamed (Q, R, dO) tiles:
 //   phase 1 : the 3 * d/16 score MFMAs of the NEXT row block (S1 = Q K^T, S2 = R K^T, A = dO V^T
@@ -698,9 +721,13 @@ struct ColumnList {
 // one float4 per register, read one slot ahead of their use.
 // WINDOW: key j is seen by the rows [j - off, j - off + window) only; the row tiles past the
 // last of them are not visited, those cut by the upper edge take the masked form.
+// SINKS: a key below p.sinks is seen by every row from its own position on. A block that holds such keys would walk the
+// rows of the whole sequence while the others walk a window's, so its row tiles are dealt in parts of
+// p.sink_part_tiles to workgroups of their own, whose sums go to the workspace in fp32 (sink_combine_kernel adds
+// them up). part: which of them.
 // PAIR: see bwd_passes_kernel.
-template <int D, bool CAUSAL, bool WINDOW, bool SPARSE, bool PAIR>
-__device__ __forceinline__ void bwd_dk_dv(const PrefillBwdParams &p, const int cb, const int hk, const int b, u32x4 *lds) {
+template <int D, bool CAUSAL, bool WINDOW, bool SPARSE, bool PAIR, bool SINKS>
+__device__ __forceinline__ void bwd_dk_dv(const PrefillBwdParams &p, const int cb, const int hk, const int b, const int part, u32x4 *lds) {
     static_assert(CAUSAL || !WINDOW, "a sliding window is causal");
     static_assert(!(SPARSE && WINDOW), "block lists and a sliding window do not combine");
     using TL = BwdTile<D>;
@@ -733,13 +760,19 @@ __device__ __forceinline__ void bwd_dk_dv(const PrefillBwdParams &p, const int c
     const BwdLaneOffsets<D> lo(lane);
 
     // row tiles that hold a row which sees a key of this block: rows i >= key - off
-    const int rt_lo = CAUSAL ? max(cb * KEYS - off, 0) / kTileRows : 0;
+    int rt_lo = CAUSAL ? max(cb * KEYS - off, 0) / kTileRows : 0;
     const int n_rt = (T + kTileRows - 1) / kTileRows;
+    const bool with_sinks = SINKS && cb * KEYS < p.sinks;
     // window: rows up to (last key of the block) - off + window - 1. A block no row sees at all
     // (keys before every window) still visits one tile, with every pair masked: zeros.
-    const int rt_hi =
+    int rt_hi =
         WINDOW ? max(min(n_rt, (min(cb * KEYS + KEYS - 1, Tk - 1) - off + p.window + kTileRows - 1) / kTileRows), rt_lo + 1)
                : n_rt;
+    if (with_sinks) {  // (workgroup-uniform)
+        rt_lo += part * p.sink_part_tiles;
+        rt_hi = min(rt_lo + p.sink_part_tiles, n_rt);
+        if (rt_lo >= rt_hi) return;
+    }
     const int per_head = rt_hi - rt_lo;
     int n_items = per_head * G;  // (head of the group, row tile)
     // Row tiles in which every (row, key) pair counts -- all rows exist and see every key of the
@@ -747,8 +780,12 @@ __device__ __forceinline__ void bwd_dk_dv(const PrefillBwdParams &p, const int c
     // puts those of all heads first, so that the two forms of the pipeline are two loops.
     const int rt_full_lo = max(CAUSAL ? max(cb * KEYS + KEYS - 1 - off + kTileRows - 1, 0) / kTileRows : 0, rt_lo);
     // (window: the first key of the block is the first to drop out of a row's window)
-    const int rt_full_hi =
-        (cb + 1) * KEYS <= Tk ? (WINDOW ? min(T, max(cb * KEYS - off + p.window, 0)) : T) / kTileRows : 0;
+    // (sinks: the first key behind them, if it is in the block)
+    const int first_out = SINKS ? max(cb * KEYS, p.sinks) : cb * KEYS;
+    const bool never_out = SINKS && first_out >= (cb + 1) * KEYS;
+    int rt_full_hi =
+        (cb + 1) * KEYS <= Tk ? (WINDOW && !never_out ? min(T, max(first_out - off + p.window, 0)) : T) / kTileRows : 0;
+    if (with_sinks) rt_full_hi = min(rt_full_hi, rt_hi);
     const int full_per_head = max(rt_full_hi - rt_full_lo, 0);
     const int n_full_items = full_per_head * G;
     // Block-sparse: the items are, head after head of the group, the two row tiles of every row
@@ -988,7 +1025,7 @@ __device__ __forceinline__ void bwd_dk_dv(const PrefillBwdParams &p, const int c
         // (block-sparse: a row block that does not list this wave's key tile -- none of its rows)
         const bool listed = !SPARSE || PAIR || ((flags >> (w >> 1)) & 1) != 0;
         const int first_row = (my_key < Tk && listed) ? (CAUSAL ? max(my_key - off, 0) : 0) : T;  // no row at all
-        const int end_row = WINDOW ? min(T, max(my_key - off + p.window, 0)) : T;
+        const int end_row = WINDOW && !(SINKS && my_key < p.sinks) ? min(T, max(my_key - off + p.window, 0)) : T;
         const int lo_off = max(first_row - row_base - 4 * h, 0);
         const int hi_off = end_row - row_base - 4 * h;
         neg_lo = -lo_off;
@@ -1143,6 +1180,20 @@ __device__ __forceinline__ void bwd_dk_dv(const PrefillBwdParams &p, const int c
     __syncthreads();                                  // the ring is free
 
     if constexpr (PAIR) swap_halves<D>(dk, dv, w, half, lane, lds);
+    if constexpr (SINKS)
+        if (with_sinks) {  // (stores of a wave are one contiguous KB)
+            f32x4 *rec = (f32x4 *)p.sink_sums + sink_record<D, KEYS>(p, b * p.Hkv + hk, cb, part) + (wk * 2 * NDB * 4) * 64 + lane;
+#pragma unroll
+            for (int n = 0; n < NDB; ++n)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) {
+                    if (!PAIR || half == 0)
+                        rec[(n * 4 + q4) * 64] = f32x4{dk[n][4 * q4], dk[n][4 * q4 + 1], dk[n][4 * q4 + 2], dk[n][4 * q4 + 3]};
+                    if (!PAIR || half == 1)
+                        rec[((NDB + n) * 4 + q4) * 64] = f32x4{dv[n][4 * q4], dv[n][4 * q4 + 1], dv[n][4 * q4 + 2], dv[n][4 * q4 + 3]};
+                }
+            return;
+        }
     __bf16 *dk_base = (__bf16 *)p.dk + b * p.dks[0] + hk * p.dks[1] + key0 * p.dks[2];
     __bf16 *dv_base = (__bf16 *)p.dv + b * p.dvs[0] + hk * p.dvs[1] + key0 * p.dvs[2];
     if (!PAIR || half == 0) store_rows<D>(dk, 1.f, dk_base, p.dks[2], Tk - key0, w, lane, lds);
@@ -1163,7 +1214,7 @@ __device__ __forceinline__ void bwd_dk_dv(const PrefillBwdParams &p, const int c
 // workgroup's keys are one key tile, so that nobody walks a tile that only its neighbour lists. Against that a
 // tile serves half the work per load, and the first operands of a step are read only behind its barrier.
 // Which form: backward_plan.
-template <int D, bool CAUSAL, bool WINDOW, bool SPARSE, bool PAIR_C, bool PAIR_R>
+template <int D, bool CAUSAL, bool WINDOW, bool SPARSE, bool PAIR_C, bool PAIR_R, bool SINKS = false>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void bwd_passes_kernel(PrefillBwdParams p, int n_columns) {
     __shared__ u32x4 lds[kBwdLdsChunks<D>];
     const int id = blockIdx.x;
@@ -1176,13 +1227,55 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void bwd_passes_kernel(Prefil
         }
     }
     if (id >= n_columns) {
-        bwd_dq_dr<D, CAUSAL, WINDOW, SPARSE, PAIR_R>(p, id - n_columns, lds);
+        bwd_dq_dr<D, CAUSAL, WINDOW, SPARSE, PAIR_R, SINKS>(p, id - n_columns, lds);
         return;
     }
     if constexpr (D == 64) __builtin_amdgcn_s_setprio(2);  // the longer ones first, where two share a unit
-    int cb, hk, b;
+    int cb, hk, b, part = 0;
     column_item(p, id, cb, hk, b);
-    bwd_dk_dv<D, CAUSAL, WINDOW, SPARSE, PAIR_C>(p, cb, hk, b, lds);
+    if constexpr (SINKS) {  // (the parts of the blocks with sinks come first: they are the longest)
+        const int parts = p.sink_blocks * p.sink_parts;
+        if (cb < parts) {
+            part = cb % p.sink_parts;
+            cb /= p.sink_parts;
+        } else {
+            cb += p.sink_blocks - parts;
+        }
+    }
+    bwd_dk_dv<D, CAUSAL, WINDOW, SPARSE, PAIR_C, SINKS>(p, cb, hk, b, part, lds);
+}
+
+// SINKS: dK and dV of the key blocks that hold sinks, from the sums of their parts. A wave adds up 32 keys x 32
+// dimensions of one of the two, lane (key, h) dimensions 8 q4 + 4 h .. + 3 as the records have them; bound by reading them.
+template <int D, int KEYS>
+__global__ __launch_bounds__(256) void sink_combine_kernel(PrefillBwdParams p) {
+    constexpr int NDB = D / 32;
+    const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
+    int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // (pair, block, 32 keys, dK or dV, n)
+    const int n = (int)(id % NDB);
+    id /= NDB;
+    const int which = (int)(id % 2);
+    id /= 2;
+    const int wk = (int)(id % (KEYS / 32));
+    id /= KEYS / 32;
+    const int cb = (int)(id % p.sink_blocks);
+    id /= p.sink_blocks;
+    if (id >= (int64_t)p.B * p.Hkv) return;  // (whole waves)
+    const int pair = (int)id, b = pair / p.Hkv, hk = pair - b * p.Hkv, key = cb * KEYS + wk * 32 + col;
+    const int n_rt = (p.T + kTileRows - 1) / kTileRows, rt_lo = max(cb * KEYS - (p.Tk - p.T), 0) / kTileRows;
+    const int parts = (n_rt - rt_lo + p.sink_part_tiles - 1) / p.sink_part_tiles;
+    f32x4 sum[4] = {};
+    const f32x4 *rec = (const f32x4 *)p.sink_sums + sink_record<D, KEYS>(p, pair, cb, 0) + ((wk * 2 + which) * NDB + n) * 4 * 64 + lane;
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i, rec += KEYS * D / 2)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) sum[q4] += rec[q4 * 64];
+    if (key >= p.Tk) return;
+    const int64_t *st = which ? p.dvs : p.dks;
+    __bf16 *row = (__bf16 *)(which ? p.dv : p.dk) + b * st[0] + hk * st[1] + (int64_t)key * st[2] + 32 * n + 4 * h;
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4)
+        *(u32x2 *)(row + 8 * q4) = u32x2{pack_bf16(sum[q4][0], sum[q4][1]), pack_bf16(sum[q4][2], sum[q4][3])};
 }
 
 // The form of a launch, from estimates in us: `chain`, the longest column workgroup (2.4 us per 64 rows x 128
@@ -1214,6 +1307,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void bwd_passes_kernel(Prefil
 struct BackwardPlan {
     bool pair_c, pair_r;
     int32_t list_limit;  // > 0: pair_c up to so many entries in the row lists
+    int32_t sink_part_tiles;  // row tiles per part of a key block that holds sinks
 };
 static BackwardPlan backward_plan(const PrefillBwdParams &p, int num_cus) {
     const bool sparse = p.sparse_row_ptr != nullptr, windowed = p.causal && p.window > 0 && p.window < p.Tk;
@@ -1221,9 +1315,9 @@ static BackwardPlan backward_plan(const PrefillBwdParams &p, int num_cus) {
     const double T = p.T, Tk = p.Tk, heads = (double)p.B * p.Hq, kv_heads = (double)p.B * p.Hkv, G = p.G;
     const double row_blocks = std::ceil(T / 128), key_blocks = std::ceil(Tk / 128);
     // tiles that the longest column (row) workgroup walks, per head, and cells of 64 x 128 in all
-    const double span = windowed ? (p.window + 127.0) / 64 : 1e30;
+    const double span = windowed ? (p.window + 127.0) / 64 + std::ceil(p.sinks / 64.0) : 1e30;
     const double col_tiles = std::min(std::ceil(T / 64), span), row_tiles = std::min(std::ceil(Tk / 64), span);
-    const double pairs = windowed ? T * p.window : p.causal ? T * (Tk - T) + T * T / 2 : T * Tk;
+    const double pairs = windowed ? T * ((double)p.window + p.sinks) : p.causal ? T * (Tk - T) + T * T / 2 : T * Tk;
     const double cells = pairs / (64 * 128);
     const double chain = G * col_tiles * per_item + fixed, row_chain = row_tiles * per_tile + fixed;
     const double load = (heads * ((cells + (p.causal ? key_blocks : 0)) * per_item + (cells + (p.causal ? row_blocks : 0)) * per_tile) +
@@ -1253,6 +1347,8 @@ static BackwardPlan backward_plan(const PrefillBwdParams &p, int num_cus) {
         const double limit = (p.d == 128 ? 0.75 : 0.8) * seen * p.sparse_batch * p.sparse_heads;
         plan.list_limit = (int32_t)std::min(std::max(limit, 1.0), 2147483647.0);
     }
+    // (as long as the windows' chains, or half of what every unit has to do anyway: fewer records)
+    plan.sink_part_tiles = (int32_t)std::min(std::max(col_tiles, (0.5 * load - fixed) / (G * per_item)), std::ceil(T / 64));
     plan.pair_r = plan.pair_c && !sparse && p.window <= 0 && 3 * row_tiles > 2 * G * col_tiles;
     return plan;
 }
@@ -1260,6 +1356,20 @@ static BackwardPlan backward_plan(const PrefillBwdParams &p, int num_cus) {
 int32_t backward_form_bf16(const PrefillBwdParams &p, int num_cus) {
     const BackwardPlan plan = backward_plan(p, num_cus);
     return (plan.pair_c ? 64 : 128) + 256 * (plan.pair_r ? 64 : 128) + (plan.list_limit > 0 ? 65536 : 0);
+}
+
+// Parts of the key blocks with sinks, and the bytes of their sums
+static int64_t plan_sinks(PrefillBwdParams &p, const BackwardPlan &plan) {
+    const int keys = plan.pair_c ? 64 : 128, n_rt = (p.T + kTileRows - 1) / kTileRows;
+    p.sink_part_tiles = std::max(plan.sink_part_tiles, 1);
+    p.sink_parts = (n_rt + p.sink_part_tiles - 1) / p.sink_part_tiles;
+    p.sink_blocks = (std::min(p.sinks, p.Tk) + keys - 1) / keys;
+    return (int64_t)p.B * p.Hkv * p.sink_blocks * p.sink_parts * keys * 2 * p.d * (int64_t)sizeof(float);
+}
+
+size_t backward_sinks_bytes_bf16(const PrefillBwdParams &p, int num_cus) {
+    PrefillBwdParams q = p;
+    return (size_t)plan_sinks(q, backward_plan(p, num_cus));
 }
 
 template <int D>
@@ -1290,6 +1400,22 @@ static hipError_t launch_bwd_d(const PrefillBwdParams &p, int num_cus, hipStream
         return err == hipSuccess && plan.list_limit > 0 ? run(causal, no, yes, no, no) : err;
     };
     if (p.sparse_row_ptr != nullptr) return p.causal ? lists(yes) : lists(no);  // (no window; checked by the caller)
+    if (p.sinks > 0) {  // (causal, with a window)
+        plan_sinks(q, plan);
+        auto sinks = [&](auto pair_c) {
+            constexpr bool PC = decltype(pair_c)::value;
+            constexpr int KEYS = PC ? 64 : 128;
+            const long long cols = columns(PC) + (long long)q.sink_blocks * (q.sink_parts - 1) * p.Hkv * p.B;
+            const long long waves = (long long)p.B * p.Hkv * q.sink_blocks * (KEYS / 32) * 2 * (D / 32);
+            if (cols + row_groups(false) > 0x7fffffffLL) return hipErrorInvalidValue;
+            hipLaunchKernelGGL((bwd_passes_kernel<D, true, true, false, PC, false, true>),
+                               dim3((unsigned)(cols + row_groups(false))), dim3(256), 0, stream, q, (int)cols);
+            if (hipError_t err = hipGetLastError()) return err;
+            hipLaunchKernelGGL((sink_combine_kernel<D, KEYS>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, q);
+            return hipGetLastError();
+        };
+        return plan.pair_c ? sinks(yes) : sinks(no);
+    }
     if (p.causal && p.window > 0)
         return plan.pair_c ? run(yes, yes, no, yes, no) : run(yes, yes, no, no, no);
     return p.causal ? dense(yes) : dense(no);
