@@ -12,7 +12,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB_PATH = os.path.join(PKG, "libparallax_hip.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 
-SOURCES = ["parallax_api.hip", "decode_bf16.hip", "decode_rows_bf16.hip", "decode_mla_bf16.hip", "decode_mla_wide_bf16.hip", "prefill_bf16.hip", "prefill_bwd_bf16.hip",
+SOURCES = ["parallax_api.hip", "decode_bf16.hip", "decode_rows_bf16.hip", "decode_rows_wide_bf16.hip", "decode_mla_bf16.hip", "decode_mla_wide_bf16.hip", "prefill_bf16.hip", "prefill_bwd_bf16.hip",
            "generic_f32.hip", "prefill_f32.hip", "block_lists.hip", "cache_pages.hip", "norm_rope.hip", "util_kernels.hip"]
 
 # packed-fp32 instructions are disabled for all device code (hipcc's host pass prints a
@@ -92,6 +92,11 @@ def _check_decode_assembly() -> None:
     bad = {n: c for n, c in _spills("decode_bf16.hip", "decode_bf16_kernel").items() if c > (16 if n.endswith(prep) else 0)}
     if bad:
         raise RuntimeError("decode_bf16.hip: register spills in a decode kernel (%s)" % bad)
+    # (a reload waits for all tile loads in front of it: forms of the wide kernel with 100 spilled took three times as long)
+    for src in ("decode_rows_bf16.hip", "decode_rows_wide_bf16.hip"):
+        bad = {n: c for n, c in _spills(src, "decode_rows").items() if c > 0}
+        if bad:
+            raise RuntimeError("%s: register spills in a decode kernel (%s)" % (src, bad))
 
 
 def _check_f32_assembly() -> None:
@@ -126,6 +131,8 @@ def build_library(extra_flags: list[str] | None = None, verbose: bool = True) ->
         objs = list(pool.map(lambda src: _compile(src, extra), SOURCES))
     _check_pipelined_assembly("prefill_bf16.hip", True)
     _check_pipelined_assembly("prefill_bwd_bf16.hip", False)
+    _check_pipelined_assembly("decode_rows_bf16.hip", False)
+    _check_pipelined_assembly("decode_rows_wide_bf16.hip", False)
     _check_pipelined_assembly("decode_mla_bf16.hip", False)
     _check_pipelined_assembly("decode_mla_wide_bf16.hip", False)
     _check_decode_assembly()

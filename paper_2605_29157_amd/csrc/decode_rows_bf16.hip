@@ -1,49 +1,33 @@
 // Split-KV Parallax decode for several rows whose key sets differ, bf16, gfx950: drafted nodes that see the cache and
-// their own ancestors (tree masks), and rows with a sliding window and a few first tokens that stay visible (sinks).
+// their own ancestors (tree masks), and rows with a sliding window and a few first tokens that stay visible (sinks). Here:
+// up to 16 columns (rows x heads of a GQA group); decode_rows_wide_bf16.hip has the kernel for more.
 //
 // What it computes: the forward of the paper (Sec. 3.1, Algorithm 1) over the key set J of each row,
 //     p = softmax_J(scale q.k),  u = rho.k,  o = sum_J p (1 + sum_J p u - u) v,   empty J: zeros,
 // in one pass with the running state (m, d1, d2, O1, O2); the key range is split over workgroups whose records are
 // merged as in App. C by the combine kernel of decode_bf16.hip (same record format).
 //
-// What bounds it: the bytes of K and V while the rows of a GQA group are few. A key costs 4 D bytes and 8 D flop
-// per column, so at 16 NCB columns per workgroup a byte feeds 32 NCB flop; the matrix pipe (2.5 PFLOP/s against 6 TB/s)
-// is the bound from about 200 columns on, and the L2 before that, as every group of columns reads the keys again.
+// What bounds it: the bytes of K and V (a key costs 4 D bytes and 8 D flop per column, 32 flop a byte).
 //
 // Layout. As decode_bf16.hip: four waves, each with its own 32-key tiles (no barrier in the loop), K and V rows parked in
 // registers one tile ahead and staged through the wave's own LDS tile, S^T = K [Q; R]^T on 16x16x32 MFMAs with the
-// columns (row, head of the group) as MFMA columns, P kept in its lane. What differs:
-//   * NCB blocks of 16 columns share every K and V fragment read from LDS (NCB = 2: 32 columns, one workgroup per unit);
-//   * the tiles walked are those of the sinks, then those from the first key any window reaches: tile number v of this
-//     sequence of tiles is key tile v, or v - n_sink_tiles + first_tile. A key lies in one of the two only;
+// columns as MFMA columns, P kept in its lane; two workgroups per compute unit. What differs:
+//   * the tiles walked are those of the sinks, then those from the first key any window reaches (RowsScope);
 //   * tiles that every column sees completely take no masks. In the others a key that a column does not see must
 //     not reach it whatever its row holds (unwritten rows, freed pages): scores are selected, not multiplied, and
-//     values that are not finite are taken out of the V operand and reach the columns that do see their key
+//     values that are not finite are taken out of the V tile and reach the columns that do see their key
 //     through a product that overflows (2^127 * 2^127), so those columns come out infinite or NaN.
-#include "plx_device.h"
-#include "plx_kernels.h"
+#include "plx_rows.h"
 
 namespace plx {
 
 namespace {
-
-constexpr int kRowsTile = 32;   // keys per wave tile
+constexpr int kRowsTile = 32;  // keys per wave tile
 constexpr int kRowsWaves = 4;
-// How the rows of a tile are found; as in decode_bf16.hip: halves of 16 keys that follow each other in memory (contiguous,
-// pages of a multiple of 16), or row by row.
-enum RowsCache { kRowsContiguous, kRowsPagedRuns, kRowsAny };
-
-// The dword's bf16 halves that are infinite or NaN, as a mask of whole halves
-__device__ __forceinline__ uint32_t not_finite_halves(uint32_t x) {
-    const uint32_t lo = (x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-    return lo | hi;
-}
-constexpr uint32_t kBigHalves = 0x7f007f00u;  // two bf16 of 2^127
-
 }  // namespace
 
-template <int D, bool USE_R, int CACHE, int NCB, bool TREE>
-__global__ __launch_bounds__(256, NCB == 1 ? 2 : 1) void decode_rows_kernel(DecodeRowsParams P) {
+template <int D, bool USE_R, int CACHE, bool TREE>
+__global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P) {
     const DecodeParams &p = P.d;
     constexpr int CPR = D / 8;            // 16-byte chunks per K/V row
     constexpr int KPI = 64 / CPR;         // rows covered by one wave-wide 16-byte load
@@ -55,81 +39,31 @@ __global__ __launch_bounds__(256, NCB == 1 ? 2 : 1) void decode_rows_kernel(Deco
     const int tid = threadIdx.x;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int c = lane & 15, g = lane >> 4;
-    // Work item: the column groups of one (split, key head, sequence) follow each other on one XCD (workgroups
-    // are dealt over the eight of them in turn), whose L2 they share.
-    int cg, split, hk, b;
-    {
-        const int id = blockIdx.x, j = id >> 3;
-        cg = j % P.col_groups;
-        const int unit = j / P.col_groups * 8 + (id & 7);
-        if (unit >= p.S * p.Hkv * p.B) return;
-        split = unit % p.S;
-        const int pair = unit / p.S;
-        hk = pair % p.Hkv, b = pair / p.Hkv;
-    }
+    const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
     const int G = p.G, S = p.S, Tq = p.Tq, n_cols = G * Tq;
-    const int x0 = cg * (16 * NCB);  // first column of this workgroup
 
-    int Lb = p.seq_lens ? p.seq_lens[b] : p.Lmax;
-    Lb = min(max(Lb, 0), p.Lmax);
-    // drafted rows: the last n of the cached tokens, behind `base` committed ones
-    int n = Tq;
-    if constexpr (TREE) n = min(P.draft_lens ? min(max(P.draft_lens[b], 0), Tq) : Tq, Lb);
-    const int base = Lb - n;
-    const int t_first = x0 / G, t_last = min(x0 + 16 * NCB - 1, n_cols - 1) / G;
-    // keys some column may see, [lo_any, end_any) and the sinks; keys every column sees, [lo_all, end_all)
-    int lo_any = 0, lo_all = 0, end_any, end_all;
-    if constexpr (TREE) {
-        end_any = t_first < n ? Lb : 0, end_all = base;
-        if (p.window > 0) lo_any = max(base + 1 - p.window, 0), lo_all = min(max(base + n - p.window, 0), base);
-        lo_any = min(lo_any, base);
-    } else {
-        end_any = max(base + t_last + 1, 0), end_all = max(base + t_first + 1, 0);
-        if (p.window > 0) lo_any = max(base + t_first + 1 - p.window, 0), lo_all = max(base + t_last + 1 - p.window, 0);
-    }
-    const int sinks = p.window > 0 ? P.sinks : 0;
-    const int n_sink_tiles = (min(sinks, end_any) + kRowsTile - 1) / kRowsTile;
-    const int first_tile = max(lo_any / kRowsTile, n_sink_tiles);
-    const int n_virtual = n_sink_tiles + max((end_any + kRowsTile - 1) / kRowsTile - first_tile, 0);
-    const int per = ((n_virtual + S - 1) / S + kRowsWaves - 1) / kRowsWaves * kRowsWaves;
-    const int v_lo = split * per, v_hi = min(v_lo + per, n_virtual);
-    auto key_of = [&](int v) { return kRowsTile * (v < n_sink_tiles ? v : v - n_sink_tiles + first_tile); };
+    const RowsScope<TREE, kRowsTile> scope(P, b, 0, 16);
+    const int Lb = scope.Lb;
+    // (splits in whole rounds of the four waves)
+    const int per = ((scope.n_virtual + S - 1) / S + kRowsWaves - 1) / kRowsWaves * kRowsWaves;
+    const int v_lo = split * per, v_hi = min(v_lo + per, scope.n_virtual);
 
-    // ---- this lane's columns: q and rho operands, key set -------------------------------------------------
-    u32x4 qf[NCB][KSTEPS], rf[NCB][KSTEPS];
-    int col_end[NCB], col_lo[NCB];
-    const uint64_t *col_words[NCB];
-#pragma unroll
-    for (int cb = 0; cb < NCB; ++cb) {
-        const int x = x0 + 16 * cb + c;
-        const bool live = x < n_cols;
-        const int t = live ? x / G : 0, h = live ? x - t * G : 0;
+    // ---- this lane's column: q and rho operands, key set ---------------------------------------------------
+    u32x4 qf[KSTEPS], rf[KSTEPS];
+    int col_end, col_lo;
+    const uint64_t *col_words;
+    {
+        const bool live = c < n_cols;
+        const int t = live ? c / G : 0, h = live ? c - t * G : 0;
         const int64_t row = (((int64_t)b * p.Hq + (int64_t)hk * G + h) * Tq + t) * D;
         const __bf16 *qrow = (const __bf16 *)p.q + row, *rrow = (const __bf16 *)p.r + row;
 #pragma unroll
         for (int s = 0; s < KSTEPS; ++s) {
             const u32x4 z = {0u, 0u, 0u, 0u};
-            qf[cb][s] = live ? *(const u32x4 *)(qrow + 8 * (4 * s + g)) : z;
-            if constexpr (USE_R) rf[cb][s] = live ? *(const u32x4 *)(rrow + 8 * (4 * s + g)) : z;
+            qf[s] = live ? *(const u32x4 *)(qrow + 8 * (4 * s + g)) : z;
+            if constexpr (USE_R) rf[s] = live ? *(const u32x4 *)(rrow + 8 * (4 * s + g)) : z;
         }
-        col_words[cb] = nullptr;
-        if constexpr (TREE) {
-            col_words[cb] = P.mask + (int64_t)b * P.mask_stride_b + (int64_t)t * P.mask_words;
-            col_end[cb] = live && t < n ? Lb : 0;
-            col_lo[cb] = 0;
-            if (p.window > 0) {
-                int ancestors = 0;  // set bits among the n drafted nodes: the node's depth, itself included
-                for (int i = 0; i < P.mask_words && 64 * i < n; ++i) {
-                    const int left = n - 64 * i;
-                    ancestors += __popcll(col_words[cb][i] & (left >= 64 ? ~0ull : (1ull << left) - 1));
-                }
-                const int pos = base + max(ancestors - 1, 0);
-                col_lo[cb] = min(max(pos - p.window + 1, 0), base);
-            }
-        } else {
-            col_end[cb] = live ? max(base + t + 1, 0) : 0;
-            col_lo[cb] = p.window > 0 ? max(col_end[cb] - p.window, 0) : 0;
-        }
+        scope.column(P, b, t, live, col_lo, col_end, col_words);
     }
 
     const __bf16 *kbase = (const __bf16 *)p.k + (p.block_table == nullptr ? (int64_t)b * p.ksb : 0) + (int64_t)hk * p.ksh;
@@ -139,26 +73,21 @@ __global__ __launch_bounds__(256, NCB == 1 ? 2 : 1) void decode_rows_kernel(Deco
 
     const int ld_row = lane / CPR, ld_chunk = lane % CPR;
     u32x4 kst[NLD], vst[NLD];
-    const int32_t *table = p.block_table + (int64_t)b * p.table_stride;
+    const RowsPages pages(p, b);
     const int last16 = max(Lb - 1, 0) & ~15;  // first key of the last half tile that exists
-    auto first_of_page = [&](int key, int64_t &ko, int64_t &vo) {  // element offsets of a key's row
-        const int page_no = key / p.page_size, row = key - page_no * p.page_size;
-        const int64_t page = min(max(table[page_no], 0), p.num_pages - 1);
-        ko = page * p.ksb + (int64_t)row * p.ksl, vo = page * p.vsb + (int64_t)row * p.vsl;
-    };
     // kRowsPagedRuns: offsets of the halves of this wave's next 32 tiles, lane 2 * j + half
     int run_k[2] = {0, 0}, run_v[2] = {0, 0}, run_slot = 0;
     auto lookup_runs = [&](int v) {
-        const int key = min(key_of(min(v + (lane >> 1) * kRowsWaves, max(n_virtual - 1, 0))) + 16 * (lane & 1), last16);
+        const int ahead = min(v + (lane >> 1) * kRowsWaves, max(scope.n_virtual - 1, 0));
         int64_t ko, vo;
-        first_of_page(key, ko, vo);
+        pages.offsets(min(scope.key_of(ahead) + 16 * (lane & 1), last16), ko, vo);
         run_k[0] = (int)ko, run_k[1] = (int)(ko >> 32);
         run_v[0] = (int)vo, run_v[1] = (int)(vo >> 32);
         run_slot = 0;
     };
     const uint32_t k_row_bytes = (uint32_t)p.ksl * 2u, v_row_bytes = (uint32_t)p.vsl * 2u;
     auto issue_loads = [&](int v) {
-        const int tk0 = key_of(v);
+        const int tk0 = scope.key_of(v);
         if constexpr (CACHE != kRowsAny) {
             if constexpr (CACHE == kRowsPagedRuns)
                 if (run_slot == 64) lookup_runs(v);  // (uniform)
@@ -188,22 +117,18 @@ __global__ __launch_bounds__(256, NCB == 1 ? 2 : 1) void decode_rows_kernel(Deco
             for (int i = 0; i < NLD; ++i) {
                 const int key = min(tk0 + i * KPI + ld_row, Lb - 1);
                 int64_t ko = (int64_t)key * p.ksl, vo = (int64_t)key * p.vsl;
-                if (p.block_table != nullptr) first_of_page(key, ko, vo);  // (uniform)
+                if (p.block_table != nullptr) pages.offsets(key, ko, vo);  // (uniform)
                 kst[i] = *(const u32x4 *)(kbase + ko + ld_chunk * 8);
                 vst[i] = *(const u32x4 *)(vbase + vo + ld_chunk * 8);
             }
         }
     };
 
-    // ---- running state (per lane: its columns, partial over this lane's keys) ------------------------------
-    float m_run[NCB], dsum1[NCB], dsum2[NCB];
-    f32x4 o1[NCB][NDB], o2[NCB][NDB];
+    // ---- running state (per lane: its column, partial over this lane's keys) --------------------------------
+    float m_run = kNegInf, dsum1 = 0.f, dsum2 = 0.f;
+    f32x4 o1[NDB], o2[NDB];
 #pragma unroll
-    for (int cb = 0; cb < NCB; ++cb) {
-        m_run[cb] = kNegInf, dsum1[cb] = dsum2[cb] = 0.f;
-#pragma unroll
-        for (int i = 0; i < NDB; ++i) o1[cb][i] = o2[cb][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int i = 0; i < NDB; ++i) o1[i] = o2[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float scale_log2 = p.scale * kLog2e;
     // A operand of O^T += V^T P^T for 16 output dimensions: the 8 keys of this lane's B operand
     const int tr_key = 4 * g + (c >> 2), tr_half = (c & 1) * 4;
@@ -221,118 +146,6 @@ __global__ __launch_bounds__(256, NCB == 1 ? 2 : 1) void decode_rows_kernel(Deco
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     };
 
-    // One tile: scores, softmax, outputs
-    auto tile = [&](int tk, bool whole) __attribute__((always_inline)) {
-        uint32_t seen[NCB];  // bit 4 * sub + i: key tk + 16 sub + 4 g + i is this lane's column's
-#pragma unroll
-        for (int cb = 0; cb < NCB; ++cb) seen[cb] = 0xffu;
-        if (!whole) {  // (uniform) some column does not see all of the keys
-#pragma unroll
-            for (int cb = 0; cb < NCB; ++cb) {
-                uint32_t bits = 0xffffffffu;
-                if constexpr (TREE)
-                    if (tk + kRowsTile > base) bits = tree_bits(col_words[cb], P.mask_words, tk - base);
-                seen[cb] = 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int at = 16 * (e >> 2) + 4 * g + (e & 3), key = tk + at;
-                    const bool ok = key < col_end[cb] && (key >= col_lo[cb] || key < sinks) && ((bits >> at) & 1u);
-                    seen[cb] |= ok ? 1u << e : 0u;
-                }
-            }
-            // values that are not finite: out of the V tile, and into the columns that see their key
-            u32x4 big[NCB];
-#pragma unroll
-            for (int cb = 0; cb < NCB; ++cb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    big[cb][e] = kBigHalves & (((seen[cb] >> (2 * e)) & 1u ? 0xffffu : 0u) |
-                                               ((seen[cb] >> (2 * e + 1)) & 1u ? 0xffff0000u : 0u));
-#pragma unroll
-            for (int i = 0; i < NDB; ++i) {
-                u32x4 bad = v_fragment(i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) bad[e] = not_finite_halves(bad[e]) & kBigHalves;
-#pragma unroll
-                for (int cb = 0; cb < NCB; ++cb) o1[cb][i] = mfma16(bad, big[cb], o1[cb][i]);
-            }
-            wave_lds_fence();
-#pragma unroll
-            for (int i = 0; i < NLD; ++i) {
-                u32x4 &x = ldsV[lds_chunk_slot<D>(i * KPI + ld_row, ld_chunk)];
-                u32x4 y = x;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] &= ~not_finite_halves(y[e]);
-                x = y;
-            }
-            wave_lds_fence();
-        }
-        f32x4 s1[NCB][2], s2[NCB][2];
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-#pragma unroll
-            for (int cb = 0; cb < NCB; ++cb) s1[cb][sub] = s2[cb][sub] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < KSTEPS; ++s) {
-                const u32x4 kf = ldsK[lds_chunk_slot<D>(16 * sub + c, 4 * s + g)];
-#pragma unroll
-                for (int cb = 0; cb < NCB; ++cb) {
-                    s1[cb][sub] = mfma16(kf, qf[cb][s], s1[cb][sub]);
-                    if constexpr (USE_R) s2[cb][sub] = mfma16(kf, rf[cb][s], s2[cb][sub]);
-                }
-            }
-        }
-        u32x4 pb1[NCB], pb2[NCB];
-#pragma unroll
-        for (int cb = 0; cb < NCB; ++cb) {
-            float x[8], tmax = kNegInf;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[e] = s1[cb][e >> 2][e & 3] * scale_log2;
-                x[e] = (seen[cb] >> e) & 1u ? x[e] : kNegInf;
-                tmax = fmaxf(tmax, x[e]);
-            }
-            tmax = rows_max(tmax);
-            const float m_new = fmaxf(m_run[cb], tmax), m_use = m_new == kNegInf ? 0.f : m_new;
-            const float alpha = fast_exp2(m_run[cb] - m_use);  // 0 on the first tile that is seen
-            m_run[cb] = m_new;
-            // P1 and P2 are rounded to bf16 once, as matrix operands; d1 and d2 add the rounded values, so
-            // that the weights still sum to one.
-            float p1[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) p1[e] = fast_exp2(x[e] - m_use);
-            dsum1[cb] *= alpha;
-            pb1[cb] = pack8_bf16_accumulate(p1[0], p1[1], p1[2], p1[3], p1[4], p1[5], p1[6], p1[7], dsum1[cb]);
-            pb2[cb] = u32x4{0u, 0u, 0u, 0u};
-            if constexpr (USE_R) {
-                float p2[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    p2[e] = p1[e] * s2[cb][e >> 2][e & 3];
-                    p2[e] = (seen[cb] >> e) & 1u ? p2[e] : 0.f;
-                }
-                dsum2[cb] *= alpha;
-                pb2[cb] = pack8_bf16_accumulate(p2[0], p2[1], p2[2], p2[3], p2[4], p2[5], p2[6], p2[7], dsum2[cb]);
-            }
-            if (!__all(alpha == 1.f)) {
-#pragma unroll
-                for (int i = 0; i < NDB; ++i) {
-                    o1[cb][i] *= alpha;
-                    if constexpr (USE_R) o2[cb][i] *= alpha;
-                }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < NDB; ++i) {
-            const u32x4 vt = v_fragment(i);
-#pragma unroll
-            for (int cb = 0; cb < NCB; ++cb) {
-                o1[cb][i] = mfma16(vt, pb1[cb], o1[cb][i]);
-                if constexpr (USE_R) o2[cb][i] = mfma16(vt, pb2[cb], o2[cb][i]);
-            }
-        }
-    };
-
     int v = v_lo + w;
     if (v < v_hi) {
         if constexpr (CACHE == kRowsPagedRuns) lookup_runs(v);
@@ -347,25 +160,93 @@ __global__ __launch_bounds__(256, NCB == 1 ? 2 : 1) void decode_rows_kernel(Deco
         }
         if (v + kRowsWaves < v_hi) issue_loads(v + kRowsWaves);
         wave_lds_fence();
-        const int tk = __builtin_amdgcn_readfirstlane(key_of(v)), tk_end = tk + kRowsTile;
-        tile(tk, (tk >= lo_all || tk_end <= sinks) && tk_end <= end_all);
+        const int tk = __builtin_amdgcn_readfirstlane(scope.key_of(v));
+        uint32_t seen = 0xffu;
+        if (!scope.whole(tk, kRowsTile)) {  // (uniform) some column does not see all of the keys
+            seen = scope.seen(P, col_words, col_lo, col_end, tk, g);
+            // values that are not finite: into the columns that see their key, and out of the V tile
+            const u32x4 big = big_halves(seen);
+#pragma unroll
+            for (int i = 0; i < NDB; ++i) {
+                u32x4 bad = v_fragment(i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) bad[e] = not_finite_halves(bad[e]) & kBigHalves;
+                o1[i] = mfma16(bad, big, o1[i]);
+            }
+            wave_lds_fence();
+#pragma unroll
+            for (int i = 0; i < NLD; ++i) {
+                u32x4 &x = ldsV[lds_chunk_slot<D>(i * KPI + ld_row, ld_chunk)];
+                u32x4 y = x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] &= ~not_finite_halves(y[e]);
+                x = y;
+            }
+            wave_lds_fence();
+        }
+        f32x4 s1[2], s2[2];
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            s1[sub] = s2[sub] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KSTEPS; ++s) {
+                const u32x4 kf = ldsK[lds_chunk_slot<D>(16 * sub + c, 4 * s + g)];
+                s1[sub] = mfma16(kf, qf[s], s1[sub]);
+                if constexpr (USE_R) s2[sub] = mfma16(kf, rf[s], s2[sub]);
+            }
+        }
+        float x[8], tmax = kNegInf;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] = (seen >> e) & 1u ? s1[e >> 2][e & 3] * scale_log2 : kNegInf;
+            tmax = fmaxf(tmax, x[e]);
+        }
+        tmax = rows_max(tmax);
+        const float m_new = fmaxf(m_run, tmax), m_use = m_new == kNegInf ? 0.f : m_new;
+        const float alpha = fast_exp2(m_run - m_use);  // 0 on the first tile that is seen
+        m_run = m_new;
+        // P1 and P2 are rounded to bf16 once, as matrix operands; d1 and d2 add the rounded values, so
+        // that the weights still sum to one.
+        float p1[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p1[e] = fast_exp2(x[e] - m_use);
+        dsum1 *= alpha;
+        const u32x4 pb1 = pack8_bf16_accumulate(p1[0], p1[1], p1[2], p1[3], p1[4], p1[5], p1[6], p1[7], dsum1);
+        u32x4 pb2 = {0u, 0u, 0u, 0u};
+        if constexpr (USE_R) {
+            float p2[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p2[e] = (seen >> e) & 1u ? p1[e] * s2[e >> 2][e & 3] : 0.f;
+            dsum2 *= alpha;
+            pb2 = pack8_bf16_accumulate(p2[0], p2[1], p2[2], p2[3], p2[4], p2[5], p2[6], p2[7], dsum2);
+        }
+        if (!__all(alpha == 1.f)) {
+#pragma unroll
+            for (int i = 0; i < NDB; ++i) {
+                o1[i] *= alpha;
+                if constexpr (USE_R) o2[i] *= alpha;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NDB; ++i) {
+            const u32x4 vt = v_fragment(i);
+            o1[i] = mfma16(vt, pb1, o1[i]);
+            if constexpr (USE_R) o2[i] = mfma16(vt, pb2, o2[i]);
+        }
         wave_lds_fence();
     }
 
-    // ---- the four waves' states, 16 columns at a time, then the record or the output row --------------------
+    // ---- the four waves' states, then the record or the output row --------------------------------------------
     float *mrg = (float *)lds;
     float *mrg_m = mrg, *mrg_d1 = mrg + kRowsWaves * 16, *mrg_d2 = mrg + 2 * kRowsWaves * 16;  // [wave][16]
     float *mrg_o1 = mrg + 3 * kRowsWaves * 16, *mrg_o2 = mrg_o1 + kRowsWaves * 16 * D;         // [wave][16][D]
-#pragma unroll
-    for (int cb = 0; cb < NCB; ++cb) {
-        const int cols = min(n_cols - (x0 + 16 * cb), 16);  // (uniform)
-        if (cols <= 0) break;
-        __syncthreads();  // every wave is done with its tiles, or with the columns before
-        const float s1 = rows_sum(dsum1[cb]), s2 = rows_sum(dsum2[cb]);
+    __syncthreads();  // every wave is done with its tiles
+    {
+        const float s1 = rows_sum(dsum1), s2 = rows_sum(dsum2);
         // a node behind the sequence's drafted ones sees nothing, also where all others see everything
-        const bool none = col_end[cb] == 0;
+        const bool none = col_end == 0;
         if (g == 0) {
-            mrg_m[w * 16 + c] = none ? kNegInf : m_run[cb];
+            mrg_m[w * 16 + c] = none ? kNegInf : m_run;
             mrg_d1[w * 16 + c] = none ? 0.f : s1;
             mrg_d2[w * 16 + c] = none ? 0.f : s2;
         }
@@ -373,67 +254,58 @@ __global__ __launch_bounds__(256, NCB == 1 ? 2 : 1) void decode_rows_kernel(Deco
         for (int i = 0; i < NDB; ++i) {
             const int at = (w * 16 + c) * D + 16 * i + 4 * g;
             const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            *(f32x4 *)(mrg_o1 + at) = none ? zero : o1[cb][i];
-            *(f32x4 *)(mrg_o2 + at) = none || !USE_R ? zero : o2[cb][i];
+            *(f32x4 *)(mrg_o1 + at) = none ? zero : o1[i];
+            *(f32x4 *)(mrg_o2 + at) = none || !USE_R ? zero : o2[i];
         }
-        __syncthreads();
-        for (int idx = tid; idx < cols * D; idx += 256) {
-            const int hh = idx / D, dim = idx - hh * D;
-            float m_star = kNegInf;
+    }
+    __syncthreads();
+    for (int idx = tid; idx < n_cols * D; idx += 256) {
+        const int x = idx / D, dim = idx - x * D;
+        float m_star = kNegInf;
 #pragma unroll
-            for (int ww = 0; ww < kRowsWaves; ++ww) m_star = fmaxf(m_star, mrg_m[ww * 16 + hh]);
-            float d1 = 0.f, d2 = 0.f, a1 = 0.f, a2 = 0.f;
+        for (int ww = 0; ww < kRowsWaves; ++ww) m_star = fmaxf(m_star, mrg_m[ww * 16 + x]);
+        float d1 = 0.f, d2 = 0.f, a1 = 0.f, a2 = 0.f;
 #pragma unroll
-            for (int ww = 0; ww < kRowsWaves; ++ww) {
-                // (a reference of -inf with a sum that is not zero: scores of NaN only, which must reach the result)
-                const float mw = mrg_m[ww * 16 + hh], dw = mrg_d1[ww * 16 + hh];
-                const float wt = mw == kNegInf && dw == 0.f ? 0.f : fast_exp2(mw - m_star);
-                d1 += wt * dw;
-                d2 += wt * mrg_d2[ww * 16 + hh];
-                a1 += wt * mrg_o1[(ww * 16 + hh) * D + dim];
-                a2 += wt * mrg_o2[(ww * 16 + hh) * D + dim];
+        for (int ww = 0; ww < kRowsWaves; ++ww) {
+            // (a reference of -inf with a sum that is not zero: scores of NaN only, which must reach the result)
+            const float mw = mrg_m[ww * 16 + x], dw = mrg_d1[ww * 16 + x];
+            const float wt = mw == kNegInf && dw == 0.f ? 0.f : fast_exp2(mw - m_star);
+            d1 += wt * dw;
+            d2 += wt * mrg_d2[ww * 16 + x];
+            a1 += wt * mrg_o1[(ww * 16 + x) * D + dim];
+            a2 += wt * mrg_o2[(ww * 16 + x) * D + dim];
+        }
+        const int ot = x / G, oh = x - ot * G;
+        const int64_t row = ((int64_t)b * p.Hq + (int64_t)hk * G + oh) * Tq + ot;
+        if (p.direct_out) {
+            float out = 0.f;  // empty key set: zeros
+            if (d1 != 0.f) {
+                const float inv = 1.f / d1;
+                out = a1 * inv * (1.f + d2 * inv) - a2 * inv;
             }
-            const int x = x0 + 16 * cb + hh, ot = x / G, oh = x - ot * G;
-            const int64_t row = ((int64_t)b * p.Hq + (int64_t)hk * G + oh) * Tq + ot;
-            if (p.direct_out) {
-                float out = 0.f;  // empty key set: zeros
-                if (d1 != 0.f) {
-                    const float inv = 1.f / d1;
-                    out = a1 * inv * (1.f + d2 * inv) - a2 * inv;
-                }
-                ((__bf16 *)p.o)[row * D + dim] = (__bf16)out;
-            } else {
-                float *rec = p.ws + (row * S + split) * (int64_t)(2 * D + 4);
-                if (d1 != d1) m_star = 3.0e38f, d1 = -kNegInf, a1 = __builtin_nanf("");  // the merge takes it alone
-                if (dim == 0) *(f32x4 *)rec = f32x4{m_star, d1, d2, 0.f};
-                rec[4 + dim] = a1;
-                rec[4 + D + dim] = a2;
-            }
+            ((__bf16 *)p.o)[row * D + dim] = (__bf16)out;
+        } else {
+            float *rec = p.ws + (row * S + split) * (int64_t)(2 * D + 4);
+            if (d1 != d1) m_star = 3.0e38f, d1 = -kNegInf, a1 = __builtin_nanf("");  // the merge takes it alone
+            if (dim == 0) *(f32x4 *)rec = f32x4{m_star, d1, d2, 0.f};
+            rec[4 + dim] = a1;
+            rec[4 + D + dim] = a2;
         }
     }
 }
 
-// Columns per workgroup: 32 from 17 columns (rows x heads of a group) on
-int decode_rows_columns(int n_cols) { return n_cols <= 16 ? 16 : 32; }
-
-template <int D, bool USE_R, int CACHE, int NCB>
-static void launch_rows_form(const DecodeRowsParams &P, dim3 grid, hipStream_t stream) {
-    if (P.mask != nullptr)
-        hipLaunchKernelGGL((decode_rows_kernel<D, USE_R, CACHE, NCB, true>), grid, dim3(256), 0, stream, P);
-    else
-        hipLaunchKernelGGL((decode_rows_kernel<D, USE_R, CACHE, NCB, false>), grid, dim3(256), 0, stream, P);
-}
+// Columns per workgroup: 16 with private tiles, 64 or 128 with shared ones. (Private tiles with 32 columns a wave, one
+// workgroup per unit, took 26 nodes x 2 heads over 16 x 6000 keys, which the columns read twice, in 135 us.)
+int decode_rows_columns(int n_cols) { return n_cols <= 16 ? 16 : n_cols <= 64 ? 64 : 128; }
+int decode_rows_tile(int columns) { return columns == 64 ? 128 : 64; }
 
 template <int D, bool USE_R, int CACHE>
-static void launch_rows_columns(DecodeRowsParams P, hipStream_t stream) {
-    const int n_cols = P.d.G * P.d.Tq, cols = decode_rows_columns(n_cols);
-    P.col_groups = (n_cols + cols - 1) / cols;
-    const int64_t units = ((int64_t)P.d.S * P.d.Hkv * P.d.B + 7) / 8 * 8;  // (whole turns of the eight XCDs)
-    const dim3 grid((unsigned)(units * P.col_groups));
-    if (cols == 16)
-        launch_rows_form<D, USE_R, CACHE, 1>(P, grid, stream);
+static void launch_rows_form(const DecodeRowsParams &P, hipStream_t stream) {
+    const dim3 grid(P.d.S, P.d.Hkv, P.d.B);
+    if (P.mask != nullptr)
+        hipLaunchKernelGGL((decode_rows_kernel<D, USE_R, CACHE, true>), grid, dim3(256), 0, stream, P);
     else
-        launch_rows_form<D, USE_R, CACHE, 2>(P, grid, stream);
+        hipLaunchKernelGGL((decode_rows_kernel<D, USE_R, CACHE, false>), grid, dim3(256), 0, stream, P);
 }
 
 template <int D, bool USE_R>
@@ -441,14 +313,15 @@ static void launch_rows_cache(const DecodeRowsParams &P, hipStream_t stream) {
     const DecodeParams &p = P.d;
     const bool short_rows = p.ksl < (1 << 23) && p.vsl < (1 << 23);  // (24-bit products, see decode_bf16.hip)
     if (short_rows && p.block_table == nullptr)
-        launch_rows_columns<D, USE_R, kRowsContiguous>(P, stream);
+        launch_rows_form<D, USE_R, kRowsContiguous>(P, stream);
     else if (short_rows && p.page_size % 16 == 0)
-        launch_rows_columns<D, USE_R, kRowsPagedRuns>(P, stream);
+        launch_rows_form<D, USE_R, kRowsPagedRuns>(P, stream);
     else
-        launch_rows_columns<D, USE_R, kRowsAny>(P, stream);
+        launch_rows_form<D, USE_R, kRowsAny>(P, stream);
 }
 
 hipError_t launch_decode_rows_bf16(const DecodeRowsParams &P, hipStream_t stream) {
+    if (decode_rows_columns(P.d.G * P.d.Tq) > 16) return launch_decode_rows_wide_bf16(P, stream);
     if (P.d.d == 128)
         P.d.use_r ? launch_rows_cache<128, true>(P, stream) : launch_rows_cache<128, false>(P, stream);
     else

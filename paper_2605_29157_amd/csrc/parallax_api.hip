@@ -434,8 +434,13 @@ plx_status prepare_decode_rows(const plx_decode_args *a, const plx_decode_tree_a
     return PLX_OK;
 }
 
-// Split count of such a call: that of a plain one over as many keys, a pair of workgroup columns for every
-// group of columns
+// Split count of such a call. Up to 16 columns: that of a plain one over as many keys. Beyond them (one workgroup of eight waves per
+// compute unit, decode_rows_wide_bf16.hip) from a model fitted to sweeps of S on MI355X, in us: a round of at most one workgroup
+// per unit takes 6 and for each 128 keys (d = 128; shorter rows in proportion) 2.25 of arithmetic with 64 columns, 4.1 with
+// 128, and a third of the time in which the memory brings in what the workgroups of the round read at 5 TB/s, which is also the
+// least; the merge takes 5 and writing and reading of the records at 4 TB/s. Measured for 32 sequence heads x 16384 keys, d = 128, in
+// front of 128 columns: S = 1 533, 4 167, 6 122, 8 107, 10 152, 16 120 (the model takes 8); for 128 x up to 6000, 64 columns: S = 1
+// 133, 2 99, 3 108, 4 101 (2; the rule for plain rows took 1).
 int32_t pick_splits_rows(const plx_decode_args *a, const plx::DecodeRowsParams &p) {
     if (a->num_splits > 0) return a->num_splits;
     const int64_t in_window = (int64_t)a->window + p.d.Tq - 1 + p.sinks;
@@ -446,7 +451,23 @@ int32_t pick_splits_rows(const plx_decode_args *a, const plx::DecodeRowsParams &
         return pick_splits_f32(&plain, p.d.Tq);
     }
     const int32_t cols = p.d.G * p.d.Tq, per = plx::decode_rows_columns(cols);
-    return parallax_decode_num_splits(a->B, a->Hq, a->Hkv * ((cols + per - 1) / per), keys, a->d, 0);
+    if (per == 16) return parallax_decode_num_splits(a->B, a->Hq, a->Hkv, keys, a->d, 0);
+    const int64_t pairs = (int64_t)a->B * a->Hkv * ((cols + per - 1) / per), cus = query_num_cus();
+    const int32_t tile = plx::decode_rows_tile(per), tiles = (keys + tile - 1) / tile;
+    const double share = tile / 128.0 * a->d / 128.0, compute = share * (per == 64 ? 2.25 : 4.1), memory = share * 65536e-6 / 5.0;
+    const double record_us = 2.0 * (double)a->B * a->Hq * p.d.Tq * (2 * a->d + 4) * 4e-6 / 4.0;
+    auto round = [&](int64_t workgroups, int64_t n) {
+        const double fetch = memory * (double)workgroups;
+        return 6.0 + (double)n * std::max(fetch, compute + fetch / 3);
+    };
+    auto cost = [&](int32_t s) {
+        const int64_t w = pairs * s, n = (tiles + s - 1) / s, full = w / cus, rest = w % cus;
+        return (double)full * round(cus, n) + (rest ? round(rest, n) : 0.0) + (s > 1 ? 5.0 + s * record_us : 0.0);
+    };
+    int32_t best = 1;
+    for (int32_t s = 2; s <= std::min(tiles, PLX_MAX_SPLITS); ++s)
+        if (cost(s) < cost(best)) best = s;
+    return best;
 }
 
 int32_t decode_rows_splits(const plx_decode_args *a, const plx_decode_tree_args *tree, int32_t sinks) {
