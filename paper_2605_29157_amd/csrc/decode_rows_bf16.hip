@@ -51,7 +51,7 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
     // ---- this lane's column: q and rho operands, key set ---------------------------------------------------
     u32x4 qf[KSTEPS], rf[KSTEPS];
     int col_end, col_lo;
-    const uint64_t *col_words;
+    TreeRow col_nodes{};
     {
         const bool live = c < n_cols;
         const int t = live ? c / G : 0, h = live ? c - t * G : 0;
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
             qf[s] = live ? *(const u32x4 *)(qrow + 8 * (4 * s + g)) : z;
             if constexpr (USE_R) rf[s] = live ? *(const u32x4 *)(rrow + 8 * (4 * s + g)) : z;
         }
-        scope.column(P, b, t, live, col_lo, col_end, col_words);
+        scope.column(P, b, t, live, col_lo, col_end, col_nodes);
     }
 
     const __bf16 *kbase = (const __bf16 *)p.k + (p.block_table == nullptr ? (int64_t)b * p.ksb : 0) + (int64_t)hk * p.ksh;
@@ -91,6 +91,8 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
         if constexpr (CACHE != kRowsAny) {
             if constexpr (CACHE == kRowsPagedRuns)
                 if (run_slot == 64) lookup_runs(v);  // (uniform)
+            int l = lane;
+            asm volatile("" : "+v"(l));  // (the lane's offsets are worked out here: kept across the loop they would be spilled)
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
                 const int key0 = __builtin_amdgcn_readfirstlane(min(tk0 + 16 * hf, last16));
@@ -106,9 +108,9 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
                 const int last = Lb - 1 - key0;  // rows past the sequence end re-read its last row (masked below)
 #pragma unroll
                 for (int i = 0; i < NLD / 2; ++i) {
-                    const uint32_t row = (uint32_t)min(i * KPI + ld_row, last);
-                    kst[hf * (NLD / 2) + i] = *(const u32x4 *)(kp + (__umul24(row, k_row_bytes) + 16u * ld_chunk));
-                    vst[hf * (NLD / 2) + i] = *(const u32x4 *)(vp + (__umul24(row, v_row_bytes) + 16u * ld_chunk));
+                    const uint32_t row = (uint32_t)min(i * KPI + l / CPR, last);
+                    kst[hf * (NLD / 2) + i] = *(const u32x4 *)(kp + (__umul24(row, k_row_bytes) + 16u * (uint32_t)(l % CPR)));
+                    vst[hf * (NLD / 2) + i] = *(const u32x4 *)(vp + (__umul24(row, v_row_bytes) + 16u * (uint32_t)(l % CPR)));
                 }
             }
             run_slot += 2;
@@ -152,37 +154,51 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
         issue_loads(v);
     }
     for (; v < v_hi; v += kRowsWaves) {
+        const int tk = __builtin_amdgcn_readfirstlane(scope.key_of(v));
+        const bool whole = scope.whole(tk, kRowsTile);  // (uniform) every column sees all of the keys
+        bool any_bad = false;
+        if (!whole) {
+            uint32_t bad = 0;
+#pragma unroll
+            for (int i = 0; i < NLD; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) bad |= not_finite_halves(vst[i][e]);
+            any_bad = __any(bad != 0);
+        }
+        int l = lane;
+        asm volatile("" : "+v"(l));  // (as above)
 #pragma unroll
         for (int i = 0; i < NLD; ++i) {
-            const int slot = lds_chunk_slot<D>(i * KPI + ld_row, ld_chunk);
+            const int slot = lds_chunk_slot<D>(i * KPI + l / CPR, l % CPR);
             ldsK[slot] = kst[i];
             ldsV[slot] = vst[i];
         }
         if (v + kRowsWaves < v_hi) issue_loads(v + kRowsWaves);
         wave_lds_fence();
-        const int tk = __builtin_amdgcn_readfirstlane(scope.key_of(v));
         uint32_t seen = 0xffu;
-        if (!scope.whole(tk, kRowsTile)) {  // (uniform) some column does not see all of the keys
-            seen = scope.seen(P, col_words, col_lo, col_end, tk, g);
-            // values that are not finite: into the columns that see their key, and out of the V tile
-            const u32x4 big = big_halves(seen);
+        if (!whole) {
+            seen = scope.seen(P, col_nodes, col_lo, col_end, tk, g);
+            if (__builtin_expect(any_bad, 0)) {
+                // values that are not finite: into the columns that see their key, and out of the V tile
+                const u32x4 big = big_halves(seen);
 #pragma unroll
-            for (int i = 0; i < NDB; ++i) {
-                u32x4 bad = v_fragment(i);
+                for (int i = 0; i < NDB; ++i) {
+                    u32x4 bad = v_fragment(i);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) bad[e] = not_finite_halves(bad[e]) & kBigHalves;
-                o1[i] = mfma16(bad, big, o1[i]);
+                    for (int e = 0; e < 4; ++e) bad[e] = not_finite_halves(bad[e]) & kBigHalves;
+                    o1[i] = mfma16(bad, big, o1[i]);
+                }
+                wave_lds_fence();
+#pragma unroll
+                for (int i = 0; i < NLD; ++i) {
+                    u32x4 &x = ldsV[lds_chunk_slot<D>(i * KPI + ld_row, ld_chunk)];
+                    u32x4 y = x;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] &= ~not_finite_halves(y[e]);
+                    x = y;
+                }
+                wave_lds_fence();
             }
-            wave_lds_fence();
-#pragma unroll
-            for (int i = 0; i < NLD; ++i) {
-                u32x4 &x = ldsV[lds_chunk_slot<D>(i * KPI + ld_row, ld_chunk)];
-                u32x4 y = x;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] &= ~not_finite_halves(y[e]);
-                x = y;
-            }
-            wave_lds_fence();
         }
         f32x4 s1[2], s2[2];
 #pragma unroll
@@ -236,10 +252,11 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
         wave_lds_fence();
     }
 
-    // ---- the four waves' states, then the record or the output row --------------------------------------------
-    float *mrg = (float *)lds;
-    float *mrg_m = mrg, *mrg_d1 = mrg + kRowsWaves * 16, *mrg_d2 = mrg + 2 * kRowsWaves * 16;  // [wave][16]
-    float *mrg_o1 = mrg + 3 * kRowsWaves * 16, *mrg_o2 = mrg_o1 + kRowsWaves * 16 * D;         // [wave][16][D]
+    // ---- the four waves' states (in the order of the lanes' registers: no bank conflicts), then the record or the output row ----
+    constexpr int QUADS = NDB * 64;  // of four dimensions: quad 64 i + lane' is column lane' % 16, dimensions 16 i + 4 (lane' / 16) ..
+    f32x4 *mrg1 = (f32x4 *)lds, *mrg2 = mrg1 + kRowsWaves * QUADS;  // [wave][quad]
+    float *mrg_m = (float *)(lds + kRowsWaves * 2 * TILE_CHUNKS), *mrg_d1 = mrg_m + kRowsWaves * 16, *mrg_d2 = mrg_d1 + kRowsWaves * 16;
+    static_assert(2 * kRowsWaves * QUADS <= kRowsWaves * 2 * TILE_CHUNKS, "the states of four waves");
     __syncthreads();  // every wave is done with its tiles
     {
         const float s1 = rows_sum(dsum1), s2 = rows_sum(dsum2);
@@ -252,45 +269,34 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
         }
 #pragma unroll
         for (int i = 0; i < NDB; ++i) {
-            const int at = (w * 16 + c) * D + 16 * i + 4 * g;
             const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            *(f32x4 *)(mrg_o1 + at) = none ? zero : o1[i];
-            *(f32x4 *)(mrg_o2 + at) = none || !USE_R ? zero : o2[i];
+            mrg1[w * QUADS + 64 * i + lane] = none ? zero : o1[i];
+            if constexpr (USE_R) mrg2[w * QUADS + 64 * i + lane] = none ? zero : o2[i];
         }
     }
     __syncthreads();
-    for (int idx = tid; idx < n_cols * D; idx += 256) {
-        const int x = idx / D, dim = idx - x * D;
-        float m_star = kNegInf;
+    if (c >= n_cols) return;  // (a thread's column is the same in all of its quads)
+    float m_star = kNegInf, wt[kRowsWaves], d1 = 0.f, d2 = 0.f;
 #pragma unroll
-        for (int ww = 0; ww < kRowsWaves; ++ww) m_star = fmaxf(m_star, mrg_m[ww * 16 + x]);
-        float d1 = 0.f, d2 = 0.f, a1 = 0.f, a2 = 0.f;
+    for (int ww = 0; ww < kRowsWaves; ++ww) m_star = fmaxf(m_star, mrg_m[ww * 16 + c]);
+#pragma unroll
+    for (int ww = 0; ww < kRowsWaves; ++ww) {
+        // (a reference of -inf with a sum that is not zero: scores of NaN only, which must reach the result)
+        const float mw = mrg_m[ww * 16 + c], dw = mrg_d1[ww * 16 + c];
+        wt[ww] = mw == kNegInf && dw == 0.f ? 0.f : fast_exp2(mw - m_star);
+        d1 += wt[ww] * dw;
+        d2 += wt[ww] * mrg_d2[ww * 16 + c];
+    }
+    const RowsColumn<D> column(p, b, hk, c, split, m_star, d1, d2, false, w == 0 && g == 0);
+#pragma unroll
+    for (int quad = tid; quad < QUADS; quad += 256) {
+        f32x4 a1 = {0.f, 0.f, 0.f, 0.f}, a2 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ww = 0; ww < kRowsWaves; ++ww) {
-            // (a reference of -inf with a sum that is not zero: scores of NaN only, which must reach the result)
-            const float mw = mrg_m[ww * 16 + x], dw = mrg_d1[ww * 16 + x];
-            const float wt = mw == kNegInf && dw == 0.f ? 0.f : fast_exp2(mw - m_star);
-            d1 += wt * dw;
-            d2 += wt * mrg_d2[ww * 16 + x];
-            a1 += wt * mrg_o1[(ww * 16 + x) * D + dim];
-            a2 += wt * mrg_o2[(ww * 16 + x) * D + dim];
+            a1 += wt[ww] * mrg1[ww * QUADS + quad];
+            if constexpr (USE_R) a2 += wt[ww] * mrg2[ww * QUADS + quad];
         }
-        const int ot = x / G, oh = x - ot * G;
-        const int64_t row = ((int64_t)b * p.Hq + (int64_t)hk * G + oh) * Tq + ot;
-        if (p.direct_out) {
-            float out = 0.f;  // empty key set: zeros
-            if (d1 != 0.f) {
-                const float inv = 1.f / d1;
-                out = a1 * inv * (1.f + d2 * inv) - a2 * inv;
-            }
-            ((__bf16 *)p.o)[row * D + dim] = (__bf16)out;
-        } else {
-            float *rec = p.ws + (row * S + split) * (int64_t)(2 * D + 4);
-            if (d1 != d1) m_star = 3.0e38f, d1 = -kNegInf, a1 = __builtin_nanf("");  // the merge takes it alone
-            if (dim == 0) *(f32x4 *)rec = f32x4{m_star, d1, d2, 0.f};
-            rec[4 + dim] = a1;
-            rec[4 + D + dim] = a2;
-        }
+        column.store(16 * (quad >> 6) + 4 * g, a1, a2);
     }
 }
 

@@ -137,39 +137,6 @@ __device__ __forceinline__ bool wide_item(const DecodeRowsParams &P, int &cg, in
     hk = pair % p.Hkv, b = pair / p.Hkv;
     return true;
 }
-
-// Four dimensions of a finished column: of its record, or of its output row
-template <int D>
-struct WideColumn {
-    const DecodeParams &p;
-    int64_t row;
-    float d1, d2, inv, gain;
-    float *rec;
-    bool none, nan;
-    __device__ __forceinline__ WideColumn(const DecodeParams &p, int b, int hk, int x, int split, float m, float d1_, float d2_, bool none, bool head)
-        : p(p), d1(none ? 0.f : d1_), d2(none ? 0.f : d2_), none(none) {
-        const int t = x / p.G, h = x - t * p.G;
-        row = ((int64_t)b * p.Hq + (int64_t)hk * p.G + h) * p.Tq + t;
-        nan = d1 != d1;
-        inv = d1 != 0.f ? 1.f / d1 : 0.f, gain = inv * (1.f + d2 * inv);
-        rec = p.ws + (row * p.S + split) * (int64_t)(2 * D + 4);
-        // (NaN: a record that the merge takes alone)
-        if (!p.direct_out && head) *(f32x4 *)rec = nan ? f32x4{3.0e38f, -kNegInf, 0.f, 0.f} : f32x4{none ? kNegInf : m, d1, d2, 0.f};
-    }
-    __device__ __forceinline__ void store(int dim, f32x4 a1, f32x4 a2) const {
-        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        if (none) a1 = a2 = zero;
-        if (p.direct_out) {
-            f32x4 y = zero;  // empty key set: zeros
-            if (d1 != 0.f) y = a1 * gain - a2 * inv;
-            *(u32x2 *)((__bf16 *)p.o + row * D + dim) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
-        } else {
-            if (nan) a1[0] = a1[1] = a1[2] = a1[3] = __builtin_nanf("");
-            *(f32x4 *)(rec + 4 + dim) = a1;
-            *(f32x4 *)(rec + 4 + D + dim) = a2;
-        }
-    }
-};
 }  // namespace
 
 // Eight waves, two per SIMD. KH = 2: 64 columns per workgroup, wave w owns columns 16 (w % 4) .. + 15 and half w / 4 of the
@@ -206,7 +173,7 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
     // ---- this lane's column: q and rho operands, key set ----------------------------------------------------
     u32x4 qf[KSTEPS], rf[KSTEPS];
     int col_end, col_lo;
-    const uint64_t *col_words;
+    TreeRow col_nodes{};
     const int x = x0 + 16 * cw + c;
     {
         const bool live = x < n_cols;
@@ -219,7 +186,7 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
             qf[s] = live ? *(const u32x4 *)(qrow + 8 * (4 * s + g)) : z;
             if constexpr (USE_R) rf[s] = live ? *(const u32x4 *)(rrow + 8 * (4 * s + g)) : z;
         }
-        scope.column(P, b, t, live, col_lo, col_end, col_words);
+        scope.column(P, b, t, live, col_lo, col_end, col_nodes);
     }
     float m_run = kNegInf, dsum1 = 0.f, dsum2 = 0.f;
     f32x4 o1[NDB], o2[NDB];
@@ -241,7 +208,7 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
     // 32 keys of a tile that some column does not see completely: which keys, and the values of V that are not finite reach the
     // columns that see their key; then (behind a barrier) they are taken out of the tile.
     auto mask_tile = [&](const u32x4 *tileV, int tk, uint32_t &seen) __attribute__((always_inline)) {
-        seen = scope.seen(P, col_words, col_lo, col_end, tk, g);
+        seen = scope.seen(P, col_nodes, col_lo, col_end, tk, g);
         const u32x4 big = big_halves(seen);
 #pragma unroll
         for (int i = 0; i < NDB; ++i) {
@@ -358,7 +325,7 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
     }
     if (x >= n_cols) return;
     // (a node behind the drafted ones sees nothing, also where all others see everything)
-    const WideColumn<D> column(p, b, hk, x, split, m_star, w0 * e1 + w1 * f1, w0 * e2 + w1 * f2, col_end == 0, g == 0);
+    const RowsColumn<D> column(p, b, hk, x, split, m_star, w0 * e1 + w1 * f1, w0 * e2 + w1 * f2, col_end == 0, g == 0);
 #pragma unroll
     for (int i = 0; i < NDB; ++i) {
         f32x4 a1 = o1[i], a2 = o2[i];

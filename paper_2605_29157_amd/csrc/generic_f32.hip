@@ -244,11 +244,12 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_forward_ke
     int all_lo = row_lo(t1), all_end = row_end(t0);  // every column sees [all_lo, all_end)
     int lo = row_lo(t0) / 16, hi = (row_end(t1) + 15) / 16;  // 16-key blocks of the union
     int last_key = row_end(t1) - 1;
-    const uint64_t *words = nullptr;
+    TreeRow nodes{};
     int sinks = 0, n_sink_blocks = 0, skip = 0;  // VIS: block i of the walk is key block i, or i + skip behind the sinks'
     if constexpr (VIS) {
         if (tree) {
-            words = p.mask + (int64_t)b * p.mask_stride_b + (int64_t)t * p.mask_words;
+            const uint64_t *words = p.mask + (int64_t)b * p.mask_stride_b + (int64_t)t * p.mask_words;
+            nodes = {words, *words};
             my_end = t < n ? len : 0, my_lo = 0;
             all_lo = 0, all_end = base, lo = 0;
             hi = t0 < n ? (len + 15) / 16 : 0, last_key = len - 1;
@@ -340,7 +341,7 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_forward_ke
         const bool whole = (key0 >= all_lo || (VIS && key0 + 16 <= sinks)) && key0 + 16 <= all_end;  // uniform
         uint32_t bits = 0xffffffffu;  // (of the block's keys, from key0 on)
         if constexpr (VIS)
-            if (tree && key0 + 16 > base) bits = tree_bits(words, p.mask_words, key0 - base);
+            if (tree && key0 + 16 > base) bits = tree_bits(nodes, p.mask_words, key0 - base);
         unsigned seen = 15u;
         float tmax = kNegInf;
 #pragma unroll

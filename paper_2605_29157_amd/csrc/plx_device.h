@@ -136,14 +136,19 @@ __device__ __forceinline__ int lds_chunk_slot(int row, int chunk) {
     return row * CPR + (chunk ^ lds_row_swizzle<D>(row));
 }
 
+// A node's row of a tree mask; its first word is fetched in advance
+struct TreeRow {
+    const uint64_t *words;
+    uint64_t first;
+};
 // The bits of a node's mask for keys base + rel .. base + rel + 31 (committed keys, rel < 0, count as set)
-__device__ __forceinline__ uint32_t tree_bits(const uint64_t *words, int n_words, int rel) {
+__device__ __forceinline__ uint32_t tree_bits(const TreeRow &row, int n_words, int rel) {
     if (rel <= -32) return 0xffffffffu;
-    if (rel < 0) return ((uint32_t)words[0] << -rel) | ((1u << -rel) - 1u);
+    if (rel < 0) return ((uint32_t)row.first << -rel) | ((1u << -rel) - 1u);
     const int w = rel >> 6, s = rel & 63;
     if (w >= n_words) return 0u;
-    uint64_t x = words[w] >> s;
-    if (s > 32 && w + 1 < n_words) x |= words[w + 1] << (64 - s);
+    uint64_t x = (w == 0 ? row.first : row.words[w]) >> s;
+    if (s > 32 && w + 1 < n_words) x |= row.words[w + 1] << (64 - s);
     return (uint32_t)x;
 }
 

@@ -63,11 +63,10 @@ struct RowsScope {
         return (key >= lo_all || key + count <= sinks) && key + count <= end_all;
     }
     // Keys of one column: [lo, end) and the sinks below end, of the drafted ones those whose bit is set
-    __device__ __forceinline__ void column(const DecodeRowsParams &P, int b, int t, bool live, int &lo, int &end,
-                                           const uint64_t *&words) const {
-        words = nullptr;
+    __device__ __forceinline__ void column(const DecodeRowsParams &P, int b, int t, bool live, int &lo, int &end, TreeRow &nodes) const {
         if constexpr (TREE) {
-            words = P.mask + (int64_t)b * P.mask_stride_b + (int64_t)t * P.mask_words;
+            const uint64_t *words = P.mask + (int64_t)b * P.mask_stride_b + (int64_t)t * P.mask_words;
+            nodes = {words, *words};
             end = live && t < n ? Lb : 0;
             lo = 0;
             if (P.d.window > 0) {
@@ -84,10 +83,10 @@ struct RowsScope {
         }
     }
     // Bit e of the result: the column sees key first + 16 (e / 4) + e % 4 (first = key + 4 g of a 32-key block)
-    __device__ __forceinline__ uint32_t seen(const DecodeRowsParams &P, const uint64_t *words, int lo, int end, int key, int g) const {
+    __device__ __forceinline__ uint32_t seen(const DecodeRowsParams &P, const TreeRow &nodes, int lo, int end, int key, int g) const {
         uint32_t bits = 0xffffffffu, out = 0;
         if constexpr (TREE)
-            if (key + 32 > base) bits = tree_bits(words, P.mask_words, key - base);
+            if (key + 32 > base) bits = tree_bits(nodes, P.mask_words, key - base);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int at = 16 * (e >> 2) + 4 * g + (e & 3), k = key + at;
@@ -107,6 +106,39 @@ struct RowsPages {
         const int page_no = key / p.page_size, row = key - page_no * p.page_size;
         const int64_t page = min(max(table[page_no], 0), p.num_pages - 1);
         ko = page * p.ksb + (int64_t)row * p.ksl, vo = page * p.vsb + (int64_t)row * p.vsl;
+    }
+};
+
+// Four dimensions of a finished column: of its record, or of its output row
+template <int D>
+struct RowsColumn {
+    const DecodeParams &p;
+    int64_t row;
+    float d1, d2, inv, gain;
+    float *rec;
+    bool none, nan;
+    __device__ __forceinline__ RowsColumn(const DecodeParams &p, int b, int hk, int x, int split, float m, float d1_, float d2_, bool none, bool head)
+        : p(p), d1(none ? 0.f : d1_), d2(none ? 0.f : d2_), none(none) {
+        const int t = x / p.G, h = x - t * p.G;
+        row = ((int64_t)b * p.Hq + (int64_t)hk * p.G + h) * p.Tq + t;
+        nan = d1 != d1;
+        inv = d1 != 0.f ? 1.f / d1 : 0.f, gain = inv * (1.f + d2 * inv);
+        rec = p.ws + (row * p.S + split) * (int64_t)(2 * D + 4);
+        // (NaN: a record that the merge takes alone)
+        if (!p.direct_out && head) *(f32x4 *)rec = nan ? f32x4{3.0e38f, -kNegInf, 0.f, 0.f} : f32x4{none ? kNegInf : m, d1, d2, 0.f};
+    }
+    __device__ __forceinline__ void store(int dim, f32x4 a1, f32x4 a2) const {
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        if (none) a1 = a2 = zero;
+        if (p.direct_out) {
+            f32x4 y = zero;  // empty key set: zeros
+            if (d1 != 0.f) y = a1 * gain - a2 * inv;
+            *(u32x2 *)((__bf16 *)p.o + row * D + dim) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+        } else {
+            if (nan) a1[0] = a1[1] = a1[2] = a1[3] = __builtin_nanf("");
+            *(f32x4 *)(rec + 4 + dim) = a1;
+            *(f32x4 *)(rec + 4 + D + dim) = a2;
+        }
     }
 };
 
