@@ -340,6 +340,23 @@ def _stream_ptr(stream) -> int:
     return int(stream.cuda_stream)
 
 
+def _here() -> int:
+    return _raw_device() if _raw_device is not None else torch.cuda.current_device()
+
+
+def _on_current_device(where, *tensors):
+    """Refuses tensors (None: left out) that are not all on the current device, where the launch goes."""
+    here = -1
+    for t in tensors:
+        if t is not None:
+            at = t.get_device()
+            if at < 0 or (here >= 0 and at != here):
+                raise ValueError("%s needs device tensors of one device" % where)
+            here = at
+    if here != _here():
+        raise ValueError("%s: the tensors are on device %d, which is not the current one" % (where, here))
+
+
 def _bytes(t) -> int:
     return t.numel() * t.element_size()
 
@@ -501,33 +518,32 @@ def parallax_decode(q, r, k, v, scale, seq_lens=None, use_r=True, num_splits=0, 
 def _decode_rows(q, r, k, v, scale, seq_lens, use_r, num_splits, workspace, out, stream, block_table, max_len, window,
                  sinks, tree_mask=None, draft_lens=None):
     """parallax_decode_sinks, or parallax_decode_tree with a tree_mask."""
+    # (a step of one sequence is bound by the host: each property of a tensor is asked for once)
     where = "parallax_decode_sinks" if tree_mask is None else "parallax_decode_tree"
-    for t in (q, r, k, v, out, seq_lens, block_table, tree_mask, draft_lens, workspace):
-        if t is not None and (not t.is_cuda or t.device != q.device):
-            raise ValueError("%s needs device tensors of one device" % where)
-    if q.dim() not in (3, 4) or k.dim() != 4 or v.shape != k.shape or k.shape[3] != q.shape[-1]:
+    _on_current_device(where, q, r, k, v, out, seq_lens, block_table, tree_mask, draft_lens, workspace)
+    shape, cache, dtype = q.shape, k.shape, q.dtype
+    if len(shape) not in (3, 4) or len(cache) != 4 or v.shape != cache or cache[3] != shape[-1]:
         raise ValueError("q [B, Hq, (Tq,) d], k and v of one shape [.., Hkv, .., d]")
     if use_r and r is None:
         raise ValueError("r is needed unless use_r=False")
-    for t in (r, out):
-        if t is not None and t.shape != q.shape:
-            raise ValueError("r and out have the shape of q")
-    for t in (r, k, v, out):
-        if t is not None and t.dtype != q.dtype:
-            raise TypeError("q, r, k, v and out have one dtype")
-    if k.stride(-1) != 1 or v.stride(-1) != 1 or not all(t is None or t.is_contiguous() for t in (q, r, out)):
+    if (r is not None and r.shape != shape) or (out is not None and out.shape != shape):
+        raise ValueError("r and out have the shape of q")
+    if k.dtype != dtype or v.dtype != dtype or (r is not None and r.dtype != dtype) or (out is not None and out.dtype != dtype):
+        raise TypeError("q, r, k, v and out have one dtype")
+    if (k.stride(-1) != 1 or v.stride(-1) != 1 or not q.is_contiguous() or (r is not None and not r.is_contiguous())
+            or (out is not None and not out.is_contiguous())):
         raise ValueError("q, r, out must be contiguous and k, v contiguous in the last dimension")
-    B, Hq, d = q.shape[0], q.shape[1], q.shape[-1]
-    Tq = q.shape[2] if q.dim() == 4 else 1
+    B, Hq, d = shape[0], shape[1], shape[-1]
+    Tq = shape[2] if len(shape) == 4 else 1
     for name, t in (("seq_lens", seq_lens), ("draft_lens", draft_lens)):
-        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (B,) or not t.is_contiguous()):
+        if t is not None and (t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous()):
             raise TypeError("%s must be a contiguous int32 tensor [B]" % name)
     if block_table is not None:
         if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.stride(1) != 1:
             raise TypeError("block_table must be an int32 device tensor [B, pages per sequence]")
         if block_table.shape[0] != B:
             raise ValueError("block_table needs one row per sequence")
-    elif k.shape[0] != B:
+    elif cache[0] != B:
         raise ValueError("k and v need one cache per sequence")
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError("the workspace must be contiguous")
@@ -541,15 +557,15 @@ def _decode_rows(q, r, k, v, scale, seq_lens, use_r, num_splits, workspace, out,
         words = -(-Tq // 64)
         if tree_mask.dtype != torch.int64 or not tree_mask.is_contiguous():
             raise TypeError("tree_mask must be a contiguous int64 tensor of 64-bit words")
-        shape = tuple(tree_mask.shape)
-        if words == 1 and shape in ((Tq,), (1, Tq), (B, Tq)):
-            shape += (1,)
-        if len(shape) == 2:
-            shape = (1,) + shape
-        if shape not in ((1, Tq, words), (B, Tq, words)):
+        rows = tuple(tree_mask.shape)
+        if words == 1 and rows in ((Tq,), (1, Tq), (B, Tq)):
+            rows += (1,)
+        if len(rows) == 2:
+            rows = (1,) + rows
+        if rows not in ((1, Tq, words), (B, Tq, words)):
             raise ValueError("tree_mask must be [(1 or B,) Tq, ceil(Tq/64)]")
         tree = plx_decode_tree_args()
-        tree.decode, tree.tree_mask, tree.mask_batch = a, tree_mask.data_ptr(), shape[0]
+        tree.decode, tree.tree_mask, tree.mask_batch = a, tree_mask.data_ptr(), rows[0]
         tree.draft_lens, tree.sinks = _ptr(draft_lens), sinks
         a = tree.decode  # (the copy inside)
         splits, call, head = lib.parallax_decode_tree_call_splits, lib.parallax_decode_tree, (ctypes.byref(tree),)
@@ -939,13 +955,21 @@ def parallax_decode_mla(q, r, ckv, scale, seq_lens=None, num_splits=0, out=None,
 
 
 def _int_list(where, name, t, n=None, device=None):
-    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
+    at = t.get_device()
+    if at < 0 or t.dtype != torch.int32 or not t.is_contiguous():
         raise TypeError("%s: %s must be a contiguous int32 device tensor" % (where, name))
     if n is not None and t.numel() != n:
         raise ValueError("%s: %s must have %d entries" % (where, name, n))
-    if device is not None and t.device != device:
+    if device is not None and at != device:
         raise ValueError("%s: %s is on another device" % (where, name))
     return t.data_ptr()
+
+
+def _table_device(where, pages):
+    """The device of a PageTable, which is the one that the launch goes to."""
+    if pages._device != _here():
+        raise ValueError("%s: the table is on device %d, which is not the current one" % (where, pages._device))
+    return pages._device
 
 
 class PageTable:
@@ -954,17 +978,17 @@ class PageTable:
     tensors are the caller's and are what parallax_decode and the others take as block_table and seq_lens; `empty` makes
     those of a cache nobody uses yet."""
 
-    __slots__ = ("block_table", "seq_lens", "page_refs", "free_pages", "free_count", "page_size", "_args")
+    __slots__ = ("block_table", "seq_lens", "page_refs", "free_pages", "free_count", "page_size", "_args", "_device")
 
     def __init__(self, block_table, seq_lens, page_refs, free_pages, free_count, page_size):
         if block_table.dtype != torch.int32 or not block_table.is_cuda or block_table.dim() != 2 or block_table.stride(1) != 1:
             raise TypeError("block_table must be an int32 device tensor [sequences, pages per sequence]")
-        device, (sequences, width), pages = block_table.device, block_table.shape, page_refs.numel()
+        device, (sequences, width), pages = block_table.get_device(), block_table.shape, page_refs.numel()
         ptrs = [_int_list("PageTable", name, t, n, device) for name, t, n in (
             ("seq_lens", seq_lens, sequences), ("page_refs", page_refs, pages), ("free_pages", free_pages, pages),
             ("free_count", free_count, 1))]
         self.block_table, self.seq_lens, self.page_refs = block_table, seq_lens, page_refs
-        self.free_pages, self.free_count, self.page_size = free_pages, free_count, int(page_size)
+        self.free_pages, self.free_count, self.page_size, self._device = free_pages, free_count, int(page_size), device
         self._args = _filled(plx_page_table, block_table.data_ptr(), *ptrs, sequences, width,
                              block_table.stride(0) if sequences > 1 else width, pages, _i32(page_size))
 
@@ -980,13 +1004,14 @@ def _pools(where, k, v):
     """The fields of a plx_cache_pools: [pages, heads, rows, d], or [pages, rows, d] for one head."""
     if k.dim() == 3:
         k = k.unsqueeze(1)
-    if k.dim() != 4 or not k.is_cuda or k.stride(-1) != 1:
+    _on_current_device(where, k, v)
+    if k.dim() != 4 or k.stride(-1) != 1:
         raise ValueError("%s needs device pools [num_pages, (heads,) page_size, d], contiguous in the last dimension" % where)
     vs = (0, 0, 0)
     if v is not None:
         if v.dim() == 3:
             v = v.unsqueeze(1)
-        if v.shape != k.shape or v.dtype != k.dtype or v.device != k.device or v.stride(-1) != 1:
+        if v.shape != k.shape or v.dtype != k.dtype or v.stride(-1) != 1:
             raise ValueError("%s: k and v are pools of one shape and type" % where)
         vs = v.stride()[:3]
     pages, heads, rows, d = k.shape
@@ -995,7 +1020,8 @@ def _pools(where, k, v):
 
 def parallax_cache_fork(pages, parents, children, stream=None):
     """Sequence children[i] (empty) becomes a copy of parents[i] that shares its pages; see parallax_cache_fork in the header."""
-    where, device = "parallax_cache_fork", pages.block_table.device
+    where = "parallax_cache_fork"
+    device = _table_device(where, pages)
     n = parents.numel()
     ptrs = _int_list(where, "parents", parents, None, device), _int_list(where, "children", children, n, device)
     st = load_library().parallax_cache_fork(ctypes.byref(pages._args), *ptrs, n, _stream_ptr(stream))
@@ -1008,7 +1034,8 @@ def parallax_cache_extend(pages, seqs, new_lens, *pools, stream=None):
     last pages that are replaced are copied in all of them. Returns `missing` (int32 [1] on the device: 0, or how many
     pages were lacking, and then nothing was changed). Without pools (missing, src, dst, rows) is returned, and
     parallax_cache_copy(k, v, src, dst, rows) is the caller's to call for every layer."""
-    where, device = "parallax_cache_extend", pages.block_table.device
+    where = "parallax_cache_extend"
+    device = _table_device(where, pages)
     n = seqs.numel()
     ptrs = _int_list(where, "seqs", seqs, None, device), _int_list(where, "new_lens", new_lens, n, device)
     if len(pools) % 2:
@@ -1016,7 +1043,7 @@ def parallax_cache_extend(pages, seqs, new_lens, *pools, stream=None):
     for k in pools[::2]:
         if k.shape[0] != pages.page_refs.numel() or k.shape[-2] != pages.page_size:
             raise ValueError("the pools have the pages of the table")
-    buf = _result_maker(stream, torch.empty)(3 * n + 1, dtype=torch.int32, device=device)
+    buf = _result_maker(stream, torch.empty)(3 * n + 1, dtype=torch.int32, device=pages.block_table.device)
     at = buf.data_ptr()
     src, dst, rows, missing = at, at + 4 * n, at + 8 * n, at + 12 * n
     lib, where_to = load_library(), _stream_ptr(stream)
@@ -1034,7 +1061,8 @@ def parallax_cache_extend(pages, seqs, new_lens, *pools, stream=None):
 def parallax_cache_free(pages, seqs, first=None, last=None, stream=None):
     """Sequence seqs[i] gives back the whole pages in its tokens first[i] .. last[i] - 1 (default: all of them; a last[i] at or
     behind its length takes the partial last page along and shortens the sequence to first[i])."""
-    where, device = "parallax_cache_free", pages.block_table.device
+    where = "parallax_cache_free"
+    device = _table_device(where, pages)
     n = seqs.numel()
     ptrs = [_int_list(where, "seqs", seqs, None, device)]
     ptrs += [0 if t is None else _int_list(where, name, t, n, device) for name, t in (("first", first), ("last", last))]
@@ -1048,8 +1076,8 @@ def parallax_cache_copy(k, v, src, dst, rows=None, stream=None):
     where = "parallax_cache_copy"
     a = _filled(plx_cache_pools, *_pools(where, k, v))
     n = src.numel()
-    ptrs = [_int_list(where, "src", src, None, k.device), _int_list(where, "dst", dst, n, k.device)]
-    ptrs.append(0 if rows is None else _int_list(where, "rows", rows, n, k.device))
+    ptrs = [_int_list(where, "src", src, None, _here()), _int_list(where, "dst", dst, n, _here())]
+    ptrs.append(0 if rows is None else _int_list(where, "rows", rows, n, _here()))
     st = load_library().parallax_cache_copy(ctypes.byref(a), *ptrs, n, _stream_ptr(stream))
     if st != PLX_OK:
         raise ParallaxError(st, where)
@@ -1071,12 +1099,13 @@ def parallax_cache_compact(k, v, seq_lens, draft_lens, accepted, n_accepted, blo
         max_draft = 256
     if new_lens is None:
         new_lens = _result_maker(stream, torch.empty)(B, dtype=torch.int32, device=k.device)
-    ptrs = [0 if t is None else _int_list(where, name, t, m, k.device) for name, t, m in (
+    here = k.get_device()
+    ptrs = [0 if t is None else _int_list(where, name, t, m, here) for name, t, m in (
         ("seq_lens", seq_lens, B), ("draft_lens", draft_lens, B), ("accepted", accepted, B * most),
         ("n_accepted", n_accepted, B), ("new_lens", new_lens, B))]
     table, stride = 0, 0
     if block_table is not None:
-        if block_table.dtype != torch.int32 or block_table.device != k.device or block_table.stride(1) != 1:
+        if block_table.dtype != torch.int32 or block_table.get_device() != here or block_table.stride(1) != 1:
             raise TypeError("block_table must be an int32 device tensor [B, pages per sequence]")
         if block_table.shape[0] != B:
             raise ValueError("block_table needs one row per sequence")
