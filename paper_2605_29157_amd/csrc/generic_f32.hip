@@ -726,6 +726,14 @@ struct F32ColsLds {
     };
 };
 
+// SINKS: where the sums of one part of a key block that holds sinks are, in floats from p.sink_sums on: [dK | dV][16 keys][d]
+__device__ __forceinline__ int64_t f32_sink_record(const PrefillBwdParams &p, int64_t pair, int block, int part) {
+    return ((pair * p.sink_blocks + block) * p.sink_parts + part) * (2 * 16 * (int64_t)p.d);
+}
+
+// SINKS: a block of keys that holds sinks is seen by all rows from it on; its items (row tiles of all heads of the group) are
+// cut into p.sink_parts parts of p.sink_part_tiles, workgroups of their own whose sums f32_sink_combine_kernel adds up.
+// In one piece the pass took 334 us for 8 heads x 8192 rows, window 96, 4 sinks, against 63 without sinks; in parts 85 and 4 for adding them up.
 template <int DP, bool FULL, bool SINKS = false>
 __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_bwd_cols_kernel(PrefillBwdParams p) {
     __shared__ F32ColsLds<DP> lds;
@@ -734,11 +742,20 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_bwd_cols_k
     const int c = lane & 15, g = lane >> 4, d = FULL ? DP : p.d, off = p.Tk - p.T;
     const int n_blocks = (p.Tk + 15) / 16;
     int64_t id = f32_block_id();
-    if (id >= (int64_t)n_blocks * p.B * p.Hkv) return;
+    const int n_parts = SINKS ? p.sink_blocks * p.sink_parts : 0;
+    if (id >= ((int64_t)n_blocks + (SINKS ? n_parts - p.sink_blocks : 0)) * p.B * p.Hkv) return;
     const int hk = (int)(id % p.Hkv);
     id /= p.Hkv;
     const int b = (int)(id % p.B);
-    const int j0 = 16 * (int)(id / p.B);  // first key; causal: the first keys are seen by most rows
+    int block = (int)(id / p.B), part = 0;  // causal: the first keys are seen by most rows
+    if constexpr (SINKS) {
+        if (block < n_parts)
+            part = block % p.sink_parts, block /= p.sink_parts;
+        else
+            block -= n_parts - p.sink_blocks;
+    }
+    const int j0 = 16 * block;  // first key
+    const bool with_sinks = SINKS && j0 < p.sinks;
     const int64_t khead = ((int64_t)b * p.Hkv + hk) * p.Tk;
     for (int e = tid; e < 16 * (DP / 4); e += kF32Threads) {
         const int row = e / (DP / 4), dim = 4 * (e % (DP / 4));
@@ -755,11 +772,13 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_bwd_cols_k
     auto key_end = [&](int j) { return p.window > 0 ? min(p.T, max(j - off + p.window, 0)) : p.T; };
     const int j_last = min(j0 + 15, p.Tk - 1), j = min(j0 + c, j_last);
     const int my_lo = key_lo(j), my_end = SINKS && j < p.sinks ? p.T : key_end(j);
-    const int lo = key_lo(j0) / 16, end = SINKS && j0 < p.sinks ? p.T : key_end(j_last);  // union (both bounds grow with the key)
+    const int lo = key_lo(j0) / 16, end = with_sinks ? p.T : key_end(j_last);  // union (both bounds grow with the key)
     // (sinks: the first key behind them drops out first)
     const int first_out = SINKS ? max(j0, p.sinks) : j0;
     const int all_lo = key_lo(j_last), all_end = SINKS && first_out > j_last ? p.T : key_end(first_out);
-    const int per_head = max((end + 15) / 16 - lo, 0), n_items = per_head * p.G;
+    const int per_head = max((end + 15) / 16 - lo, 0), all_items = per_head * p.G;
+    const int first_item = with_sinks ? min(part * p.sink_part_tiles, all_items) : 0;
+    const int n_items = with_sinks ? min(first_item + p.sink_part_tiles, all_items) : all_items;
 
     f32x4 xq[NA], xr[NA], xg[NA];
     auto load = [&](f32x4(&x)[NA], const void *base, int item) {
@@ -771,7 +790,7 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_bwd_cols_k
 #pragma unroll
     for (int n = 0; n < NA; ++n) dk[n] = dv[n] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float scale_log2 = p.scale * kLog2e;
-    int item = w;
+    int item = first_item + w;
     if (item < n_items) load(xq, p.q, item), load(xr, p.r, item), load(xg, p.d_o, item);
     __syncthreads();
     for (; item < n_items; item += kF32Waves) {
@@ -810,18 +829,54 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_bwd_cols_k
         add(xr, p.r, g2, dk);
         add(xg, p.d_o, wt, dv);
     }
-    f32_sum_waves<NA>(dk, dv, lds.merge, w, lane, n_items);
+    f32_sum_waves<NA>(dk, dv, lds.merge, w, lane, n_items - first_item);
     if (w != 0 || j0 + c >= p.Tk) return;
-    const int64_t e0 = (khead + j0 + c) * d;
+    const int64_t e0 = with_sinks ? c * d : (khead + j0 + c) * d;
+    float *const out_k = with_sinks ? p.sink_sums + f32_sink_record(p, (int64_t)b * p.Hkv + hk, block, part) : (float *)p.dk;
+    float *const out_v = with_sinks ? out_k + 16 * d : (float *)p.dv;
 #pragma unroll
     for (int m = 0; m < DP / 64; ++m)
 #pragma unroll
         for (int rr = 0; rr < 4; ++rr) {
             const int dim = 64 * m + 16 * g + 4 * rr;
             if (dim >= d) continue;
-            *(f32x4 *)((float *)p.dk + e0 + dim) = f32x4{dk[4 * m][rr], dk[4 * m + 1][rr], dk[4 * m + 2][rr], dk[4 * m + 3][rr]};
-            *(f32x4 *)((float *)p.dv + e0 + dim) = f32x4{dv[4 * m][rr], dv[4 * m + 1][rr], dv[4 * m + 2][rr], dv[4 * m + 3][rr]};
+            *(f32x4 *)(out_k + e0 + dim) = f32x4{dk[4 * m][rr], dk[4 * m + 1][rr], dk[4 * m + 2][rr], dk[4 * m + 3][rr]};
+            *(f32x4 *)(out_v + e0 + dim) = f32x4{dv[4 * m][rr], dv[4 * m + 1][rr], dv[4 * m + 2][rr], dv[4 * m + 3][rr]};
         }
+}
+
+// dK and dV of the key blocks that hold sinks: the sums of their parts, in order. Four dimensions of a key a thread.
+__global__ __launch_bounds__(kF32Threads) void f32_sink_combine_kernel(PrefillBwdParams p) {
+    const int quads = p.d / 4, keys = min(16 * p.sink_blocks, p.Tk);
+    int64_t id = (int64_t)blockIdx.x * kF32Threads + threadIdx.x;
+    if (id >= (int64_t)p.B * p.Hkv * keys * 2 * quads) return;
+    const int dim = 4 * (int)(id % quads);
+    id /= quads;
+    const int j = (int)(id % keys);
+    id /= keys;
+    const int which = (int)(id & 1);
+    const int64_t pair = id >> 1;
+    const float *rec = p.sink_sums + f32_sink_record(p, pair, j / 16, 0) + (which * 16 + j % 16) * p.d + dim;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int part = 0; part < p.sink_parts; ++part) sum += *(const f32x4 *)(rec + (int64_t)part * 2 * 16 * p.d);
+    *(f32x4 *)((float *)(which ? p.dv : p.dk) + (pair * p.Tk + j) * p.d + dim) = sum;
+}
+
+// Parts of the key blocks with sinks, and the bytes of their sums. A part has as many items as a block behind the sinks, or a
+// 512th of all where that is more (two workgroups a unit; so there are never many more than 512 parts).
+static int64_t plan_sinks_f32(PrefillBwdParams &p) {
+    const int64_t tiles = (p.T + 15) / 16, key_blocks = (p.Tk + 15) / 16, pairs = (int64_t)p.B * p.Hkv;
+    const int64_t ordinary = p.G * std::min((int64_t)p.window / 16 + 2, tiles);
+    p.sink_blocks = (int)((std::min(p.sinks, p.Tk) + 15) / 16);
+    const int64_t all = pairs * (key_blocks * ordinary + p.sink_blocks * tiles * p.G);
+    p.sink_part_tiles = (int)std::min(std::max({ordinary, (int64_t)8, all / 512}), tiles * p.G);
+    p.sink_parts = (int)((tiles * p.G + p.sink_part_tiles - 1) / p.sink_part_tiles);
+    return pairs * p.sink_blocks * p.sink_parts * 2 * 16 * p.d * (int64_t)sizeof(float);
+}
+
+size_t backward_sinks_bytes_f32(const PrefillBwdParams &p) {
+    PrefillBwdParams q = p;
+    return (size_t)plan_sinks_f32(q);
 }
 
 int32_t backward_form_f32(const PrefillBwdParams &p) {
@@ -838,7 +893,13 @@ static hipError_t launch_backward(const PrefillBwdParams &p, hipStream_t stream)
     if (p.sinks > 0) {
         hipLaunchKernelGGL((f32_bwd_rows_kernel<DP, FULL, true>), f32_grid(row_blocks * p.B * p.Hq), dim3(kF32Threads), 0, stream, p);
         if (hipError_t err = hipGetLastError()) return err;
-        hipLaunchKernelGGL((f32_bwd_cols_kernel<DP, FULL, true>), f32_grid(key_blocks * p.B * p.Hkv), dim3(kF32Threads), 0, stream, p);
+        PrefillBwdParams q = p;
+        plan_sinks_f32(q);
+        const int64_t cols = key_blocks + (int64_t)q.sink_blocks * (q.sink_parts - 1);
+        hipLaunchKernelGGL((f32_bwd_cols_kernel<DP, FULL, true>), f32_grid(cols * p.B * p.Hkv), dim3(kF32Threads), 0, stream, q);
+        if (hipError_t err = hipGetLastError()) return err;
+        const int64_t threads = (int64_t)p.B * p.Hkv * std::min(16 * q.sink_blocks, p.Tk) * 2 * (p.d / 4);
+        hipLaunchKernelGGL(f32_sink_combine_kernel, dim3((unsigned)((threads + kF32Threads - 1) / kF32Threads)), dim3(kF32Threads), 0, stream, q);
         return hipGetLastError();
     }
     if (form / 256) {

@@ -894,8 +894,8 @@ plx_status prepare_backward_sinks(const plx_prefill_bwd_args *a, int32_t sinks, 
     if (st != PLX_OK) return st;
     const size_t rows = parallax_prefill_backward_workspace_bytes(a->B, a->Hq, a->T);
     *bytes = rows;
-    if (p.sinks > 0 && a->dtype == PLX_BF16) {
-        *bytes += plx::backward_sinks_bytes_bf16(p, query_num_cus());
+    if (p.sinks > 0) {
+        *bytes += a->dtype == PLX_F32 ? plx::backward_sinks_bytes_f32(p) : plx::backward_sinks_bytes_bf16(p, query_num_cus());
         p.sink_sums = reinterpret_cast<float *>(static_cast<char *>(b.workspace) + rows);
     }
     if (need_workspace && a->workspace_bytes < *bytes) return PLX_ERR_WORKSPACE;

@@ -121,8 +121,8 @@ struct PrefillBwdParams {
     // this many entries, the other one if they hold more
     int32_t list_limit;
     int32_t sinks;  // > 0 (window > 0): the first `sinks` keys stay visible
-    // bf16: the key blocks with sinks (sink_blocks per head) are cut into sink_parts parts of sink_part_tiles 64-row tiles (set by
-    // the launcher), whose sums are in sink_sums
+    // the key blocks with sinks (sink_blocks per head) are cut into sink_parts parts of sink_part_tiles row tiles (set by the
+    // launcher; bf16: 64 rows, fp32: 16 rows of one head of the group), whose sums are in sink_sums
     int32_t sink_part_tiles, sink_parts, sink_blocks;
     float *sink_sums;
 };
@@ -191,6 +191,7 @@ size_t plan_prefill_bf16(PrefillParams &p, int num_cus, bool with_ranges);
 // keys per workgroup of the column pass, plus 256 * rows per workgroup of the row pass, plus 65536 where the lists decide
 int32_t backward_form_bf16(const PrefillBwdParams &p, int num_cus);
 size_t backward_sinks_bytes_bf16(const PrefillBwdParams &p, int num_cus);  // of sink_sums
+size_t backward_sinks_bytes_f32(const PrefillBwdParams &p);
 hipError_t launch_prefill_bwd_bf16(const PrefillBwdParams &p, int num_cus, hipStream_t stream);
 // 32 for a pass in bf16 thirds (prefill_f32.hip), 0 on the fp32 instruction; the backward as backward_form_bf16
 int32_t prefill_form_f32(const PrefillParams &p);
