@@ -3,16 +3,18 @@
 // decode_rows_bf16.hip; here the waves of a workgroup share the keys instead of the columns.
 //
 // What bounds it: by the counts, up to 64 columns the bytes of K and V (every key is fetched once for all columns), with 128 the
-// matrix work (8 D flop a score). In fact the three things that a tile takes of a compute unit add up more than they overlap:
-// for 64 keys x 128 columns at D = 128 its matrix instructions 1.1 us, its reads of LDS 0.9 (a wave reads all of its keys' K and V
-// for 16 columns), its exponentials and other vector work 0.5; measured 2.5 with all units at work, 2.05 with few.
+// matrix work (8 D flop a score). In fact the two waves of a SIMD overlap only in part: for 64 keys x 128 columns at D = 128
+// the matrix instructions take 1.1 us, vector work 0.6 (exponentials: 16 clocks each); measured 2.3 with all units at work,
+// 1.9 with few.
 //
 // Layout:
 //   * eight waves, two per SIMD, so that the vector work of one runs under the matrix instructions of the other: up to 64 columns
 //     four blocks of 16 columns and two halves of a tile of 128 keys, beyond eight blocks of 16 columns and tiles of 64. A wave
-//     takes its 64 keys in one go, one test and no branch between their products. Measured (us; 16 x up to 6000 keys, 8 key heads,
-//     52 columns, 2 splits; 8 x 16384 keys, 4 key heads, 256 columns, 4 splits): 32 keys in one go 107, 188; 64 99, 177. Four waves
-//     of 32 columns, which halve the reads of LDS, their steps pipelined by hand: 210 for the second;
+//     takes its 64 keys in one go, one test and no branch between their products, and reads its operands four fragments
+//     ahead. Measured (us; 16 x up to 6000 keys, 8 key heads, 52 columns, 2 splits; 8 x 16384 keys, 4 key heads, 256
+//     columns, 4 splits): 32 keys in one go 107, 188; 64 99, 177; reads ahead and no bank conflicts 96, 170; the waves with matrix
+//     work preferred 95.5, 167. Four waves of 32 columns, which halve the reads of LDS, their steps pipelined by hand: 210 for
+//     the second;
 //   * tiles in a ring of 128 KB of LDS, filled by direct global -> LDS loads (no registers parked), 64 - 96 KB of it on
 //     their way; one barrier per tile;
 //   * the reference of the exponentials is moved only when a score exceeds it by 2^6 (then the sums are rescaled): no
@@ -24,11 +26,16 @@
 namespace plx {
 
 namespace {
-// Chunk c of a tile's row is at row * CPR + (c ^ rows_swizzle(row)): eight rows of one chunk (a K operand read by eight lanes)
-// and four rows of two chunks (a transposing V read by sixteen) are in different 128 bytes each.
-__device__ __forceinline__ int rows_swizzle(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+// Chunk c of a tile's row is at row * CPR + (c ^ rows_swizzle(row)). At D = 128 a row is 256 bytes, all 64 banks once: the sixteen rows of
+// one chunk that a K operand reads get sixteen different chunks, the eight rows of two chunks of a transposing V read sixteen as
+// well (with eight different chunks only, every second access waited for a bank).
 template <int D>
-__device__ __forceinline__ int rows_chunk_slot(int row, int chunk) { return row * (D / 8) + (chunk ^ rows_swizzle(row)); }
+__device__ __forceinline__ int rows_swizzle(int row) {
+    const int low = ((row & 3) << 1) | ((row >> 2) & 1);
+    return D == 128 ? low | (((row << 1) ^ row) & 8) : low;
+}
+template <int D>
+__device__ __forceinline__ int rows_chunk_slot(int row, int chunk) { return row * (D / 8) + (chunk ^ rows_swizzle<D>(row)); }
 
 constexpr float kWideSlack = 6.f;  // in the exponent of 2
 
@@ -86,14 +93,14 @@ struct WideLoader {
                 const uint32_t k0 = __umul24((uint32_t)row0, k_row_bytes), v0 = __umul24((uint32_t)row0, v_row_bytes);
 #pragma unroll
                 for (int i = 0; i < LOADS; ++i) {
-                    const uint32_t chunk = 16u * (uint32_t)((l % CPR) ^ rows_swizzle(run_first + row0 + RPL * i));
+                    const uint32_t chunk = 16u * (uint32_t)((l % CPR) ^ rows_swizzle<D>(run_first + row0 + RPL * i));
                     tile_load16_uniform<false>(k0 + (uint32_t)(RPL * i) * k_row_bytes + chunk, kp, dk + 1024u * i);
                     tile_load16_uniform<false>(v0 + (uint32_t)(RPL * i) * v_row_bytes + chunk, vp, dv + 1024u * i);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < LOADS; ++i) {
-                    const uint32_t chunk = 16u * (uint32_t)((l % CPR) ^ rows_swizzle(run_first + row0 + RPL * i));
+                    const uint32_t chunk = 16u * (uint32_t)((l % CPR) ^ rows_swizzle<D>(run_first + row0 + RPL * i));
                     const uint32_t at = (uint32_t)min(row0 + RPL * i, last);
                     tile_load16_uniform<false>(__umul24(at, k_row_bytes) + chunk, kp, dk + 1024u * i);
                     tile_load16_uniform<false>(__umul24(at, v_row_bytes) + chunk, vp, dv + 1024u * i);
@@ -105,7 +112,7 @@ struct WideLoader {
                 const int row = ROWS * w + RPL * i + l / CPR, key = min(tk + row, scope.Lb - 1);
                 int64_t ko = (int64_t)key * p.ksl, vo = (int64_t)key * p.vsl;
                 if (p.block_table != nullptr) pages.offsets(key, ko, vo);  // (uniform)
-                const int chunk = (l % CPR) ^ rows_swizzle(row);
+                const int chunk = (l % CPR) ^ rows_swizzle<D>(row);
                 tile_load16<64>(kbase + ko + 8 * chunk, dk + 1024u * i);
                 tile_load16<64>(vbase + vo + 8 * chunk, dv + 1024u * i);
             }
@@ -188,8 +195,8 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
         }
         scope.column(P, b, t, live, col_lo, col_end, col_nodes);
     }
-    float m_run = kNegInf, dsum1 = 0.f, dsum2 = 0.f;
-    f32x4 o1[NDB], o2[NDB];
+    float m_run = kNegInf;
+    f32x4 o1[NDB], o2[NDB], dsum1 = {0.f, 0.f, 0.f, 0.f}, dsum2 = dsum1;  // (four times the same sum: a product with ones)
 #pragma unroll
     for (int i = 0; i < NDB; ++i) o1[i] = o2[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float scale_log2 = p.scale * kLog2e;
@@ -220,26 +227,40 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
     };
     // 64 keys x 16 columns
     auto tile = [&](const u32x4 *tileK, bool whole) __attribute__((always_inline)) {
+        constexpr int LOOK = 4, QK = 4 * KSTEPS, PV = 2 * NDB;  // fragments read ahead of their products; fragments of K, of V
+        u32x4 kf[QK], vt[PV];
+        auto load_k = [&](int f) { kf[f] = tileK[rows_chunk_slot<D>(16 * (f / KSTEPS) + c, 4 * (f % KSTEPS) + g)]; };
+        auto load_v = [&](int f) { vt[f] = v_fragment(tileK + TILE_CHUNKS + 32 * (f / NDB) * CPR, f % NDB); };
         f32x4 s1[4], s2[4];
 #pragma unroll
-        for (int sub = 0; sub < 4; ++sub) {
-            s1[sub] = s2[sub] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int sub = 0; sub < 4; ++sub) s1[sub] = s2[sub] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int s = 0; s < KSTEPS; ++s) {
-                const u32x4 kf = tileK[rows_chunk_slot<D>(16 * sub + c, 4 * s + g)];
-                s1[sub] = mfma16(kf, qf[s], s1[sub]);
-                if constexpr (USE_R) s2[sub] = mfma16(kf, rf[s], s2[sub]);
-            }
+        for (int f = 0; f < LOOK; ++f) load_k(f);
+#pragma unroll
+        for (int f = 0; f < QK; ++f) {
+            if (f + LOOK < QK)
+                load_k(f + LOOK);
+            else
+                load_v(f + LOOK - QK);
+            s1[f / KSTEPS] = mfma16(kf[f], qf[f % KSTEPS], s1[f / KSTEPS]);
+            if constexpr (USE_R) s2[f / KSTEPS] = mfma16(kf[f], rf[f % KSTEPS], s2[f / KSTEPS]);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
+        float factor = scale_log2;
+        if (__builtin_expect(!whole, 0)) {  // (uniform)
 #pragma unroll
-        for (int sub = 0; sub < 4; ++sub) s1[sub] *= scale_log2;
-        if (__builtin_expect(!whole, 0))  // (uniform)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (!((seen[e >> 3] >> (e & 7)) & 1u)) s1[e >> 2][e & 3] = kNegInf, s2[e >> 2][e & 3] = 0.f;
+            for (int e = 0; e < 16; ++e) {
+                const bool ok = (seen[e >> 3] >> (e & 7)) & 1u;
+                s1[e >> 2][e & 3] = ok ? s1[e >> 2][e & 3] * factor : kNegInf;
+                if (!ok) s2[e >> 2][e & 3] = 0.f;
+            }
+            factor = 1.f;
+        }
         float tmax = kNegInf;
 #pragma unroll
         for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, s1[e >> 2][e & 3]);
+        tmax *= factor;
         if (__builtin_expect(__any(tmax > m_run + kWideSlack), 0)) {  // (rare, but for the first tile)
             tmax = rows_max(tmax);
             const float m_new = fmaxf(m_run, tmax);
@@ -252,29 +273,32 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
                 if constexpr (USE_R) o2[i] *= alpha;
             }
         }
-        const float m_use = m_run == kNegInf ? 0.f : m_run;
+        const float neg_m = m_run == kNegInf ? 0.f : -m_run;
         // P1 and P2 are rounded to bf16 once, as matrix operands; d1 and d2 add the rounded values, so that the
-        // weights still sum to one.
+        // weights still sum to one (by the matrix instruction: four vector instructions a score less).
         u32x4 pb1[2], pb2[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float p1[8], p2[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                p1[e] = fast_exp2(s1[2 * h + (e >> 2)][e & 3] - m_use);
-                if constexpr (USE_R) p2[e] = p1[e] * s2[2 * h + (e >> 2)][e & 3];
+            for (int e = 0; e < 4; ++e) {
+                const f32x4 &x = s1[2 * h + (e >> 1)], &u = s2[2 * h + (e >> 1)];
+                const int at = 2 * (e & 1);
+                const float p0 = fast_exp2(fmaf(x[at], factor, neg_m)), p1 = fast_exp2(fmaf(x[at + 1], factor, neg_m));
+                pb1[h][e] = pack_bf16(p0, p1);
+                if constexpr (USE_R) pb2[h][e] = pack_bf16(p0 * u[at], p1 * u[at + 1]);
             }
-            pb1[h] = pack8_bf16_accumulate(p1[0], p1[1], p1[2], p1[3], p1[4], p1[5], p1[6], p1[7], dsum1);
-            if constexpr (USE_R) pb2[h] = pack8_bf16_accumulate(p2[0], p2[1], p2[2], p2[3], p2[4], p2[5], p2[6], p2[7], dsum2);
+            const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+            dsum1 = mfma16(ones, pb1[h], dsum1);
+            if constexpr (USE_R) dsum2 = mfma16(ones, pb2[h], dsum2);
         }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < NDB; ++i) {
-                const u32x4 vt = v_fragment(tileK + TILE_CHUNKS + 32 * h * CPR, i);
-                o1[i] = mfma16(vt, pb1[h], o1[i]);
-                if constexpr (USE_R) o2[i] = mfma16(vt, pb2[h], o2[i]);
-            }
+        for (int f = 0; f < PV; ++f) {
+            if (f + LOOK < PV) load_v(f + LOOK);
+            o1[f % NDB] = mfma16(vt[f], pb1[f / NDB], o1[f % NDB]);
+            if constexpr (USE_R) o2[f % NDB] = mfma16(vt[f], pb2[f / NDB], o2[f % NDB]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
 
     // Ring: at the top of a round the tiles v .. v + AHEAD - 1 are on their way; the wait leaves those behind v, the barrier
@@ -302,7 +326,7 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
     }
 
     // ---- the two halves of the keys (KH = 2); then the record or the output row --------------------------------
-    const float e1 = rows_sum(dsum1), e2 = rows_sum(dsum2);
+    const float e1 = dsum1[0], e2 = dsum2[0];
     float m_star = m_run, w0 = 1.f, w1 = 0.f, f1 = 0.f, f2 = 0.f;
     f32x4 *mine = (f32x4 *)lds + cw * (2 * NDB * 64) + lane;
     if constexpr (KH == 2) {
