@@ -237,7 +237,7 @@ plx_status parallax_decode_sinks(const plx_decode_args *args, int32_t sinks, voi
  * sees every committed key (the L_b - n_b before them) and the drafted key m iff bit m % 64 of word m / 64 of its mask is
  * set: its ancestors and itself, in whatever order the nodes lie (bits from n_b on are ignored). Rows t >= n_b,
  * and rows that see nothing, return zeros. The rest is parallax_decode over Tq rows: q, r, o [B, Hq, Tq, d], the cache
- * contiguous or paged and read once for up to 32 (head of a group, node) pairs, bf16 and fp32, workspace and
+ * contiguous or paged and read once for up to 128 (head of a group, node) pairs (fp32: 16), bf16 and fp32, workspace and
  * split counts. A key that a node does not see does not reach it, whatever its row holds.
  *   tree_mask   [mask_batch][Tq][ceil(Tq / 64)] on the device, 8-byte aligned; mask_batch 1 (one tree for all) or B
  *   draft_lens  [B] int32 on the device, or NULL = Tq
