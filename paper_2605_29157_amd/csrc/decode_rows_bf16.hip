@@ -300,6 +300,59 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
     }
 }
 
+// The records of a row, up to N of them: D / 4 lanes a row, all loads at once, no exchange between lanes. The merge of
+// decode_bf16.hip, a workgroup a row, is for many records; with many rows it is bound by the workgroups' starts: 6656 rows x
+// 2 records 18.3 us, 8192 x 4 23.8; here 5.0 and 6.6, 8192 x 8 11.6 (few rows: 4 us with either).
+template <int D, int N>
+__global__ __launch_bounds__(256) void rows_combine_kernel(DecodeParams p) {
+    constexpr int DL = D / 4, REC = 2 * D + 4;
+    const int64_t row = (int64_t)blockIdx.x * (256 / DL) + threadIdx.x / DL;
+    if (row >= (int64_t)p.B * p.Hq * p.Tq) return;
+    const int dim = 4 * (threadIdx.x % DL);
+    f32x4 head[N], a1[N], a2[N];
+#pragma unroll
+    for (int s = 0; s < N; ++s) {  // (past the last one: that again, with no weight)
+        const float *rec = p.ws + (row * p.S + min(s, p.S - 1)) * REC;
+        head[s] = *(const f32x4 *)rec;
+        a1[s] = *(const f32x4 *)(rec + 4 + dim);
+        a2[s] = *(const f32x4 *)(rec + 4 + D + dim);
+    }
+    float m_star = kNegInf, d1 = 0.f, d2 = 0.f;
+    f32x4 o1 = {0.f, 0.f, 0.f, 0.f}, o2 = o1;
+#pragma unroll
+    for (int s = 0; s < N; ++s) m_star = fmaxf(m_star, head[s][0]);
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+        const float w = s >= p.S || head[s][0] == kNegInf ? 0.f : fast_exp2(head[s][0] - m_star);
+        d1 += w * head[s][1], d2 += w * head[s][2];
+        o1 += w * a1[s], o2 += w * a2[s];
+    }
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};  // empty key set: zeros
+    if (d1 != 0.f) {
+        const float inv = 1.f / d1;
+        y = o1 * (inv * (1.f + d2 * inv)) - o2 * inv;
+    }
+    *(u32x2 *)((__bf16 *)p.o + row * D + dim) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+}
+
+template <int D>
+static void launch_rows_combine(const DecodeParams &p, int64_t rows, hipStream_t stream) {
+    const dim3 grid((unsigned)((rows * (D / 4) + 255) / 256));
+    if (p.S <= 2)
+        hipLaunchKernelGGL((rows_combine_kernel<D, 2>), grid, dim3(256), 0, stream, p);
+    else if (p.S <= 4)
+        hipLaunchKernelGGL((rows_combine_kernel<D, 4>), grid, dim3(256), 0, stream, p);
+    else
+        hipLaunchKernelGGL((rows_combine_kernel<D, 8>), grid, dim3(256), 0, stream, p);
+}
+
+hipError_t launch_decode_rows_combine(const DecodeParams &p, hipStream_t stream) {
+    const int64_t rows = (int64_t)p.B * p.Hq * p.Tq;
+    if (p.S > 8) return launch_decode_combine(p, stream);
+    p.d == 128 ? launch_rows_combine<128>(p, rows, stream) : launch_rows_combine<64>(p, rows, stream);
+    return hipGetLastError();
+}
+
 // Columns per workgroup: 16 with private tiles, 64 or 128 with shared ones. (Private tiles with 32 columns a wave, one
 // workgroup per unit, took 26 nodes x 2 heads over 16 x 6000 keys, which the columns read twice, in 135 us.)
 int decode_rows_columns(int n_cols) { return n_cols <= 16 ? 16 : n_cols <= 64 ? 64 : 128; }

@@ -438,9 +438,9 @@ plx_status prepare_decode_rows(const plx_decode_args *a, const plx_decode_tree_a
 // compute unit, decode_rows_wide_bf16.hip) from a model fitted to sweeps of S on MI355X, in us: a round of at most one workgroup
 // per unit takes 6 and for each 128 keys (d = 128; shorter rows in proportion) 2.25 of arithmetic with 64 columns, 4.1 with
 // 128, and a third of the time in which the memory brings in what the workgroups of the round read at 5 TB/s, which is also the
-// least; the merge takes 5 and writing and reading of the records at 4 TB/s. Measured for 32 sequence heads x 16384 keys, d = 128, in
+// least; the merge takes 5 and writing and reading of the records at 6 TB/s. Measured for 32 sequence heads x 16384 keys, d = 128, in
 // front of 128 columns: S = 1 533, 4 167, 6 122, 8 107, 10 152, 16 120 (the model takes 8); for 128 x up to 6000, 64 columns: S = 1
-// 133, 2 99, 3 108, 4 101 (2; the rule for plain rows took 1).
+// 128, 2 86, 3 101, 4 97 (2; the rule for plain rows took 1).
 int32_t pick_splits_rows(const plx_decode_args *a, const plx::DecodeRowsParams &p) {
     if (a->num_splits > 0) return a->num_splits;
     const int64_t in_window = (int64_t)a->window + p.d.Tq - 1 + p.sinks;
@@ -455,7 +455,7 @@ int32_t pick_splits_rows(const plx_decode_args *a, const plx::DecodeRowsParams &
     const int64_t pairs = (int64_t)a->B * a->Hkv * ((cols + per - 1) / per), cus = query_num_cus();
     const int32_t tile = plx::decode_rows_tile(per), tiles = (keys + tile - 1) / tile;
     const double share = tile / 128.0 * a->d / 128.0, compute = share * (per == 64 ? 2.25 : 4.1), memory = share * 65536e-6 / 5.0;
-    const double record_us = 2.0 * (double)a->B * a->Hq * p.d.Tq * (2 * a->d + 4) * 4e-6 / 4.0;
+    const double record_us = 2.0 * (double)a->B * a->Hq * p.d.Tq * (2 * a->d + 4) * 4e-6 / 6.0;
     auto round = [&](int64_t workgroups, int64_t n) {
         const double fetch = memory * (double)workgroups;
         return 6.0 + (double)n * std::max(fetch, compute + fetch / 3);
@@ -494,7 +494,7 @@ plx_status decode_rows(const plx_decode_args *a, const plx_decode_tree_args *tre
         if (st != PLX_OK) return st;
     }
     if (plx::launch_decode_rows_bf16(p, stream) != hipSuccess) return PLX_ERR_LAUNCH;
-    if (S > 1 && plx::launch_decode_combine(p.d, stream) != hipSuccess) return PLX_ERR_LAUNCH;
+    if (S > 1 && plx::launch_decode_rows_combine(p.d, stream) != hipSuccess) return PLX_ERR_LAUNCH;
     return PLX_OK;
 }
 

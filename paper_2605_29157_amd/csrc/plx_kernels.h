@@ -182,6 +182,7 @@ hipError_t launch_decode_rows_bf16(const DecodeRowsParams &p, hipStream_t stream
 hipError_t launch_decode_rows_wide_bf16(const DecodeRowsParams &p, hipStream_t stream);  // ... for more than 16 columns
 int decode_rows_columns(int n_cols);  // columns of a workgroup, of n_cols = heads of a group x rows
 int decode_rows_tile(int columns);    // keys of a tile of such a workgroup
+hipError_t launch_decode_rows_combine(const DecodeParams &p, hipStream_t stream);
 hipError_t launch_decode_rows_f32(const DecodeRowsParams &p, hipStream_t stream);
 hipError_t launch_decode_combine(const DecodeParams &p, hipStream_t stream);
 hipError_t launch_prefill_bf16(const PrefillParams &p, hipStream_t stream);
