@@ -434,7 +434,9 @@ plx_status prepare_decode_rows(const plx_decode_args *a, const plx_decode_tree_a
     return PLX_OK;
 }
 
-// Split count of such a call. Up to 16 columns: that of a plain one over as many keys. Beyond them (one workgroup of eight waves per
+// Split count of such a call. Up to 16 columns: that of a plain one over as many keys, doubled while half of the units stay idle
+// and every wave keeps a tile of 32 keys (kernel alone, us, 8 key heads: one row, 1028 keys S = 4 10.9, 8 8.4; 8 nodes x 2 heads,
+// 1500 keys S = 6 10.2, 12 8.0). Beyond them (one workgroup of eight waves per
 // compute unit, decode_rows_wide_bf16.hip) from a model fitted to sweeps of S on MI355X, in us: a round of at most one workgroup
 // per unit takes 6 and for each 128 keys (d = 128; shorter rows in proportion) 2.25 of arithmetic with 64 columns, 4.1 with
 // 128, and a third of the time in which the memory brings in what the workgroups of the round read at 5 TB/s, which is also the
@@ -451,8 +453,13 @@ int32_t pick_splits_rows(const plx_decode_args *a, const plx::DecodeRowsParams &
         return pick_splits_f32(&plain, p.d.Tq);
     }
     const int32_t cols = p.d.G * p.d.Tq, per = plx::decode_rows_columns(cols);
-    if (per == 16) return parallax_decode_num_splits(a->B, a->Hq, a->Hkv, keys, a->d, 0);
     const int64_t pairs = (int64_t)a->B * a->Hkv * ((cols + per - 1) / per), cus = query_num_cus();
+    if (per == 16) {
+        const int32_t block_tiles = (keys + plx::kDecodeBlockKeys - 1) / plx::kDecodeBlockKeys;
+        int32_t s = parallax_decode_num_splits(a->B, a->Hq, a->Hkv, keys, a->d, 0);
+        while (s > 1 && 2 * pairs * s <= cus && 2 * s <= std::min(block_tiles, PLX_MAX_SPLITS)) s *= 2;
+        return s;
+    }
     const int32_t tile = plx::decode_rows_tile(per), tiles = (keys + tile - 1) / tile;
     const double share = tile / 128.0 * a->d / 128.0, compute = share * (per == 64 ? 2.25 : 4.1), memory = share * 65536e-6 / 5.0;
     const double record_us = 2.0 * (double)a->B * a->Hq * p.d.Tq * (2 * a->d + 4) * 4e-6 / 6.0;

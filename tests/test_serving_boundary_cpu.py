@@ -122,7 +122,9 @@ def test_splits_of_a_tree_call(binding):
     assert splits(16, 8, 2, 26, 6000) == 2     # 256 of 64
     assert splits(64, 8, 2, 26, 6000) == 1     # two rounds as it is
     assert splits(16, 8, 2, 26, 200) == 1      # two tiles: a merge costs more
-    assert splits(1, 8, 2, 8, 1500) >= 4       # up to 16 columns: as plain rows over as many keys
+    # up to 16 columns: as plain rows over as many keys, more where units stay idle
+    assert [splits(1, 8, 2, 8, L) for L in (500, 1028, 1500)] == [1, 8, 12]
+    assert splits(16, 8, 2, 8, 16384) == binding.parallax_decode_num_splits(16, 16, 8, 16384, 128, 256)
     assert splits(1, 8, 2, 8, 100000, window=512, sinks=4) == splits(1, 8, 2, 8, 523)
     assert splits(1, 8, 2, 26, 100000, window=500, sinks=4) == splits(1, 8, 2, 26, 529)
     for shape in ((1, 1, 16, 256, 1 << 20), (1, 1, 16, 256, 1), (300, 8, 2, 100, 40000), (1, 8, 2, 20, 131072)):
