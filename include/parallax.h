@@ -319,7 +319,7 @@ plx_status parallax_cache_copy(const plx_cache_pools *pools, const int32_t *src,
  * n_accepted[b]) in ascending order, move together behind the committed rows: row base + accepted[b][i] to base +
  * i, base = L_b - n_b, n_b = min(draft_lens[b], max_draft, L_b). new_lens[b] = base + n_accepted[b] (at most n_b of them).
  * What lies behind is left as it was; parallax_cache_free gives its pages back. Numbers are clamped to [i, n_b);
- * a list that does not ascend moves the wrong rows. pools as above; without a block table [B, heads, capacity, d] with
+ * a list that does not ascend moves the wrong rows, and no row is moved from or to a table entry that is no page. pools as above; without a block table [B, heads, capacity, d] with
  * the sequence's stride first and page_size = capacity, num_pages = B. The pages of the drafted rows must not be shared.
  * new_lens must not be seq_lens. max_accepted <= max_draft <= PLX_MAX_TREE_NODES.
  */

@@ -281,13 +281,14 @@ __global__ __launch_bounds__(256) void cache_compact_kernel(CacheCompact a) {
     if (blockIdx.y == 0 && tid == 0) a.new_lens[b] = base + count;
     auto row_at = [&](int key, const int64_t (&st)[3]) -> int64_t {
         if (a.block_table == nullptr) return (int64_t)b * st[0] + (int64_t)key * st[2];
-        const int page = min(max(a.block_table[(int64_t)b * a.table_stride + key / c.page_size], 0), c.num_pages - 1);
-        return page * st[0] + (int64_t)(key % c.page_size) * st[2];
+        const int page = a.block_table[(int64_t)b * a.table_stride + key / c.page_size];
+        if (page < 0 || page >= c.num_pages) return -1;  // (no page: no row is moved from or to it)
+        return (int64_t)page * st[0] + (int64_t)(key % c.page_size) * st[2];
     };
     for (int i = tid; i < count; i += 256) {
         const int node = min(max(a.accepted[(int64_t)b * a.max_accepted + i], i), n - 1);
-        moves[i] = node != i;
         at[0][0][i] = row_at(base + node, c.ks), at[0][1][i] = row_at(base + i, c.ks);
+        moves[i] = node != i && at[0][0][i] >= 0 && at[0][1][i] >= 0;
         if (c.v) at[1][0][i] = row_at(base + node, c.vs), at[1][1][i] = row_at(base + i, c.vs);
     }
     __syncthreads();

@@ -177,6 +177,29 @@ def test_compact(plx, dtype, page, Tq, most):
         np.testing.assert_array_equal(host(p), w)
 
 
+def test_compact_leaves_rows_without_a_page(plx):
+    """Table entries that are no page (-1, past the pool): nothing moves from or to them, the other rows do."""
+    page, n_pages, cap = 4, 6, 20
+    pools = [torch.randn(n_pages, 2, page, 64, device=DEV).to(torch.bfloat16) for _ in range(2)]
+    want = [p.clone() for p in pools]
+    table = [[0, 2, -1, 3, n_pages], [5, 4, -1, -1, -1]]
+    lens, drafted, accepted = [cap, 6], [cap, 5], [[1, 4, 5, 6, 9, 13, 17], [1, 3, -1, -1, -1, -1, -1]]
+    base = [n - m for n, m in zip(lens, drafted)]
+    new = plx.parallax_cache_compact(pools[0], pools[1], _ints(lens), _ints(drafted), _ints(accepted), _ints([7, 2]),
+                                     block_table=_ints(table))
+    assert new.tolist() == [7, 3]
+    for w in want:
+        old = w.clone()
+        for b, count in ((0, 7), (1, 2)):
+            for i in range(count):
+                src, dst = (divmod(base[b] + x, page) for x in (accepted[b][i], i))
+                src, dst = (table[b][src[0]], src[1]), (table[b][dst[0]], dst[1])
+                if 0 <= src[0] < n_pages and 0 <= dst[0] < n_pages:
+                    w[dst[0], :, dst[1]] = old[src[0], :, src[1]]
+    for p, w in zip(pools, want):
+        assert torch.equal(p, w)
+
+
 def test_serving_with_drafts(plx):
     """A cache from its first prompt on: extend, fork, drafted trees, verification, acceptance, and pages behind the window given
     back; after every step the attention equals the oracle's over the tokens that the sequence is made of."""
