@@ -344,6 +344,26 @@ def _here() -> int:
     return _raw_device() if _raw_device is not None else torch.cuda.current_device()
 
 
+def _launch_stream(where, stream) -> int:
+    """_stream_ptr, of a stream of the current device only."""
+    at = getattr(stream, "device_index", None)
+    if at is not None and at != _here():
+        raise ValueError("%s: the stream is one of device %d, which is not the current one" % (where, at))
+    return _stream_ptr(stream)
+
+
+def _sink_shapes(where, q, like_q, k, v):
+    """Refuses tensors that do not fit each other: [B, Hq, T, d] and [B, Hkv, Tkv, d] of one type on the current device."""
+    _on_current_device(where, q, k, v, *like_q)
+    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
+        raise ValueError("%s: q [B, Hq, T, d], k and v [B, Hkv, Tkv, d]" % where)
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise TypeError("%s: q, k and v have one dtype" % where)
+    for t in like_q:
+        if t is not None and (t.shape != q.shape or t.dtype != q.dtype or t.stride(-1) != 1):
+            raise ValueError("%s: r, the outputs and their gradients have the shape and dtype of q" % where)
+
+
 def _on_current_device(where, *tensors):
     """Refuses tensors (None: left out) that are not all on the current device, where the launch goes."""
     here = -1
@@ -574,7 +594,7 @@ def _decode_rows(q, r, k, v, scale, seq_lens, use_r, num_splits, workspace, out,
         if S > 1:
             workspace = _scratch(stream, B * Hq * Tq * S * (2 * d + 4), q.device)
             a.workspace, a.workspace_bytes = workspace.data_ptr(), _bytes(workspace)
-    st = call(*head, _stream_ptr(stream))
+    st = call(*head, _launch_stream(where, stream))
     if st != PLX_OK:
         raise ParallaxError(st, where)
     return out
@@ -765,8 +785,12 @@ def parallax_prefill(q, r, k, v, scale, causal=True, use_r=True, out=None, strea
     T positions of the Tkv-long sequence). With save_for_backward the kernel also writes the row
     cache of the backward pass and (out, vbar, row_stats) is returned. With sinks > 0 the first tokens stay visible
     behind the sliding window (no block_mask, no prep)."""
-    if sinks and (block_mask is not None or prep is not None):
-        raise ValueError("sinks go with neither block_mask nor prep")
+    if sinks:
+        if block_mask is not None or prep is not None:
+            raise ValueError("sinks go with neither block_mask nor prep")
+        _sink_shapes("parallax_prefill_sinks", q, (r, out), k, v)
+        if use_r and r is None:
+            raise ValueError("r is needed unless use_r=False")
     for t in (q, k, v) + ((r,) if r is not None else ()):
         if not t.is_cuda:
             raise ValueError("parallax_prefill needs device tensors")
@@ -791,7 +815,7 @@ def parallax_prefill(q, r, k, v, scale, causal=True, use_r=True, out=None, strea
         B, Hq, T, _ = q.shape
         row_stats = _result_maker(stream, torch.empty)(B, Hq, T, 2, dtype=torch.float32, device=q.device)
         _ROW_CACHE.pack_into(a, plx_prefill_args.vbar.offset, vbar.data_ptr(), row_stats.data_ptr())
-    lib, where = load_library(), _stream_ptr(stream)
+    lib, where = load_library(), _launch_stream("parallax_prefill_sinks", stream) if sinks else _stream_ptr(stream)
     split_bytes = 0 if sinks else lib.parallax_prefill_workspace_bytes(ctypes.byref(a))
     if sinks:
         st = lib.parallax_prefill_sinks(ctypes.byref(a), _i32(sinks), where)
@@ -831,8 +855,12 @@ def parallax_prefill_backward(q, r, k, v, o, vbar, row_stats, d_o, scale, causal
                               workspace=None, window=0, block_mask=None, sinks=0):
     """Gradients (dq, dr, dk, dv) of parallax_prefill for the upstream gradient d_o, from the
     forward's output and row cache (save_for_backward=True, same causal / window / block_mask / sinks)."""
-    if sinks and block_mask is not None:
-        raise ValueError("sinks do not go with a block_mask")
+    if sinks:
+        if block_mask is not None:
+            raise ValueError("sinks do not go with a block_mask")
+        _sink_shapes("parallax_prefill_backward_sinks", q, (r, o, vbar, d_o), k, v)
+        if row_stats.dtype != torch.float32 or row_stats.shape != (*q.shape[:3], 2) or row_stats.device != q.device:
+            raise ValueError("row_stats is the float32 [B, Hq, T, 2] of the forward")
     like = _result_maker(stream, torch.empty_like)
     dq, dr, dk, dv = like(q), like(q), like(k), like(k)
     own_scratch = workspace is None
@@ -845,9 +873,10 @@ def parallax_prefill_backward(q, r, k, v, o, vbar, row_stats, d_o, scale, causal
         lib = load_library()
         if own_scratch:
             need = lib.parallax_prefill_backward_sinks_workspace_bytes(ctypes.byref(a), _i32(sinks))  # (0: refused below)
-            workspace = _scratch(stream, (need + 3) // 4, q.device)
-            a.workspace, a.workspace_bytes = workspace.data_ptr(), need
-        st = lib.parallax_prefill_backward_sinks(ctypes.byref(a), _i32(sinks), _stream_ptr(stream))
+            workspace = _scratch(stream, max(need // 4, 2 * row_stats.numel()), q.device)
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), _bytes(workspace)
+        st = lib.parallax_prefill_backward_sinks(ctypes.byref(a), _i32(sinks),
+                                                 _launch_stream("parallax_prefill_backward_sinks", stream))
         if st != PLX_OK:
             raise ParallaxError(st, "parallax_prefill_backward_sinks")
         return dq, dr, dk, dv
@@ -1024,7 +1053,7 @@ def parallax_cache_fork(pages, parents, children, stream=None):
     device = _table_device(where, pages)
     n = parents.numel()
     ptrs = _int_list(where, "parents", parents, None, device), _int_list(where, "children", children, n, device)
-    st = load_library().parallax_cache_fork(ctypes.byref(pages._args), *ptrs, n, _stream_ptr(stream))
+    st = load_library().parallax_cache_fork(ctypes.byref(pages._args), *ptrs, n, _launch_stream(where, stream))
     if st != PLX_OK:
         raise ParallaxError(st, where)
 
@@ -1046,7 +1075,7 @@ def parallax_cache_extend(pages, seqs, new_lens, *pools, stream=None):
     buf = _result_maker(stream, torch.empty)(3 * n + 1, dtype=torch.int32, device=pages.block_table.device)
     at = buf.data_ptr()
     src, dst, rows, missing = at, at + 4 * n, at + 8 * n, at + 12 * n
-    lib, where_to = load_library(), _stream_ptr(stream)
+    lib, where_to = load_library(), _launch_stream(where, stream)
     st = lib.parallax_cache_extend(ctypes.byref(pages._args), *ptrs, n, src, dst, rows, missing, where_to)
     if st != PLX_OK:
         raise ParallaxError(st, where)
@@ -1066,7 +1095,7 @@ def parallax_cache_free(pages, seqs, first=None, last=None, stream=None):
     n = seqs.numel()
     ptrs = [_int_list(where, "seqs", seqs, None, device)]
     ptrs += [0 if t is None else _int_list(where, name, t, n, device) for name, t in (("first", first), ("last", last))]
-    st = load_library().parallax_cache_free(ctypes.byref(pages._args), *ptrs, n, _stream_ptr(stream))
+    st = load_library().parallax_cache_free(ctypes.byref(pages._args), *ptrs, n, _launch_stream(where, stream))
     if st != PLX_OK:
         raise ParallaxError(st, where)
 
@@ -1078,7 +1107,7 @@ def parallax_cache_copy(k, v, src, dst, rows=None, stream=None):
     n = src.numel()
     ptrs = [_int_list(where, "src", src, None, _here()), _int_list(where, "dst", dst, n, _here())]
     ptrs.append(0 if rows is None else _int_list(where, "rows", rows, n, _here()))
-    st = load_library().parallax_cache_copy(ctypes.byref(a), *ptrs, n, _stream_ptr(stream))
+    st = load_library().parallax_cache_copy(ctypes.byref(a), *ptrs, n, _launch_stream(where, stream))
     if st != PLX_OK:
         raise ParallaxError(st, where)
 
@@ -1111,7 +1140,7 @@ def parallax_cache_compact(k, v, seq_lens, draft_lens, accepted, n_accepted, blo
             raise ValueError("block_table needs one row per sequence")
         table, stride = block_table.data_ptr(), block_table.stride(0) if B > 1 else block_table.shape[1]
     a = _filled(plx_cache_compact_args, *pools, table, *ptrs, B, stride, _i32(max_draft), most)
-    st = load_library().parallax_cache_compact(ctypes.byref(a), _stream_ptr(stream))
+    st = load_library().parallax_cache_compact(ctypes.byref(a), _launch_stream(where, stream))
     if st != PLX_OK:
         raise ParallaxError(st, where)
     return new_lens

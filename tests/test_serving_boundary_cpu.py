@@ -328,6 +328,25 @@ def test_binding_refuses_other_devices(binding, monkeypatch):
             binding._on_current_device("x", *tensors)
 
 
+def test_binding_refuses_streams_of_other_devices(binding, monkeypatch):
+    monkeypatch.setattr(binding, "_here", lambda: 0)
+    stream = type("Stream", (), dict(device_index=1, cuda_stream=0x70))()
+    with pytest.raises(ValueError):
+        binding._launch_stream("x", stream)
+    stream.device_index = 0
+    assert binding._launch_stream("x", stream) == 0x70
+
+
+def test_binding_refuses_tensors_that_do_not_fit(binding, monkeypatch):
+    monkeypatch.setattr(binding, "_on_current_device", lambda *a: None)
+    q, k = torch.zeros(1, 4, 8, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 32, 64, dtype=torch.bfloat16)
+    binding._sink_shapes("x", q, (q, None), k, k)
+    for args in ((q, (q[:, :2],), k, k), (q, (q,), k, k[:, :, :30]), (q, (q.float(),), k, k), (q, (q,), k.float(), k.float()),
+                 (q[0], (), k, k), (q, (q,), k[..., :32], k[..., :32]), (q, (q.transpose(2, 3),), k, k)):
+        with pytest.raises((ValueError, TypeError)):
+            binding._sink_shapes("x", *args)
+
+
 def test_binding_refuses_host_tensors(binding):
     q, k = torch.zeros(1, 4, 8, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 32, 64, dtype=torch.bfloat16)
     mask, lens = _chain_of_words(binding, 8), torch.zeros(1, dtype=torch.int32)
