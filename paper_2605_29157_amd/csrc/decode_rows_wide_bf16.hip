@@ -13,8 +13,10 @@
 //     takes its 64 keys in one go, one test and no branch between their products, and reads its operands four fragments
 //     ahead. Measured (us; 16 x up to 6000 keys, 8 key heads, 52 columns, 2 splits; 8 x 16384 keys, 4 key heads, 256
 //     columns, 4 splits): 32 keys in one go 107, 188; 64 99, 177; reads ahead and no bank conflicts 96, 170; the waves with matrix
-//     work preferred 95.5, 167. Four waves of 32 columns, which halve the reads of LDS, their steps pipelined by hand: 210 for
-//     the second;
+//     work preferred 95.5, 167; with a faster merge 86, 161. Four waves of 32 columns, which halve the reads of LDS, their
+//     steps pipelined by hand: 210 for the second;
+//   * a tile with masks is first looked through for values of V that are not finite, and only then treated for them
+//     (48 nodes x 2 heads, window 321, 6 sequences: 31 -> 23; 16 rows x 2, window 256, 8 sequences 31 -> 21);
 //   * tiles in a ring of 128 KB of LDS, filled by direct global -> LDS loads (no registers parked), 64 - 96 KB of it on
 //     their way; one barrier per tile;
 //   * the reference of the exponentials is moved only when a score exceeds it by 2^6 (then the sums are rescaled): no
@@ -118,7 +120,18 @@ struct WideLoader {
             }
         }
     }
-    // Values that are not finite out of this wave's V rows of a tile
+    // Is a value in this wave's V rows of a tile not finite?
+    __device__ __forceinline__ bool not_finite(const u32x4 *tileV) const {
+        uint32_t bad = 0;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const u32x4 x = tileV[ROWS * w * CPR + 64 * i + lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bad |= not_finite_halves(x[e]);
+        }
+        return __any(bad != 0);
+    }
+    // Such values out of these rows
     __device__ __forceinline__ void clean(u32x4 *tileV) const {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
@@ -158,6 +171,7 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
     static_assert(2 * 4 * NDB * 64 <= STAGES * STAGE_CHUNKS, "the states of four waves");
     constexpr int CW = 8 / KH, COLS = 16 * CW;  // waves side by side over the columns
     __shared__ float head[CW][3][16];
+    __shared__ int some_bad[2];  // of the masked tile in turn: V holds a value that is not finite
 
     const int tid = threadIdx.x;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -165,6 +179,7 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
     const int cw = w % CW, kh = w / CW;
     int cg, split, hk, b;
     if (!wide_item(P, cg, split, hk, b)) return;
+    if (tid < 2) some_bad[tid] = 0;  // (the ring's first barrier is in front of its use)
     const int G = p.G, S = p.S, Tq = p.Tq, n_cols = G * Tq, x0 = cg * COLS;
     const RowsScope<TREE, TILE> scope(P, b, x0, COLS);
     const int per = (scope.n_virtual + S - 1) / S;
@@ -212,10 +227,9 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
         return u32x4{lo[0], lo[1], hi[0], hi[1]};
     };
     uint32_t seen[2];  // of the two 32-key blocks of this wave's 64 keys
-    // 32 keys of a tile that some column does not see completely: which keys, and the values of V that are not finite reach the
+    // 32 keys of a tile that some column does not see completely and that holds values of V that are not finite: these reach the
     // columns that see their key; then (behind a barrier) they are taken out of the tile.
-    auto mask_tile = [&](const u32x4 *tileV, int tk, uint32_t &seen) __attribute__((always_inline)) {
-        seen = scope.seen(P, col_nodes, col_lo, col_end, tk, g);
+    auto spread_not_finite = [&](const u32x4 *tileV, uint32_t seen) __attribute__((always_inline)) {
         const u32x4 big = big_halves(seen);
 #pragma unroll
         for (int i = 0; i < NDB; ++i) {
@@ -303,7 +317,7 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
 
     // Ring: at the top of a round the tiles v .. v + AHEAD - 1 are on their way; the wait leaves those behind v, the barrier
     // says that v has landed for all waves and that nobody reads tile v - 1 any more, whose stage takes tile v + AHEAD.
-    int stage = 0;
+    int stage = 0, masked = 0;
     for (int v = v_lo; v < v_hi; ++v) {
         if (v + AHEAD <= v_hi)  // (uniform)
             tile_barrier<LOADS *(AHEAD - 1)>();
@@ -314,12 +328,21 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
         const int tk = __builtin_amdgcn_readfirstlane(scope.key_of(v));
         const bool whole = scope.whole(tk, TILE);
         if (!whole) {  // (the same for all waves)
-            if (live_wave)
+            if (loader.not_finite(tileK + TILE_CHUNKS) && lane == 0) some_bad[masked & 1] = 1;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) mask_tile(tileK + TILE_CHUNKS + (64 * kh + 32 * h) * CPR, tk + 64 * kh + 32 * h, seen[h]);
+            for (int h = 0; h < 2; ++h) seen[h] = scope.seen(P, col_nodes, col_lo, col_end, tk + 64 * kh + 32 * h, g);
             __syncthreads();
-            loader.clean(tileK + TILE_CHUNKS);
-            __syncthreads();
+            const bool bad = some_bad[masked & 1] != 0;
+            ++masked;
+            if (tid == 0) some_bad[masked & 1] = 0;  // (read a masked tile ago; the next barrier is in front of its next use)
+            if (__builtin_expect(bad, 0)) {
+                if (live_wave)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) spread_not_finite(tileK + TILE_CHUNKS + (64 * kh + 32 * h) * CPR, seen[h]);
+                __syncthreads();
+                loader.clean(tileK + TILE_CHUNKS);
+                __syncthreads();
+            }
         }
         if (live_wave) tile(tileK + 64 * kh * CPR, whole);
         stage = stage == STAGES - 1 ? 0 : stage + 1;
