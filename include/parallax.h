@@ -267,7 +267,8 @@ plx_status parallax_decode_tree(const plx_decode_tree_args *args, void *hip_stre
  *   free_pages    [num_pages]; the first *free_count (a device int32) are the pages nobody names, the next one taken is the
  *                 last of them. To begin with: block_table all -1, seq_lens and page_refs 0, every page on the list.
  * Lists of sequences are int32 on the device; entries outside [0, sequences) are passed over, so a list may be padded
- * with -1. n = 0 is allowed and does nothing. The state after a call does not depend on the order its threads ran in.
+ * with -1. n = 0 is allowed and does nothing. The state after a call does not depend on the order its threads ran in; calls
+ * on one table have to be ordered (one stream, or events), as all that write the same memory.
  */
 typedef struct {
     int32_t *block_table, *seq_lens, *page_refs, *free_pages, *free_count;

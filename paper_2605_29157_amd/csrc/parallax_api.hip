@@ -420,7 +420,8 @@ plx_status prepare_decode_rows(const plx_decode_args *a, const plx_decode_tree_a
     if (st != PLX_OK) return st;
     if (p.d.prep.gamma_q != nullptr) return PLX_ERR_SHAPE;  // (rows prepared beforehand only)
     if (sinks < 0 || (sinks > 0 && a->window == 0)) return PLX_ERR_SHAPE;
-    p.sinks = sinks;
+    // (more than the cache holds is all of it: positions less the window, and tiles of the sinks, stay in 32 bits)
+    p.d.window = std::min(a->window, a->Lmax), p.sinks = std::min(sinks, a->Lmax);
     if (tree) {
         if (!tree->tree_mask) return PLX_ERR_NULL;
         if ((reinterpret_cast<uintptr_t>(tree->tree_mask) & 7u) || (reinterpret_cast<uintptr_t>(tree->draft_lens) & 3u))

@@ -90,6 +90,23 @@ def test_every_merge(plx, splits):
     _check(got, x, see, info=splits)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("Tq", [5, 20, 70])
+def test_the_largest_window_and_sinks(plx, dtype, Tq):
+    """2^31 - 1: all keys, also for rows in front of the first token."""
+    lens, cap, most = (200, 3, 0), 200, 2**31 - 1
+    x = _inputs(3, 4, 2, 64, Tq, cap, seed=Tq, dtype=dtype)
+    see = [rows.chain(L, Tq, cap) for L in lens]
+    bits = rows.random_tree(Tq, np.random.default_rng(Tq))
+    for window, sinks in ((most, 0), (most, 4), (most, most), (1, most), (cap, cap)):
+        if sinks:
+            got = plx.parallax_decode(x["q"], x["r"], x["k"], x["v"], x["scale"], seq_lens=_ints(lens), window=window, sinks=sinks)
+            _check(got, x, see, dtype, (window, sinks))
+        got = plx.parallax_decode_tree(x["q"], x["r"], x["k"], x["v"], x["scale"], torch.from_numpy(rows.words(bits)).to(DEV),
+                                       seq_lens=_ints(lens), window=window, sinks=sinks)
+        _check(got, x, [rows.tree(L, Tq, cap, bits) for L in lens], dtype, (window, sinks, "tree"))
+
+
 def test_captured_with_new_masks(plx):
     """A captured call is replayed with other masks, lengths and drafts, eager work of the same kind in between."""
     Tq, cap = 40, 900
