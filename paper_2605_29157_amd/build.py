@@ -92,11 +92,28 @@ def _check_decode_assembly() -> None:
     bad = {n: c for n, c in _spills("decode_bf16.hip", "decode_bf16_kernel").items() if c > (16 if n.endswith(prep) else 0)}
     if bad:
         raise RuntimeError("decode_bf16.hip: register spills in a decode kernel (%s)" % bad)
+    _check_no_load_waits("decode_rows_wide_bf16.hip", "decode_rows_wide_kernel")
     # (a reload waits for all tile loads in front of it: forms of the wide kernel with 100 spilled took three times as long)
     for src in ("decode_rows_bf16.hip", "decode_rows_wide_bf16.hip"):
         bad = {n: c for n, c in _spills(src, "decode_rows").items() if c > 0}
         if bad:
             raise RuntimeError("%s: register spills in a decode kernel (%s)" % (src, bad))
+
+
+def _check_no_load_waits(src: str, kernel: str) -> None:
+    """No block of matrix instructions waits for loads (vmcnt): such a wait, for an operand that was fetched before the loop, makes
+    every round wait for the tiles that are on their way to LDS too. Fail the build if one does."""
+    import re
+    with open(_device_asm_path(src)) as f:
+        text = f.read()
+    names = re.findall(r"^(_ZN\S*%s\S*):" % kernel, text, re.M)
+    if not names:
+        raise RuntimeError("%s: no %s kernel found" % (src, kernel))
+    for name in names:
+        start = text.index("\n" + name + ":")
+        for block in re.split(r"\n(?=\.LBB)", text[start:text.index(".Lfunc_end", start)]):
+            if "v_mfma" in block and re.search(r"s_waitcnt[^\n;]*vmcnt", block):
+                raise RuntimeError("%s: %s waits for loads between matrix instructions" % (src, name))
 
 
 def _check_f32_assembly() -> None:

@@ -2,10 +2,10 @@
 // trees of drafted nodes, several rows with a window and sinks. Same function, records and masks as
 // decode_rows_bf16.hip; here the waves of a workgroup share the keys instead of the columns.
 //
-// What bounds it: by the counts, up to 64 columns the bytes of K and V (every key is fetched once for all columns), with 128 the
-// matrix work (8 D flop a score). In fact the two waves of a SIMD overlap only in part: for 64 keys x 128 columns at D = 128
-// the matrix instructions take 1.1 us, vector work 0.6 (exponentials: 16 clocks each); measured 2.3 with all units at work,
-// 1.9 with few.
+// What bounds it: up to 64 columns the bytes of K and V, every key fetched once for all columns (128 keys at D = 128 in 2.8 us
+// with all units at work, 6.0 TB/s; 1.7 with few). With 128 columns the matrix work (8 D flop a score): 64 keys take 1.1 us of
+// matrix instructions and 0.6 of vector work (exponentials: 16 clocks each), which the two waves of a SIMD overlap only in part;
+// measured 1.9 with all units at work, 1.6 with few.
 //
 // Layout:
 //   * eight waves, two per SIMD, so that the vector work of one runs under the matrix instructions of the other: up to 64 columns
@@ -13,8 +13,8 @@
 //     takes its 64 keys in one go, one test and no branch between their products, and reads its operands four fragments
 //     ahead. Measured (us; 16 x up to 6000 keys, 8 key heads, 52 columns, 2 splits; 8 x 16384 keys, 4 key heads, 256
 //     columns, 4 splits): 32 keys in one go 107, 188; 64 99, 177; reads ahead and no bank conflicts 96, 170; the waves with matrix
-//     work preferred 95.5, 167; with a faster merge 86, 161. Four waves of 32 columns, which halve the reads of LDS, their
-//     steps pipelined by hand: 210 for the second;
+//     work preferred 95.5, 167; with a faster merge 83, 160; q and rho waited for in front of the tile loop 67, 136. Four waves
+//     of 32 columns, which halve the reads of LDS, their steps pipelined by hand: 210 for the second;
 //   * a tile with masks is first looked through for values of V that are not finite, and only then treated for them
 //     (48 nodes x 2 heads, window 321, 6 sequences: 31 -> 23; 16 rows x 2, window 256, 8 sequences 31 -> 21);
 //   * tiles in a ring of 128 KB of LDS, filled by direct global -> LDS loads (no registers parked), 64 - 96 KB of it on
@@ -181,7 +181,35 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
     if (!wide_item(P, cg, split, hk, b)) return;
     if (tid < 2) some_bad[tid] = 0;  // (the ring's first barrier is in front of its use)
     const int G = p.G, S = p.S, Tq = p.Tq, n_cols = G * Tq, x0 = cg * COLS;
+    // ---- this lane's column: q and rho operands, key set ----------------------------------------------------
+    // They are here before the first tile is asked for: waited for inside the tile loop, they would make every
+    // round wait for the tiles on their way as well (the wait counts loads, whichever they are): 1.9 us a tile of 64 keys x 128
+    // columns instead of 1.6.
+    u32x4 qf[KSTEPS], rf[KSTEPS];
+    int col_end, col_lo;
+    TreeRow col_nodes{};
+    const int x = x0 + 16 * cw + c;
+    const bool live = x < n_cols;
+    const int t = live ? x / G : 0;
+    {
+        const int h = live ? x - t * G : 0;
+        const int64_t row = (((int64_t)b * p.Hq + (int64_t)hk * G + h) * Tq + t) * D;
+        const __bf16 *qrow = (const __bf16 *)p.q + row, *rrow = (const __bf16 *)p.r + row;
+#pragma unroll
+        for (int s = 0; s < KSTEPS; ++s) {
+            const u32x4 z = {0u, 0u, 0u, 0u};
+            qf[s] = live ? *(const u32x4 *)(qrow + 8 * (4 * s + g)) : z;
+            if constexpr (USE_R) rf[s] = live ? *(const u32x4 *)(rrow + 8 * (4 * s + g)) : z;
+        }
+    }
     const RowsScope<TREE, TILE> scope(P, b, x0, COLS);
+    scope.column(P, b, t, live, col_lo, col_end, col_nodes);
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) {
+        asm volatile("" : "+v"(qf[s]));
+        if constexpr (USE_R) asm volatile("" : "+v"(rf[s]));
+    }
+    if constexpr (TREE) asm volatile("" : "+v"(col_nodes.first));
     const int per = (scope.n_virtual + S - 1) / S;
     const int v_lo = split * per, v_hi = min(v_lo + per, scope.n_virtual);
 
@@ -192,24 +220,6 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
     for (int i = 0; i < AHEAD; ++i)
         if (v_lo + i < v_hi) loader.issue(v_lo + i, i);
 
-    // ---- this lane's column: q and rho operands, key set ----------------------------------------------------
-    u32x4 qf[KSTEPS], rf[KSTEPS];
-    int col_end, col_lo;
-    TreeRow col_nodes{};
-    const int x = x0 + 16 * cw + c;
-    {
-        const bool live = x < n_cols;
-        const int t = live ? x / G : 0, h = live ? x - t * G : 0;
-        const int64_t row = (((int64_t)b * p.Hq + (int64_t)hk * G + h) * Tq + t) * D;
-        const __bf16 *qrow = (const __bf16 *)p.q + row, *rrow = (const __bf16 *)p.r + row;
-#pragma unroll
-        for (int s = 0; s < KSTEPS; ++s) {
-            const u32x4 z = {0u, 0u, 0u, 0u};
-            qf[s] = live ? *(const u32x4 *)(qrow + 8 * (4 * s + g)) : z;
-            if constexpr (USE_R) rf[s] = live ? *(const u32x4 *)(rrow + 8 * (4 * s + g)) : z;
-        }
-        scope.column(P, b, t, live, col_lo, col_end, col_nodes);
-    }
     float m_run = kNegInf;
     f32x4 o1[NDB], o2[NDB], dsum1 = {0.f, 0.f, 0.f, 0.f}, dsum2 = dsum1;  // (four times the same sum: a product with ones)
 #pragma unroll

@@ -437,13 +437,13 @@ plx_status prepare_decode_rows(const plx_decode_args *a, const plx_decode_tree_a
 
 // Split count of such a call. Up to 16 columns: that of a plain one over as many keys, doubled while half of the units stay idle
 // and every wave keeps a tile of 32 keys (kernel alone, us, 8 key heads: one row, 1028 keys S = 4 10.9, 8 8.4; 8 nodes x 2 heads,
-// 1500 keys S = 6 10.2, 12 8.0). Beyond them (one workgroup of eight waves per
-// compute unit, decode_rows_wide_bf16.hip) from a model fitted to sweeps of S on MI355X, in us: a round of at most one workgroup
-// per unit takes 6, 1.5 for a tile with masks (the first and the last) and for each 128 keys (d = 128; shorter rows in proportion) 2.25 of arithmetic with 64 columns, 4.1 with
-// 128, and a third of the time in which the memory brings in what the workgroups of the round read at 5 TB/s, which is also the
-// least; the merge takes 5 and writing and reading of the records at 6 TB/s. Measured for 32 sequence heads x 16384 keys, d = 128, in
-// front of 128 columns: S = 1 533, 4 167, 6 122, 8 107, 10 152, 16 120 (the model takes 8); for 128 x up to 6000, 64 columns: S = 1
-// 128, 2 86, 3 101, 4 97 (2; the rule for plain rows took 1).
+// 1500 keys S = 6 10.2, 12 8.0). Beyond them (one workgroup of eight waves per compute unit, decode_rows_wide_bf16.hip) from a
+// model fitted to sweeps of S on MI355X, in us: a round of at most one workgroup per unit takes 6, 1.5 for a tile with masks (the
+// first and the last) and for each 128 keys (d = 128; shorter rows in proportion) 1.72 of arithmetic with 64 columns, 3.17 with 128,
+// and a quarter of the time in which the memory brings in what the workgroups of the round read at 6 TB/s, which is also the least;
+// the merge takes 5 and writing and reading of the records at 6 TB/s. Measured for 32 sequence heads x 16384 keys, d = 128, in
+// front of 128 columns: S = 1 405, 4 118, 6 89, 8 83, 10 125, 16 106 (the model takes 8); for 128 x up to 6000, 64 columns: S = 1
+// 100, 2 67, 3 77, 4 75 (2; the rule for plain rows took 1).
 int32_t pick_splits_rows(const plx_decode_args *a, const plx::DecodeRowsParams &p) {
     if (a->num_splits > 0) return a->num_splits;
     const int64_t in_window = (int64_t)a->window + p.d.Tq - 1 + p.sinks;
@@ -462,11 +462,11 @@ int32_t pick_splits_rows(const plx_decode_args *a, const plx::DecodeRowsParams &
         return s;
     }
     const int32_t tile = plx::decode_rows_tile(per), tiles = (keys + tile - 1) / tile;
-    const double share = tile / 128.0 * a->d / 128.0, compute = share * (per == 64 ? 2.25 : 4.1), memory = share * 65536e-6 / 5.0;
+    const double share = tile / 128.0 * a->d / 128.0, compute = share * (per == 64 ? 1.72 : 3.17), memory = share * 65536e-6 / 6.0;
     const double record_us = 2.0 * (double)a->B * a->Hq * p.d.Tq * (2 * a->d + 4) * 4e-6 / 6.0;
     auto round = [&](int64_t workgroups, int64_t n) {
         const double fetch = memory * (double)workgroups;
-        return 6.0 + 1.5 * (double)std::min<int64_t>(n, 2) + (double)n * std::max(fetch, compute + fetch / 3);
+        return 6.0 + 1.5 * (double)std::min<int64_t>(n, 2) + (double)n * std::max(fetch, compute + fetch / 4);
     };
     auto cost = [&](int32_t s) {
         const int64_t w = pairs * s, n = (tiles + s - 1) / s, full = w / cus, rest = w % cus;
