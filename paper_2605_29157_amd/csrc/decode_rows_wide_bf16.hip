@@ -12,9 +12,11 @@
 //     four blocks of 16 columns and two halves of a tile of 128 keys, beyond eight blocks of 16 columns and tiles of 64. A wave
 //     takes its 64 keys in one go, one test and no branch between their products, and reads its operands four fragments
 //     ahead. Measured (us; 16 x up to 6000 keys, 8 key heads, 52 columns, 2 splits; 8 x 16384 keys, 4 key heads, 256
-//     columns, 4 splits): 32 keys in one go 107, 188; 64 99, 177; reads ahead and no bank conflicts 96, 170; the waves with matrix
-//     work preferred 95.5, 167; with a faster merge 83, 160; q and rho waited for in front of the tile loop 67, 136. Four waves
-//     of 32 columns, which halve the reads of LDS, their steps pipelined by hand: 210 for the second;
+//     columns, 4 splits): 32 keys in one go 107, 188; 64 99, 177; reads ahead and no bank conflicts 96, 170; with a
+//     faster merge 83, 160; q and rho waited for in front of the tile loop 67, 138 (since then reading two to four fragments
+//     ahead, the conflicts and s_setprio around the products make no difference). Four waves
+//     of 32 columns, which halve the reads of LDS, their steps pipelined by hand: 210 for the second (where 32 keys in one go
+//     took 188);
 //   * a tile with masks is first looked through for values of V that are not finite, and only then treated for them
 //     (48 nodes x 2 heads, window 321, 6 sequences: 31 -> 23; 16 rows x 2, window 256, 8 sequences 31 -> 21);
 //   * tiles in a ring of 128 KB of LDS, filled by direct global -> LDS loads (no registers parked), 64 - 96 KB of it on
@@ -270,7 +272,6 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
             if constexpr (USE_R) s2[f / KSTEPS] = mfma16(kf[f], rf[f % KSTEPS], s2[f / KSTEPS]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_s_setprio(0);
         float factor = scale_log2;
         if (__builtin_expect(!whole, 0)) {  // (uniform)
 #pragma unroll
@@ -315,7 +316,6 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
             dsum1 = mfma16(ones, pb1[h], dsum1);
             if constexpr (USE_R) dsum2 = mfma16(ones, pb2[h], dsum2);
         }
-        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int f = 0; f < PV; ++f) {
             if (f + LOOK < PV) load_v(f + LOOK);
