@@ -241,8 +241,9 @@ plx_status parallax_decode_sinks(const plx_decode_args *args, int32_t sinks, voi
  * split counts. A key that a node does not see does not reach it, whatever its row holds.
  *   tree_mask   [mask_batch][Tq][ceil(Tq / 64)] on the device, 8-byte aligned; mask_batch 1 (one tree for all) or B
  *   draft_lens  [B] int32 on the device, or NULL = Tq
- *   window, sinks  (decode.window, sinks; 0 = none) apply to the committed keys: node t sits at position L_b - n_b +
- *               (number of its set bits) - 1 and sees those behind that position - window, and the first `sinks`
+ *   window, sinks  (decode.window, sinks; 0 = none): node t sits at position L_b - n_b + (number of its set bits) - 1, or
+ *               L_b - n_b without any, and sees of the keys above those whose position is behind its own - window, and those at the
+ *               first `sinks` positions: what parallax_decode_sinks sees where the tokens of its path are decoded one by one
  * Tq <= PLX_MAX_TREE_NODES; decode.prep all zero (PLX_ERR_SHAPE).
  */
 #define PLX_MAX_TREE_NODES 256

@@ -3,9 +3,10 @@ loops over the definitions, for oracle/masked.py to sum over.
 
 `chain`: the rows are the last Tq positions of a sequence of L cached tokens; a row at position pos sees the keys
 j <= pos with j > pos - window or j < sinks (window 0: all).
-`tree`: the last n = min(drafted, Tq, L) cached tokens are drafted nodes behind base = L - n committed ones; node t < n
-sees the committed keys (window > 0: j > base + (number of its bits) - 1 - window, or j < sinks) and the drafted key
-base + m iff bits[t][m]; node t >= n nothing.
+`tree`: the last n = min(drafted, Tq, L) cached tokens are drafted nodes behind base = L - n committed ones. Node t < n
+is at position base + (number of its bits) - 1 (no bits: base) and sees the committed keys and the drafted key base + m of
+every node m whose bit it has, all of them with window > 0 only where their position is > its own - window, or < sinks (a
+committed key's position is its place in the cache). Node t >= n sees nothing.
 """
 from __future__ import annotations
 
@@ -25,12 +26,12 @@ def tree(L, Tq, cap, bits, drafted=None, window=0, sinks=0):
     n = min(Tq if drafted is None else max(drafted, 0), Tq, L)
     base = L - n
     see = np.zeros((Tq, cap), dtype=bool)
+    pos = [base + max(int(sum(bits[t][:n])) - 1, 0) for t in range(n)]
     for t in range(n):
-        pos = base + max(int(sum(bits[t][:n])) - 1, 0)
         for j in range(base):
-            see[t, j] = window == 0 or j > pos - window or j < sinks
+            see[t, j] = window == 0 or j > pos[t] - window or j < sinks
         for m in range(n):
-            see[t, base + m] = bits[t][m]
+            see[t, base + m] = bits[t][m] and (window == 0 or pos[m] > pos[t] - window or pos[m] < sinks)
     return see
 
 

@@ -605,7 +605,8 @@ def parallax_decode_tree(q, r, k, v, scale, tree_mask, seq_lens=None, draft_lens
     """Attention of drafted tokens that form a tree. q, r [B, Hq, Tq, d]: the nodes, whose keys and values are the last
     draft_lens[b] (default Tq) of the seq_lens[b] cached tokens. tree_mask int64 [Tq], [Tq, W], [1 or B, Tq] or
     [1 or B, Tq, W], W = ceil(Tq / 64) (tree_mask_words makes one): bit m of node t's words: it sees drafted key m. Every node sees
-    the committed keys (with window: its window's and the first `sinks`). Rows from draft_lens[b] on return zeros."""
+    the committed keys. With a window a node sees, of both, the keys inside its window and those at the first `sinks` positions, where a
+    node's position is the number of its ancestors behind the committed ones. Rows from draft_lens[b] on return zeros."""
     if q.dim() != 4:
         raise ValueError("q [B, Hq, Tq, d]")
     return _decode_rows(q, r, k, v, scale, seq_lens, use_r, num_splits, workspace, out, stream, block_table, max_len,

@@ -35,6 +35,7 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
     constexpr int KSTEPS = D / 32, NDB = D / 16;
     constexpr int TILE_CHUNKS = kRowsTile * CPR;
     __shared__ u32x4 lds[kRowsWaves * 2 * TILE_CHUNKS + 48];  // tiles; at the end the states of 16 columns
+    __shared__ TreeWords<TREE ? 16 : 0> tree_words;
 
     const int tid = threadIdx.x;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -63,7 +64,7 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
             qf[s] = live ? *(const u32x4 *)(qrow + 8 * (4 * s + g)) : z;
             if constexpr (USE_R) rf[s] = live ? *(const u32x4 *)(rrow + 8 * (4 * s + g)) : z;
         }
-        scope.column(P, b, t, live, col_lo, col_end, col_nodes);
+        scope.column(P, tree_words, 0, c, t, live, col_lo, col_end, col_nodes);
     }
 
     const __bf16 *kbase = (const __bf16 *)p.k + (p.block_table == nullptr ? (int64_t)b * p.ksb : 0) + (int64_t)hk * p.ksh;

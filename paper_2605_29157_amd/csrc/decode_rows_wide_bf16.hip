@@ -173,6 +173,7 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
     static_assert(2 * 4 * NDB * 64 <= STAGES * STAGE_CHUNKS, "the states of four waves");
     constexpr int CW = 8 / KH, COLS = 16 * CW;  // waves side by side over the columns
     __shared__ float head[CW][3][16];
+    __shared__ TreeWords<TREE ? COLS : 0> tree_words;
     __shared__ int some_bad[2];  // of the masked tile in turn: V holds a value that is not finite
 
     const int tid = threadIdx.x;
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(512, 2) void decode_rows_wide_kernel(DecodeRowsPara
         }
     }
     const RowsScope<TREE, TILE> scope(P, b, x0, COLS);
-    scope.column(P, b, t, live, col_lo, col_end, col_nodes);
+    scope.column(P, tree_words, x0, 16 * cw + c, t, live, col_lo, col_end, col_nodes);
 #pragma unroll
     for (int s = 0; s < KSTEPS; ++s) {
         asm volatile("" : "+v"(qf[s]));

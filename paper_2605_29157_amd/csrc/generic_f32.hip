@@ -210,11 +210,14 @@ union F32ForwardLds {
 };
 
 // FULL: d == DP, nothing to pad. VIS: rows whose key sets are not one range (sinks, drafted nodes): the blocks
-// walked are those of the sinks, then those from the first key any window reaches.
-template <int DP, bool PAGED, bool USE_R, bool FULL, bool VIS = false>
+// walked are those of the sinks, then those from the first key any window reaches. STAGED: drafted nodes behind a window that is
+// shorter than the draft, their masks from LDS (tree_stage; in the kernel of the others that code, never run, has the scheduler wait
+// for every LDS read of the scores at once: 16 nodes, d = 64, 4 x up to 2048 keys 24.0 -> 25.5 us).
+template <int DP, bool PAGED, bool USE_R, bool FULL, bool VIS = false, bool STAGED = false>
 __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_forward_kernel(F32Forward p) {
     __shared__ F32ForwardLds<DP> lds;
     __shared__ float sm[3][kF32Waves][16];
+    __shared__ TreeWords<STAGED ? 16 : 0> tree_words;
     constexpr int NA = DP / 16;
 
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -249,15 +252,18 @@ __global__ __launch_bounds__(kF32Threads, DP <= 128 ? 2 : 1) void f32_forward_ke
     if constexpr (VIS) {
         if (tree) {
             const uint64_t *words = p.mask + (int64_t)b * p.mask_stride_b + (int64_t)t * p.mask_words;
-            nodes = {words, *words};
+            if constexpr (STAGED) {
+                tree_stage<16>(tree_words, p.mask + (int64_t)b * p.mask_stride_b, p.mask_words, n, base, p.window, p.window > 0 ? p.sinks : 0, tid,
+                               kF32Threads, [&](int col) { return min(16 * blk + col, x_last) / p.gcols; });
+                nodes = {tree_words.of[c], tree_words.of[c][0]};
+            } else {
+                nodes = {words, *words};
+            }
             my_end = t < n ? len : 0, my_lo = 0;
             all_lo = 0, all_end = base, lo = 0;
             hi = t0 < n ? (len + 15) / 16 : 0, last_key = len - 1;
             if (p.window > 0) {
-                int ancestors = 0;  // set bits among the n drafted nodes: the node's depth, itself included
-                for (int i = 0; i < p.mask_words && 64 * i < n; ++i)
-                    ancestors += __popcll(words[i] & (n - 64 * i >= 64 ? ~0ull : (1ull << (n - 64 * i)) - 1));
-                my_lo = min(max(base + max(ancestors - 1, 0) - p.window + 1, 0), base);
+                my_lo = min(max(base + tree_position(words, p.mask_words, n) - p.window + 1, 0), base);
                 all_lo = min(max(base + n - p.window, 0), base);
                 lo = min(max(base + 1 - p.window, 0), base) / 16;
             }
@@ -512,28 +518,35 @@ __global__ __launch_bounds__(256) void f32_combine_kernel(F32Forward p) {
 static hipError_t launch_forward(F32Forward &g, hipStream_t stream) {
     g.n_blocks = (g.n_cols + 15) / 16;
     const dim3 grid = f32_grid((int64_t)g.n_blocks * g.B * g.heads * g.S), block(kF32Threads);
-    auto pick = [&](auto paged, auto use_r, auto vis) {
-        constexpr bool P = decltype(paged)::value, R = decltype(use_r)::value, V = decltype(vis)::value;
+    auto pick = [&](auto paged, auto use_r, auto sets) {
+        constexpr bool P = decltype(paged)::value, R = decltype(use_r)::value, V = decltype(sets)::value >= 1, T = decltype(sets)::value == 2;
         if (g.d == 64)
-            hipLaunchKernelGGL((f32_forward_kernel<64, P, R, true, V>), grid, block, 0, stream, g);
+            hipLaunchKernelGGL((f32_forward_kernel<64, P, R, true, V, T>), grid, block, 0, stream, g);
         else if (g.d < 64)
-            hipLaunchKernelGGL((f32_forward_kernel<64, P, R, false, V>), grid, block, 0, stream, g);
+            hipLaunchKernelGGL((f32_forward_kernel<64, P, R, false, V, T>), grid, block, 0, stream, g);
         else if (g.d == 128)
-            hipLaunchKernelGGL((f32_forward_kernel<128, P, R, true, V>), grid, block, 0, stream, g);
+            hipLaunchKernelGGL((f32_forward_kernel<128, P, R, true, V, T>), grid, block, 0, stream, g);
         else if (g.d < 128)
-            hipLaunchKernelGGL((f32_forward_kernel<128, P, R, false, V>), grid, block, 0, stream, g);
+            hipLaunchKernelGGL((f32_forward_kernel<128, P, R, false, V, T>), grid, block, 0, stream, g);
         else if (g.d == 256)
-            hipLaunchKernelGGL((f32_forward_kernel<256, P, R, true, V>), grid, block, 0, stream, g);
+            hipLaunchKernelGGL((f32_forward_kernel<256, P, R, true, V, T>), grid, block, 0, stream, g);
         else
-            hipLaunchKernelGGL((f32_forward_kernel<256, P, R, false, V>), grid, block, 0, stream, g);
+            hipLaunchKernelGGL((f32_forward_kernel<256, P, R, false, V, T>), grid, block, 0, stream, g);
     };
     const std::true_type yes;
     const std::false_type no;
-    const bool vis = g.mask != nullptr || g.sinks > 0;
-    if (g.block_table)
-        g.use_r ? (vis ? pick(yes, yes, yes) : pick(yes, yes, no)) : (vis ? pick(yes, no, yes) : pick(yes, no, no));
+    auto of_sets = [&](auto sets) {
+        if (g.block_table)
+            g.use_r ? pick(yes, yes, sets) : pick(yes, no, sets);
+        else
+            g.use_r ? pick(no, yes, sets) : pick(no, no, sets);
+    };
+    if (g.mask != nullptr && g.window > 0 && g.window < g.Tq)
+        of_sets(std::integral_constant<int, 2>{});
+    else if (g.mask != nullptr || g.sinks > 0)
+        of_sets(std::integral_constant<int, 1>{});
     else
-        g.use_r ? (vis ? pick(no, yes, yes) : pick(no, yes, no)) : (vis ? pick(no, no, yes) : pick(no, no, no));
+        of_sets(std::integral_constant<int, 0>{});
     if (hipError_t err = hipGetLastError()) return err;
     if (g.S > 1) {
         hipLaunchKernelGGL(f32_combine_kernel, f32_grid((int64_t)g.B * g.Hq * g.Tq), dim3(256), 0, stream, g);

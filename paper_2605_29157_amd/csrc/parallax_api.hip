@@ -412,6 +412,8 @@ plx_status parallax_decode_combine(const plx_decode_args *a, void *hip_stream) {
 
 namespace {
 
+static_assert(PLX_MAX_TREE_NODES == plx::kTreeNodes, "masks and positions of the nodes in LDS");
+
 // Rows whose key sets differ: sinks behind a window, drafted nodes (tree != nullptr).
 plx_status prepare_decode_rows(const plx_decode_args *a, const plx_decode_tree_args *tree, int32_t sinks, bool need_out,
                                plx::DecodeRowsParams *out) {

@@ -6,6 +6,8 @@
 
 #include <type_traits>
 
+#include "plx_kernels.h"
+
 namespace plx {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -136,7 +138,7 @@ __device__ __forceinline__ int lds_chunk_slot(int row, int chunk) {
     return row * CPR + (chunk ^ lds_row_swizzle<D>(row));
 }
 
-// A node's row of a tree mask; its first word is fetched in advance
+// A node's row of a tree mask: its first word, and where all of them are (memory or TreeWords in LDS)
 struct TreeRow {
     const uint64_t *words;
     uint64_t first;
@@ -150,6 +152,51 @@ __device__ __forceinline__ uint32_t tree_bits(const TreeRow &row, int n_words, i
     uint64_t x = (w == 0 ? row.first : row.words[w]) >> s;
     if (s > 32 && w + 1 < n_words) x |= row.words[w + 1] << (64 - s);
     return (uint32_t)x;
+}
+// Position of a drafted node, counted from the first one behind the committed keys: its ancestors among the n drafted nodes,
+// which are the bits of its mask words but its own (no bit at all: the first)
+__device__ __forceinline__ int tree_position(const uint64_t *words, int n_words, int n) {
+    int bits = 0;
+    for (int i = 0; i < n_words && 64 * i < n; ++i) {
+        const int left = n - 64 * i;
+        bits += __popcll(words[i] & (left >= 64 ? ~0ull : (1ull << left) - 1));
+    }
+    return max(bits - 1, 0);
+}
+// The mask words of a workgroup's columns, less the ancestors that a window shorter than the draft hides
+template <int COLS>
+struct TreeWords {
+    uint64_t of[COLS][kTreeNodes / 64];
+    uint16_t position[kTreeNodes];
+};
+template <>
+struct TreeWords<0> {};
+// Are they needed? (No: one word a node, in a register, and a window that no ancestor can be behind. The same for all threads)
+__device__ __forceinline__ bool tree_staged(int n_words, int window, int n) { return n_words > 1 || (window > 0 && window < n); }
+// Fills them in; node_of(column): whose they are. A node sees an ancestor inside its window, or at one of the first `sinks` positions; the
+// position of a node follows from its own mask, wherever it lies. All threads take part.
+template <int COLS, class NodeOf>
+__device__ __forceinline__ void tree_stage(TreeWords<COLS> &lds, const uint64_t *masks, int n_words, int n, int base, int window, int sinks,
+                                           int tid, int threads, NodeOf node_of) {
+    const bool cut = window > 0 && window < n;
+    if (cut) {
+        for (int m = tid; m < n; m += threads) lds.position[m] = (uint16_t)tree_position(masks + (int64_t)m * n_words, n_words, n);
+        __syncthreads();
+    }
+    for (int e = tid; e < COLS * n_words; e += threads) {
+        const int col = e / n_words, w = e - col * n_words, t = node_of(col);
+        uint64_t x = t < n ? masks[(int64_t)t * n_words + w] : 0;
+        if (cut && t < n) {
+            const int left = n - 64 * w, first = (int)lds.position[t] - window + 1;
+            if (left < 64) x &= left > 0 ? (1ull << left) - 1 : 0;
+            for (uint64_t y = x; y != 0; y &= y - 1) {
+                const int at = lds.position[64 * w + __builtin_ctzll(y)];
+                if (at < first && base + at >= sinks) x &= ~(y & -y);
+            }
+        }
+        lds.of[col][w] = x;
+    }
+    __syncthreads();
 }
 
 }  // namespace plx

@@ -40,9 +40,12 @@ struct DecodeParams {
     QrPrep prep;
 };
 
+constexpr int kTreeNodes = 256;  // the most drafted nodes of a sequence
+
 // Decode of rows whose key sets differ (decode_rows_bf16.hip; fp32: generic_f32.hip): d.window with `sinks` first tokens that
 // stay visible, and / or drafted nodes (mask != nullptr): the last n_b = min(draft_lens[b], Tq, L_b) cached tokens of a
-// sequence, node t seeing the committed keys and key L_b - n_b + j iff bit j of its mask words is set.
+// sequence, node t seeing the committed keys and key L_b - n_b + j iff bit j of its mask words is set, both inside its window
+// only (the position of a node: L_b - n_b + its ancestors).
 struct DecodeRowsParams {
     DecodeParams d;
     int32_t sinks;

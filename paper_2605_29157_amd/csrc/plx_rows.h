@@ -34,6 +34,7 @@ struct RowsScope {
     int Lb, n, base;          // cached tokens; drafted ones among them (TREE), behind `base` committed ones (else base = Lb - Tq)
     int lo_all, end_all;      // keys every column sees: [lo_all, end_all), and [0, sinks) below end_all
     int sinks, n_sink_tiles, first_tile, n_virtual;
+    const uint64_t *masks;    // TREE: the sequence's
 
     __device__ __forceinline__ RowsScope(const DecodeRowsParams &P, int b, int x0, int width) {
         const DecodeParams &p = P.d;
@@ -42,6 +43,7 @@ struct RowsScope {
         n = p.Tq;
         if constexpr (TREE) n = min(P.draft_lens ? min(max(P.draft_lens[b], 0), p.Tq) : p.Tq, Lb);
         base = Lb - n;
+        masks = TREE ? P.mask + (int64_t)b * P.mask_stride_b : nullptr;
         const int t_first = x0 / p.G, t_last = min(x0 + width - 1, p.G * p.Tq - 1) / p.G;
         int lo_any = 0, end_any;
         lo_all = 0;
@@ -62,21 +64,22 @@ struct RowsScope {
     __device__ __forceinline__ bool whole(int key, int count) const {
         return (key >= lo_all || key + count <= sinks) && key + count <= end_all;
     }
-    // Keys of one column: [lo, end) and the sinks below end, of the drafted ones those whose bit is set
-    __device__ __forceinline__ void column(const DecodeRowsParams &P, int b, int t, bool live, int &lo, int &end, TreeRow &nodes) const {
+    // Keys of column x (number `at` of the workgroup's COLS from x0 on): [lo, end) and the sinks below end, of the drafted ones those
+    // whose bit is set. All threads take part.
+    template <int COLS>
+    __device__ __forceinline__ void column(const DecodeRowsParams &P, TreeWords<COLS> &lds, int x0, int at, int t, bool live, int &lo,
+                                           int &end, TreeRow &nodes) const {
         if constexpr (TREE) {
-            const uint64_t *words = P.mask + (int64_t)b * P.mask_stride_b + (int64_t)t * P.mask_words;
-            nodes = {words, *words};
+            const uint64_t *words = masks + (int64_t)t * P.mask_words;
+            nodes = {lds.of[at], *words};
+            if (tree_staged(P.mask_words, P.d.window, n)) {  // (uniform)
+                tree_stage<COLS>(lds, masks, P.mask_words, n, base, P.d.window, sinks, threadIdx.x, blockDim.x,
+                                 [&](int col) { return (x0 + col) / P.d.G; });
+                nodes.first = lds.of[at][0];
+            }
             end = live && t < n ? Lb : 0;
             lo = 0;
-            if (P.d.window > 0) {
-                int ancestors = 0;  // set bits among the n drafted nodes: the node's depth, itself included
-                for (int i = 0; i < P.mask_words && 64 * i < n; ++i) {
-                    const int left = n - 64 * i;
-                    ancestors += __popcll(words[i] & (left >= 64 ? ~0ull : (1ull << left) - 1));
-                }
-                lo = min(max(base + max(ancestors - 1, 0) - P.d.window + 1, 0), base);
-            }
+            if (P.d.window > 0) lo = min(max(base + tree_position(words, P.mask_words, n) - P.d.window + 1, 0), base);
         } else {
             end = live ? max(base + t + 1, 0) : 0;
             lo = P.d.window > 0 ? max(end - P.d.window, 0) : 0;
