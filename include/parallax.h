@@ -293,9 +293,10 @@ typedef struct {
 plx_status parallax_cache_fork(const plx_page_table *pages, const int32_t *parents, const int32_t *children, int32_t n,
                                void *hip_stream);
 /*
- * Room for new_lens[i] tokens in sequence seqs[i] (not less than it has, no more than pages_per_sequence * page_size; listed
- * twice, the first time counts): free pages, in the order of the list, for the entries behind its last page that hold
- * none. A last page that is partly filled and that others name too when the sequence's turn comes is
+ * Room for new_lens[i] tokens in sequence seqs[i] (not less than it has, no more than pages_per_sequence * page_size: a length outside
+ * is taken as the nearer of the two, and seq_lens then says which; listed twice, the first time counts): free pages, in the order of
+ * the list, so that every new token has one: for the entries behind its last page that hold none, and for that of a partly filled last
+ * page that has been given back. A last page that is partly filled and that others name too when the sequence's turn comes is
  * replaced by a fresh one: src[i], dst[i], rows[i] then say what parallax_cache_copy has to move, in every
  * layer's pools, before the sequence is used (-1, -1, 0 otherwise). seq_lens[s] becomes new_lens[i]; the new rows hold
  * whatever was there. missing (one int32): 0, or how many pages were lacking, and then nothing was changed.

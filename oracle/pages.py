@@ -25,7 +25,7 @@ class Pages:
             self.lens[c] = self.lens[p]
 
     def extend(self, seqs, new_lens):
-        """-> (missing, moves), moves[i] = (src, dst, rows) or (-1, -1, 0)"""
+        """A page for every token that is new. -> (missing, moves), moves[i] = (src, dst, rows) or (-1, -1, 0)"""
         todo, seen, left = [], set(), dict()
         for i, (s, to) in enumerate(zip(seqs, new_lens)):
             if not self._valid(s) or s in seen:
@@ -36,7 +36,9 @@ class Pages:
             if to > n and n % self.page:
                 at = n // self.page
                 x = self.table[s][at]
-                if x >= 0:
+                if x < 0:  # given back: the new rows on it need a page
+                    entries.append((at, -1))
+                else:
                     if self.refs[x] - left.get(x, 0) > 1:
                         entries.append((at, x))
                     left[x] = left.get(x, 0) + 1

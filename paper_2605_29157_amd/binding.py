@@ -1060,9 +1060,10 @@ def parallax_cache_fork(pages, parents, children, stream=None):
 
 
 def parallax_cache_extend(pages, seqs, new_lens, *pools, stream=None):
-    """Room for new_lens[i] tokens in sequence seqs[i]. pools: k, v (, k, v ...) of the layers that the table serves; shared
-    last pages that are replaced are copied in all of them. Returns `missing` (int32 [1] on the device: 0, or how many
-    pages were lacking, and then nothing was changed). Without pools (missing, src, dst, rows) is returned, and
+    """Room for new_lens[i] tokens in sequence seqs[i] (clamped to what it has and what its table row can hold): a page for every
+    token that is new. pools: k, v (, k, v ...) of the layers that the table serves; shared last pages that are replaced are
+    copied in all of them. Returns `missing` (int32 [1] on the device: 0, or how many pages were lacking, and then nothing was
+    changed). Without pools (missing, src, dst, rows) is returned, and
     parallax_cache_copy(k, v, src, dst, rows) is the caller's to call for every layer."""
     where = "parallax_cache_extend"
     device = _table_device(where, pages)

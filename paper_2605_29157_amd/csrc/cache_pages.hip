@@ -71,8 +71,8 @@ __global__ __launch_bounds__(256) void cache_fork_kernel(PageTable t, const int3
 }
 
 // Room for new_lens[i] tokens in sequence seqs[i]: one workgroup, a thread per listed sequence, then a thread per table entry
-// to fill. The entries of all sequences are numbered one after the other: of sequence i the copy of its last
-// page, if it takes one, then the pages behind its last.
+// to fill. The entries of all sequences are numbered one after the other: of sequence i that of its partly filled last
+// page, if it takes a page there (a copy, or the first where that page had been given back), then those behind it.
 __global__ __launch_bounds__(kBookThreads) void cache_extend_kernel(PageTable t, const int32_t *seqs, const int32_t *new_lens, int n,
                                                                     int32_t *src, int32_t *dst, int32_t *rows, int32_t *missing) {
     __shared__ int wave_sums[kBookThreads / 64];
@@ -87,12 +87,14 @@ __global__ __launch_bounds__(kBookThreads) void cache_extend_kernel(PageTable t,
         if (seq[j] == seq[tid]) s = -1;
     const int capacity = t.pages_per_sequence * t.page_size;
     int length = 0, to = 0, tail = -1;
+    bool hole = false;  // the last page, partly filled, has been given back
     if (s >= 0) {
         length = min(max(t.seq_lens[s], 0), capacity);
         to = min(max(new_lens[tid], length), capacity);
         if (to > length && length % t.page_size != 0) {
             tail = t.block_table[(int64_t)s * t.stride + length / t.page_size];
-            if (tail < 0 || tail >= t.num_pages) tail = -1;
+            hole = tail < 0;
+            if (tail >= t.num_pages) tail = -1;
         }
     }
     tail_page[tid] = tail;
@@ -105,10 +107,10 @@ __global__ __launch_bounds__(kBookThreads) void cache_extend_kernel(PageTable t,
         for (int j = 0; j < tid; ++j) earlier += tail_page[j] == tail;
         copied = t.page_refs[tail] - earlier > 1;
     }
-    const int whole = pages_of(length, t.page_size);
+    const int from = pages_of(length, t.page_size) - (copied || hole ? 1 : 0);
     int n_entries;
-    const int first = block_scan((copied ? 1 : 0) + pages_of(to, t.page_size) - whole, wave_sums, n_entries);
-    first_entry[tid] = first, first_page[tid] = whole - (copied ? 1 : 0), copies[tid] = copied;
+    first_entry[tid] = block_scan(pages_of(to, t.page_size) - from, wave_sums, n_entries);
+    first_page[tid] = from, copies[tid] = copied;
     if (tid < n) src[tid] = dst[tid] = -1, rows[tid] = 0;
     __syncthreads();
     // entry e -> which of the listed sequences, and where its table entry is; does it take a page?
