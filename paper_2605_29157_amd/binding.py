@@ -1071,18 +1071,25 @@ def parallax_cache_extend(pages, seqs, new_lens, *pools, stream=None):
     ptrs = _int_list(where, "seqs", seqs, None, device), _int_list(where, "new_lens", new_lens, n, device)
     if len(pools) % 2:
         raise ValueError("pools come as k, v (v None: a single pool)")
-    for k in pools[::2]:
-        if k.shape[0] != pages.page_refs.numel() or k.shape[-2] != pages.page_size:
+    lib, where_to = load_library(), _launch_stream(where, stream)
+    # Every layer's pools are looked at before the table changes: a refusal behind that would leave shared pages replaced whose
+    # rows have not been copied. (A copy of nothing is checked like any other, and launches nothing.)
+    layers = []
+    for k, v in zip(pools[::2], pools[1::2]):
+        a = _filled(plx_cache_pools, *_pools(where, k, v))
+        if a.num_pages != pages.page_refs.numel() or a.page_size != pages.page_size:
             raise ValueError("the pools have the pages of the table")
+        st = lib.parallax_cache_copy(ctypes.byref(a), 0, 0, 0, 0, where_to)
+        if st != PLX_OK:
+            raise ParallaxError(st, "parallax_cache_copy")
+        layers.append(a)
     buf = _result_maker(stream, torch.empty)(3 * n + 1, dtype=torch.int32, device=pages.block_table.device)
     at = buf.data_ptr()
     src, dst, rows, missing = at, at + 4 * n, at + 8 * n, at + 12 * n
-    lib, where_to = load_library(), _launch_stream(where, stream)
     st = lib.parallax_cache_extend(ctypes.byref(pages._args), *ptrs, n, src, dst, rows, missing, where_to)
     if st != PLX_OK:
         raise ParallaxError(st, where)
-    for i in range(0, len(pools), 2):
-        a = _filled(plx_cache_pools, *_pools(where, pools[i], pools[i + 1]))
+    for a in layers:
         st = lib.parallax_cache_copy(ctypes.byref(a), src, dst, rows, n, where_to)
         if st != PLX_OK:
             raise ParallaxError(st, "parallax_cache_copy")
