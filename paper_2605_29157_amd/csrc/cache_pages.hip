@@ -256,11 +256,12 @@ __global__ __launch_bounds__(256) void cache_copy_kernel(CachePools c, const int
     const int i = blockIdx.x, from = src[i], to = dst[i];
     if (from < 0 || from >= c.num_pages || to < 0 || to >= c.num_pages || from == to) return;
     const int n_rows = rows ? min(max(rows[i], 0), c.page_size) : c.page_size;
-    const int pool_chunks = c.heads * n_rows * c.row_chunks;
-    const int total = c.v ? 2 * pool_chunks : pool_chunks;
-    for (int e = blockIdx.y * 256 + threadIdx.x; e < total; e += 256 * gridDim.y) {
+    // (up to 2^30 - 1 chunks a pool, 2^31 - 2 in all, and a stride of up to 2^24 behind the last: 32 bits without a sign)
+    const uint32_t pool_chunks = (uint32_t)c.heads * n_rows * c.row_chunks;
+    const uint32_t total = c.v ? 2 * pool_chunks : pool_chunks;
+    for (uint32_t e = blockIdx.y * 256 + threadIdx.x; e < total; e += 256 * gridDim.y) {
         const bool second = e >= pool_chunks;
-        const int x = second ? e - pool_chunks : e;
+        const int x = (int)(second ? e - pool_chunks : e);
         const int chunk = x % c.row_chunks, hr = x / c.row_chunks, row = hr % n_rows, head = hr / n_rows;
         char *base = second ? c.v : c.k;
         const int64_t *st = second ? c.vs : c.ks;
