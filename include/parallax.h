@@ -320,7 +320,8 @@ plx_status parallax_cache_copy(const plx_cache_pools *pools, const int32_t *src,
 /*
  * After the verification of drafted nodes (parallax_decode_tree): the rows of the accepted ones, numbers accepted[b][0 ..
  * n_accepted[b]) in ascending order, move together behind the committed rows: row base + accepted[b][i] to base +
- * i, base = L_b - n_b, n_b = min(draft_lens[b], max_draft, L_b). new_lens[b] = base + n_accepted[b] (at most n_b of them).
+ * i, base = L_b - n_b, n_b = min(draft_lens[b], max_draft, L_b): max_draft is the Tq of that call, so that
+ * both find the drafted rows in the same place. new_lens[b] = base + n_accepted[b] (at most n_b of them).
  * What lies behind is left as it was; parallax_cache_free gives its pages back. Numbers are clamped to [i, n_b);
  * a list that does not ascend moves the wrong rows, and no row is moved from or to a table entry that is no page. pools as above; without a block table [B, heads, capacity, d] with
  * the sequence's stride first and page_size = capacity, num_pages = B. The pages of the drafted rows must not be shared.

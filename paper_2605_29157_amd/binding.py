@@ -1123,8 +1123,9 @@ def parallax_cache_copy(k, v, src, dst, rows=None, stream=None):
 
 def parallax_cache_compact(k, v, seq_lens, draft_lens, accepted, n_accepted, block_table=None, new_lens=None, max_draft=None,
                            stream=None):
-    """The rows of the accepted nodes (numbers accepted[b][: n_accepted[b]], ascending) among the last draft_lens[b] cached ones
-    (None: max_draft) move together behind the committed rows. k, v: pools with a block_table, else [B, Hkv, capacity, d];
+    """The rows of the accepted nodes (numbers accepted[b][: n_accepted[b]], ascending) among the last min(draft_lens[b], max_draft)
+    cached ones (draft_lens None: max_draft) move together behind the committed rows. max_draft is the Tq of the tree that was verified (not
+    given: 256, the same where no draft_lens[b] is above Tq). k, v: pools with a block_table, else [B, Hkv, capacity, d];
     v None: k only. Returns new_lens [B] = committed + accepted; seq_lens stays as it is."""
     where = "parallax_cache_compact"
     pools = _pools(where, k, v)
