@@ -90,3 +90,50 @@ def test_ancestors_behind_the_window_hold_anything(plx, dtype):
                 _check(got[:, :, free], z, see[:, free], dtype, (heads, bad, splits))
                 for t in range(2, 2 + window):
                     assert not torch.isfinite(got[:, :, t]).all(), (t, bad)
+
+
+@pytest.mark.parametrize("d,page", [(36, 0), (64, 16), (132, 7), (200, 0), (256, 0), (256, 5)])
+@pytest.mark.parametrize("heads,Tq", [((6, 2), 5), ((2, 2), 20), ((4, 1), 100)])
+def test_f32_head_dimensions(plx, d, page, heads, Tq):
+    lens, drafted, cap, window, sinks = (333, Tq + 20), (Tq, Tq - 2), 333, 3, 7
+    rng = np.random.default_rng(d + Tq)
+    bits = np.stack([rows.random_tree(Tq, rng, reach=1) for _ in lens])
+    see = [_path_sees(L, Tq, cap, bits[b], drafted[b], window, sinks) for b, L in enumerate(lens)]
+    x = _inputs(2, *heads, d, Tq, cap, seed=d, dtype=torch.float32)
+    y, more = x, {}
+    if page:
+        y = _paged(x, page, seed=page)
+        more = dict(block_table=y["block_table"], max_len=cap)
+    mask = torch.from_numpy(rows.words(bits)).to(DEV)
+    for use_r in (True, False):
+        z = x if use_r else dict(x, r=torch.zeros_like(x["r"]))
+        for splits in (0, 3):
+            got = plx.parallax_decode_tree(y["q"], y["r"] if use_r else None, y["k"], y["v"], y["scale"], mask, seq_lens=_ints(lens),
+                                           draft_lens=_ints(drafted), window=window, sinks=sinks, use_r=use_r, num_splits=splits, **more)
+            _check(got, z, see, torch.float32, (d, page, use_r, splits))
+
+
+def test_captured_with_new_drafts(plx):
+    """The window is shorter than some of the drafts that a captured call is replayed with."""
+    Tq, cap, window = 30, 500, 6
+    rng = np.random.default_rng(5)
+    for dtype in (torch.bfloat16, torch.float32):
+        x = _inputs(2, 8, 4, 64, Tq, cap, seed=3, dtype=dtype)
+        mask = torch.from_numpy(rows.words(np.stack([rows.random_tree(Tq, rng, reach=1) for _ in range(2)]))).to(DEV)
+        lens, drafted = _ints([500, 300]), _ints([30, 5])
+        call = lambda: plx.parallax_decode_tree(x["q"], x["r"], x["k"], x["v"], x["scale"], mask, seq_lens=lens, draft_lens=drafted,
+                                                window=window, sinks=2)
+        call()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = call()
+        for new_lens, new_drafted in (([500, 300], [30, 5]), ([31, 6], [30, 6]), ([3, 0], [7, 7]), ([400, 129], [0, 30])):
+            bits = np.stack([rows.random_tree(Tq, rng, reach=1) for _ in range(2)])
+            mask.copy_(torch.from_numpy(rows.words(bits)))
+            lens.copy_(_ints(new_lens))
+            drafted.copy_(_ints(new_drafted))
+            want = call()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want), new_lens
+            _check(out, x, [_path_sees(L, Tq, cap, bits[b], new_drafted[b], window, 2) for b, L in enumerate(new_lens)], dtype, new_lens)
