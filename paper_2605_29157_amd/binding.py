@@ -615,7 +615,8 @@ def parallax_decode_tree(q, r, k, v, scale, tree_mask, seq_lens=None, draft_lens
 
 def tree_mask_words(parents):
     """Parents [.., Tq] (integers; the parent of node t lies before it, negative: a root) -> the mask words [.., Tq,
-    ceil(Tq / 64)] (int64) of parallax_decode_tree: every node sees its ancestors and itself. Index bookkeeping only."""
+    ceil(Tq / 64)] (int64) of parallax_decode_tree: every node sees its ancestors and itself. Index bookkeeping only; with the parents
+    on the device it waits for them at every node and cannot be captured."""
     Tq = parents.shape[-1]
     sees = torch.eye(Tq, dtype=torch.bool, device=parents.device).expand(*parents.shape, Tq).clone()
     for t in range(1, Tq):

@@ -16,10 +16,10 @@
 //     faster merge 83, 160; q and rho waited for in front of the tile loop 67, 138 (since then reading two to four fragments
 //     ahead, the conflicts and s_setprio around the products make no difference). Four waves
 //     of 32 columns, which halve the reads of LDS, their steps pipelined by hand: 210 for the second (where 32 keys in one go
-//     took 188);
+//     took 188; both with q and rho waited for inside the loop, not measured since);
 //   * a tile with masks is first looked through for values of V that are not finite, and only then treated for them
 //     (48 nodes x 2 heads, window 321, 6 sequences: 31 -> 23; 16 rows x 2, window 256, 8 sequences 31 -> 21);
-//   * tiles in a ring of 128 KB of LDS, filled by direct global -> LDS loads (no registers parked), 64 - 96 KB of it on
+//   * tiles in a ring of 128 KB of LDS, filled by direct global -> LDS loads (no registers parked), 64 - 112 KB of it on
 //     their way; one barrier per tile;
 //   * the reference of the exponentials is moved only when a score exceeds it by 2^6 (then the sums are rescaled): no
 //     maximum across lanes, no rescaling of accumulators in most tiles. Sums of up to 2^6 times the number of
