@@ -339,6 +339,140 @@ typedef struct {
 plx_status parallax_cache_compact(const plx_cache_compact_args *args, void *hip_stream);
 
 /*
+ * A cache held in 4 bits. A row is K and V of one token and key head, d = 64 or 128, in parallax_q4_row_bytes(d) bytes (80, 144):
+ *     d / 2 bytes of K codes, d / 2 of V codes; byte i of either: dimension 2 i in its low half, 2 i + 1 in its high one
+ *     d / 16 scale bytes of K, d / 16 of V; zeros up to a multiple of 16 bytes
+ * A code is a sign bit over one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (e2m1); a scale byte e stands for 2^(e - 127) and serves 16
+ * dimensions, 255 makes them NaN. Written rows take the power of two that brings the largest magnitude of the 16 into [3.5, 7),
+ * e within 4 .. 252 (what is left over above saturates, below becomes 0), and round to nearest, ties to the even code; 16 dimensions
+ * of which one is infinite or NaN get e = 255. Every value of such a row is exact in bf16.
+ *   rows         [B, Hkv, capacity, row] (stride[0]: sequence, [1]: head, [2]: row), or with a block table pools
+ *                [num_pages, Hkv, page_size, row] (stride[0]: page); strides in BYTES, multiples of 16, stride[2] >= the row
+ *   block_table  [B, block_table_stride] or NULL, as in plx_decode_args; capacity <= block_table_stride * page_size
+ * The page calls take such pools as one bf16 pool (v NULL) of d = row bytes / 2.
+ */
+typedef struct {
+    void *rows;
+    int64_t stride[3];
+    const int32_t *block_table;
+    int32_t page_size, block_table_stride, num_pages;
+    int32_t B, Hkv, capacity, d;
+} plx_q4_cache;
+
+int32_t parallax_q4_row_bytes(int32_t d); /* 0: not a head dimension that such caches have */
+
+/*
+ * K and V rows to and from such a cache: row t of sequence b is its token start[b] + t, t < T.
+ *   k, v     [B, Hkv, T, d], bf16 or fp32 (dtype), element strides {sequence, head, row}, last dimension contiguous, base
+ *            and strides 16-byte aligned. Read by write, written by read (T = 0: nothing is done).
+ *   start    [B] int32 on the device, or NULL = 0
+ *   counts   [B] or NULL. write: rows from counts[b] on are passed over (a padded batch). read: of the cache's tokens, those from
+ *            counts[b] on (the sequence's length) come back as zeros.
+ * Tokens outside [0, capacity), and those whose table entry is no page, are not written and come back as zeros. The pages that are
+ * written must not be shared (parallax_cache_extend makes them so).
+ */
+typedef struct {
+    plx_q4_cache cache;
+    void *k, *v;
+    int64_t k_stride[3], v_stride[3];
+    const int32_t *start, *counts;
+    int32_t T;
+    plx_dtype dtype;
+} plx_q4_rows_args;
+
+plx_status parallax_cache_write_q4(const plx_q4_rows_args *args, void *hip_stream);
+plx_status parallax_cache_read_q4(const plx_q4_rows_args *args, void *hip_stream);
+
+/*
+ * Bounds and lists of blocks: PLX_BLOCK_KEYS keys each, block j of a sequence holds its tokens 64 j .. 64 j + 63 (the last one
+ * fewer), in whatever pages they are.
+ *
+ * parallax_cache_bounds: the smallest and the largest value of every dimension over the keys of a block.
+ *   bounds     [B, Hkv, n_blocks, 2, d] bf16, contiguous, 16-byte aligned: [.., 0, :] smallest, [.., 1, :] largest (of a block with a
+ *              NaN in a dimension one of the two is NaN)
+ *   k          a bf16 cache or pool as in plx_decode_args (element strides), d 64 or 128; or NULL: the K part of q4, whose B, Hkv,
+ *              d and capacity are then the call's
+ *   seq_lens   [B] or NULL (= capacity, which is Lmax of plx_decode_args)
+ *   from_lens  [B] or NULL: only the blocks from that of token from_lens[b] on (what a sequence held when its bounds were last
+ *              brought up to date). max_new: the most tokens that any sequence has gained since; 0 = all blocks
+ * Blocks behind seq_lens, and those in front of from_lens, are left as they were.
+ */
+#define PLX_BLOCK_KEYS 64
+typedef struct {
+    const void *k;
+    int64_t k_stride[3]; /* sequence or page, head, row */
+    const int32_t *block_table;
+    int32_t page_size, block_table_stride, num_pages;
+    int32_t B, Hkv, capacity, d;
+    const plx_q4_cache *q4; /* looked at if k is NULL; read during the call only */
+    void *bounds;
+    int32_t n_blocks, max_new;
+    const int32_t *seq_lens, *from_lens;
+} plx_cache_bounds_args;
+
+plx_status parallax_cache_bounds(const plx_cache_bounds_args *args, void *hip_stream);
+
+/*
+ * The blocks that a step reads, a list for every sequence and key head: `first` ones at the start, `recent` ones at the end, and
+ * of the others those with the highest score
+ *     score_j = max over the query rows and the heads of the group of  sum_i max(q_i lo_ji, q_i hi_ji),
+ * no less than scale^-1 times the largest score of any key in the block; of equal ones the lower number. The sums
+ * are made in 64 bits (exact for any bf16 values whose products lie within 2^37 of each other, so no order of additions shows); a
+ * block with a bound that is infinite or NaN counts as the highest, and so does a sum that is NaN.
+ *   q          [B, Hq, Tq, d] bf16 contiguous, (Hq / Hkv) * Tq <= 16; Tq 0 = 1
+ *   bounds     as above
+ *   seq_lens   [B] or NULL (= 64 * n_blocks): ceil(L_b / 64) blocks, at most n_blocks
+ *   block_list [B, Hkv, keep] int32, written: ascending, -1 behind the last (a sequence with up to `keep` blocks keeps them all)
+ *   keep       >= first + recent, >= 1
+ *   workspace  parallax_select_blocks_workspace_bytes(B, Hkv, n_blocks), 16-byte aligned
+ */
+typedef struct {
+    const void *q, *bounds;
+    const int32_t *seq_lens;
+    int32_t *block_list;
+    int32_t B, Hq, Hkv, Tq, d, n_blocks, keep, first, recent;
+    void *workspace;
+    size_t workspace_bytes;
+} plx_select_blocks_args;
+
+size_t parallax_select_blocks_workspace_bytes(int32_t B, int32_t Hkv, int32_t n_blocks);
+plx_status parallax_select_blocks(const plx_select_blocks_args *args, void *hip_stream);
+
+/*
+ * Decode over the blocks of a list. Everything as parallax_decode (one row or the last Tq positions, contiguous or paged), but that
+ * a row sees of its keys those in listed blocks only. bf16, (Hq / Hkv) * Tq <= 16, no window, prep all zero (PLX_ERR_SHAPE).
+ *   block_list  [B, Hkv, n_list] int32 on the device, ascending. An entry that is no block of the sequence (-1), or not above the one in
+ *               front of it, is passed over.
+ * What lies in other blocks reaches no output. *_call_splits: as parallax_decode_call_splits.
+ */
+typedef struct {
+    plx_decode_args decode;
+    const int32_t *block_list;
+    int32_t n_list;
+} plx_decode_blocks_args;
+
+int32_t parallax_decode_blocks_call_splits(const plx_decode_blocks_args *args);
+plx_status parallax_decode_blocks(const plx_decode_blocks_args *args, void *hip_stream);
+
+/*
+ * Decode over a cache held in 4 bits: as parallax_decode with q, r, o bf16 and the values that the rows stand for.
+ *   decode      k, v, their strides and the table fields are not looked at (the cache has its own), Lmax 0 = the cache's capacity;
+ *               dtype PLX_BF16, (Hq / Hkv) * Tq <= 16, prep all zero. Workspace and splits as parallax_decode.
+ *   sinks       as parallax_decode_sinks (window 0: none)
+ *   block_list  NULL, or as parallax_decode_blocks (then no window)
+ */
+typedef struct {
+    plx_decode_args decode;
+    plx_q4_cache cache;
+    int32_t sinks;
+    int32_t n_list;
+    const int32_t *block_list;
+} plx_decode_q4_args;
+
+int32_t parallax_decode_q4_call_splits(const plx_decode_q4_args *args);
+plx_status parallax_decode_q4(const plx_decode_q4_args *args, void *hip_stream);
+
+/*
  * Prefill forward over T query rows and Tkv keys per sequence (Algorithm 1, Sec. 3.3; forward
  * equation Sec. 3.1). Tkv = 0 means Tkv = T (the paper's square case).
  * causal != 0: the query rows are the LAST T positions of the Tkv-long sequence (a prefill

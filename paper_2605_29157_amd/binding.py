@@ -31,6 +31,9 @@ EXPORTED_SYMBOLS = (
     "parallax_prefill", "parallax_prefill_split", "parallax_prefill_workspace_bytes", "parallax_prefill_form", "parallax_prefill_backward", "parallax_prefill_backward_form",
     "parallax_prefill_backward_workspace_bytes",
     "parallax_prefill_sinks", "parallax_prefill_backward_sinks", "parallax_prefill_backward_sinks_workspace_bytes",
+    "parallax_q4_row_bytes", "parallax_cache_write_q4", "parallax_cache_read_q4", "parallax_decode_q4",
+    "parallax_decode_q4_call_splits", "parallax_cache_bounds", "parallax_select_blocks",
+    "parallax_select_blocks_workspace_bytes", "parallax_decode_blocks", "parallax_decode_blocks_call_splits",
     "parallax_cache_fork", "parallax_cache_extend", "parallax_cache_free", "parallax_cache_copy", "parallax_cache_compact",
     "parallax_block_lists", "parallax_norm_rope", "parallax_rope_table", "parallax_util_copy", "parallax_util_read",
     "parallax_util_read_grid", "parallax_util_read_sink_slots", "parallax_util_mfma", "parallax_strerror", "parallax_version",
@@ -162,6 +165,43 @@ class plx_cache_compact_args(ctypes.Structure):
                 ("max_draft", ctypes.c_int32), ("max_accepted", ctypes.c_int32)]
 
 
+class plx_q4_cache(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_void_p), ("stride", ctypes.c_int64 * 3), ("block_table", ctypes.c_void_p),
+                ("page_size", ctypes.c_int32), ("block_table_stride", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("B", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("capacity", ctypes.c_int32), ("d", ctypes.c_int32)]
+
+
+class plx_q4_rows_args(ctypes.Structure):
+    _fields_ = [("cache", plx_q4_cache), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride", ctypes.c_int64 * 3),
+                ("v_stride", ctypes.c_int64 * 3), ("start", ctypes.c_void_p), ("counts", ctypes.c_void_p),
+                ("T", ctypes.c_int32), ("dtype", ctypes.c_int)]
+
+
+class plx_cache_bounds_args(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("k_stride", ctypes.c_int64 * 3), ("block_table", ctypes.c_void_p),
+                ("page_size", ctypes.c_int32), ("block_table_stride", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("B", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("capacity", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("q4", ctypes.c_void_p), ("bounds", ctypes.c_void_p), ("n_blocks", ctypes.c_int32),
+                ("max_new", ctypes.c_int32), ("seq_lens", ctypes.c_void_p), ("from_lens", ctypes.c_void_p)]
+
+
+class plx_select_blocks_args(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("bounds", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+                ("block_list", ctypes.c_void_p), ("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("Tq", ctypes.c_int32), ("d", ctypes.c_int32), ("n_blocks", ctypes.c_int32), ("keep", ctypes.c_int32),
+                ("first", ctypes.c_int32), ("recent", ctypes.c_int32), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+class plx_decode_blocks_args(ctypes.Structure):
+    _fields_ = [("decode", plx_decode_args), ("block_list", ctypes.c_void_p), ("n_list", ctypes.c_int32)]
+
+
+class plx_decode_q4_args(ctypes.Structure):
+    _fields_ = [("decode", plx_decode_args), ("cache", plx_q4_cache), ("sinks", ctypes.c_int32), ("n_list", ctypes.c_int32),
+                ("block_list", ctypes.c_void_p)]
+
+
 class plx_norm_rope_tensor(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("gamma", ctypes.c_void_p),
                 ("H", ctypes.c_int32), ("rope", ctypes.c_int32)]
@@ -187,6 +227,12 @@ _PACK = {
     plx_page_table: struct.Struct("@5P5i0P"),
     plx_cache_pools: struct.Struct("@2P4i6qi0P"),
     plx_cache_compact_args: struct.Struct("@2P4i6qi0P6P4i0P"),
+    plx_q4_cache: struct.Struct("@P3qP7i0P"),
+    plx_q4_rows_args: struct.Struct("@P3qP7i0P2P6q2P2i0P"),
+    plx_cache_bounds_args: struct.Struct("@P3qP7i2P2i2P"),
+    plx_select_blocks_args: struct.Struct("@4P9iPN0P"),
+    plx_decode_blocks_args: struct.Struct("@6P5i6qf2iPNiP3i2iP" + _PREP + "0PPi0P"),
+    plx_decode_q4_args: struct.Struct("@6P5i6qf2iPNiP3i2iP" + _PREP + "0PP3qP7i0P2iP"),
 }
 for _args, _format in _PACK.items():
     assert _format.size == ctypes.sizeof(_args), _args
@@ -279,6 +325,18 @@ def load_library() -> ctypes.CDLL:
         lib.parallax_cache_compact.argtypes = [ctypes.POINTER(plx_cache_compact_args), ctypes.c_void_p]
         for name in ("fork", "extend", "free", "copy", "compact"):
             getattr(lib, "parallax_cache_" + name).restype = ctypes.c_int
+        lib.parallax_q4_row_bytes.argtypes = [ctypes.c_int32]
+        lib.parallax_q4_row_bytes.restype = ctypes.c_int32
+        lib.parallax_select_blocks_workspace_bytes.argtypes = [ctypes.c_int32] * 3
+        lib.parallax_select_blocks_workspace_bytes.restype = ctypes.c_size_t
+        for name, args in (("parallax_cache_write_q4", plx_q4_rows_args), ("parallax_cache_read_q4", plx_q4_rows_args),
+                           ("parallax_cache_bounds", plx_cache_bounds_args), ("parallax_select_blocks", plx_select_blocks_args),
+                           ("parallax_decode_blocks", plx_decode_blocks_args), ("parallax_decode_q4", plx_decode_q4_args)):
+            getattr(lib, name).argtypes = [ctypes.POINTER(args), ctypes.c_void_p]
+            getattr(lib, name).restype = ctypes.c_int
+        for name, args in (("parallax_decode_blocks", plx_decode_blocks_args), ("parallax_decode_q4", plx_decode_q4_args)):
+            getattr(lib, name + "_call_splits").argtypes = [ctypes.POINTER(args)]
+            getattr(lib, name + "_call_splits").restype = ctypes.c_int32
         lib.parallax_norm_rope.argtypes = [ctypes.POINTER(plx_norm_rope_args), ctypes.c_void_p]
         lib.parallax_norm_rope.restype = ctypes.c_int
         lib.parallax_rope_table.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_float,
@@ -484,12 +542,19 @@ def decode_args(q, r, k, v, out, scale, seq_lens=None, use_r=True, num_splits=0,
 
 def parallax_decode(q, r, k, v, scale, seq_lens=None, use_r=True, num_splits=0, workspace=None,
                     out=None, stream=None, block_table=None, max_len=None, split_counters=None,
-                    window=0, prep=None, sinks=0):
+                    window=0, prep=None, sinks=0, block_list=None):
     """Single-step Parallax decode. Allocates `out` / `workspace` with torch when not given
     (allocation only; all arithmetic is in the library). With `split_counters` (zeroed int32
     device tensor, >= B * Hkv entries) the call goes to parallax_decode_fused: one launch, the
     last split of every group to arrive merges inside the kernel. With `sinks` > 0 the first tokens stay visible
-    behind the sliding window (parallax_decode_sinks; no split_counters, no prep)."""
+    behind the sliding window (parallax_decode_sinks; no split_counters, no prep). With `block_list` (int32 [B, Hkv, n],
+    parallax_select_blocks makes one) only the keys in the listed blocks of 64 are seen (parallax_decode_blocks, bf16; neither
+    window nor the others)."""
+    if block_list is not None:
+        if split_counters is not None or prep is not None or sinks:
+            raise ValueError("a block_list goes with neither split_counters, prep nor sinks")
+        return _decode_rows(q, r, k, v, scale, seq_lens, use_r, num_splits, workspace, out, stream, block_table,
+                            max_len, window, 0, block_list=block_list)
     if sinks:
         if split_counters is not None or prep is not None:
             raise ValueError("sinks go with neither split_counters nor prep")
@@ -536,11 +601,13 @@ def parallax_decode(q, r, k, v, scale, seq_lens=None, use_r=True, num_splits=0, 
 
 
 def _decode_rows(q, r, k, v, scale, seq_lens, use_r, num_splits, workspace, out, stream, block_table, max_len, window,
-                 sinks, tree_mask=None, draft_lens=None):
-    """parallax_decode_sinks, or parallax_decode_tree with a tree_mask."""
+                 sinks, tree_mask=None, draft_lens=None, block_list=None):
+    """parallax_decode_sinks, parallax_decode_tree with a tree_mask, or parallax_decode_blocks with a block_list."""
     # (a step of one sequence is bound by the host: each property of a tensor is asked for once)
     where = "parallax_decode_sinks" if tree_mask is None else "parallax_decode_tree"
-    _on_current_device(where, q, r, k, v, out, seq_lens, block_table, tree_mask, draft_lens, workspace)
+    if block_list is not None:
+        where = "parallax_decode_blocks"
+    _on_current_device(where, q, r, k, v, out, seq_lens, block_table, tree_mask, draft_lens, workspace, block_list)
     shape, cache, dtype = q.shape, k.shape, q.dtype
     if len(shape) not in (3, 4) or len(cache) != 4 or v.shape != cache or cache[3] != shape[-1]:
         raise ValueError("q [B, Hq, (Tq,) d], k and v of one shape [.., Hkv, .., d]")
@@ -571,7 +638,13 @@ def _decode_rows(q, r, k, v, scale, seq_lens, use_r, num_splits, workspace, out,
         out = _result_maker(stream, torch.empty_like)(q)
     a = decode_args(q, r, k, v, out, scale, seq_lens, use_r, num_splits, workspace, block_table, max_len, window)
     lib = load_library()
-    if tree_mask is None:
+    if block_list is not None:
+        n_list = _list_length(where, block_list, B, cache[1])
+        blocks = plx_decode_blocks_args()
+        blocks.decode, blocks.block_list, blocks.n_list = a, block_list.data_ptr(), n_list
+        a = blocks.decode  # (the copy inside)
+        splits, call, head = lib.parallax_decode_blocks_call_splits, lib.parallax_decode_blocks, (ctypes.byref(blocks),)
+    elif tree_mask is None:
         splits, call, head = lib.parallax_decode_sinks_call_splits, lib.parallax_decode_sinks, (ctypes.byref(a), sinks)
     else:
         words = -(-Tq // 64)
@@ -628,6 +701,205 @@ def tree_mask_words(parents):
     words = -(-Tq // 64)
     sees = torch.nn.functional.pad(sees, (0, 64 * words - Tq)).reshape(*parents.shape, words, 64)
     return (sees.long() << torch.arange(64, device=parents.device)).sum(-1)
+
+
+def _list_length(where, block_list, B, Hkv):
+    if block_list.dtype != torch.int32 or not block_list.is_contiguous():
+        raise TypeError("%s: block_list must be a contiguous int32 tensor" % where)
+    shape = block_list.shape
+    if len(shape) != 3 or shape[0] != B or shape[1] != Hkv or shape[2] < 1:
+        raise ValueError("%s: block_list [B, Hkv, n]" % where)
+    return shape[2]
+
+
+_Q4_DIMS = {144: 128, 80: 64}  # bytes of a row: its head dimension
+
+
+def parallax_q4_row_bytes(d) -> int:
+    """Bytes of a 4-bit row of K and V of one token and key head (0: not a head dimension that such caches have). A cache is a
+    uint8 tensor [B, Hkv, capacity, row bytes], or with a block table pools [num_pages, Hkv, page_size, row bytes]; the header
+    has the row."""
+    return int(load_library().parallax_q4_row_bytes(_i32(d)))
+
+
+def _table_fields(where, block_table, rows, pages, B):
+    """(block_table, page_size, block_table_stride, num_pages) of a call over B sequences, and their capacity."""
+    if block_table is None:
+        if pages != B:
+            raise ValueError("%s: a cache has one slot per sequence" % where)
+        return (0, 0, 0, 0), rows
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.stride(1) != 1:
+        raise TypeError("%s: block_table must be an int32 device tensor [B, pages per sequence]" % where)
+    if block_table.shape[0] != B:
+        raise ValueError("%s: block_table needs one row per sequence" % where)
+    width = block_table.shape[1]
+    return (block_table.data_ptr(), rows, block_table.stride(0) if B > 1 else width, pages), min(width * rows, 0x7fffffff)
+
+
+def _lens(where, name, t, B):
+    if t is None:
+        return 0
+    if t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous():
+        raise TypeError("%s: %s must be a contiguous int32 tensor [B]" % (where, name))
+    return t.data_ptr()
+
+
+def _q4_fields(where, cache, block_table, B, d=None, max_len=None):
+    """The fields of a plx_q4_cache."""
+    shape = cache.shape
+    if cache.dtype != torch.uint8 or len(shape) != 4 or cache.stride(3) != 1 or shape[3] not in _Q4_DIMS:
+        raise TypeError("%s: a 4-bit cache is a uint8 tensor [.., Hkv, .., row bytes], contiguous in the last dimension" % where)
+    if d is not None and _Q4_DIMS[shape[3]] != d:
+        raise ValueError("%s: the cache has rows of d = %d" % (where, _Q4_DIMS[shape[3]]))
+    table, capacity = _table_fields(where, block_table, shape[2], shape[0], B)
+    if max_len is not None:
+        capacity = min(_i32(max_len), capacity)
+    return (cache.data_ptr(), *cache.stride()[:3], *table, B, shape[1], capacity, _Q4_DIMS[shape[3]])
+
+
+def _q4_rows(where, call, cache, k, v, start, counts, block_table, stream):
+    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or k.stride(3) != 1 or v.stride(3) != 1:
+        raise ValueError("%s: k and v [B, Hkv, T, d] of one dtype, contiguous in the last dimension" % where)
+    B, Hkv, T, d = k.shape
+    if cache.dim() != 4 or cache.shape[1] != Hkv:
+        raise ValueError("%s: the cache has as many heads as k and v" % where)
+    a = _filled(plx_q4_rows_args, *_q4_fields(where, cache, block_table, B, d), k.data_ptr(), v.data_ptr(), *k.stride()[:3],
+                *v.stride()[:3], _lens(where, "start", start, B), _lens(where, "counts", counts, B), T, _dtype_code(k))
+    if T == 0:
+        return
+    st = call(ctypes.byref(a), _launch_stream(where, stream))
+    if st != PLX_OK:
+        raise ParallaxError(st, where)
+
+
+def parallax_cache_write_q4(k, v, cache, start=None, counts=None, block_table=None, stream=None):
+    """Rows of K and V [B, Hkv, T, d] (bf16 or fp32) into a 4-bit cache: row t of sequence b becomes its token start[b] + t
+    (default 0); rows from counts[b] on are passed over. Tokens outside the cache, and those without a page, are not written."""
+    where = "parallax_cache_write_q4"
+    _on_current_device(where, k, v, cache, start, counts, block_table)
+    _q4_rows(where, load_library().parallax_cache_write_q4, cache, k, v, start, counts, block_table, stream)
+
+
+def parallax_cache_read_q4(cache, d, T, start=None, seq_lens=None, dtype=torch.bfloat16, block_table=None, out=None,
+                           stream=None):
+    """The values that T tokens of every sequence stand for, from start[b] (default 0) on, as k, v [B, Hkv, T, d] in `dtype` (bf16: exact):
+    what parallax_prefill takes as the keys in front of the next chunk. Tokens from seq_lens[b] on, outside the cache or without a page:
+    zeros. out: (k, v) to write."""
+    where = "parallax_cache_read_q4"
+    _on_current_device(where, cache, start, seq_lens, block_table, *(out or ()))
+    B = cache.shape[0] if block_table is None else block_table.shape[0]
+    if out is None:
+        make = _result_maker(stream, torch.empty)
+        out = [make((B, cache.shape[1], T, d), dtype=dtype, device=cache.device) for _ in range(2)]
+    k, v = out
+    if tuple(k.shape) != (B, cache.shape[1], T, d) or any(s == 0 and n > 1 for t in (k, v) for s, n in zip(t.stride(), t.shape)):
+        raise ValueError("%s: out is (k, v), each [B, Hkv, T, d] with a place for every value" % where)
+    _q4_rows(where, load_library().parallax_cache_read_q4, cache, k, v, start, seq_lens, block_table, stream)
+    return k, v
+
+
+def parallax_decode_q4(q, r, cache, scale, seq_lens=None, use_r=True, num_splits=0, workspace=None, out=None, stream=None,
+                       block_table=None, max_len=None, window=0, sinks=0, block_list=None):
+    """parallax_decode over a cache held in 4 bits: q, r [B, Hq, (Tq,) d] bf16, at most 16 rows x heads of a group; window and
+    sinks as parallax_decode, or a block_list."""
+    where = "parallax_decode_q4"
+    _on_current_device(where, q, r, cache, out, seq_lens, block_table, block_list, workspace)
+    shape = q.shape
+    if len(shape) not in (3, 4):
+        raise ValueError("q [B, Hq, (Tq,) d]")
+    if use_r and r is None:
+        raise ValueError("r is needed unless use_r=False")
+    for t in (q, r, out):
+        if t is not None and (t.shape != shape or t.dtype != torch.bfloat16 or not t.is_contiguous()):
+            raise ValueError("q, r and out are contiguous bf16 tensors of one shape")
+    B, Hq, d = shape[0], shape[1], shape[-1]
+    Tq = shape[2] if len(shape) == 4 else 1
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    fields = _q4_fields(where, cache, block_table, B, d, max_len)
+    Hkv = fields[9]
+    n_list = 0 if block_list is None else _list_length(where, block_list, B, Hkv)
+    if out is None:
+        out = _result_maker(stream, torch.empty_like)(q)
+    # (in one go: see _PACK)
+    a = _filled(plx_decode_q4_args, q.data_ptr(), _ptr(r), 0, 0, out.data_ptr(), _lens(where, "seq_lens", seq_lens, B), B, Hq, Hkv,
+                fields[10], d, 0, 0, 0, 0, 0, 0, _f32(scale), 1 if use_r else 0, _i32(num_splits), _ptr(workspace),
+                0 if workspace is None else _bytes(workspace), PLX_BF16, 0, 0, 0, 0, Tq, _i32(window), 0, *_NO_PREP,
+                *fields, _i32(sinks), n_list, _ptr(block_list))
+    lib = load_library()
+    if workspace is None and num_splits != 1:
+        S = lib.parallax_decode_q4_call_splits(ctypes.byref(a))  # (0: refused below)
+        if S > 1:
+            workspace = _scratch(stream, B * Hq * Tq * S * (2 * d + 4), q.device)
+            a.decode.workspace, a.decode.workspace_bytes = workspace.data_ptr(), _bytes(workspace)
+    st = lib.parallax_decode_q4(ctypes.byref(a), _launch_stream(where, stream))
+    if st != PLX_OK:
+        raise ParallaxError(st, where)
+    return out
+
+
+def parallax_cache_bounds(k, bounds, seq_lens=None, from_lens=None, max_new=0, block_table=None, stream=None):
+    """The smallest and largest key of every block of 64 tokens, by dimension, into bounds [B, Hkv, n_blocks, 2, d] (bf16), which is
+    returned. k: the bf16 keys [B, Hkv, capacity, d] or pools of a block_table, or a 4-bit cache. from_lens: what the sequences held
+    when their bounds were last brought up to date; only blocks from there on are looked at. max_new: no sequence has gained more
+    tokens since (0: not known)."""
+    where = "parallax_cache_bounds"
+    _on_current_device(where, k, bounds, seq_lens, from_lens, block_table)
+    if k.dim() != 4 or bounds.dim() != 5:
+        raise ValueError("%s: keys [.., Hkv, .., d], bounds [B, Hkv, n_blocks, 2, d]" % where)
+    B, Hkv, n_blocks, two, d = bounds.shape
+    if bounds.dtype != torch.bfloat16 or not bounds.is_contiguous() or two != 2 or k.shape[1] != Hkv:
+        raise ValueError("%s: bounds is a contiguous bf16 tensor [B, Hkv, n_blocks, 2, d]" % where)
+    most = min(64 * n_blocks, 0x7fffffff)
+    if block_table is None and k.shape[2] > most:
+        raise ValueError("%s: bounds for %d blocks are too few for %d tokens" % (where, n_blocks, k.shape[2]))
+    lens = _lens(where, "seq_lens", seq_lens, B), _lens(where, "from_lens", from_lens, B)
+    tail = (bounds.data_ptr(), n_blocks, _i32(max_new), *lens)
+    if k.dtype == torch.uint8:
+        cache = _filled(plx_q4_cache, *_q4_fields(where, k, block_table, B, d, most))
+        a = _filled(plx_cache_bounds_args, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, ctypes.addressof(cache), *tail)
+    else:
+        if k.dtype != torch.bfloat16 or k.stride(3) != 1 or k.shape[3] != d:
+            raise TypeError("%s: keys are bf16 [.., Hkv, .., d], contiguous in the last dimension, or a 4-bit cache" % where)
+        table, capacity = _table_fields(where, block_table, k.shape[2], k.shape[0], B)
+        a = _filled(plx_cache_bounds_args, k.data_ptr(), *k.stride()[:3], *table, B, Hkv, min(capacity, most), d, 0, *tail)
+    st = load_library().parallax_cache_bounds(ctypes.byref(a), _launch_stream(where, stream))
+    if st != PLX_OK:
+        raise ParallaxError(st, where)
+    return bounds
+
+
+def parallax_select_blocks(q, bounds, seq_lens, keep, first=1, recent=2, out=None, workspace=None, stream=None):
+    """The blocks that a step with queries q [B, Hq, (Tq,) d] reads: int32 [B, Hkv, keep], ascending, -1 behind the last: the
+    `first` ones, the `recent` last ones, and of the others those with the highest bound on a product with one of the queries
+    (of the rows and heads that share a key head; of equal ones the lower number)."""
+    where = "parallax_select_blocks"
+    _on_current_device(where, q, bounds, seq_lens, out, workspace)
+    shape = q.shape
+    if len(shape) not in (3, 4) or q.dtype != torch.bfloat16 or not q.is_contiguous():
+        raise ValueError("%s: q is a contiguous bf16 tensor [B, Hq, (Tq,) d]" % where)
+    B, Hq, d = shape[0], shape[1], shape[-1]
+    Tq = shape[2] if len(shape) == 4 else 1
+    if bounds.dim() != 5 or bounds.dtype != torch.bfloat16 or not bounds.is_contiguous() or bounds.shape[0] != B or (
+            tuple(bounds.shape[3:]) != (2, d)):
+        raise ValueError("%s: bounds is a contiguous bf16 tensor [B, Hkv, n_blocks, 2, d]" % where)
+    _, Hkv, n_blocks, _, _ = bounds.shape
+    lens, keep = _lens(where, "seq_lens", seq_lens, B), _i32(keep)
+    if out is None:
+        out = _result_maker(stream, torch.empty)((B, Hkv, max(keep, 0)), dtype=torch.int32, device=q.device)
+    elif _list_length(where, out, B, Hkv) != keep:
+        raise ValueError("%s: out [B, Hkv, keep]" % where)
+    lib = load_library()
+    if workspace is None:
+        workspace = _scratch(stream, lib.parallax_select_blocks_workspace_bytes(B, Hkv, n_blocks) // 4, q.device)
+    elif not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    a = _filled(plx_select_blocks_args, q.data_ptr(), bounds.data_ptr(), lens, out.data_ptr(), B, Hq, Hkv, Tq, d, n_blocks, keep,
+                _i32(first), _i32(recent), workspace.data_ptr(), _bytes(workspace))
+    st = lib.parallax_select_blocks(ctypes.byref(a), _launch_stream(where, stream))
+    if st != PLX_OK:
+        raise ParallaxError(st, where)
+    return out
 
 
 def parallax_decode_static_scratch_bytes() -> int:
@@ -1032,7 +1304,10 @@ class PageTable:
 
 
 def _pools(where, k, v):
-    """The fields of a plx_cache_pools: [pages, heads, rows, d], or [pages, rows, d] for one head."""
+    """The fields of a plx_cache_pools: [pages, heads, rows, d], or [pages, rows, d] for one head; pools of 4-bit rows (uint8, no v)
+    as pools of bf16 rows of half as many numbers."""
+    if k.dtype == torch.uint8 and v is None:
+        k = k.view(torch.bfloat16)
     if k.dim() == 3:
         k = k.unsqueeze(1)
     _on_current_device(where, k, v)

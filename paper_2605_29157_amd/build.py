@@ -12,8 +12,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB_PATH = os.path.join(PKG, "libparallax_hip.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 
-SOURCES = ["parallax_api.hip", "decode_bf16.hip", "decode_rows_bf16.hip", "decode_rows_wide_bf16.hip", "decode_mla_bf16.hip", "decode_mla_wide_bf16.hip", "prefill_bf16.hip", "prefill_bwd_bf16.hip",
-           "generic_f32.hip", "prefill_f32.hip", "block_lists.hip", "cache_pages.hip", "norm_rope.hip", "util_kernels.hip"]
+SOURCES = ["parallax_api.hip", "decode_bf16.hip", "decode_rows_bf16.hip", "decode_rows_wide_bf16.hip", "decode_q4_bf16.hip", "decode_mla_bf16.hip", "decode_mla_wide_bf16.hip", "prefill_bf16.hip", "prefill_bwd_bf16.hip",
+           "generic_f32.hip", "prefill_f32.hip", "block_lists.hip", "cache_pages.hip", "cache_q4.hip", "block_select.hip", "norm_rope.hip", "util_kernels.hip"]
 
 # packed-fp32 instructions are disabled for all device code (hipcc's host pass prints a
 # harmless "not a recognized feature" note for the flag)
@@ -98,6 +98,9 @@ def _check_decode_assembly() -> None:
         bad = {n: c for n, c in _spills(src, "decode_rows").items() if c > 0}
         if bad:
             raise RuntimeError("%s: register spills in a decode kernel (%s)" % (src, bad))
+    bad = {n: c for n, c in _spills("decode_q4_bf16.hip", "decode_q4").items() if c > 0}
+    if bad:
+        raise RuntimeError("decode_q4_bf16.hip: register spills in a decode kernel (%s)" % bad)
 
 
 def _check_no_load_waits(src: str, kernel: str) -> None:

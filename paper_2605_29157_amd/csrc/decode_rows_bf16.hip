@@ -1,6 +1,6 @@
 // Split-KV Parallax decode for several rows whose key sets differ, bf16, gfx950: drafted nodes that see the cache and
-// their own ancestors (tree masks), and rows with a sliding window and a few first tokens that stay visible (sinks). Here:
-// up to 16 columns (rows x heads of a GQA group); decode_rows_wide_bf16.hip has the kernel for more.
+// their own ancestors (tree masks), rows with a sliding window and a few first tokens that stay visible (sinks), and rows that
+// see the blocks of a list only. Here: up to 16 columns (rows x heads of a GQA group); decode_rows_wide_bf16.hip has the kernel for more.
 //
 // What it computes: the forward of the paper (Sec. 3.1, Algorithm 1) over the key set J of each row,
 //     p = softmax_J(scale q.k),  u = rho.k,  o = sum_J p (1 + sum_J p u - u) v,   empty J: zeros,
@@ -12,7 +12,8 @@
 // Layout. As decode_bf16.hip: four waves, each with its own 32-key tiles (no barrier in the loop), K and V rows parked in
 // registers one tile ahead and staged through the wave's own LDS tile, S^T = K [Q; R]^T on 16x16x32 MFMAs with the
 // columns as MFMA columns, P kept in its lane; two workgroups per compute unit. What differs:
-//   * the tiles walked are those of the sinks, then those from the first key any window reaches (RowsScope);
+//   * the tiles walked are those of the sinks, then those from the first key any window reaches (RowsScope), or those of the
+//     list's blocks: a wave looks the entries of its next 32 tiles up at once, like the pages, and goes past those that are none;
 //   * tiles that every column sees completely take no masks. In the others a key that a column does not see must
 //     not reach it whatever its row holds (unwritten rows, freed pages): scores are selected, not multiplied, and
 //     values that are not finite are taken out of the V tile and reach the columns that do see their key
@@ -26,7 +27,7 @@ constexpr int kRowsTile = 32;  // keys per wave tile
 constexpr int kRowsWaves = 4;
 }  // namespace
 
-template <int D, bool USE_R, int CACHE, bool TREE>
+template <int D, bool USE_R, int CACHE, bool TREE, bool LIST = false>
 __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P) {
     const DecodeParams &p = P.d;
     constexpr int CPR = D / 8;            // 16-byte chunks per K/V row
@@ -43,7 +44,7 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
     const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
     const int G = p.G, S = p.S, Tq = p.Tq, n_cols = G * Tq;
 
-    const RowsScope<TREE, kRowsTile> scope(P, b, 0, 16);
+    const RowsScope<TREE, kRowsTile, LIST> scope(P, b, 0, 16, hk);
     const int Lb = scope.Lb;
     // (splits in whole rounds of the four waves)
     const int per = ((scope.n_virtual + S - 1) / S + kRowsWaves - 1) / kRowsWaves * kRowsWaves;
@@ -77,20 +78,38 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
     const RowsPages pages(p, b);
     const int last16 = max(Lb - 1, 0) & ~15;  // first key of the last half tile that exists
     // kRowsPagedRuns: offsets of the halves of this wave's next 32 tiles, lane 2 * j + half
-    int run_k[2] = {0, 0}, run_v[2] = {0, 0}, run_slot = 0;
+    constexpr bool RUNS = CACHE == kRowsPagedRuns || LIST;
+    int run_k[2] = {0, 0}, run_v[2] = {0, 0}, run_slot = LIST ? 64 : 0, run_key = 0;  // LIST: and the keys
     auto lookup_runs = [&](int v) {
         const int ahead = min(v + (lane >> 1) * kRowsWaves, max(scope.n_virtual - 1, 0));
         int64_t ko, vo;
-        pages.offsets(min(scope.key_of(ahead) + 16 * (lane & 1), last16), ko, vo);
+        int key = scope.key_of(ahead);
+        if constexpr (LIST) run_key = key, key = max(key, 0);
+        key = min(key + 16 * (lane & 1), last16);
+        if constexpr (CACHE == kRowsContiguous)
+            ko = (int64_t)key * p.ksl, vo = (int64_t)key * p.vsl;
+        else if constexpr (CACHE == kRowsPagedRuns)
+            pages.offsets(key, ko, vo);
+        else
+            ko = vo = 0;
         run_k[0] = (int)ko, run_k[1] = (int)(ko >> 32);
         run_v[0] = (int)vo, run_v[1] = (int)(vo >> 32);
         run_slot = 0;
     };
     const uint32_t k_row_bytes = (uint32_t)p.ksl * 2u, v_row_bytes = (uint32_t)p.vsl * 2u;
+    int list_key = 0;  // LIST: of the tile that is loaded next
+    auto list_tile = [&](int &v) {  // LIST: the first tile at or behind number v that there is
+        for (; v < v_hi; v += kRowsWaves) {
+            if (run_slot == 64) lookup_runs(v);  // (uniform)
+            list_key = __builtin_amdgcn_readlane(run_key, run_slot);
+            if (list_key >= 0) break;
+            run_slot += 2;
+        }
+    };
     auto issue_loads = [&](int v) {
-        const int tk0 = scope.key_of(v);
+        const int tk0 = LIST ? list_key : scope.key_of(v);
         if constexpr (CACHE != kRowsAny) {
-            if constexpr (CACHE == kRowsPagedRuns)
+            if constexpr (CACHE == kRowsPagedRuns && !LIST)
                 if (run_slot == 64) lookup_runs(v);  // (uniform)
             int l = lane;
             asm volatile("" : "+v"(l));  // (the lane's offsets are worked out here: kept across the loop they would be spilled)
@@ -98,7 +117,7 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
             for (int hf = 0; hf < 2; ++hf) {
                 const int key0 = __builtin_amdgcn_readfirstlane(min(tk0 + 16 * hf, last16));
                 int64_t ko = (int64_t)key0 * p.ksl, vo = (int64_t)key0 * p.vsl;
-                if constexpr (CACHE == kRowsPagedRuns) {
+                if constexpr (RUNS) {
                     auto pick = [&](const int(&x)[2]) {
                         return ((int64_t)__builtin_amdgcn_readlane(x[1], run_slot + hf) << 32) |
                                (uint32_t)__builtin_amdgcn_readlane(x[0], run_slot + hf);
@@ -124,6 +143,7 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
                 kst[i] = *(const u32x4 *)(kbase + ko + ld_chunk * 8);
                 vst[i] = *(const u32x4 *)(vbase + vo + ld_chunk * 8);
             }
+            if constexpr (LIST) run_slot += 2;
         }
     };
 
@@ -150,12 +170,14 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
     };
 
     int v = v_lo + w;
+    if constexpr (LIST) list_tile(v);
     if (v < v_hi) {
-        if constexpr (CACHE == kRowsPagedRuns) lookup_runs(v);
+        if constexpr (CACHE == kRowsPagedRuns && !LIST) lookup_runs(v);
         issue_loads(v);
     }
-    for (; v < v_hi; v += kRowsWaves) {
-        const int tk = __builtin_amdgcn_readfirstlane(scope.key_of(v));
+    for (int v_next; v < v_hi; v = v_next) {
+        const int tk = LIST ? list_key : __builtin_amdgcn_readfirstlane(scope.key_of(v));
+        v_next = v + kRowsWaves;
         const bool whole = scope.whole(tk, kRowsTile);  // (uniform) every column sees all of the keys
         bool any_bad = false;
         if (!whole) {
@@ -174,7 +196,8 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
             ldsK[slot] = kst[i];
             ldsV[slot] = vst[i];
         }
-        if (v + kRowsWaves < v_hi) issue_loads(v + kRowsWaves);
+        if constexpr (LIST) list_tile(v_next);
+        if (v_next < v_hi) issue_loads(v_next);
         wave_lds_fence();
         uint32_t seen = 0xffu;
         if (!whole) {
@@ -362,7 +385,9 @@ int decode_rows_tile(int columns) { return columns == 64 ? 128 : 64; }
 template <int D, bool USE_R, int CACHE>
 static void launch_rows_form(const DecodeRowsParams &P, hipStream_t stream) {
     const dim3 grid(P.d.S, P.d.Hkv, P.d.B);
-    if (P.mask != nullptr)
+    if (P.block_list != nullptr)
+        hipLaunchKernelGGL((decode_rows_kernel<D, USE_R, CACHE, false, true>), grid, dim3(256), 0, stream, P);
+    else if (P.mask != nullptr)
         hipLaunchKernelGGL((decode_rows_kernel<D, USE_R, CACHE, true>), grid, dim3(256), 0, stream, P);
     else
         hipLaunchKernelGGL((decode_rows_kernel<D, USE_R, CACHE, false>), grid, dim3(256), 0, stream, P);

@@ -528,6 +528,234 @@ plx_status parallax_decode_tree(const plx_decode_tree_args *a, void *hip_stream)
 
 namespace {
 
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+static_assert(PLX_BLOCK_KEYS == plx::kListBlock, "keys of a block");
+
+plx_status take_q4_cache(const plx_q4_cache &a, plx::Q4Cache *out) {
+    if (!a.rows) return PLX_ERR_NULL;
+    const int32_t row = parallax_q4_row_bytes(a.d);
+    if (a.B < 1 || a.Hkv < 1 || a.B > 65535 || a.Hkv > 65535 || a.capacity < 1 || row == 0) return PLX_ERR_SHAPE;
+    if (!aligned16(a.rows) || !aligned4(a.block_table)) return PLX_ERR_ALIGN;
+    for (int64_t s : a.stride) {
+        if (s < 0) return PLX_ERR_SHAPE;
+        if (s % 16 != 0) return PLX_ERR_ALIGN;
+    }
+    if (a.stride[2] < row) return PLX_ERR_SHAPE;
+    plx::Q4Cache c{};
+    c.rows = static_cast<char *>(a.rows);
+    for (int i = 0; i < 3; ++i) c.stride[i] = a.stride[i];
+    c.B = a.B, c.Hkv = a.Hkv, c.capacity = a.capacity, c.d = a.d;
+    if (a.block_table) {
+        if (a.page_size < 1 || a.num_pages < 1 || a.block_table_stride < 1) return PLX_ERR_SHAPE;
+        if ((int64_t)a.block_table_stride * a.page_size < a.capacity) return PLX_ERR_SHAPE;
+        c.block_table = a.block_table, c.table_stride = a.block_table_stride;
+        c.page_size = a.page_size, c.num_pages = a.num_pages;
+    }
+    *out = c;
+    return PLX_OK;
+}
+
+// What both decode calls over lists and 4-bit rows have: up to 16 columns, rows prepared beforehand, a list or none
+plx_status take_block_list(const plx_decode_args *a, const int32_t *list, int32_t n_list, plx::DecodeRowsParams *p) {
+    if (a->dtype != PLX_BF16) return PLX_ERR_DTYPE;
+    if (p->d.prep.gamma_q != nullptr || p->d.G * p->d.Tq > 16) return PLX_ERR_SHAPE;
+    if (!list) return PLX_OK;
+    if (!aligned4(list)) return PLX_ERR_ALIGN;
+    if (n_list < 1 || n_list > (1 << 29) || a->window != 0) return PLX_ERR_SHAPE;
+    p->block_list = list, p->n_list = n_list;
+    return PLX_OK;
+}
+
+plx_status prepare_decode_blocks(const plx_decode_blocks_args *a, bool need_out, plx::DecodeRowsParams *out) {
+    if (!a || !a->block_list) return PLX_ERR_NULL;
+    plx::DecodeRowsParams p{};
+    plx_status st = prepare_decode(&a->decode, true, need_out, &p.d);
+    if (st == PLX_OK) st = take_block_list(&a->decode, a->block_list, a->n_list, &p);
+    if (st == PLX_OK) *out = p;
+    return st;
+}
+
+plx_status prepare_decode_q4(const plx_decode_q4_args *a, bool need_out, plx::DecodeRowsParams *out) {
+    if (!a) return PLX_ERR_NULL;
+    plx::Q4Cache c{};
+    plx_status st = take_q4_cache(a->cache, &c);
+    if (st != PLX_OK) return st;
+    plx_decode_args d = a->decode;
+    if (d.Lmax == 0) d.Lmax = c.capacity;
+    if (d.B != c.B || d.Hkv != c.Hkv || d.d != c.d || d.Lmax > c.capacity) return PLX_ERR_SHAPE;
+    // (the cache describes its rows itself: something valid in their place)
+    d.k = d.v = c.rows, d.block_table = nullptr;
+    d.k_stride_b = d.k_stride_h = d.v_stride_b = d.v_stride_h = 0, d.k_stride_l = d.v_stride_l = d.d;
+    plx::DecodeRowsParams p{};
+    st = prepare_decode(&d, true, need_out, &p.d);
+    if (st == PLX_OK) st = take_block_list(&d, a->block_list, a->n_list, &p);
+    if (st != PLX_OK) return st;
+    if (a->sinks < 0 || (a->sinks > 0 && d.window == 0)) return PLX_ERR_SHAPE;
+    p.d.window = std::min(d.window, d.Lmax), p.sinks = std::min(a->sinks, d.Lmax);
+    p.d.k = p.d.v = c.rows;
+    p.d.ksb = c.stride[0], p.d.ksh = c.stride[1], p.d.ksl = c.stride[2];
+    p.d.block_table = c.block_table, p.d.table_stride = (int32_t)c.table_stride, p.d.page_size = c.page_size, p.d.num_pages = c.num_pages;
+    *out = p;
+    return PLX_OK;
+}
+
+// Keys that a call over 4-bit rows or lists reads of a sequence
+int32_t keys_of_lists(const plx::DecodeRowsParams &p) {
+    if (p.block_list) return (int32_t)std::min<int64_t>((int64_t)p.n_list * PLX_BLOCK_KEYS, p.d.Lmax);
+    const int64_t in_window = (int64_t)p.d.window + p.d.Tq - 1 + p.sinks;
+    return p.d.window > 0 && in_window < p.d.Lmax ? (int32_t)in_window : p.d.Lmax;
+}
+
+int32_t pick_splits_lists(const plx_decode_args *a, const plx::DecodeRowsParams &p) {
+    if (a->num_splits > 0) return a->num_splits;
+    const int32_t keys = keys_of_lists(p);
+    const int64_t pairs = (int64_t)p.d.B * p.d.Hkv, cus = query_num_cus();
+    const int32_t block_tiles = (keys + plx::kDecodeBlockKeys - 1) / plx::kDecodeBlockKeys;
+    int32_t s = parallax_decode_num_splits(p.d.B, p.d.Hq, p.d.Hkv, keys, p.d.d, 0);
+    while (s > 1 && 2 * pairs * s <= cus && 2 * s <= std::min(block_tiles, PLX_MAX_SPLITS)) s *= 2;
+    return s;
+}
+
+plx_status decode_lists(const plx_decode_args *a, plx::DecodeRowsParams &p, bool q4, void *hip_stream) {
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const int32_t S = pick_splits_lists(a, p);
+    p.d.S = S, p.d.direct_out = S == 1;
+    if (S > 1) {
+        const plx_status st = attach_workspace(a, S, &p.d);
+        if (st != PLX_OK) return st;
+    }
+    if ((q4 ? plx::launch_decode_q4(p, stream) : plx::launch_decode_rows_bf16(p, stream)) != hipSuccess) return PLX_ERR_LAUNCH;
+    if (S > 1 && plx::launch_decode_rows_combine(p.d, stream) != hipSuccess) return PLX_ERR_LAUNCH;
+    return PLX_OK;
+}
+
+}  // namespace
+
+int32_t parallax_decode_blocks_call_splits(const plx_decode_blocks_args *a) {
+    plx::DecodeRowsParams p{};
+    return prepare_decode_blocks(a, false, &p) == PLX_OK ? pick_splits_lists(&a->decode, p) : 0;
+}
+
+plx_status parallax_decode_blocks(const plx_decode_blocks_args *a, void *hip_stream) {
+    plx::DecodeRowsParams p{};
+    const plx_status st = prepare_decode_blocks(a, true, &p);
+    return st == PLX_OK ? decode_lists(&a->decode, p, false, hip_stream) : st;
+}
+
+int32_t parallax_decode_q4_call_splits(const plx_decode_q4_args *a) {
+    plx::DecodeRowsParams p{};
+    return prepare_decode_q4(a, false, &p) == PLX_OK ? pick_splits_lists(&a->decode, p) : 0;
+}
+
+plx_status parallax_decode_q4(const plx_decode_q4_args *a, void *hip_stream) {
+    plx::DecodeRowsParams p{};
+    const plx_status st = prepare_decode_q4(a, true, &p);
+    return st == PLX_OK ? decode_lists(&a->decode, p, true, hip_stream) : st;
+}
+
+int32_t parallax_q4_row_bytes(int32_t d) { return d == 64 || d == 128 ? (d + d / 8 + 15) / 16 * 16 : 0; }
+
+namespace {
+
+plx_status take_q4_rows(const plx_q4_rows_args *a, plx::Q4Rows *out) {
+    if (!a || !a->k || !a->v) return PLX_ERR_NULL;
+    if (a->dtype != PLX_BF16 && a->dtype != PLX_F32) return PLX_ERR_DTYPE;
+    plx::Q4Rows p{};
+    const plx_status st = take_q4_cache(a->cache, &p.cache);
+    if (st != PLX_OK) return st;
+    if (a->T < 0 || (int64_t)a->cache.B * a->cache.Hkv * a->T > 0x7fffffffLL) return PLX_ERR_SHAPE;
+    if (!aligned16(a->k) || !aligned16(a->v) || !aligned4(a->start) || !aligned4(a->counts)) return PLX_ERR_ALIGN;
+    for (int i = 0; i < 3; ++i) {
+        if (a->k_stride[i] < 0 || a->v_stride[i] < 0) return PLX_ERR_SHAPE;
+        if (!stride_aligned(a->k_stride[i], a->dtype) || !stride_aligned(a->v_stride[i], a->dtype)) return PLX_ERR_ALIGN;
+        p.ks[i] = a->k_stride[i], p.vs[i] = a->v_stride[i];
+    }
+    if (a->T > 1 && (a->k_stride[2] < a->cache.d || a->v_stride[2] < a->cache.d)) return PLX_ERR_SHAPE;
+    p.k = a->k, p.v = a->v, p.start = a->start, p.counts = a->counts, p.T = a->T, p.f32 = a->dtype == PLX_F32;
+    *out = p;
+    return PLX_OK;
+}
+
+}  // namespace
+
+plx_status parallax_cache_write_q4(const plx_q4_rows_args *a, void *hip_stream) {
+    plx::Q4Rows p{};
+    const plx_status st = take_q4_rows(a, &p);
+    if (st != PLX_OK || a->T == 0) return st;
+    return plx::launch_cache_write_q4(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PLX_OK : PLX_ERR_LAUNCH;
+}
+
+plx_status parallax_cache_read_q4(const plx_q4_rows_args *a, void *hip_stream) {
+    plx::Q4Rows p{};
+    const plx_status st = take_q4_rows(a, &p);
+    if (st != PLX_OK || a->T == 0) return st;
+    return plx::launch_cache_read_q4(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PLX_OK : PLX_ERR_LAUNCH;
+}
+
+plx_status parallax_cache_bounds(const plx_cache_bounds_args *a, void *hip_stream) {
+    if (!a || !a->bounds || (!a->k && !a->q4)) return PLX_ERR_NULL;
+    plx::BlockBounds p{};
+    if (a->k) {
+        if (a->B < 1 || a->Hkv < 1 || a->B > 65535 || a->Hkv > 65535 || a->capacity < 1 || (a->d != 64 && a->d != 128)) return PLX_ERR_SHAPE;
+        if (!aligned16(a->k) || !aligned4(a->block_table)) return PLX_ERR_ALIGN;
+        for (int i = 0; i < 3; ++i) {
+            if (a->k_stride[i] < 0) return PLX_ERR_SHAPE;
+            if (!stride_aligned(a->k_stride[i], PLX_BF16)) return PLX_ERR_ALIGN;
+            p.stride[i] = 2 * a->k_stride[i];
+        }
+        if (a->k_stride[2] < a->d) return PLX_ERR_SHAPE;
+        p.keys = static_cast<const char *>(a->k);
+        p.B = a->B, p.Hkv = a->Hkv, p.capacity = a->capacity, p.d = a->d;
+        if (a->block_table) {
+            if (a->page_size < 1 || a->num_pages < 1 || a->block_table_stride < 1) return PLX_ERR_SHAPE;
+            if ((int64_t)a->block_table_stride * a->page_size < a->capacity) return PLX_ERR_SHAPE;
+            p.block_table = a->block_table, p.table_stride = a->block_table_stride;
+            p.page_size = a->page_size, p.num_pages = a->num_pages;
+        }
+    } else {
+        plx::Q4Cache c{};
+        const plx_status st = take_q4_cache(*a->q4, &c);
+        if (st != PLX_OK) return st;
+        p.keys = c.rows, p.q4 = 1;
+        for (int i = 0; i < 3; ++i) p.stride[i] = c.stride[i];
+        p.B = c.B, p.Hkv = c.Hkv, p.capacity = c.capacity, p.d = c.d;
+        p.block_table = c.block_table, p.table_stride = c.table_stride, p.page_size = c.page_size, p.num_pages = c.num_pages;
+    }
+    const int32_t blocks = (int32_t)(((int64_t)p.capacity + PLX_BLOCK_KEYS - 1) / PLX_BLOCK_KEYS);
+    if (a->n_blocks < blocks || a->max_new < 0) return PLX_ERR_SHAPE;
+    if (!aligned16(a->bounds) || !aligned4(a->seq_lens) || !aligned4(a->from_lens)) return PLX_ERR_ALIGN;
+    p.bounds = a->bounds, p.n_blocks = a->n_blocks, p.seq_lens = a->seq_lens, p.from_lens = a->from_lens;
+    p.most = blocks;
+    // (n tokens from any one on lie in at most (n + 62) / 64 + 1 blocks)
+    if (a->from_lens && a->max_new > 0)
+        p.most = (int32_t)std::min<int64_t>(p.most, ((int64_t)a->max_new + PLX_BLOCK_KEYS - 2) / PLX_BLOCK_KEYS + 1);
+    return plx::launch_cache_bounds(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PLX_OK : PLX_ERR_LAUNCH;
+}
+
+size_t parallax_select_blocks_workspace_bytes(int32_t B, int32_t Hkv, int32_t n_blocks) {
+    return B < 1 || Hkv < 1 || n_blocks < 1 ? 0 : (size_t)B * (size_t)Hkv * (size_t)n_blocks * sizeof(uint64_t);
+}
+
+plx_status parallax_select_blocks(const plx_select_blocks_args *a, void *hip_stream) {
+    if (!a || !a->q || !a->bounds || !a->block_list) return PLX_ERR_NULL;
+    if (a->B < 1 || a->Hq < 1 || a->Hkv < 1 || a->B > 65535 || a->Hq > 65535 || a->Hq % a->Hkv != 0) return PLX_ERR_SHAPE;
+    if (a->d != 64 && a->d != 128) return PLX_ERR_SHAPE;
+    if (a->Tq < 0 || a->Tq > 16 || a->Hq / a->Hkv * std::max(a->Tq, 1) > 16) return PLX_ERR_SHAPE;
+    // (the numbers of a block's keys are int32)
+    if (a->n_blocks < 1 || a->n_blocks > 0x7fffffff / PLX_BLOCK_KEYS) return PLX_ERR_SHAPE;
+    if (a->keep < 1 || a->first < 0 || a->recent < 0 || (int64_t)a->first + a->recent > a->keep) return PLX_ERR_SHAPE;
+    if (!aligned16(a->q) || !aligned16(a->bounds) || !aligned4(a->seq_lens) || !aligned4(a->block_list)) return PLX_ERR_ALIGN;
+    if (!a->workspace || !aligned16(a->workspace) ||
+        a->workspace_bytes < parallax_select_blocks_workspace_bytes(a->B, a->Hkv, a->n_blocks))
+        return PLX_ERR_WORKSPACE;
+    const plx::BlockSelect p{a->q, a->bounds, a->seq_lens, a->block_list, static_cast<uint64_t *>(a->workspace),
+                             a->B, a->Hq, a->Hkv, std::max(a->Tq, 1), a->d, a->n_blocks, a->keep, a->first, a->recent};
+    return plx::launch_select_blocks(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PLX_OK : PLX_ERR_LAUNCH;
+}
+
+namespace {
+
 // Validation of a prefill call; fills the launch parameters.
 plx_status prepare_prefill(const plx_prefill_args *a, plx::PrefillParams *out) {
     if (!a) return PLX_ERR_NULL;

@@ -54,6 +54,46 @@ struct DecodeRowsParams {
     int32_t mask_words;
     const int32_t *draft_lens;  // [B] or nullptr: Tq
     int32_t col_groups;  // set by the launcher
+    // the blocks of kListBlock keys that are looked at, [B][Hkv][n_list] ascending, or nullptr: all (bf16 and 4-bit rows)
+    const int32_t *block_list;
+    int32_t n_list;
+};
+constexpr int kListBlock = 64;
+
+// A cache of 4-bit rows (plx_q4.h has the row): [B][Hkv][capacity][row], or pools [num_pages][Hkv][page_size][row] behind a
+// block table; strides in bytes. decode_q4_bf16.hip takes the same as DecodeParams, k and its strides in bytes.
+struct Q4Cache {
+    char *rows;
+    int64_t stride[3];
+    const int32_t *block_table;
+    int64_t table_stride;
+    int32_t page_size, num_pages, B, Hkv, capacity, d;
+};
+// Rows [B][Hkv][T][d] of K and V (strides in elements) that become, or come from, tokens start[b] + t
+struct Q4Rows {
+    Q4Cache cache;
+    void *k, *v;
+    int64_t ks[3], vs[3];
+    const int32_t *start, *counts;
+    int32_t T, f32;
+};
+// Smallest and largest key of every block of kListBlock tokens (block_select.hip): bounds [B][Hkv][n_blocks][2][d] bf16
+struct BlockBounds {
+    const char *keys;  // rows of bf16 keys or, q4, 4-bit rows; strides in bytes
+    int64_t stride[3];
+    const int32_t *block_table;
+    int64_t table_stride;
+    int32_t page_size, num_pages, B, Hkv, capacity, d, q4;
+    void *bounds;
+    int32_t n_blocks, most;  // blocks of a sequence that a call looks at
+    const int32_t *seq_lens, *from_lens;
+};
+struct BlockSelect {
+    const void *q, *bounds;
+    const int32_t *seq_lens;
+    int32_t *block_list;
+    uint64_t *keys;  // [B][Hkv][n_blocks]: the scores, as integers of the same order
+    int32_t B, Hq, Hkv, Tq, d, n_blocks, keep, first, recent;
 };
 
 struct PrefillParams {
@@ -210,6 +250,11 @@ hipError_t launch_cache_extend(const PageTable &t, const int32_t *seqs, const in
 hipError_t launch_cache_free(const PageTable &t, const int32_t *seqs, const int32_t *first, const int32_t *last, int n, hipStream_t stream);
 hipError_t launch_cache_copy(const CachePools &c, const int32_t *src, const int32_t *dst, const int32_t *rows, int n, hipStream_t stream);
 hipError_t launch_cache_compact(const CacheCompact &a, hipStream_t stream);
+hipError_t launch_cache_write_q4(const Q4Rows &p, hipStream_t stream);
+hipError_t launch_cache_read_q4(const Q4Rows &p, hipStream_t stream);
+hipError_t launch_cache_bounds(const BlockBounds &p, hipStream_t stream);
+hipError_t launch_select_blocks(const BlockSelect &p, hipStream_t stream);
+hipError_t launch_decode_q4(const DecodeRowsParams &p, hipStream_t stream);  // the split kernel only; k: 4-bit rows, strides in bytes
 hipError_t launch_norm_rope(const NormRopeParams &p, bool f32, hipStream_t stream);
 hipError_t launch_rope_table(float *table, int n_pos, int d, float theta, hipStream_t stream);
 hipError_t launch_decode_mla(const MlaDecodeParams &p, hipStream_t stream);

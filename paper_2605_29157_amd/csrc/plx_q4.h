@@ -1,0 +1,42 @@
+// The row of a 4-bit cache: K and V of one token and key head (cache_q4.hip writes and reads them, decode_q4_bf16.hip and
+// block_select.hip read them).
+//
+// Codes are e2m1 (sign, 2 bits of exponent, 1 of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6), which this chip's conversions take eight to a
+// dword together with a scale 2^(e - 127), given as the float that has e as its exponent bits (e = 255: NaN). A scale serves 16
+// dimensions: with K and V in one row, which is a multiple of 16 bytes, 16 cost no more than 32 would (d = 128: 128 bytes of codes
+// and 16 or 8 of scales, 144 both ways; d = 64: 64 and 8 or 4, 80 both ways).
+#pragma once
+#include "plx_device.h"
+
+namespace plx {
+
+template <int D>
+struct Q4Row {
+    static constexpr int kV = D / 2;                 // V codes (K codes: 0)
+    static constexpr int kKScale = D;                // scale bytes of K
+    static constexpr int kVScale = D + D / 16;       // ... of V
+    static constexpr int kEnd = D + D / 8;           // zeros from here
+    static constexpr int kBytes = (kEnd + 15) / 16 * 16;
+};
+
+__device__ __forceinline__ float q4_scale(uint32_t e) { return __builtin_bit_cast(float, e << 23); }
+
+// Eight codes times their scale, as bf16 (exact but for overflow, which is infinite)
+__device__ __forceinline__ u32x4 q4_to_bf16(uint32_t codes, float scale) {
+    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
+}
+
+// Where the row of a token is: byte offset of its head 0 from the pools' (or caches') base, or -1 (no page)
+__device__ __forceinline__ int64_t q4_token_offset(const int32_t *table, int64_t table_stride, int page_size, int num_pages,
+                                                   const int64_t (&stride)[3], int b, int64_t token) {
+    if (table == nullptr) return (int64_t)b * stride[0] + token * stride[2];
+    const int page_no = (int)(token / page_size), row = (int)(token - (int64_t)page_no * page_size);
+    const int page = table[(int64_t)b * table_stride + page_no];
+    if (page < 0 || page >= num_pages) return -1;
+    return (int64_t)page * stride[0] + (int64_t)row * stride[2];
+}
+
+}  // namespace plx

@@ -29,14 +29,16 @@ __device__ __forceinline__ u32x4 big_halves(uint32_t seen) {
 // The keys that the columns [x0, x0 + width) of (sequence b, key head) see, columns x = row * G + head of the group, and
 // the tiles of TILE keys that are walked for them: those of the sinks, then those from the first key any window
 // reaches. Tile number v of this walk holds the keys from key_of(v) on; no key is in two of them.
-template <bool TREE, int TILE>
+// LIST: the tiles are those of the blocks of a list (one for each key head, hk). A tile's key is then -1 where its entry is passed over.
+template <bool TREE, int TILE, bool LIST = false>
 struct RowsScope {
     int Lb, n, base;          // cached tokens; drafted ones among them (TREE), behind `base` committed ones (else base = Lb - Tq)
     int lo_all, end_all;      // keys every column sees: [lo_all, end_all), and [0, sinks) below end_all
     int sinks, n_sink_tiles, first_tile, n_virtual;
     const uint64_t *masks;    // TREE: the sequence's
+    const int32_t *list;      // LIST: the sequence's and key head's
 
-    __device__ __forceinline__ RowsScope(const DecodeRowsParams &P, int b, int x0, int width) {
+    __device__ __forceinline__ RowsScope(const DecodeRowsParams &P, int b, int x0, int width, int hk = 0) {
         const DecodeParams &p = P.d;
         Lb = p.seq_lens ? p.seq_lens[b] : p.Lmax;
         Lb = min(max(Lb, 0), p.Lmax);
@@ -58,8 +60,22 @@ struct RowsScope {
         n_sink_tiles = (min(sinks, end_any) + TILE - 1) / TILE;
         first_tile = max(lo_any / TILE, n_sink_tiles);
         n_virtual = n_sink_tiles + max((end_any + TILE - 1) / TILE - first_tile, 0);
+        list = nullptr;
+        if constexpr (LIST) {
+            list = P.block_list + ((int64_t)b * p.Hkv + hk) * P.n_list;
+            n_virtual = end_any > 0 ? P.n_list * kTilesPerBlock : 0;
+        }
     }
-    __device__ __forceinline__ int key_of(int v) const { return TILE * (v < n_sink_tiles ? v : v - n_sink_tiles + first_tile); }
+    static constexpr int kTilesPerBlock = LIST ? kListBlock / TILE : 1;
+    __device__ __forceinline__ int key_of(int v) const {
+        if constexpr (LIST) {
+            const int i = v / kTilesPerBlock, block = list[i], before = i > 0 ? list[i - 1] : -1;
+            if (block < 0 || block <= before || block > (Lb - 1) / kListBlock) return -1;
+            const int key = block * kListBlock + TILE * (v % kTilesPerBlock);
+            return key < Lb ? key : -1;
+        }
+        return TILE * (v < n_sink_tiles ? v : v - n_sink_tiles + first_tile);
+    }
     // does every column see the keys [key, key + count)?
     __device__ __forceinline__ bool whole(int key, int count) const {
         return (key >= lo_all || key + count <= sinks) && key + count <= end_all;
