@@ -153,6 +153,7 @@ def build_library(extra_flags: list[str] | None = None, verbose: bool = True) ->
     _check_pipelined_assembly("prefill_bwd_bf16.hip", False)
     _check_pipelined_assembly("decode_rows_bf16.hip", False)
     _check_pipelined_assembly("decode_rows_wide_bf16.hip", False)
+    _check_pipelined_assembly("decode_q4_bf16.hip", False)
     _check_pipelined_assembly("decode_mla_bf16.hip", False)
     _check_pipelined_assembly("decode_mla_wide_bf16.hip", False)
     _check_decode_assembly()

@@ -5,37 +5,93 @@
 // with k and v the values that the codes and scales stand for, in one pass with the running state (m, d1, d2, O1, O2); splits and
 // records as in decode_bf16.hip. J: the keys a row sees behind a window and sinks, or those in the blocks of a list.
 //
-// What bounds it: 9 D / 8 bytes a key (144 at D = 128, where bf16 takes 512) against the same 8 D flop per column and, beside them, the
-// conversion of 2 D codes.
+// What bounds it: 9 D / 8 bytes a key (144 at D = 128, where bf16 takes 512) against the same 8 D flop per column; beside them the
+// conversion of 2 D codes, and LDS.
 //
-// Layout. As decode_rows_bf16.hip: four waves with 32-key tiles of their own, S^T = K [Q; R]^T on 16x16x32 MFMAs, P kept in its
-// lane. What differs:
-//   * a lane's 16 bytes (D = 128; D = 64: 8) of a K row are its operands of all k-steps: the order of the dimensions is the
-//     product's to choose, so lane (key c, g) takes dimensions D / 4 g .. of its key, and q and rho are fetched to match. Codes become
-//     bf16 (one conversion for two, with their scale: exact) as they are used.
-//   * V has to be turned round (a lane's operand is 8 keys of one dimension), which its scales, one for each key, do not survive in
-//     4 bits: it is converted first and goes through the wave's LDS tile as bf16.
+// Layout. Four waves with 64-key tiles of their own (no barrier in the loop), S^T = K [Q; R]^T on 16x16x32 MFMAs, P kept in its
+// lane, as decode_bf16.hip. A tile comes into LDS as it is (direct loads, 1 KB each, two tiles a wave: one is worked on while the other is
+// on its way), and the codes stay codes until they are operands:
+//   * K: a lane's 16 bytes (D = 64: 8) of a row are its operands of all k-steps: the order of the dimensions is the product's to
+//     choose, so lane (key c, g) takes dimensions D / 4 g .. of its key, and q and rho are fetched to match. Codes become bf16
+//     with their scale, two in one conversion, exactly.
+//   * V has to be turned round (a lane's operand is 8 keys of one dimension): the 4-bit transposing read gives a lane 16 keys of its
+//     dimension at once, but a scale serves 16 dimensions of one key, so it cannot be applied there. It goes to the other side of
+//     the product, P: of the 16 columns of the matrix only those of the group's heads x rows are needed, and the copies of such a
+//     column hold P times the scales of one group of 16 dimensions each: 8 groups x 2 columns at D = 128 (C = 2). The product for a
+//     group's dimensions is right in its own copy only, and only that is kept. With more columns (C) the groups do not fit beside each
+//     other and P is multiplied 2, 4 or 8 times. A power of two changes no bit of P but its exponent. A key that a column does not see
+//     has the scale 0, so nothing in its row can reach it.
+// Steps, us for 16 x 32768 keys, 8 key heads, d = 128, and for 1 x 65536 at 8 splits (a workgroup a unit, 64 units): tiles in registers, V as bf16
+// through LDS, 32 keys at a time 130 and 81; two tiles in LDS 117, 77; 64 keys at a time, no bank conflicts 116, 61 (now bound by
+// LDS: 16 KB of V written at 64 bytes a cycle, and every read costs 6); scales with P instead 115, 50.
+#include "plx_lds_dma.h"
 #include "plx_q4.h"
 #include "plx_rows.h"
 
 namespace plx {
 
 namespace {
-constexpr int kQ4Tile = 32;  // keys per wave tile
+constexpr int kQ4Tile = 64;  // keys per wave tile
 constexpr int kQ4Waves = 4;
+constexpr float kQ4Slack = 6.f;  // in the exponent of 2
+
+// How the rows of a tile are found: 64 that follow each other in memory, counted from the start of the cache or looked up ahead
+// (lists; pages of a multiple of 64), four runs of 16 (other pages of a multiple of 16), or row by row.
+enum Q4Form { kQ4Direct, kQ4Runs64, kQ4Runs16, kQ4Any };
+
+// The tiles of a workgroup: those of a list's blocks, or RowsScope's
+struct Q4Scope : RowsScope<false, kQ4Tile> {
+    const int32_t *list;
+    __device__ __forceinline__ Q4Scope(const DecodeRowsParams &P, int b, int hk) : RowsScope<false, kQ4Tile>(P, b, 0, 16), list(nullptr) {
+        static_assert(kListBlock == kQ4Tile, "a tile is a block");
+        if (P.block_list != nullptr) {
+            list = P.block_list + ((int64_t)b * P.d.Hkv + hk) * P.n_list;
+            n_virtual = Lb > 0 ? P.n_list : 0;
+        }
+    }
+    __device__ __forceinline__ int key_of(int v) const {
+        return list != nullptr ? listed_key<kQ4Tile>(list, v, Lb) : RowsScope<false, kQ4Tile>::key_of(v);
+    }
+};
+
+// x of the lane whose number in its row of 16 is 4 less (or 12 more), in the banks of 4 lanes of BANKS; the others keep `old`
+template <int BANKS>
+__device__ __forceinline__ uint32_t from_other_quad(uint32_t old, uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)x, 0x124, 0xf, BANKS, false);  // row_ror:4
+}
+template <int A, int B>
+__device__ __forceinline__ uint32_t from_quad(uint32_t x) {  // lanes A, B, A, B of the quad
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, A | B << 2 | A << 4 | B << 6, 0xf, 0xf, true);
+}
+// Group (16 dimensions) 16 / C * J + c % (16 / C) of the scales for operand J of C columns. own: the tr_b8 read's, D = 128: group c % 8,
+// D = 64: scales of K (c % 8 < 4) and then of V.
+template <int D, int C, int J>
+__device__ __forceinline__ uint32_t operand_scales(uint32_t own) {
+    if constexpr (D == 128 && C == 2) return own;
+    // groups 4 h + c % 4 of V
+    constexpr int H = D == 128 ? 16 / C * J / 4 : 1;
+    const uint32_t x = from_other_quad<H == 0 ? 0xA : 0x5>(own, own);
+    if constexpr (C == 4) return x;
+    if constexpr (C == 8) return from_quad<2 * (J & 1), 2 * (J & 1) + 1>(x);
+    return from_quad<J & 3, J & 3>(x);
+}
 }  // namespace
 
-template <int D, bool USE_R, int CACHE, bool LIST>
+// C: columns (rows x heads of a group) there is room for, 2 (D = 128 only), 4, 8 or 16
+template <int D, int C, bool USE_R, int FORM>
 __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
     const DecodeParams &p = P.d;
     using Row = Q4Row<D>;
-    constexpr int CPR = D / 8;             // 16-byte chunks of a bf16 V row
     constexpr int KSTEPS = D / 32, NDB = D / 16;
-    constexpr int TILE_CHUNKS = kQ4Tile * CPR;
-    constexpr int KW = D / 32;             // dwords of K codes a lane has of a key (KSTEPS of them)
-    constexpr int VLPR = D / 32;           // lanes of a row of V codes, 16 bytes each
-    constexpr int VRPL = 64 / VLPR, NV = kQ4Tile / VRPL;  // rows of a load; loads
-    __shared__ u32x4 lds[kQ4Waves * TILE_CHUNKS > 2 * kQ4Waves * NDB * 64 + 48 ? kQ4Waves * TILE_CHUNKS : 2 * kQ4Waves * NDB * 64 + 48];
+    constexpr int REP = 16 / C, OPERANDS = NDB / REP;  // matrix columns of a column; sets of them
+    static_assert(REP <= NDB, "no more copies than groups of dimensions");
+    constexpr int RPC = Row::kBytes / 16;            // 16-byte chunks of a row
+    constexpr int RAW = kQ4Tile * RPC;               // ... of a tile
+    constexpr int RUNS = FORM == kQ4Runs16 ? 4 : 1, RUN = RAW / RUNS;  // of rows that follow each other; chunks of one
+    constexpr int FULL = RUN / 64, REST = RUN % 64, LOADS = FULL + (REST != 0);  // of a run
+    static_assert(REST == 0 || REST == 16, "the last load of 16 rows takes 16 lanes");
+    __shared__ u32x4 lds[kQ4Waves * 2 * RAW + 48];  // two tiles a wave; at the end the states of 16 columns
+    static_assert(2 * NDB * 64 <= 2 * RAW, "the states of four waves");
     __shared__ TreeWords<0> no_words;
 
     const int tid = threadIdx.x;
@@ -44,7 +100,7 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
     const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
     const int G = p.G, S = p.S, Tq = p.Tq, n_cols = G * Tq;
 
-    const RowsScope<false, kQ4Tile, LIST> scope(P, b, 0, 16, hk);
+    const Q4Scope scope(P, b, hk);
     const int Lb = scope.Lb;
     // (splits in whole rounds of the four waves)
     const int per = ((scope.n_virtual + S - 1) / S + kQ4Waves - 1) / kQ4Waves * kQ4Waves;
@@ -55,8 +111,9 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
     int col_end, col_lo;
     TreeRow col_nodes{};
     {
-        const bool live = c < n_cols;
-        const int t = live ? c / G : 0, h = live ? c - t * G : 0;
+        const int col = c / REP;
+        const bool live = col < n_cols;
+        const int t = live ? col / G : 0, h = live ? col - t * G : 0;
         const int64_t row = (((int64_t)b * p.Hq + (int64_t)hk * G + h) * Tq + t) * D + D / 4 * g;
         const __bf16 *qrow = (const __bf16 *)p.q + row, *rrow = (const __bf16 *)p.r + row;
 #pragma unroll
@@ -69,89 +126,93 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
     }
 
     const char *base = (const char *)p.k + (p.block_table == nullptr ? (int64_t)b * p.ksb : 0) + (int64_t)hk * p.ksh;
-    u32x4 *ldsV = lds + w * TILE_CHUNKS;
-    const unsigned short *ldsV16 = (const unsigned short *)ldsV;
+    u32x4 *raw = lds + w * 2 * RAW;
     const int32_t *table = p.block_table + (int64_t)b * p.table_stride;
-    auto paged_offset = [&](int key) {
+    auto offset_of = [&](int key) -> int64_t {
+        if (FORM == kQ4Direct || p.block_table == nullptr) return (int64_t)key * p.ksl;
         const int page_no = key / p.page_size;
         const int64_t page = min(max(table[page_no], 0), p.num_pages - 1);
         return page * p.ksb + (int64_t)(key - page_no * p.page_size) * p.ksl;
     };
-    const int last16 = max(Lb - 1, 0) & ~15;  // first key of the last half tile that exists
     const uint32_t row_bytes = (uint32_t)p.ksl;
 
     // ---- the wave's tiles --------------------------------------------------------------------------------
-    // Keys and (runs) the halves' offsets of its next 32 tiles, lane 2 * j + half
-    constexpr bool AHEAD = LIST || CACHE == kRowsPagedRuns;
+    // Keys and offsets of the runs of its next 64 / RUNS tiles, lane RUNS * j + run
     int ahead_key = 0, ahead_off[2] = {0, 0}, slot = 64;
     auto look_ahead = [&](int v) {
-        const int key = scope.key_of(min(v + (lane >> 1) * kQ4Waves, scope.n_virtual - 1));
+        const int key = scope.key_of(min(v + lane / RUNS * kQ4Waves, scope.n_virtual - 1));
         ahead_key = key;
-        if constexpr (CACHE != kRowsAny) {
-            const int first = min(max(key, 0) + 16 * (lane & 1), last16);
-            const int64_t off = CACHE == kRowsPagedRuns ? paged_offset(first) : (int64_t)first * p.ksl;
+        if constexpr (FORM != kQ4Any) {
+            // (runs behind the last token: the one that it is in)
+            const int64_t off = offset_of(min(max(key, 0) + 16 * (lane % RUNS), (Lb - 1) & ~15));
             ahead_off[0] = (int)off, ahead_off[1] = (int)(off >> 32);
         }
         slot = 0;
     };
-    // The first tile at or behind number v: its key and the addresses of its halves (CACHE kRowsAny: not these)
-    auto next_tile = [&](int &v, int &key, const char *(&half)[2]) -> bool {
+    // The first tile at or behind number v: its key and the addresses of its runs (kQ4Any: the offset of this lane's row)
+    int64_t row_off = 0;
+    auto next_tile = [&](int &v, int &key, const char *(&run)[RUNS]) -> bool {
         for (; v < v_hi; v += kQ4Waves) {
-            if constexpr (AHEAD) {
+            if constexpr (FORM != kQ4Direct) {
                 if (slot == 64) look_ahead(v);
                 key = __builtin_amdgcn_readlane(ahead_key, slot);
-                if constexpr (CACHE != kRowsAny)
+                if constexpr (FORM != kQ4Any)
 #pragma unroll
-                    for (int hf = 0; hf < 2; ++hf)
-                        half[hf] = base + (((int64_t)__builtin_amdgcn_readlane(ahead_off[1], slot + hf) << 32) |
-                                           (uint32_t)__builtin_amdgcn_readlane(ahead_off[0], slot + hf));
-                slot += 2;
-                if (LIST && key < 0) continue;
+                    for (int i = 0; i < RUNS; ++i)
+                        run[i] = base + (((int64_t)__builtin_amdgcn_readlane(ahead_off[1], slot + i) << 32) |
+                                         (uint32_t)__builtin_amdgcn_readlane(ahead_off[0], slot + i));
+                slot += RUNS;
+                if (key < 0) continue;  // (an entry of a list that is passed over)
+                if constexpr (FORM == kQ4Any) row_off = offset_of(min(key + lane, Lb - 1));
             } else {
                 key = __builtin_amdgcn_readfirstlane(scope.key_of(v));
-                if constexpr (CACHE != kRowsAny)
-#pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) half[hf] = base + (int64_t)min(key + 16 * hf, last16) * p.ksl;
+                run[0] = base + (int64_t)key * p.ksl;
             }
             return true;
         }
         return false;
     };
-    // row of key `key` + 16 hf + i (rows past the sequence end: its last one, masked below)
-    auto row_of = [&](int key, const char *const(&half)[2], int hf, int i) -> const char * {
-        if constexpr (CACHE != kRowsAny) {
-            const int last = Lb - 1 - min(key + 16 * hf, last16);
-            return half[hf] + __umul24((uint32_t)min(i, last), row_bytes);
-        } else {
-            const int k = min(key + 16 * hf + i, Lb - 1);
-            return base + (p.block_table != nullptr ? paged_offset(k) : (int64_t)k * p.ksl);
+    // Chunk n of a run is chunk n % RPC of its row n / RPC; this lane's of load i is n = 64 i + lane
+    uint32_t chunk_off[LOADS];
+    if constexpr (FORM != kQ4Any)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t n = 64 * i + lane;
+            chunk_off[i] = __umul24(n / RPC, row_bytes) + 16 * (n % RPC);
         }
-    };
-    uint32_t k_codes[2][KW], v_codes[NV][4], k_scales[2], v_scales[NV];
-    auto issue = [&](int key, const char *const(&half)[2]) {
+    // A tile's rows on their way into stage 0 or 1 (rows past the sequence end: its last one, masked below)
+    const uint32_t raw_address = lds_byte_address(raw);
+    auto issue = [&](int key, const char *const(&run)[RUNS], int stage) {
+        const uint32_t to = raw_address + 16 * RAW * stage;
+        if constexpr (FORM != kQ4Any) {
+            const bool exists = key + kQ4Tile <= Lb;  // (uniform) all of it
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-            const char *row = row_of(key, half, hf, c);
-            if constexpr (D == 128) {
-                const u32x4 x = *(const u32x4 *)(row + 16 * g);
+            for (int r = 0; r < RUNS; ++r) {
+                const uint32_t dst = to + 16 * RUN * r;
+                if (__builtin_expect(exists, 1)) {
 #pragma unroll
-                for (int s = 0; s < KW; ++s) k_codes[hf][s] = x[s];
-                k_scales[hf] = *(const uint16_t *)(row + Row::kKScale + 2 * g);
-            } else {
-                const u32x2 x = *(const u32x2 *)(row + 8 * g);
+                    for (int i = 0; i < FULL; ++i) tile_load16_uniform<false>(chunk_off[i], run[r], dst + 1024 * i);
+                    if constexpr (REST != 0) tile_load16_uniform<true>(chunk_off[FULL], run[r], dst + 1024 * FULL);
+                } else {
+                    const int last = Lb - 1 - min(key + 16 * r, (Lb - 1) & ~15);
 #pragma unroll
-                for (int s = 0; s < KW; ++s) k_codes[hf][s] = x[s];
-                k_scales[hf] = *(const uint8_t *)(row + Row::kKScale + g);
+                    for (int i = 0; i < LOADS; ++i) {
+                        const int n = 64 * i + lane;
+                        const uint32_t off = __umul24((uint32_t)min(n / RPC, last), row_bytes) + 16u * (n % RPC);
+                        if (i < FULL)
+                            tile_load16_uniform<false>(off, run[r], dst + 1024 * i);
+                        else
+                            tile_load16_uniform<true>(off, run[r], dst + 1024 * i);
+                    }
+                }
             }
-        }
+        } else {
 #pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            const int i = VRPL * n + lane / VLPR;
-            const char *row = NV == 2 ? row_of(key, half, n, lane / VLPR) : (i < 16 ? row_of(key, half, 0, i & 15) : row_of(key, half, 1, i & 15));
-            const u32x4 x = *(const u32x4 *)(row + Row::kV + 16 * (lane % VLPR));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v_codes[n][e] = x[e];
-            v_scales[n] = *(const uint16_t *)(row + Row::kVScale + 2 * (lane % VLPR));
+            for (int i = 0; i < LOADS; ++i) {  // (from the lane that has the row's offset)
+                const int n = 64 * i + lane, row = n / RPC;
+                const int lo = __shfl((int)row_off, row, 64), hi = __shfl((int)(row_off >> 32), row, 64);
+                tile_load16<64>(base + (((int64_t)hi << 32) | (uint32_t)lo) + 16 * (n % RPC), to + 1024 * i);
+            }
         }
     };
 
@@ -161,137 +222,172 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
 #pragma unroll
     for (int i = 0; i < NDB; ++i) o1[i] = o2[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float scale_log2 = p.scale * kLog2e;
-    // A operand of O^T += V^T P^T for 16 output dimensions: the 8 keys of this lane's B operand
-    const int tr_key = 4 * g + (c >> 2), tr_half = (c & 1) * 4;
-    auto v_fragment = [&](int i) __attribute__((always_inline)) {
-        const int chunk = 2 * i + ((c & 3) >> 1);
-        const u32x2 lo = lds_read_tr16(ldsV16 + lds_chunk_slot<D>(tr_key, chunk) * 8 + tr_half);
-        const u32x2 hi = lds_read_tr16(ldsV16 + lds_chunk_slot<D>(16 + tr_key, chunk) * 8 + tr_half);
-        return u32x4{lo[0], lo[1], hi[0], hi[1]};
-    };
-    // lanes exchange data through LDS inside one wave: LDS executes a wave's accesses in
-    // order, the fence only stops the compiler from moving reads above the writes
-    auto wave_lds_fence = [&]() __attribute__((always_inline)) {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    };
 
-    int v = v_lo + w, key = 0;
-    const char *half[2] = {base, base};
-    bool have = next_tile(v, key, half);
-    if (have) issue(key, half);
+    // This lane's places in a tile: of the K rows, and of the rows it gives the transposing reads (element i of a lane's 4-bit
+    // operand is key 32 (i / 8) + 16 (i / 4 % 2) + 4 g + i % 4, of its scales, 32 keys at a time, likewise)
+    const uint32_t k_at = (uint32_t)c * Row::kBytes + (D == 128 ? 16 : 8) * g, k_scale_at = (uint32_t)c * Row::kBytes + Row::kKScale + (D == 128 ? 2 : 1) * g;
+    const uint32_t v_at = (uint32_t)(32 * (c >> 3) + 16 * ((c >> 2) & 1) + 4 * g + (c & 3)) * Row::kBytes + Row::kV;
+    const uint32_t v_scale_at = (uint32_t)(16 * (c >> 3) + 4 * g + ((c >> 1) & 3)) * Row::kBytes + (D == 128 ? Row::kVScale : Row::kKScale);
+
+    int v = v_lo + w, key = 0, key_next = 0, stage = 0;
+    const char *run[RUNS];
+    bool have = next_tile(v, key, run), have_next = false;
+    if (have) {
+        issue(key, run, 0);
+        v += kQ4Waves;
+        have_next = next_tile(v, key_next, run);
+        if (have_next) issue(key_next, run, 1);
+    }
+    // (q and rho, asked for in front of the first tiles, are waited for here: inside the loop every round would wait for them, and with
+    // them for the tiles on their way)
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) {
+        asm volatile("" : "+v"(qf[s]));
+        if constexpr (USE_R) asm volatile("" : "+v"(rf[s]));
+    }
     while (have) {
         const int tk = key;
         const bool whole = scope.whole(tk, kQ4Tile);  // (uniform) every column sees all of the keys
-        uint32_t kc[2][KW], ks[2];
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-            ks[hf] = k_scales[hf];
-#pragma unroll
-            for (int s = 0; s < KW; ++s) kc[hf][s] = k_codes[hf][s];
+        if (have_next)                                // (uniform) the tile is here, the next one may not be
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(RUNS * LOADS) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const char *tile = (const char *)(raw + stage * RAW);
+        int key_third = 0;  // the tile behind the next one is looked for here, and asked for when this one has been read
+        bool have_third = false;
+        if (have_next) {
+            v += kQ4Waves;
+            have_third = next_tile(v, key_third, run);
         }
-        bool any_bad = false;
-        if (!whole) {  // scales above 252 stand for values that are not finite, or not in bf16
-            bool bad = false;
+
+        // ---- S1^T = K q^T, S2^T = K rho^T -------------------------------------------------------------------
+        f32x4 s1[4], s2[4];
 #pragma unroll
-            for (int n = 0; n < NV; ++n) bad = bad || (v_scales[n] & 255u) > 252u || (v_scales[n] >> 8) > 252u;
-            any_bad = __any(bad);
-        }
-#pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            const int i = VRPL * n + lane / VLPR;
-            const float lo = q4_scale(v_scales[n] & 255u), hi = q4_scale(v_scales[n] >> 8);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                ldsV[lds_chunk_slot<D>(i, 4 * (lane % VLPR) + e)] = q4_to_bf16(v_codes[n][e], e < 2 ? lo : hi);
-        }
-        v += kQ4Waves;
-        have = next_tile(v, key, half);
-        if (have) issue(key, half);
-        wave_lds_fence();
-        uint32_t seen = 0xffu;
-        if (!whole) {
-            seen = scope.seen(P, col_nodes, col_lo, col_end, tk, g);
-            if (__builtin_expect(any_bad, 0)) {
-                // values that are not finite: into the columns that see their key, and out of the V tile
-                const u32x4 big = big_halves(seen);
-#pragma unroll
-                for (int i = 0; i < NDB; ++i) {
-                    u32x4 bad = v_fragment(i);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) bad[e] = not_finite_halves(bad[e]) & kBigHalves;
-                    o1[i] = mfma16(bad, big, o1[i]);
-                }
-                wave_lds_fence();
-#pragma unroll
-                for (int i = 0; i < TILE_CHUNKS / 64; ++i) {
-                    u32x4 &x = ldsV[64 * i + lane];
-                    u32x4 y = x;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] &= ~not_finite_halves(y[e]);
-                    x = y;
-                }
-                wave_lds_fence();
-            }
-        }
-        f32x4 s1[2], s2[2];
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
+        for (int sub = 0; sub < 4; ++sub) {
             s1[sub] = s2[sub] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const float lo = q4_scale(ks[sub] & 255u), hi = q4_scale(ks[sub] >> 8);
+            const char *row = tile + 16 * sub * Row::kBytes;
+            if constexpr (D == 128) {
+                const u32x4 codes = *(const u32x4 *)(row + k_at);
+                const uint32_t scales = *(const uint16_t *)(row + k_scale_at);
+                const float lo = q4_scale(scales & 255u), hi = q4_scale(scales >> 8);
 #pragma unroll
-            for (int s = 0; s < KSTEPS; ++s) {
-                const u32x4 kf = q4_to_bf16(kc[sub][s], D == 64 || s < 2 ? lo : hi);
-                s1[sub] = mfma16(kf, qf[s], s1[sub]);
-                if constexpr (USE_R) s2[sub] = mfma16(kf, rf[s], s2[sub]);
+                for (int s = 0; s < KSTEPS; ++s) {
+                    const u32x4 kf = q4_to_bf16(codes[s], s < 2 ? lo : hi);
+                    s1[sub] = mfma16(kf, qf[s], s1[sub]);
+                    if constexpr (USE_R) s2[sub] = mfma16(kf, rf[s], s2[sub]);
+                }
+            } else {
+                const u32x2 codes = *(const u32x2 *)(row + k_at);
+                const float scale = q4_scale(*(const uint8_t *)(row + k_scale_at));
+#pragma unroll
+                for (int s = 0; s < KSTEPS; ++s) {
+                    const u32x4 kf = q4_to_bf16(codes[s], scale);
+                    s1[sub] = mfma16(kf, qf[s], s1[sub]);
+                    if constexpr (USE_R) s2[sub] = mfma16(kf, rf[s], s2[sub]);
+                }
             }
         }
-        float x[8], tmax = kNegInf;
+        u32x2 scales[2];  // of V, 8 keys each
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x[e] = (seen >> e) & 1u ? s1[e >> 2][e & 3] * scale_log2 : kNegInf;
-            tmax = fmaxf(tmax, x[e]);
+        for (int h = 0; h < 2; ++h) scales[h] = lds_read_tr8(tile + 32 * h * Row::kBytes + v_scale_at);
+        u32x2 keep[2] = {{~0u, ~0u}, {~0u, ~0u}};  // bytes of the keys that are seen
+        float factor = scale_log2;
+        if (__builtin_expect(!whole, 0)) {
+            uint32_t seen[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) seen[h] = scope.seen(P, col_nodes, col_lo, col_end, tk + 32 * h, g);
+            asm volatile("" : "+v"(seen[0]), "+v"(seen[1]));  // (not to be worked out for every tile)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const bool ok = (seen[e >> 3] >> (e & 7)) & 1u;
+                s1[e >> 2][e & 3] = ok ? s1[e >> 2][e & 3] * factor : kNegInf;
+                if constexpr (USE_R) s2[e >> 2][e & 3] = ok ? s2[e >> 2][e & 3] : 0.f;
+                if (!ok) keep[e >> 3][(e >> 2) & 1] &= ~(255u << (8 * (e & 3)));
+            }
+            factor = 1.f;
         }
-        tmax = rows_max(tmax);
-        const float m_new = fmaxf(m_run, tmax), m_use = m_new == kNegInf ? 0.f : m_new;
-        const float alpha = fast_exp2(m_run - m_use);  // 0 on the first tile that is seen
-        m_run = m_new;
-        // P1 and P2 are rounded to bf16 once, as matrix operands; d1 and d2 add the rounded values, so
-        // that the weights still sum to one.
-        float p1[8];
+        // Any reference near the row's largest score does: it moves (and everything with it) only when a score is 2^6 above it
+        float tmax = kNegInf;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p1[e] = fast_exp2(x[e] - m_use);
-        dsum1 *= alpha;
-        const u32x4 pb1 = pack8_bf16_accumulate(p1[0], p1[1], p1[2], p1[3], p1[4], p1[5], p1[6], p1[7], dsum1);
-        u32x4 pb2 = {0u, 0u, 0u, 0u};
-        if constexpr (USE_R) {
-            float p2[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) p2[e] = (seen >> e) & 1u ? p1[e] * s2[e >> 2][e & 3] : 0.f;
-            dsum2 *= alpha;
-            pb2 = pack8_bf16_accumulate(p2[0], p2[1], p2[2], p2[3], p2[4], p2[5], p2[6], p2[7], dsum2);
-        }
-        if (!__all(alpha == 1.f)) {
+        for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, s1[e >> 2][e & 3]);
+        tmax *= factor;
+        if (__builtin_expect(__any(tmax > m_run + kQ4Slack), 0)) {  // (rare, but for the first tile)
+            tmax = rows_max(tmax);
+            const float m_new = fmaxf(m_run, tmax);
+            const float alpha = fast_exp2(m_run - (m_new == kNegInf ? 0.f : m_new));
+            m_run = m_new;
+            dsum1 *= alpha, dsum2 *= alpha;
 #pragma unroll
             for (int i = 0; i < NDB; ++i) {
                 o1[i] *= alpha;
                 if constexpr (USE_R) o2[i] *= alpha;
             }
         }
+        const float neg_m = m_run == kNegInf ? 0.f : -m_run;
+        // P1 and P2 are rounded to bf16 once, as matrix operands (the scales, powers of two, change no bit of them); d1 and d2 add the
+        // rounded values, so that the weights still sum to one.
+        float p1[16], p2[16];
 #pragma unroll
-        for (int i = 0; i < NDB; ++i) {
-            const u32x4 vt = v_fragment(i);
-            o1[i] = mfma16(vt, pb1, o1[i]);
-            if constexpr (USE_R) o2[i] = mfma16(vt, pb2, o2[i]);
+        for (int e = 0; e < 16; ++e) {
+            p1[e] = fast_exp2(fmaf(s1[e >> 2][e & 3], factor, neg_m));
+            p2[e] = USE_R ? p1[e] * s2[e >> 2][e & 3] : 0.f;
         }
-        wave_lds_fence();
+#pragma unroll
+        for (int e = 0; e < 16; e += 8) {
+            pack8_bf16_accumulate(p1[e], p1[e + 1], p1[e + 2], p1[e + 3], p1[e + 4], p1[e + 5], p1[e + 6], p1[e + 7], dsum1);
+            if constexpr (USE_R)
+                pack8_bf16_accumulate(p2[e], p2[e + 1], p2[e + 2], p2[e + 3], p2[e + 4], p2[e + 5], p2[e + 6], p2[e + 7], dsum2);
+        }
+        // ---- O1^T += V^T P1^T, O2^T += V^T P2^T, 16 * REP dimensions with the same operands --------------------
+        auto products = [&](auto j) __attribute__((always_inline)) {
+            constexpr int J = decltype(j)::value;
+            u32x4 pb1[2], pb2[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float x[8];
+#pragma unroll
+                for (int d = 0; d < 2; ++d) {
+                    const uint32_t e4 = operand_scales<D, C, J>(scales[h][d]) & keep[h][d];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[4 * d + e] = q4_scale((e4 >> (8 * e)) & 255u);
+                }
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = p1[8 * h + e] * x[e];
+                pb1[h] = u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
+                if constexpr (USE_R) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = p2[8 * h + e] * x[e];
+                    pb2[h] = u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < REP; ++n) {
+                const int i = REP * J + n;
+                const u32x2 codes = lds_read_tr4(tile + v_at + 8 * i);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const u32x4 x = q4_to_bf16(codes[h], 1.f);
+                    o1[i] = mfma16(x, pb1[h], o1[i]);
+                    if constexpr (USE_R) o2[i] = mfma16(x, pb2[h], o2[i]);
+                }
+            }
+        };
+        each_of<OPERANDS>(products);
+
+        if (have_third) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (read before it is written again)
+            issue(key_third, run, stage);
+        }
+        key = key_next, key_next = key_third;
+        have = have_next, have_next = have_third;
+        stage ^= 1;
     }
 
     // ---- the four waves' states (in the order of the lanes' registers: no bank conflicts), then the record or the output row ----
-    constexpr int QUADS = NDB * 64;  // of four dimensions: quad 64 i + lane' is column lane' % 16, dimensions 16 i + 4 (lane' / 16) ..
+    constexpr int QUADS = NDB * 64;  // of four dimensions: quad 64 i + lane' is matrix column lane' % 16, dimensions 16 i + 4 (lane' / 16) ..
     f32x4 *mrg1 = (f32x4 *)lds, *mrg2 = mrg1 + kQ4Waves * QUADS;  // [wave][quad]
-    float *mrg_m = (float *)(lds + 2 * kQ4Waves * QUADS), *mrg_d1 = mrg_m + kQ4Waves * 16, *mrg_d2 = mrg_d1 + kQ4Waves * 16;
+    float *mrg_m = (float *)(lds + kQ4Waves * 2 * RAW), *mrg_d1 = mrg_m + kQ4Waves * 16, *mrg_d2 = mrg_d1 + kQ4Waves * 16;
     __syncthreads();  // every wave is done with its tiles
     {
         const float s1 = rows_sum(dsum1), s2 = rows_sum(dsum2);
@@ -305,62 +401,61 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
 #pragma unroll
         for (int i = 0; i < NDB; ++i) {
             const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+            if (c % REP != i % REP) continue;  // (the copies with other groups' scales)
             mrg1[w * QUADS + 64 * i + lane] = none ? zero : o1[i];
             if constexpr (USE_R) mrg2[w * QUADS + 64 * i + lane] = none ? zero : o2[i];
         }
     }
     __syncthreads();
-    if (c >= n_cols) return;  // (a thread's column is the same in all of its quads)
-    float m_star = kNegInf, wt[kQ4Waves], d1 = 0.f, d2 = 0.f;
+    for (int at = tid; at < NDB * 4 * C; at += 256) {
+        const int i = at / (4 * C), quarter = at / C % 4, col = at % C, x = col * REP + i % REP;  // x: matrix column
+        if (col >= n_cols) continue;
+        float m_star = kNegInf, wt[kQ4Waves], d1 = 0.f, d2 = 0.f;
 #pragma unroll
-    for (int ww = 0; ww < kQ4Waves; ++ww) m_star = fmaxf(m_star, mrg_m[ww * 16 + c]);
-#pragma unroll
-    for (int ww = 0; ww < kQ4Waves; ++ww) {
-        // (a reference of -inf with a sum that is not zero: scores of NaN only, which must reach the result)
-        const float mw = mrg_m[ww * 16 + c], dw = mrg_d1[ww * 16 + c];
-        wt[ww] = mw == kNegInf && dw == 0.f ? 0.f : fast_exp2(mw - m_star);
-        d1 += wt[ww] * dw;
-        d2 += wt[ww] * mrg_d2[ww * 16 + c];
-    }
-    const RowsColumn<D> column(p, b, hk, c, split, m_star, d1, d2, false, w == 0 && g == 0);
-#pragma unroll
-    for (int quad = tid; quad < QUADS; quad += 256) {
+        for (int ww = 0; ww < kQ4Waves; ++ww) m_star = fmaxf(m_star, mrg_m[ww * 16 + x]);
         f32x4 a1 = {0.f, 0.f, 0.f, 0.f}, a2 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ww = 0; ww < kQ4Waves; ++ww) {
-            a1 += wt[ww] * mrg1[ww * QUADS + quad];
-            if constexpr (USE_R) a2 += wt[ww] * mrg2[ww * QUADS + quad];
+            // (a reference of -inf with a sum that is not zero: scores of NaN only, which must reach the result)
+            const float mw = mrg_m[ww * 16 + x], dw = mrg_d1[ww * 16 + x];
+            wt[ww] = mw == kNegInf && dw == 0.f ? 0.f : fast_exp2(mw - m_star);
+            d1 += wt[ww] * dw;
+            d2 += wt[ww] * mrg_d2[ww * 16 + x];
+            a1 += wt[ww] * mrg1[ww * QUADS + 64 * i + 16 * quarter + x];
+            if constexpr (USE_R) a2 += wt[ww] * mrg2[ww * QUADS + 64 * i + 16 * quarter + x];
         }
-        column.store(16 * (quad >> 6) + 4 * g, a1, a2);
+        const RowsColumn<D> column(p, b, hk, col, split, m_star, d1, d2, false, i == 0 && quarter == 0);
+        column.store(16 * i + 4 * quarter, a1, a2);
     }
 }
 
-template <int D, bool USE_R, int CACHE>
+template <int D, int C, bool USE_R>
 static void launch_q4_form(const DecodeRowsParams &P, hipStream_t stream) {
-    const dim3 grid(P.d.S, P.d.Hkv, P.d.B);
-    if (P.block_list != nullptr)
-        hipLaunchKernelGGL((decode_q4_kernel<D, USE_R, CACHE, true>), grid, dim3(256), 0, stream, P);
+    const DecodeParams &p = P.d;
+    const dim3 grid(p.S, p.Hkv, p.B);
+    const bool short_rows = p.ksl < (1 << 24);  // (24-bit products of a row number below 64 and the row stride)
+    if (short_rows && p.block_table == nullptr && P.block_list == nullptr)
+        hipLaunchKernelGGL((decode_q4_kernel<D, C, USE_R, kQ4Direct>), grid, dim3(256), 0, stream, P);
+    else if (short_rows && (p.block_table == nullptr || p.page_size % 64 == 0))
+        hipLaunchKernelGGL((decode_q4_kernel<D, C, USE_R, kQ4Runs64>), grid, dim3(256), 0, stream, P);
+    else if (short_rows && p.page_size % 16 == 0)
+        hipLaunchKernelGGL((decode_q4_kernel<D, C, USE_R, kQ4Runs16>), grid, dim3(256), 0, stream, P);
     else
-        hipLaunchKernelGGL((decode_q4_kernel<D, USE_R, CACHE, false>), grid, dim3(256), 0, stream, P);
+        hipLaunchKernelGGL((decode_q4_kernel<D, C, USE_R, kQ4Any>), grid, dim3(256), 0, stream, P);
 }
 
-template <int D, bool USE_R>
-static void launch_q4_cache(const DecodeRowsParams &P, hipStream_t stream) {
-    const DecodeParams &p = P.d;
-    const bool short_rows = p.ksl < (1 << 24);  // (24-bit products of a row number below 16 and the row stride)
-    if (short_rows && p.block_table == nullptr)
-        launch_q4_form<D, USE_R, kRowsContiguous>(P, stream);
-    else if (short_rows && p.page_size % 16 == 0)
-        launch_q4_form<D, USE_R, kRowsPagedRuns>(P, stream);
-    else
-        launch_q4_form<D, USE_R, kRowsAny>(P, stream);
+template <int D>
+static void launch_q4_columns(const DecodeRowsParams &P, hipStream_t stream) {
+    const int cols = P.d.G * P.d.Tq;
+    if (!P.d.use_r) return cols <= 4 ? launch_q4_form<D, 4, false>(P, stream) : launch_q4_form<D, 16, false>(P, stream);
+    if constexpr (D == 128)
+        if (cols <= 2) return launch_q4_form<D, 2, true>(P, stream);
+    if (cols <= 4) return launch_q4_form<D, 4, true>(P, stream);
+    cols <= 8 ? launch_q4_form<D, 8, true>(P, stream) : launch_q4_form<D, 16, true>(P, stream);
 }
 
 hipError_t launch_decode_q4(const DecodeRowsParams &P, hipStream_t stream) {
-    if (P.d.d == 128)
-        P.d.use_r ? launch_q4_cache<128, true>(P, stream) : launch_q4_cache<128, false>(P, stream);
-    else
-        P.d.use_r ? launch_q4_cache<64, true>(P, stream) : launch_q4_cache<64, false>(P, stream);
+    P.d.d == 128 ? launch_q4_columns<128>(P, stream) : launch_q4_columns<64>(P, stream);
     return hipGetLastError();
 }
 

@@ -607,8 +607,9 @@ int32_t keys_of_lists(const plx::DecodeRowsParams &p) {
     return p.d.window > 0 && in_window < p.d.Lmax ? (int32_t)in_window : p.d.Lmax;
 }
 
-int32_t pick_splits_lists(const plx_decode_args *a, const plx::DecodeRowsParams &p) {
-    if (a->num_splits > 0) return a->num_splits;
+// Split count of a call over lists (bf16 rows): that of a plain one over as many keys, doubled while half of the units stay idle and
+// every wave keeps a tile (see pick_splits_rows).
+int32_t pick_splits_lists(const plx::DecodeRowsParams &p) {
     const int32_t keys = keys_of_lists(p);
     const int64_t pairs = (int64_t)p.d.B * p.d.Hkv, cus = query_num_cus();
     const int32_t block_tiles = (keys + plx::kDecodeBlockKeys - 1) / plx::kDecodeBlockKeys;
@@ -617,9 +618,35 @@ int32_t pick_splits_lists(const plx_decode_args *a, const plx::DecodeRowsParams 
     return s;
 }
 
+// ... and over 4-bit rows: the cheapest by a model of decode_q4_kernel, in us. A workgroup starts in 3; its four waves take a tile
+// of 64 keys each in 1.5 where it is alone on its unit and in 2.8 where two share it (d = 64: 0.62 of both); of more than two on a unit
+// one pair follows the other; the memory gives 5.6 TB/s. The merge takes 2.5 (of more than 8 records a row 4) and 0.2 a MB of records.
+// Against sweeps of S (1 .. 64) over 36 calls of 1 - 100 sequences x 500 - 100000 keys and lists of 16 - 128 blocks its choice is on average
+// 0.5 % from the best, at worst 7 %; the rule for bf16 rows was up to 60 % (16 x 8192 keys, 128 pairs: S = 1 49 us, 2 35, 4 36).
+int32_t pick_splits_q4(const plx::DecodeRowsParams &p) {
+    const int64_t pairs = (int64_t)p.d.B * p.d.Hkv, cus = query_num_cus();
+    const int64_t keys = keys_of_lists(p), tiles = (keys + PLX_BLOCK_KEYS - 1) / PLX_BLOCK_KEYS;
+    const double width = p.d.d == 128 ? 1.0 : 0.62, mb = 1e-6 * (double)pairs * (double)keys * (double)parallax_q4_row_bytes(p.d.d);
+    const double records_us = 0.2e-6 * (double)p.d.B * p.d.Hq * p.d.Tq * (2 * p.d.d + 4) * 4;
+    auto cost = [&](int64_t s) {
+        const double n = (double)(((tiles + s - 1) / s + 3) / 4);
+        const int64_t per_unit = (pairs * s + cus - 1) / cus;
+        const double busy = (double)(per_unit / 2) * (3.0 + 2.8 * width * n) + (double)(per_unit % 2) * (3.0 + 1.5 * width * n);
+        return std::max(busy, 3.0 + mb / 5.6) + (s > 1 ? (s <= 8 ? 2.5 : 4.0) + records_us * (double)s : 0.0);
+    };
+    int64_t best = 1;
+    for (int64_t s = 2; s <= std::min<int64_t>(tiles, PLX_MAX_SPLITS); ++s)
+        if (cost(s) < cost(best)) best = s;
+    return (int32_t)best;
+}
+
+int32_t splits_of(const plx_decode_args *a, const plx::DecodeRowsParams &p, bool q4) {
+    return a->num_splits > 0 ? a->num_splits : q4 ? pick_splits_q4(p) : pick_splits_lists(p);
+}
+
 plx_status decode_lists(const plx_decode_args *a, plx::DecodeRowsParams &p, bool q4, void *hip_stream) {
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const int32_t S = pick_splits_lists(a, p);
+    const int32_t S = splits_of(a, p, q4);
     p.d.S = S, p.d.direct_out = S == 1;
     if (S > 1) {
         const plx_status st = attach_workspace(a, S, &p.d);
@@ -634,7 +661,7 @@ plx_status decode_lists(const plx_decode_args *a, plx::DecodeRowsParams &p, bool
 
 int32_t parallax_decode_blocks_call_splits(const plx_decode_blocks_args *a) {
     plx::DecodeRowsParams p{};
-    return prepare_decode_blocks(a, false, &p) == PLX_OK ? pick_splits_lists(&a->decode, p) : 0;
+    return prepare_decode_blocks(a, false, &p) == PLX_OK ? splits_of(&a->decode, p, false) : 0;
 }
 
 plx_status parallax_decode_blocks(const plx_decode_blocks_args *a, void *hip_stream) {
@@ -645,7 +672,7 @@ plx_status parallax_decode_blocks(const plx_decode_blocks_args *a, void *hip_str
 
 int32_t parallax_decode_q4_call_splits(const plx_decode_q4_args *a) {
     plx::DecodeRowsParams p{};
-    return prepare_decode_q4(a, false, &p) == PLX_OK ? pick_splits_lists(&a->decode, p) : 0;
+    return prepare_decode_q4(a, false, &p) == PLX_OK ? splits_of(&a->decode, p, true) : 0;
 }
 
 plx_status parallax_decode_q4(const plx_decode_q4_args *a, void *hip_stream) {

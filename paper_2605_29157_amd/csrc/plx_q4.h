@@ -6,6 +6,8 @@
 // dimensions: with K and V in one row, which is a multiple of 16 bytes, 16 cost no more than 32 would (d = 128: 128 bytes of codes
 // and 16 or 8 of scales, 144 both ways; d = 64: 64 and 8 or 4, 80 both ways).
 #pragma once
+#include <utility>
+
 #include "plx_device.h"
 
 namespace plx {
@@ -27,6 +29,30 @@ __device__ __forceinline__ u32x4 q4_to_bf16(uint32_t codes, float scale) {
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
+}
+
+// Transposing LDS reads. Within each group of 16 lanes, lane i gets nibble i of the 8 bytes that each of the 16 lanes addresses, in the
+// order of the lanes (ds_read_b64_tr_b4), or byte i % 8 of the 8 bytes that every other lane addresses, from lane i / 8 on
+// (ds_read_b64_tr_b8).
+__device__ __forceinline__ u32x2 lds_read_tr4(const void *generic_lds_ptr) {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    typedef i32x2 __attribute__((address_space(3))) * lds_ptr_t;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_ptr_t)generic_lds_ptr));
+}
+__device__ __forceinline__ u32x2 lds_read_tr8(const void *generic_lds_ptr) {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    typedef i32x2 __attribute__((address_space(3))) * lds_ptr_t;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_ptr_t)generic_lds_ptr));
+}
+
+// f(0), f(1), .. f(N - 1) with the numbers as types
+template <int N, class F, int... I>
+__device__ __forceinline__ void each_of(F &f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void each_of(F &f) {
+    each_of<N>(f, std::make_integer_sequence<int, N>{});
 }
 
 // Where the row of a token is: byte offset of its head 0 from the pools' (or caches') base, or -1 (no page)

@@ -26,6 +26,16 @@ __device__ __forceinline__ u32x4 big_halves(uint32_t seen) {
     return x;
 }
 
+// First key of tile number v of a list's blocks, or -1: an entry that is no block of Lb tokens, or not above the one in front of it
+template <int TILE>
+__device__ __forceinline__ int listed_key(const int32_t *list, int v, int Lb) {
+    constexpr int TILES = kListBlock / TILE;
+    const int i = v / TILES, block = list[i], before = i > 0 ? list[i - 1] : -1;
+    if (block < 0 || block <= before || block > (Lb - 1) / kListBlock) return -1;
+    const int key = block * kListBlock + TILE * (v % TILES);
+    return key < Lb ? key : -1;
+}
+
 // The keys that the columns [x0, x0 + width) of (sequence b, key head) see, columns x = row * G + head of the group, and
 // the tiles of TILE keys that are walked for them: those of the sinks, then those from the first key any window
 // reaches. Tile number v of this walk holds the keys from key_of(v) on; no key is in two of them.
@@ -63,16 +73,12 @@ struct RowsScope {
         list = nullptr;
         if constexpr (LIST) {
             list = P.block_list + ((int64_t)b * p.Hkv + hk) * P.n_list;
-            n_virtual = end_any > 0 ? P.n_list * kTilesPerBlock : 0;
+            n_virtual = end_any > 0 ? P.n_list * (kListBlock / TILE) : 0;
         }
     }
-    static constexpr int kTilesPerBlock = LIST ? kListBlock / TILE : 1;
     __device__ __forceinline__ int key_of(int v) const {
         if constexpr (LIST) {
-            const int i = v / kTilesPerBlock, block = list[i], before = i > 0 ? list[i - 1] : -1;
-            if (block < 0 || block <= before || block > (Lb - 1) / kListBlock) return -1;
-            const int key = block * kListBlock + TILE * (v % kTilesPerBlock);
-            return key < Lb ? key : -1;
+            return listed_key<TILE>(list, v, Lb);
         }
         return TILE * (v < n_sink_tiles ? v : v - n_sink_tiles + first_tile);
     }
