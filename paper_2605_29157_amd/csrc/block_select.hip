@@ -11,6 +11,7 @@
 // a block, 1 / 64 of the cache's) beside 2 D additions in 64 bits a column; the choice, one workgroup a list, latency.
 #include "plx_kernels.h"
 #include "plx_q4.h"
+#include "plx_rows.h"
 
 namespace plx {
 
@@ -33,8 +34,9 @@ __device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
 
 }  // namespace
 
-// One wave a block. A lane has 16 bytes of bf16 (8 dimensions) or 8 bytes of codes (16 dimensions, one scale) of each of its keys.
-template <int D, bool Q4>
+// One wave a block. A lane has 16 bytes of bf16 (8 dimensions) or 8 bytes of codes (16 dimensions, one scale) of each of its keys; all
+// of them are on their way at once. PAGED: lane l looks up key l of the block and hands its place to those that read it.
+template <int D, bool Q4, bool PAGED>
 __global__ __launch_bounds__(256) void cache_bounds_kernel(BlockBounds p) {
     constexpr int DIMS = Q4 ? 16 : 8, LPR = D / DIMS, RPL = 64 / LPR, N = kListBlock / RPL, W = DIMS / 2;
     using Row = Q4Row<D>;
@@ -46,35 +48,39 @@ __global__ __launch_bounds__(256) void cache_bounds_kernel(BlockBounds p) {
     const int j = from + (int)blockIdx.x * 4 + w;
     if ((int)blockIdx.x * 4 + w >= p.most || j >= p.n_blocks || (int64_t)j * kListBlock >= length) return;
     const int row = lane / LPR, part = lane % LPR;
+    const char *keys = p.keys + (PAGED ? 0 : (int64_t)b * p.stride[0]) + h * p.stride[1];
+    int64_t mine = 0;
+    if constexpr (PAGED) {  // (a table entry that is no page: page 0 or the last, as the decode kernels)
+        const int key = min(j * kListBlock + lane, length - 1), page_no = key / p.page_size;
+        const int64_t page = min(max(p.block_table[(int64_t)b * p.table_stride + page_no], 0), p.num_pages - 1);
+        mine = page * p.stride[0] + (int64_t)(key - page_no * p.page_size) * p.stride[2];
+    }
+    u32x4 raw[N];
+    uint32_t scale[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        int64_t at;  // (keys behind the last: that one again)
+        if constexpr (PAGED)
+            at = ((int64_t)__shfl((int)(mine >> 32), RPL * n + row, 64) << 32) | (uint32_t)__shfl((int)mine, RPL * n + row, 64);
+        else
+            at = (int64_t)min(j * kListBlock + RPL * n + row, length - 1) * p.stride[2];
+        if constexpr (Q4) {
+            const u32x2 codes = *(const u32x2 *)(keys + at + 8 * part);
+            raw[n] = u32x4{codes[0], codes[1], 0u, 0u};
+            scale[n] = *(const uint8_t *)(keys + at + Row::kKScale + part);
+        } else {
+            raw[n] = *(const u32x4 *)(keys + at + 16 * part);
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
     uint32_t lo[W], hi[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) lo[i] = 0x7fff7fffu, hi[i] = 0x80008000u;
-    u32x4 raw[N];
-    float scale[N];
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-        // (keys behind the last: that one again. A table entry that is no page: page 0, as the decode kernels)
-        const int key = min(j * kListBlock + RPL * n + row, length - 1);
-        int64_t at = (int64_t)b * p.stride[0] + (int64_t)key * p.stride[2];
-        if (p.block_table != nullptr) {
-            const int page_no = key / p.page_size;
-            const int64_t page = min(max(p.block_table[(int64_t)b * p.table_stride + page_no], 0), p.num_pages - 1);
-            at = page * p.stride[0] + (int64_t)(key - page_no * p.page_size) * p.stride[2];
-        }
-        const char *src = p.keys + at + h * p.stride[1];
-        if constexpr (Q4) {
-            const u32x2 codes = *(const u32x2 *)(src + 8 * part);
-            raw[n] = u32x4{codes[0], codes[1], 0u, 0u};
-            scale[n] = q4_scale(*(const uint8_t *)(src + Row::kKScale + part));
-        } else {
-            raw[n] = *(const u32x4 *)(src + 16 * part);
-        }
-    }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         uint32_t x[W];
         if constexpr (Q4) {
-            const u32x4 a = q4_to_bf16(raw[n][0], scale[n]), c = q4_to_bf16(raw[n][1], scale[n]);
+            const u32x4 a = q4_to_bf16(raw[n][0], q4_scale(scale[n])), c = q4_to_bf16(raw[n][1], q4_scale(scale[n]));
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = c[i];
         } else {
@@ -105,8 +111,6 @@ __global__ __launch_bounds__(256) void cache_bounds_kernel(BlockBounds p) {
 
 namespace {
 
-constexpr int kScoreBlocks = 64;  // blocks of a workgroup of the score kernel, 16 a wave
-
 // Scores as 64-bit integers of the same order; a NaN is the largest score there is
 __device__ __forceinline__ uint64_t score_key(double x) {
     const uint64_t u = __builtin_bit_cast(uint64_t, x);
@@ -114,139 +118,174 @@ __device__ __forceinline__ uint64_t score_key(double x) {
     return u >> 63 ? ~u : u | (1ull << 63);
 }
 
-template <int N>
-__device__ __forceinline__ double lanes_sum(double x) {
+template <int CTRL>
+__device__ __forceinline__ double moved(double x) {  // by a data-parallel-primitive pattern inside a row of 16 lanes
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)u, CTRL, 0xf, 0xf, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, 0xf, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// x[0 .. N) summed over pairs of lanes, half of them in each lane of a pair: upper lanes (bit) keep x[N / 2 ..)
+template <int CTRL, int N>
+__device__ __forceinline__ void halve(double (&x)[N], bool upper) {
 #pragma unroll
-    for (int step = 1; step < N; step <<= 1) x += __shfl_xor(x, step, 64);
-    return x;
+    for (int i = 0; i < N / 2; ++i) {
+        const double keep = upper ? x[N / 2 + i] : x[i], give = upper ? x[i] : x[N / 2 + i];
+        x[i] = keep + moved<CTRL>(give);
+    }
 }
 
-}  // namespace
-
-// A lane has 8 dimensions of a block's bounds and of COLS columns (query rows x heads of the group) at a time.
-template <int D, int COLS>
-__global__ __launch_bounds__(256) void block_score_kernel(BlockSelect p) {
-    constexpr int LPB = D / 8, BPL = 64 / LPB;  // lanes of a block; blocks of a wave at a time
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, part = lane % LPB;
-    const int h = blockIdx.y, b = blockIdx.z;
-    int held = p.n_blocks;
-    if (p.seq_lens != nullptr) held = min((int)(((int64_t)max(p.seq_lens[b], 0) + kListBlock - 1) / kListBlock), held);
-    const int j0 = ((int)blockIdx.x * 4 + w) * (kScoreBlocks / 4);
-    if (j0 >= held || held <= p.keep) return;  // (all are kept)
-    const int G = p.Hq / p.Hkv, n_cols = G * p.Tq;
-    const __bf16 *bounds = (const __bf16 *)p.bounds + ((int64_t)b * p.Hkv + h) * p.n_blocks * 2 * D + 8 * part;
-    uint64_t *keys = p.keys + ((int64_t)b * p.Hkv + h) * p.n_blocks;
-    constexpr int STEPS = kScoreBlocks / 4 / BPL;
-    uint64_t best[STEPS];
+// The bounds of 16 blocks, from `held` on those of the last one: a lane has 8 dimensions
+template <int D>
+struct Bounds16 {
+    static constexpr int LPB = D / 8, BPL = 64 / LPB, STEPS = 16 / BPL;  // lanes of a block; blocks of a wave at a time; times
+    u32x4 lo[STEPS], hi[STEPS];
+    __device__ __forceinline__ void load(const BlockSelect &p, int b, int h, int j0, int held) {
+        const int lane = threadIdx.x & 63;
+        const __bf16 *bounds = (const __bf16 *)p.bounds + ((int64_t)b * p.Hkv + h) * p.n_blocks * 2 * D + 8 * (lane % LPB);
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) best[s] = 0;
+        for (int s = 0; s < STEPS; ++s) {
+            const int j = min(j0 + BPL * s + lane / LPB, held - 1);
+            lo[s] = *(const u32x4 *)(bounds + (int64_t)j * 2 * D), hi[s] = *(const u32x4 *)(bounds + (int64_t)j * 2 * D + D);
+        }
+    }
+};
+// The score's key of one of these blocks, the same for the four lanes from 4 n on, which share it; its number among the 16 is returned.
+// COLS columns (query rows x heads of the group) at a time.
+template <int D, int COLS>
+__device__ __forceinline__ int score_blocks(const BlockSelect &p, int b, int h, const Bounds16<D> &bounds, uint64_t &best) {
+    constexpr int LPB = Bounds16<D>::LPB, BPL = Bounds16<D>::BPL, STEPS = Bounds16<D>::STEPS;
+    const int lane = threadIdx.x & 63, part = lane % LPB;
+    const int G = p.Hq / p.Hkv, n_cols = G * p.Tq;
+    const auto &lo = bounds.lo, &hi = bounds.hi;
+    best = 0;
     for (int x0 = 0; x0 < n_cols; x0 += COLS) {
-        double up[COLS][8], down[COLS][8];
+        double sum[COLS][STEPS];
 #pragma unroll
         for (int c = 0; c < COLS; ++c) {
             const int x = min(x0 + c, n_cols - 1), t = x / G, head = x - t * G;  // (past the last column: that again)
             const u32x4 q = *(const u32x4 *)((const __bf16 *)p.q + (((int64_t)b * p.Hq + (int64_t)h * G + head) * p.Tq + t) * D + 8 * part);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float y0 = bf16_lo_f32(q[i]), y1 = bf16_hi_f32(q[i]);
-                // (a NaN stays one in both)
-                up[c][2 * i] = (double)(y0 < 0.f ? 0.f : y0), down[c][2 * i] = (double)(y0 > 0.f ? 0.f : y0);
-                up[c][2 * i + 1] = (double)(y1 < 0.f ? 0.f : y1), down[c][2 * i + 1] = (double)(y1 > 0.f ? 0.f : y1);
-            }
-        }
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const int j = min(j0 + BPL * s + lane / LPB, held - 1);
-            const u32x4 lo = *(const u32x4 *)(bounds + (int64_t)j * 2 * D), hi = *(const u32x4 *)(bounds + (int64_t)j * 2 * D + D);
-            double sum[COLS];
-#pragma unroll
-            for (int c = 0; c < COLS; ++c) sum[c] = 0.0;
+            for (int s = 0; s < STEPS; ++s) sum[c][s] = 0.0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const double l0 = (double)bf16_lo_f32(lo[i]), l1 = (double)bf16_hi_f32(lo[i]);
-                const double h0 = (double)bf16_lo_f32(hi[i]), h1 = (double)bf16_hi_f32(hi[i]);
+                const double q0 = (double)bf16_lo_f32(q[i]), q1 = (double)bf16_hi_f32(q[i]);
+                // of negative q the smallest key counts
+                const uint32_t down = ((q[i] & 0x8000u) ? 0xffffu : 0u) | ((q[i] & 0x80000000u) ? 0xffff0000u : 0u);
 #pragma unroll
-                for (int c = 0; c < COLS; ++c) {
-                    sum[c] = fma(up[c][2 * i], h0, sum[c]), sum[c] = fma(down[c][2 * i], l0, sum[c]);
-                    sum[c] = fma(up[c][2 * i + 1], h1, sum[c]), sum[c] = fma(down[c][2 * i + 1], l1, sum[c]);
+                for (int s = 0; s < STEPS; ++s) {
+                    const uint32_t y = (lo[s][i] & down) | (hi[s][i] & ~down);
+                    sum[c][s] = fma(q0, (double)bf16_lo_f32(y), sum[c][s]);
+                    sum[c][s] = fma(q1, (double)bf16_hi_f32(y), sum[c][s]);
                 }
             }
+        }
 #pragma unroll
-            for (int c = 0; c < COLS; ++c) {
-                const uint64_t key = score_key(lanes_sum<LPB>(sum[c]));
-                best[s] = key > best[s] ? key : best[s];
+        for (int c = 0; c < COLS; ++c) {
+            double *x = sum[c];
+            if constexpr (D == 128) {
+                halve<0x128, 4>(sum[c], (lane & 8) != 0);                                  // row_ror:8: lane ^ 8
+                double two[2] = {x[0], x[1]};
+                halve<0x141, 2>(two, (lane & 4) != 0);                                     // row_half_mirror: lane ^ 7
+                x[0] = two[0];
+            } else {
+                halve<0x141, 2>(sum[c], (lane & 4) != 0);
             }
+            x[0] += moved<0x4E>(x[0]);  // quad_perm [2, 3, 0, 1]: lane ^ 2
+            x[0] += moved<0xB1>(x[0]);  // quad_perm [1, 0, 3, 2]: lane ^ 1
+            const uint64_t key = score_key(x[0]);
+            best = key > best ? key : best;
         }
     }
+    // a bound that is not finite: the highest, whichever way the queries point
+    uint32_t odd = 0;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-        const int j = j0 + BPL * s + lane / LPB;
-        if (part == 0 && j < held) keys[j] = best[s];
+        uint32_t x = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x |= not_finite_halves(lo[s][i]) | not_finite_halves(hi[s][i]);
+        odd |= x != 0 ? 1u << s : 0u;
     }
+    const int mine = D == 128 ? (lane & 8 ? 2 : 0) + (lane & 4 ? 1 : 0) : (lane & 4 ? 1 : 0);
+    if (__builtin_expect(__any(odd != 0), 0)) {
+#pragma unroll
+        for (int step = 1; step < LPB; step <<= 1) odd |= (uint32_t)__shfl_xor((int)odd, step, 64);
+        if (odd >> mine & 1u) best = 0xfff0000000000000ull;
+    }
+    return BPL * mine + lane / LPB;
 }
 
-namespace {
-constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64;
+__device__ __forceinline__ int held_blocks(const BlockSelect &p, int b) {
+    return p.seq_lens == nullptr ? p.n_blocks : min((int)(((int64_t)max(p.seq_lens[b], 0) + kListBlock - 1) / kListBlock), p.n_blocks);
 }
 
-// The list of one (sequence, key head). Of the blocks between the first and the recent ones the `need` largest keys, found by digits
-// of 8 bits below the highest bit in which they differ; of equal ones the lowest numbers.
-__global__ __launch_bounds__(kPickThreads) void block_pick_kernel(BlockSelect p) {
-    __shared__ uint64_t ends[2][kPickWaves];
-    __shared__ int hist[256];
-    __shared__ int digit_at, digit_above, digit_count;
-    __shared__ int wave_above[kPickWaves], wave_equal[kPickWaves];
+// Blocks up to which one launch does it all, a workgroup reading its list's bounds alone. Two launches / one in a replayed graph, us,
+// d = 128, two columns: 8 lists of 64 blocks 8.8 / 7.1, 128 blocks 8.2 / 7.4, 512 11.7 / 17.2; 128 lists 9.0 / 7.4, 10.1 / 9.0,
+// 16.2 / 17.9; 512 lists 13.9 / 13.3, 17.8 / 15.9, 42.5 / 39.4 (and on a stream the host saves a launch).
+constexpr int kOneLaunchBlocks = 128;
+constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64;
+constexpr int kPickKeys = 4096;  // that are kept in LDS
+constexpr int kDigits = 512;     // values of a digit of 9 bits
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    auto with = [](uint32_t y, auto ctrl) {
+        return max(y, (uint32_t)__builtin_amdgcn_update_dpp((int)y, (int)y, decltype(ctrl)::value, 0xf, 0xf, false));
+    };
+    x = with(x, std::integral_constant<int, 0xB1>{});   // quad_perm [1, 0, 3, 2]
+    x = with(x, std::integral_constant<int, 0x4E>{});   // quad_perm [2, 3, 0, 1]
+    x = with(x, std::integral_constant<int, 0x141>{});  // row_half_mirror
+    x = with(x, std::integral_constant<int, 0x140>{});  // row_mirror
+    const uint32_t a = max((uint32_t)__builtin_amdgcn_readlane((int)x, 0), (uint32_t)__builtin_amdgcn_readlane((int)x, 16));
+    return max(a, max((uint32_t)__builtin_amdgcn_readlane((int)x, 32), (uint32_t)__builtin_amdgcn_readlane((int)x, 48)));
+}
+
+struct PickScratch {
+    uint32_t ends[2][kPickWaves];
+    int hist[kDigits];
+    int digit_at, digit_above, digit_count;
+    int above[kPickWaves], equal[kPickWaves];
+};
+
+// The list of one (sequence, key head) that holds more blocks than are kept. Of those between the first and the recent ones the `need`
+// with the largest keys, found by digits below the highest bit in which they differ; of equal ones the lowest numbers. All
+// kPickThreads threads take part; keys: LDS or memory.
+template <class Keys>
+__device__ __forceinline__ void pick_blocks(const BlockSelect &p, int held, const Keys &keys, int32_t *out, PickScratch &lds) {
     const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
-    const int64_t list = (int64_t)blockIdx.y * p.Hkv + blockIdx.x;
-    int32_t *out = p.block_list + list * p.keep;
-    int held = p.n_blocks;
-    if (p.seq_lens != nullptr) held = min((int)(((int64_t)max(p.seq_lens[blockIdx.y], 0) + kListBlock - 1) / kListBlock), held);
-    if (held <= p.keep) {  // (uniform)
-        for (int i = tid; i < p.keep; i += kPickThreads) out[i] = i < held ? i : -1;
-        return;
-    }
-    const uint64_t *keys = p.keys + list * p.n_blocks;
     const int lo = p.first, hi = held - p.recent;  // candidates
     int need = p.keep - p.first - p.recent;
     for (int i = tid; i < p.first; i += kPickThreads) out[i] = i;
     for (int i = tid; i < p.recent; i += kPickThreads) out[p.keep - p.recent + i] = hi + i;
     if (need == 0) return;  // (uniform)
 
-    // ---- the range of the keys ----------------------------------------------------------------------------
-    uint64_t least = ~0ull, most = 0;
+    // ---- the range of the keys' upper halves ---------------------------------------------------------------
+    uint32_t least = ~0u, most = 0;
     for (int i = lo + tid; i < hi; i += kPickThreads) {
-        const uint64_t k = keys[i];
-        least = k < least ? k : least, most = k > most ? k : most;
+        const uint32_t k = (uint32_t)(keys[i] >> 32);
+        least = min(least, k), most = max(most, k);
     }
-#pragma unroll
-    for (int step = 1; step < 64; step <<= 1) {
-        const uint64_t a = __shfl_xor((unsigned long long)least, step, 64), c = __shfl_xor((unsigned long long)most, step, 64);
-        least = a < least ? a : least, most = c > most ? c : most;
-    }
-    if (lane == 0) ends[0][w] = least, ends[1][w] = most;
+    least = ~wave_max(~least), most = wave_max(most);
+    if (lane == 0) lds.ends[0][w] = least, lds.ends[1][w] = most;
+    for (int i = tid; i < kDigits; i += kPickThreads) lds.hist[i] = 0;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kPickWaves; ++i) {
-        least = ends[0][i] < least ? ends[0][i] : least;
-        most = ends[1][i] > most ? ends[1][i] : most;
-    }
+    for (int i = 0; i < kPickWaves; ++i) least = min(least, lds.ends[0][i]), most = max(most, lds.ends[1][i]);
+    const uint64_t base_key = (uint64_t)least << 32;
     // ---- the smallest key that is kept, digit by digit ------------------------------------------------------
-    // Keys are looked at as key - least; `prefix` are the digits found, `shift` the bits below them.
-    int shift = most == least ? 0 : 64 - __builtin_clzll(most - least);
+    // Keys are looked at as key - base_key; `prefix` are the digits found, `shift` the bits below them.
+    int shift = 64 - __builtin_clz((most - least) | 1u) - (most == least);
     uint64_t prefix = 0;
     while (shift > 0) {
-        const int bits = min(shift, 8), below = shift - bits;
-        for (int i = tid; i < 256; i += kPickThreads) hist[i] = 0;
-        __syncthreads();
+        const int bits = min(shift, 9), below = shift - bits;
         for (int i = lo + tid; i < hi; i += kPickThreads) {
-            const uint64_t k = keys[i] - least;
-            if (shift == 64 || k >> shift == prefix) atomicAdd(&hist[(k >> below) & ((1 << bits) - 1)], 1);
+            const uint64_t k = keys[i] - base_key;
+            if (shift == 64 || k >> shift == prefix) atomicAdd(&lds.hist[(k >> below) & ((1 << bits) - 1)], 1);
         }
         __syncthreads();
-        if (w == 0) {  // lane l: digits 4 l .. 4 l + 3
-            int own[4], sum = 0;
+        if (w == 0) {  // lane l: digits 8 l .. 8 l + 7
+            int own[8], sum = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) own[i] = hist[4 * lane + i], sum += own[i];
+            for (int i = 0; i < 8; ++i) own[i] = lds.hist[8 * lane + i], lds.hist[8 * lane + i] = 0, sum += own[i];
             int above = sum;  // counts of this lane's digits and of those above them
 #pragma unroll
             for (int step = 1; step < 64; step <<= 1) {
@@ -255,35 +294,34 @@ __global__ __launch_bounds__(kPickThreads) void block_pick_kernel(BlockSelect p)
             }
             above -= sum;
 #pragma unroll
-            for (int i = 3; i >= 0; --i) {
-                if (above < need && need <= above + own[i]) digit_at = 4 * lane + i, digit_above = above, digit_count = own[i];
+            for (int i = 7; i >= 0; --i) {
+                if (above < need && need <= above + own[i]) lds.digit_at = 8 * lane + i, lds.digit_above = above, lds.digit_count = own[i];
                 above += own[i];
             }
         }
         __syncthreads();
-        prefix = (prefix << bits) | (uint64_t)digit_at;
-        need -= digit_above;
+        prefix = (prefix << bits) | (uint64_t)lds.digit_at;
+        need -= lds.digit_above;
         shift = below;
-        const bool all = digit_count == need;  // every key of this digit is kept
-        __syncthreads();                       // (hist and the digit are written again)
-        if (all) break;
+        if (lds.digit_count == need) break;  // every key of this digit is kept
+        __syncthreads();                     // (the digit is written again)
     }
     // ---- the list, in ascending order ---------------------------------------------------------------------
     int before_above = 0, before_equal = 0;
     for (int base = lo; base < hi; base += kPickThreads) {
         const int i = base + tid;
         uint64_t k = 0;
-        if (i < hi) k = keys[i] - least;
+        if (i < hi) k = keys[i] - base_key;
         const uint64_t top = shift == 64 ? 0 : k >> shift;
         const bool above = i < hi && top > prefix, equal = i < hi && top == prefix;
         const uint64_t above_mask = __ballot(above), equal_mask = __ballot(equal), mine = (1ull << lane) - 1;
-        if (lane == 0) wave_above[w] = __popcll(above_mask), wave_equal[w] = __popcll(equal_mask);
+        if (lane == 0) lds.above[w] = __popcll(above_mask), lds.equal[w] = __popcll(equal_mask);
         __syncthreads();
         int a = before_above, e = before_equal;
 #pragma unroll
         for (int n = 0; n < kPickWaves; ++n) {
-            if (n < w) a += wave_above[n], e += wave_equal[n];
-            before_above += wave_above[n], before_equal += wave_equal[n];
+            if (n < w) a += lds.above[n], e += lds.equal[n];
+            before_above += lds.above[n], before_equal += lds.equal[n];
         }
         a += __popcll(above_mask & mine), e += __popcll(equal_mask & mine);
         if (above || (equal && e < need)) out[p.first + a + min(e, need)] = i;
@@ -291,38 +329,103 @@ __global__ __launch_bounds__(kPickThreads) void block_pick_kernel(BlockSelect p)
     }
 }
 
-hipError_t launch_cache_bounds(const BlockBounds &p, hipStream_t stream) {
-    const dim3 grid((p.most + 3) / 4, p.Hkv, p.B);
-    if (p.d == 128) {
-        if (p.q4)
-            hipLaunchKernelGGL((cache_bounds_kernel<128, true>), grid, dim3(256), 0, stream, p);
-        else
-            hipLaunchKernelGGL((cache_bounds_kernel<128, false>), grid, dim3(256), 0, stream, p);
+// A sequence with up to `keep` blocks keeps them all
+__device__ __forceinline__ bool all_kept(const BlockSelect &p, int held, int32_t *out) {
+    if (held > p.keep) return false;
+    for (int i = threadIdx.x; i < p.keep; i += blockDim.x) out[i] = i < held ? i : -1;
+    return true;
+}
+
+}  // namespace
+
+// Scores alone, 64 blocks a workgroup. (32 or 64 blocks a wave, all on their way at once: 1 list set of 8 x 512 blocks 9.2 -> 11.0, 14.8
+// with the pick, 128 lists x 2048 34.2 -> 35.3, 41.8.)
+template <int D, int COLS>
+__global__ __launch_bounds__(256) void block_score_kernel(BlockSelect p) {
+    const int h = blockIdx.y, b = blockIdx.z, held = held_blocks(p, b);
+    const int j0 = ((int)blockIdx.x * 4 + (threadIdx.x >> 6)) * 16;
+    if (j0 >= held || held <= p.keep) return;
+    Bounds16<D> bounds;
+    bounds.load(p, b, h, j0, held);
+    uint64_t key;
+    const int j = j0 + score_blocks<D, COLS>(p, b, h, bounds, key);
+    if ((threadIdx.x & 3) == 0 && j < held) p.keys[((int64_t)b * p.Hkv + h) * p.n_blocks + j] = key;
+}
+
+__global__ __launch_bounds__(kPickThreads) void block_pick_kernel(BlockSelect p) {
+    __shared__ PickScratch scratch;
+    __shared__ uint64_t keys[kPickKeys];
+    const int h = blockIdx.x, b = blockIdx.y, held = held_blocks(p, b);
+    const int64_t list = (int64_t)b * p.Hkv + h;
+    int32_t *out = p.block_list + list * p.keep;
+    if (all_kept(p, held, out)) return;
+    const uint64_t *src = p.keys + list * p.n_blocks;
+    if (held > kPickKeys) {
+        pick_blocks(p, held, src, out, scratch);
     } else {
-        if (p.q4)
-            hipLaunchKernelGGL((cache_bounds_kernel<64, true>), grid, dim3(256), 0, stream, p);
-        else
-            hipLaunchKernelGGL((cache_bounds_kernel<64, false>), grid, dim3(256), 0, stream, p);
+        for (int i = threadIdx.x; i < held; i += kPickThreads) keys[i] = src[i];
+        __syncthreads();
+        pick_blocks(p, held, keys, out, scratch);
     }
+}
+
+// Both in one launch, a workgroup a list, for few blocks
+template <int D, int COLS>
+__global__ __launch_bounds__(kPickThreads) void block_select_kernel(BlockSelect p) {
+    __shared__ PickScratch scratch;
+    __shared__ uint64_t keys[kPickKeys];
+    const int h = blockIdx.x, b = blockIdx.y, held = held_blocks(p, b);
+    int32_t *out = p.block_list + ((int64_t)b * p.Hkv + h) * p.keep;
+    if (all_kept(p, held, out)) return;
+    for (int j0 = (threadIdx.x >> 6) * 16; j0 < held; j0 += kPickWaves * 16) {
+        Bounds16<D> bounds;
+        bounds.load(p, b, h, j0, held);
+        uint64_t key;
+        const int j = j0 + score_blocks<D, COLS>(p, b, h, bounds, key);
+        if ((threadIdx.x & 3) == 0 && j < held) keys[j] = key;
+    }
+    __syncthreads();
+    pick_blocks(p, held, keys, out, scratch);
+}
+
+template <int D, bool Q4>
+static void launch_bounds_form(const BlockBounds &p, hipStream_t stream) {
+    const dim3 grid((p.most + 3) / 4, p.Hkv, p.B);
+    if (p.block_table != nullptr)
+        hipLaunchKernelGGL((cache_bounds_kernel<D, Q4, true>), grid, dim3(256), 0, stream, p);
+    else
+        hipLaunchKernelGGL((cache_bounds_kernel<D, Q4, false>), grid, dim3(256), 0, stream, p);
+}
+
+hipError_t launch_cache_bounds(const BlockBounds &p, hipStream_t stream) {
+    if (p.d == 128)
+        p.q4 ? launch_bounds_form<128, true>(p, stream) : launch_bounds_form<128, false>(p, stream);
+    else
+        p.q4 ? launch_bounds_form<64, true>(p, stream) : launch_bounds_form<64, false>(p, stream);
+    return hipGetLastError();
+}
+
+template <int D, int COLS>
+static hipError_t launch_select_form(const BlockSelect &p, hipStream_t stream) {
+    const dim3 lists(p.Hkv, p.B);
+    if (p.n_blocks <= kOneLaunchBlocks) {
+        hipLaunchKernelGGL((block_select_kernel<D, COLS>), lists, dim3(kPickThreads), 0, stream, p);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((block_score_kernel<D, COLS>), dim3((p.n_blocks + 63) / 64, p.Hkv, p.B), dim3(256), 0, stream, p);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    hipLaunchKernelGGL(block_pick_kernel, lists, dim3(kPickThreads), 0, stream, p);
     return hipGetLastError();
 }
 
 template <int D>
-static void launch_scores(const BlockSelect &p, hipStream_t stream) {
-    const dim3 grid((p.n_blocks + kScoreBlocks - 1) / kScoreBlocks, p.Hkv, p.B);
-    const int cols = p.Hq / p.Hkv * p.Tq;
-    if (cols == 1)
-        hipLaunchKernelGGL((block_score_kernel<D, 1>), grid, dim3(256), 0, stream, p);
-    else
-        hipLaunchKernelGGL((block_score_kernel<D, 2>), grid, dim3(256), 0, stream, p);
+static hipError_t launch_select_columns(const BlockSelect &p, hipStream_t stream) {
+    return p.Hq / p.Hkv * p.Tq == 1 ? launch_select_form<D, 1>(p, stream) : launch_select_form<D, 2>(p, stream);
 }
 
 hipError_t launch_select_blocks(const BlockSelect &p, hipStream_t stream) {
-    p.d == 128 ? launch_scores<128>(p, stream) : launch_scores<64>(p, stream);
-    const hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
-    hipLaunchKernelGGL(block_pick_kernel, dim3(p.Hkv, p.B), dim3(kPickThreads), 0, stream, p);
-    return hipGetLastError();
+    return p.d == 128 ? launch_select_columns<128>(p, stream) : launch_select_columns<64>(p, stream);
 }
 
 }  // namespace plx

@@ -5,8 +5,9 @@
 // relative error of a row: 0.110; with s <= max / 4 < 2 s, whose largest magnitudes saturate at 6, 0.118; with max / s <= 6 0.113; 32
 // dimensions to a scale 0.112 - 0.115.) x / s is exact, so the one rounding is that to the code, to nearest, ties to even.
 //
-// What bounds them: the bytes of the rows, 4 D of bf16 and 9 D / 8 of the cache; few rows: one launch. A thread has 16 dimensions, one
-// scale: no exchange between lanes.
+// What bounds them: the bytes of the rows, 4 D of bf16 and 9 D / 8 of the cache; few rows: one launch. A thread has 8 dimensions (16 bytes
+// of bf16) of each of its rows, two neighbours share a scale, and the scale bytes of eight threads are put together, so that
+// a row goes out in whole dwords. Many rows: four a thread, all on their way at once.
 #include "plx_kernels.h"
 #include "plx_q4.h"
 
@@ -14,120 +15,150 @@ namespace plx {
 
 namespace {
 
-// Thread -> (row, K or V, 16 of its dimensions)
+// bf16 rows from which a thread takes four: us, written / read, one a thread and four: 1600 rows of d = 128 2.9 / 3.0 and 3.9 / 3.9, 16000
+// 5.0 / 5.1 and 5.0 / 5.4, 32000 7.4 / 7.5 and 7.1 / 7.4, 262144 (172 MB) 42 / 42 and 36 / 35. (fp32, which has twice the bytes
+// on their way: 131072 rows 29 / 39 and 30 / 43.)
+constexpr int64_t kManyRows = 32000;
+
+// Thread -> (K or V, 8 of its dimensions) of the rows row0, row0 + step, ..
 template <int D>
 struct Q4Place {
-    static constexpr int kGroups = D / 16, kThreads = 2 * kGroups;  // of a tensor's row; of a row
-    int b, h, t, group;
-    bool is_v, any;
-    __device__ __forceinline__ Q4Place(const Q4Rows &p) {
-        const int64_t row = (int64_t)blockIdx.x * (256 / kThreads) + threadIdx.x / kThreads;
-        const int part = threadIdx.x % kThreads;
-        is_v = part >= kGroups, group = part % kGroups;
+    static constexpr int kLanes = D / 8, kThreads = 2 * kLanes;  // of a tensor's row; of a row
+    static constexpr int kRows = 256 / kThreads;                 // of a workgroup at a time
+    int part;
+    bool is_v;
+    __device__ __forceinline__ Q4Place() : part(threadIdx.x % kLanes), is_v(threadIdx.x / kLanes % 2 != 0) {}
+};
+struct Q4Token {
+    int b, h, t;
+    bool any;
+    __device__ __forceinline__ Q4Token(const Q4Rows &p, int64_t row) {
         any = row < (int64_t)p.cache.B * p.cache.Hkv * p.T;
-        const int64_t bh = row / p.T;
-        t = (int)(row - bh * p.T);
-        b = (int)(bh / p.cache.Hkv), h = (int)(bh - (int64_t)b * p.cache.Hkv);
+        const uint32_t r = any ? (uint32_t)row : 0, bh = r / (uint32_t)p.T;
+        t = (int)(r - bh * p.T);
+        b = (int)(bh / p.cache.Hkv), h = (int)(bh - b * p.cache.Hkv);
     }
-    // byte offset of this row in the cache, or -1
+    // byte offset of a token's row in the cache, or -1
     __device__ __forceinline__ int64_t row_of(const Q4Rows &p, int64_t token) const {
         const Q4Cache &c = p.cache;
         if (token < 0 || token >= c.capacity) return -1;
         const int64_t at = q4_token_offset(c.block_table, c.table_stride, c.page_size, c.num_pages, c.stride, b, token);
         return at < 0 ? -1 : at + h * c.stride[1];
     }
-    __device__ __forceinline__ int64_t element(const Q4Rows &p) const {  // of this thread's dimensions in k or v
-        const int64_t(&s)[3] = is_v ? p.vs : p.ks;
-        return b * s[0] + h * s[1] + t * s[2] + 16 * group;
-    }
+    __device__ __forceinline__ int64_t element(const int64_t (&s)[3]) const { return b * s[0] + h * s[1] + t * s[2]; }
 };
 
 }  // namespace
 
-template <int D, bool F32>
+template <int D, bool F32, int ROWS>
 __global__ __launch_bounds__(256) void cache_write_q4_kernel(Q4Rows p) {
     using Row = Q4Row<D>;
-    const Q4Place<D> me(p);
-    if (!me.any || (p.counts != nullptr && me.t >= p.counts[me.b])) return;
-    const int64_t at = me.row_of(p, (int64_t)(p.start != nullptr ? p.start[me.b] : 0) + me.t);
-    if (at < 0) return;
-    float x[16];
+    using Place = Q4Place<D>;
+    const Place me;
+    const int64_t row0 = (int64_t)blockIdx.x * (Place::kRows * ROWS) + threadIdx.x / Place::kThreads;
     const void *src = me.is_v ? p.v : p.k;
-    if constexpr (F32) {
+    int64_t at[ROWS];
+    u32x4 raw[ROWS];
+    f32x4 wide[ROWS][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 y = *(const f32x4 *)((const float *)src + me.element(p) + 4 * i);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * i + e] = y[e];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const u32x4 y = *(const u32x4 *)((const __bf16 *)src + me.element(p) + 8 * i);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[8 * i + 2 * e] = bf16_lo_f32(y[e]), x[8 * i + 2 * e + 1] = bf16_hi_f32(y[e]);
+    for (int i = 0; i < ROWS; ++i) {
+        const Q4Token x(p, row0 + Place::kRows * i);
+        const bool counted = x.any && (p.counts == nullptr || x.t < p.counts[x.b]);
+        at[i] = counted ? x.row_of(p, (int64_t)(p.start != nullptr ? p.start[x.b] : 0) + x.t) : -1;
+        const int64_t e = x.element(me.is_v ? p.vs : p.ks) + 8 * me.part;
+        if constexpr (F32) {
+            wide[i][0] = *(const f32x4 *)((const float *)src + e), wide[i][1] = *(const f32x4 *)((const float *)src + e + 4);
+        } else {
+            raw[i] = *(const u32x4 *)((const __bf16 *)src + e);
         }
     }
-    uint32_t top = 0;  // of the magnitudes' bits: infinities and NaN are the largest
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, __builtin_bit_cast(uint32_t, x[i]) & 0x7fffffffu);
-    const bool bad = top >= 0x7f800000u;
-    const uint32_t e = (uint32_t)min(max((int)((top + 0x200000u) >> 23) - 2, 4), 252);
-    const float scale = q4_scale(e);
-    u32x2 codes = {0u, 0u};
+    for (int i = 0; i < ROWS; ++i) {
+        float x[8];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        uint32_t c = 0;
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[8 * i + 0], x[8 * i + 1], scale, 0);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[8 * i + 2], x[8 * i + 3], scale, 1);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[8 * i + 4], x[8 * i + 5], scale, 2);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[8 * i + 6], x[8 * i + 7], scale, 3);
-        codes[i] = bad ? 0u : c;
-    }
-    char *row = p.cache.rows + at;
-    *(u32x2 *)(row + (me.is_v ? Row::kV : 0) + 8 * me.group) = codes;
-    *(uint8_t *)(row + (me.is_v ? Row::kVScale : Row::kKScale) + me.group) = (uint8_t)(bad ? 255u : e);
-    if constexpr (Row::kBytes > Row::kEnd) {
-        static_assert(Row::kBytes - Row::kEnd == 8 && Row::kEnd % 8 == 0, "one store");
-        if (me.is_v && me.group == 0) *(u32x2 *)(row + Row::kEnd) = u32x2{0u, 0u};
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (F32)
+                x[e] = wide[i][0][e], x[4 + e] = wide[i][1][e];
+            else
+                x[2 * e] = bf16_lo_f32(raw[i][e]), x[2 * e + 1] = bf16_hi_f32(raw[i][e]);
+        }
+        uint32_t top = 0;  // of the magnitudes' bits: infinities and NaN are the largest
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __builtin_bit_cast(uint32_t, x[e]) & 0x7fffffffu);
+        top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, true));  // quad_perm [1, 0, 3, 2]
+        const bool bad = top >= 0x7f800000u;
+        const uint32_t e = (uint32_t)min(max((int)((top + 0x200000u) >> 23) - 2, 4), 252);
+        const float scale = q4_scale(e);
+        uint32_t codes = 0;
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], scale, 0);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], scale, 1);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], scale, 2);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], scale, 3);
+        uint32_t scales = (bad ? 255u : e) << (8 * (me.part / 2 & 3));  // four scales of eight lanes
+        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x4E, 0xf, 0xf, true);   // quad_perm [2, 3, 0, 1]
+        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x141, 0xf, 0xf, true);  // row_half_mirror
+        if (at[i] < 0) continue;
+        char *row = p.cache.rows + at[i];
+        *(uint32_t *)(row + (me.is_v ? Row::kV : 0) + 4 * me.part) = bad ? 0u : codes;
+        if (me.part % 8 == 0) *(uint32_t *)(row + (me.is_v ? Row::kVScale : Row::kKScale) + me.part / 2) = scales;
+        if constexpr (Row::kBytes > Row::kEnd) {
+            static_assert(Row::kBytes - Row::kEnd == 8, "one store");
+            if (me.is_v && me.part == 1) *(u32x2 *)(row + Row::kEnd) = u32x2{0u, 0u};
+        }
     }
 }
 
-template <int D, bool F32>
+template <int D, bool F32, int ROWS>
 __global__ __launch_bounds__(256) void cache_read_q4_kernel(Q4Rows p) {
     using Row = Q4Row<D>;
-    const Q4Place<D> me(p);
-    if (!me.any) return;
-    const int64_t token = (int64_t)(p.start != nullptr ? p.start[me.b] : 0) + me.t;
-    const int64_t at = p.counts != nullptr && token >= p.counts[me.b] ? -1 : me.row_of(p, token);
-    u32x4 y[2] = {{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
-    if (at >= 0) {
-        const char *row = p.cache.rows + at;
-        const u32x2 codes = *(const u32x2 *)(row + (me.is_v ? Row::kV : 0) + 8 * me.group);
-        const float scale = q4_scale(*(const uint8_t *)(row + (me.is_v ? Row::kVScale : Row::kKScale) + me.group));
-        y[0] = q4_to_bf16(codes[0], scale), y[1] = q4_to_bf16(codes[1], scale);
+    using Place = Q4Place<D>;
+    const Place me;
+    const int64_t row0 = (int64_t)blockIdx.x * (Place::kRows * ROWS) + threadIdx.x / Place::kThreads;
+    uint32_t codes[ROWS], scales[ROWS];
+    int64_t to[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const Q4Token x(p, row0 + Place::kRows * i);
+        const int64_t token = (int64_t)(p.start != nullptr ? p.start[x.b] : 0) + x.t;
+        const int64_t at = p.counts != nullptr && token >= p.counts[x.b] ? -1 : x.row_of(p, token);
+        codes[i] = scales[i] = 0;
+        if (x.any && at >= 0) {
+            const char *row = p.cache.rows + at;
+            codes[i] = *(const uint32_t *)(row + (me.is_v ? Row::kV : 0) + 4 * me.part);
+            scales[i] = *(const uint8_t *)(row + (me.is_v ? Row::kVScale : Row::kKScale) + me.part / 2);
+        }
+        to[i] = x.any ? x.element(me.is_v ? p.vs : p.ks) + 8 * me.part : -1;
     }
     void *dst = me.is_v ? p.v : p.k;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
+        if (to[i] < 0) continue;
+        const u32x4 y = q4_to_bf16(codes[i], q4_scale(scales[i]));
         if constexpr (F32) {
-            float *out = (float *)dst + me.element(p) + 8 * i;
-            *(f32x4 *)out = f32x4{bf16_lo_f32(y[i][0]), bf16_hi_f32(y[i][0]), bf16_lo_f32(y[i][1]), bf16_hi_f32(y[i][1])};
-            *(f32x4 *)(out + 4) = f32x4{bf16_lo_f32(y[i][2]), bf16_hi_f32(y[i][2]), bf16_lo_f32(y[i][3]), bf16_hi_f32(y[i][3])};
+            float *out = (float *)dst + to[i];
+            *(f32x4 *)out = f32x4{bf16_lo_f32(y[0]), bf16_hi_f32(y[0]), bf16_lo_f32(y[1]), bf16_hi_f32(y[1])};
+            *(f32x4 *)(out + 4) = f32x4{bf16_lo_f32(y[2]), bf16_hi_f32(y[2]), bf16_lo_f32(y[3]), bf16_hi_f32(y[3])};
         } else {
-            *(u32x4 *)((__bf16 *)dst + me.element(p) + 8 * i) = y[i];
+            *(u32x4 *)((__bf16 *)dst + to[i]) = y;
         }
     }
+}
+
+template <int D, bool F32, int ROWS>
+static void launch_rows_q4_form(const Q4Rows &p, bool write, hipStream_t stream) {
+    constexpr int64_t PER = Q4Place<D>::kRows * ROWS;
+    const dim3 grid((unsigned)(((int64_t)p.cache.B * p.cache.Hkv * p.T + PER - 1) / PER));
+    if (write)
+        hipLaunchKernelGGL((cache_write_q4_kernel<D, F32, ROWS>), grid, dim3(256), 0, stream, p);
+    else
+        hipLaunchKernelGGL((cache_read_q4_kernel<D, F32, ROWS>), grid, dim3(256), 0, stream, p);
 }
 
 template <int D, bool F32>
 static void launch_rows_q4(const Q4Rows &p, bool write, hipStream_t stream) {
-    constexpr int64_t PER = 256 / Q4Place<D>::kThreads;
-    const dim3 grid((unsigned)(((int64_t)p.cache.B * p.cache.Hkv * p.T + PER - 1) / PER));
-    if (write)
-        hipLaunchKernelGGL((cache_write_q4_kernel<D, F32>), grid, dim3(256), 0, stream, p);
-    else
-        hipLaunchKernelGGL((cache_read_q4_kernel<D, F32>), grid, dim3(256), 0, stream, p);
+    if constexpr (!F32)
+        if ((int64_t)p.cache.B * p.cache.Hkv * p.T >= kManyRows) return launch_rows_q4_form<D, F32, 4>(p, write, stream);
+    launch_rows_q4_form<D, F32, 1>(p, write, stream);
 }
 
 static hipError_t launch_rows_q4(const Q4Rows &p, bool write, hipStream_t stream) {
