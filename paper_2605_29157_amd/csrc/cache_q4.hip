@@ -5,9 +5,12 @@
 // relative error of a row: 0.110; with s <= max / 4 < 2 s, whose largest magnitudes saturate at 6, 0.118; with max / s <= 6 0.113; 32
 // dimensions to a scale 0.112 - 0.115.) x / s is exact, so the one rounding is that to the code, to nearest, ties to even.
 //
-// What bounds them: the bytes of the rows, 4 D of bf16 and 9 D / 8 of the cache; few rows: one launch. A thread has 8 dimensions (16 bytes
-// of bf16) of each of its rows, two neighbours share a scale, and the scale bytes of eight threads are put together, so that
-// a row goes out in whole dwords. Many rows: four a thread, all on their way at once.
+// What bounds them: the bytes of the rows, 4 D of bf16 and 9 D / 8 of the cache; few rows: one launch. A thread has 16 bytes
+// of bf16 of each of its rows, two neighbours share a scale, and the scale bytes of eight threads are put together, so that
+// a row goes out in whole dwords. Many rows: four a thread, all on their way at once, of one sequence and head, whose numbers, first token
+// and count are the workgroup's: with divisions by T, Hkv and the page size a row (the last in 64 bits) a kernel that moves 172 MB
+// through pages of 16 took 47 us to write and 55 to read, now 37 and 27 (4.7, 6.5 TB/s). K and V pass through once and are asked for and stored
+// as such: read back 34 without, and 38 written.
 #include "plx_kernels.h"
 #include "plx_q4.h"
 
@@ -15,29 +18,36 @@ namespace plx {
 
 namespace {
 
-// bf16 rows from which a thread takes four: us, written / read, one a thread and four: 1600 rows of d = 128 2.9 / 3.0 and 3.9 / 3.9, 16000
-// 5.0 / 5.1 and 5.0 / 5.4, 32000 7.4 / 7.5 and 7.1 / 7.4, 262144 (172 MB) 42 / 42 and 36 / 35. (fp32, which has twice the bytes
-// on their way: 131072 rows 29 / 39 and 30 / 43.)
+// Rows from which a thread takes four: us, written / read, one a thread and four: d = 128 3200 rows 3.0 / 3.1 and 3.9 / 3.7, 16000
+// 5.0 / 4.4 and 4.9 / 4.4, 32000 7.7 / 6.2 and 6.8 / 5.6, 262144 (172 MB) 42 / 30 and 35 / 28; fp32 131072 29 / 29 and 31 / 26. And
+// tokens of a sequence from which it does, in workgroups: 33 tokens (two workgroups of 32) 8.0 / 6.4 and 8.9 / 7.2, 64 12.9 / 9.4 and 10.7 / 9.0.
 constexpr int64_t kManyRows = 32000;
+constexpr int kManyRuns = 2;
 
-// Thread -> (K or V, 8 of its dimensions) of the rows row0, row0 + step, ..
-template <int D>
+// Thread -> (K or V, DIMS of its dimensions) of ROWS rows: of one row in the order of (b, h, t), or of tokens that follow one another at a
+// distance in one sequence and head, whose numbers are then the workgroup's
+template <int D, int ROWS, int DIMS = 8>
 struct Q4Place {
-    static constexpr int kLanes = D / 8, kThreads = 2 * kLanes;  // of a tensor's row; of a row
+    static constexpr int kLanes = D / DIMS, kThreads = 2 * kLanes;  // of a tensor's row; of a row
     static constexpr int kRows = 256 / kThreads;                 // of a workgroup at a time
-    int part;
-    bool is_v;
-    __device__ __forceinline__ Q4Place() : part(threadIdx.x % kLanes), is_v(threadIdx.x / kLanes % 2 != 0) {}
-};
-struct Q4Token {
-    int b, h, t;
-    bool any;
-    __device__ __forceinline__ Q4Token(const Q4Rows &p, int64_t row) {
-        any = row < (int64_t)p.cache.B * p.cache.Hkv * p.T;
-        const uint32_t r = any ? (uint32_t)row : 0, bh = r / (uint32_t)p.T;
-        t = (int)(r - bh * p.T);
-        b = (int)(bh / p.cache.Hkv), h = (int)(bh - b * p.cache.Hkv);
+    static constexpr int kTokens = kRows * ROWS;                 // of a workgroup
+    int part, b, h, t;
+    bool is_v, any;
+    __device__ __forceinline__ Q4Place(const Q4Rows &p) : part(threadIdx.x % kLanes), is_v(threadIdx.x / kLanes % 2 != 0) {
+        uint32_t bh;
+        if constexpr (ROWS == 1) {
+            const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kThreads;
+            any = row < (int64_t)p.cache.B * p.cache.Hkv * p.T;
+            const uint32_t r = any ? (uint32_t)row : 0;
+            bh = r / (uint32_t)p.T, t = (int)(r - bh * p.T);
+        } else {
+            const uint32_t runs = ((uint32_t)p.T + kTokens - 1) / kTokens;
+            bh = blockIdx.x / runs, t = (int)((blockIdx.x - bh * runs) * kTokens + threadIdx.x / kThreads), any = true;
+        }
+        b = (int)(bh / (uint32_t)p.cache.Hkv), h = (int)(bh - b * p.cache.Hkv);
     }
+    __device__ __forceinline__ int token(int i) const { return t + kRows * i; }
+    __device__ __forceinline__ bool has(const Q4Rows &p, int i) const { return any && (ROWS == 1 || token(i) < p.T); }
     // byte offset of a token's row in the cache, or -1
     __device__ __forceinline__ int64_t row_of(const Q4Rows &p, int64_t token) const {
         const Q4Cache &c = p.cache;
@@ -45,7 +55,7 @@ struct Q4Token {
         const int64_t at = q4_token_offset(c.block_table, c.table_stride, c.page_size, c.num_pages, c.stride, b, token);
         return at < 0 ? -1 : at + h * c.stride[1];
     }
-    __device__ __forceinline__ int64_t element(const int64_t (&s)[3]) const { return b * s[0] + h * s[1] + t * s[2]; }
+    __device__ __forceinline__ int64_t element(const int64_t (&s)[3], int i) const { return b * s[0] + h * s[1] + token(i) * s[2] + DIMS * part; }
 };
 
 }  // namespace
@@ -53,24 +63,26 @@ struct Q4Token {
 template <int D, bool F32, int ROWS>
 __global__ __launch_bounds__(256) void cache_write_q4_kernel(Q4Rows p) {
     using Row = Q4Row<D>;
-    using Place = Q4Place<D>;
-    const Place me;
-    const int64_t row0 = (int64_t)blockIdx.x * (Place::kRows * ROWS) + threadIdx.x / Place::kThreads;
+    const Q4Place<D, ROWS> me(p);
+    const int64_t start = p.start != nullptr ? p.start[me.b] : 0;
+    const int count = p.counts != nullptr ? p.counts[me.b] : p.T;
     const void *src = me.is_v ? p.v : p.k;
     int64_t at[ROWS];
     u32x4 raw[ROWS];
     f32x4 wide[ROWS][2];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-        const Q4Token x(p, row0 + Place::kRows * i);
-        const bool counted = x.any && (p.counts == nullptr || x.t < p.counts[x.b]);
-        at[i] = counted ? x.row_of(p, (int64_t)(p.start != nullptr ? p.start[x.b] : 0) + x.t) : -1;
-        const int64_t e = x.element(me.is_v ? p.vs : p.ks) + 8 * me.part;
+        at[i] = -1;
+        wide[i][0] = wide[i][1] = f32x4{};
+        raw[i] = u32x4{};
+        if (!me.has(p, i)) continue;
+        const int64_t e = me.element(me.is_v ? p.vs : p.ks, i);
         if constexpr (F32) {
             wide[i][0] = *(const f32x4 *)((const float *)src + e), wide[i][1] = *(const f32x4 *)((const float *)src + e + 4);
         } else {
-            raw[i] = *(const u32x4 *)((const __bf16 *)src + e);
+            raw[i] = __builtin_nontemporal_load((const u32x4 *)((const __bf16 *)src + e));
         }
+        if (me.token(i) < count) at[i] = me.row_of(p, start + me.token(i));
     }
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
@@ -111,54 +123,60 @@ __global__ __launch_bounds__(256) void cache_write_q4_kernel(Q4Rows p) {
 template <int D, bool F32, int ROWS>
 __global__ __launch_bounds__(256) void cache_read_q4_kernel(Q4Rows p) {
     using Row = Q4Row<D>;
-    using Place = Q4Place<D>;
-    const Place me;
-    const int64_t row0 = (int64_t)blockIdx.x * (Place::kRows * ROWS) + threadIdx.x / Place::kThreads;
+    constexpr int DIMS = F32 ? 4 : 8;  // 16 bytes to store: halves of a line go to memory apart (fp32, eight: 66 us)
+    using Codes = std::conditional_t<F32, uint16_t, uint32_t>;
+    const Q4Place<D, ROWS, DIMS> me(p);
+    const int64_t start = p.start != nullptr ? p.start[me.b] : 0;
+    const int64_t count = p.counts != nullptr ? p.counts[me.b] : p.cache.capacity;
     uint32_t codes[ROWS], scales[ROWS];
     int64_t to[ROWS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-        const Q4Token x(p, row0 + Place::kRows * i);
-        const int64_t token = (int64_t)(p.start != nullptr ? p.start[x.b] : 0) + x.t;
-        const int64_t at = p.counts != nullptr && token >= p.counts[x.b] ? -1 : x.row_of(p, token);
-        codes[i] = scales[i] = 0;
-        if (x.any && at >= 0) {
+        codes[i] = scales[i] = 0, to[i] = -1;
+        if (!me.has(p, i)) continue;
+        const int64_t token = start + me.token(i), at = token < count ? me.row_of(p, token) : -1;
+        if (at >= 0) {
             const char *row = p.cache.rows + at;
-            codes[i] = *(const uint32_t *)(row + (me.is_v ? Row::kV : 0) + 4 * me.part);
-            scales[i] = *(const uint8_t *)(row + (me.is_v ? Row::kVScale : Row::kKScale) + me.part / 2);
+            codes[i] = *(const Codes *)(row + (me.is_v ? Row::kV : 0) + DIMS / 2 * me.part);
+            scales[i] = *(const uint8_t *)(row + (me.is_v ? Row::kVScale : Row::kKScale) + me.part / (16 / DIMS));
         }
-        to[i] = x.any ? x.element(me.is_v ? p.vs : p.ks) + 8 * me.part : -1;
+        to[i] = me.element(me.is_v ? p.vs : p.ks, i);
     }
     void *dst = me.is_v ? p.v : p.k;
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         if (to[i] < 0) continue;
         const u32x4 y = q4_to_bf16(codes[i], q4_scale(scales[i]));
-        if constexpr (F32) {
-            float *out = (float *)dst + to[i];
-            *(f32x4 *)out = f32x4{bf16_lo_f32(y[0]), bf16_hi_f32(y[0]), bf16_lo_f32(y[1]), bf16_hi_f32(y[1])};
-            *(f32x4 *)(out + 4) = f32x4{bf16_lo_f32(y[2]), bf16_hi_f32(y[2]), bf16_lo_f32(y[3]), bf16_hi_f32(y[3])};
-        } else {
-            *(u32x4 *)((__bf16 *)dst + to[i]) = y;
-        }
+        if constexpr (F32)
+            __builtin_nontemporal_store(f32x4{bf16_lo_f32(y[0]), bf16_hi_f32(y[0]), bf16_lo_f32(y[1]), bf16_hi_f32(y[1])},
+                                        (f32x4 *)((float *)dst + to[i]));
+        else
+            __builtin_nontemporal_store(y, (u32x4 *)((__bf16 *)dst + to[i]));
     }
+}
+
+template <class Place>
+static dim3 grid_rows_q4(const Q4Rows &p, int rows) {
+    const int64_t heads = (int64_t)p.cache.B * p.cache.Hkv;
+    return dim3((unsigned)(rows == 1 ? (heads * p.T + Place::kRows - 1) / Place::kRows : heads * ((p.T + Place::kTokens - 1) / Place::kTokens)));
 }
 
 template <int D, bool F32, int ROWS>
 static void launch_rows_q4_form(const Q4Rows &p, bool write, hipStream_t stream) {
-    constexpr int64_t PER = Q4Place<D>::kRows * ROWS;
-    const dim3 grid((unsigned)(((int64_t)p.cache.B * p.cache.Hkv * p.T + PER - 1) / PER));
+    using Written = Q4Place<D, ROWS>;
+    using Read = Q4Place<D, ROWS, F32 ? 4 : 8>;
     if (write)
-        hipLaunchKernelGGL((cache_write_q4_kernel<D, F32, ROWS>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((cache_write_q4_kernel<D, F32, ROWS>), grid_rows_q4<Written>(p, ROWS), dim3(256), 0, stream, p);
     else
-        hipLaunchKernelGGL((cache_read_q4_kernel<D, F32, ROWS>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((cache_read_q4_kernel<D, F32, ROWS>), grid_rows_q4<Read>(p, ROWS), dim3(256), 0, stream, p);
 }
 
 template <int D, bool F32>
 static void launch_rows_q4(const Q4Rows &p, bool write, hipStream_t stream) {
-    if constexpr (!F32)
-        if ((int64_t)p.cache.B * p.cache.Hkv * p.T >= kManyRows) return launch_rows_q4_form<D, F32, 4>(p, write, stream);
-    launch_rows_q4_form<D, F32, 1>(p, write, stream);
+    if (p.T >= kManyRuns * Q4Place<D, 4>::kTokens && (int64_t)p.cache.B * p.cache.Hkv * p.T >= kManyRows)
+        launch_rows_q4_form<D, F32, 4>(p, write, stream);
+    else
+        launch_rows_q4_form<D, F32, 1>(p, write, stream);
 }
 
 static hipError_t launch_rows_q4(const Q4Rows &p, bool write, hipStream_t stream) {

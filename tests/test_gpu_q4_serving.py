@@ -279,3 +279,31 @@ def test_refusals_of_the_binding(plx):  # noqa: F811
         with pytest.raises((ValueError, TypeError, RuntimeError)):
             call()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("d,page", [(128, 0), (128, 24), (64, 1), (64, 64)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_many_rows_are_as_few(plx, d, page, dtype):  # noqa: F811
+    """More rows than a launch takes one by one, ragged: the bytes and rows that calls over 50 tokens give."""
+    B, Hkv, T, room = 3, 8, 1700, 1800
+    k, v = (_normal((B, Hkv, T, d), s).to(dtype) for s in (1, 2))
+    k[1, 2, 1699, 3] = float("inf")
+    start, counts = _ints([0, 99, 500]), _ints([T, 1699, T])  # (of the last 400 tokens have no room)
+    more, shape = {}, (B, Hkv, room)
+    if page:
+        per = -(-room // page)
+        table = torch.from_numpy(np.random.default_rng(3).permutation(B * per).astype(np.int32).reshape(B, per)).to(DEV)
+        table[0, 1] = -1
+        more, shape = dict(block_table=table), (B * per, Hkv, page)
+    many = torch.full((*shape, blocks.row_bytes(d)), 0x11, dtype=torch.uint8, device=DEV)
+    few = many.clone()
+    plx.parallax_cache_write_q4(k, v, many, start=start, counts=counts, **more)
+    for t in range(0, T, 50):
+        plx.parallax_cache_write_q4(k[:, :, t: t + 50], v[:, :, t: t + 50], few, start=start + t, counts=(counts - t).clamp(0, 50), **more)
+    assert torch.equal(many, few)
+    lens = _ints([room - 3, 1700, room])
+    at = dict(seq_lens=lens, dtype=dtype, **more)
+    got = plx.parallax_cache_read_q4(many, d, T, start=start, **at)
+    for t in range(0, T, 50):
+        part = plx.parallax_cache_read_q4(many, d, 50, start=start + t, **at)
+        assert all(torch.equal(a[:, :, t: t + 50].view(torch.uint8), b.view(torch.uint8)) for a, b in zip(got, part)), t
