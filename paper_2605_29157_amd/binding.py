@@ -246,11 +246,11 @@ def _filled(args, *values):
 
 
 def _f32(x) -> float:  # (as a C float takes it: too large becomes infinite, not an error here)
-    return ctypes.c_float(float(x)).value
+    return x if type(x) is float and -3.4e38 < x < 3.4e38 else ctypes.c_float(float(x)).value
 
 
 def _i32(x) -> int:  # (as a C int takes it)
-    return ctypes.c_int32(int(x)).value
+    return x if type(x) is int and -0x80000000 <= x < 0x80000000 else ctypes.c_int32(int(x)).value
 
 
 class ParallaxError(RuntimeError):
@@ -522,8 +522,8 @@ def parallax_decode_num_splits(B, Hq, Hkv, Lmax, d, num_cus=0) -> int:
 
 
 def decode_args(q, r, k, v, out, scale, seq_lens=None, use_r=True, num_splits=0, workspace=None,
-                block_table=None, max_len=None, window=0):
-    """Fill a plx_decode_args from tensors: q, r, out [B, Hq, d]; k, v [B, Hkv, Lmax, d], or,
+                block_table=None, max_len=None, window=0, kind=plx_decode_args, tail=()):
+    """Fill a plx_decode_args (or a `kind` that begins with one and goes on with the fields of `tail`) from tensors: q, r, out [B, Hq, d]; k, v [B, Hkv, Lmax, d], or,
     with block_table [B, pages per sequence] (int32), page pools [num_pages, Hkv, page_size, d]
     (max_len = largest logical length, default: pages per sequence x page_size).
     q, r, out may also be [B, Hq, Tq, d]: Tq query rows, the last Tq positions of each sequence."""
@@ -534,10 +534,10 @@ def decode_args(q, r, k, v, out, scale, seq_lens=None, use_r=True, num_splits=0,
     if block_table is not None:
         paged = (block_table.data_ptr(), Lmax, block_table.stride(0), num_pages)
         Lmax = _i32(max_len if max_len is not None else block_table.shape[1] * Lmax)
-    return _filled(plx_decode_args, q.data_ptr(), _ptr(r), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(seq_lens),
+    return _filled(kind, q.data_ptr(), _ptr(r), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(seq_lens),
                    B, Hq, Hkv, Lmax, d, *k.stride()[:3], *v.stride()[:3], _f32(scale), 1 if use_r else 0, _i32(num_splits),
                    _ptr(workspace), 0 if workspace is None else _bytes(workspace), _dtype_code(q), *paged, Tq,
-                   _i32(window), 0, *_NO_PREP)
+                   _i32(window), 0, *_NO_PREP, *tail)
 
 
 def parallax_decode(q, r, k, v, scale, seq_lens=None, use_r=True, num_splits=0, workspace=None,
@@ -636,15 +636,14 @@ def _decode_rows(q, r, k, v, scale, seq_lens, use_r, num_splits, workspace, out,
         raise ValueError("the workspace must be contiguous")
     if out is None:
         out = _result_maker(stream, torch.empty_like)(q)
-    a = decode_args(q, r, k, v, out, scale, seq_lens, use_r, num_splits, workspace, block_table, max_len, window)
+    given = (q, r, k, v, out, scale, seq_lens, use_r, num_splits, workspace, block_table, max_len, window)
     lib = load_library()
     if block_list is not None:
-        n_list = _list_length(where, block_list, B, cache[1])
-        blocks = plx_decode_blocks_args()
-        blocks.decode, blocks.block_list, blocks.n_list = a, block_list.data_ptr(), n_list
-        a = blocks.decode  # (the copy inside)
+        blocks = decode_args(*given, plx_decode_blocks_args, (block_list.data_ptr(), _list_length(where, block_list, B, cache[1])))
+        a = blocks.decode  # (in place)
         splits, call, head = lib.parallax_decode_blocks_call_splits, lib.parallax_decode_blocks, (ctypes.byref(blocks),)
     elif tree_mask is None:
+        a = decode_args(*given)
         splits, call, head = lib.parallax_decode_sinks_call_splits, lib.parallax_decode_sinks, (ctypes.byref(a), sinks)
     else:
         words = -(-Tq // 64)
@@ -658,7 +657,7 @@ def _decode_rows(q, r, k, v, scale, seq_lens, use_r, num_splits, workspace, out,
         if rows not in ((1, Tq, words), (B, Tq, words)):
             raise ValueError("tree_mask must be [(1 or B,) Tq, ceil(Tq/64)]")
         tree = plx_decode_tree_args()
-        tree.decode, tree.tree_mask, tree.mask_batch = a, tree_mask.data_ptr(), rows[0]
+        tree.decode, tree.tree_mask, tree.mask_batch = decode_args(*given), tree_mask.data_ptr(), rows[0]
         tree.draft_lens, tree.sinks = _ptr(draft_lens), sinks
         a = tree.decode  # (the copy inside)
         splits, call, head = lib.parallax_decode_tree_call_splits, lib.parallax_decode_tree, (ctypes.byref(tree),)
