@@ -879,10 +879,10 @@ def parallax_select_blocks(q, bounds, seq_lens, keep, first=1, recent=2, out=Non
         raise ValueError("%s: q is a contiguous bf16 tensor [B, Hq, (Tq,) d]" % where)
     B, Hq, d = shape[0], shape[1], shape[-1]
     Tq = shape[2] if len(shape) == 4 else 1
-    if bounds.dim() != 5 or bounds.dtype != torch.bfloat16 or not bounds.is_contiguous() or bounds.shape[0] != B or (
-            tuple(bounds.shape[3:]) != (2, d)):
+    held = bounds.shape
+    if len(held) != 5 or bounds.dtype != torch.bfloat16 or not bounds.is_contiguous() or held[0] != B or held[3] != 2 or held[4] != d:
         raise ValueError("%s: bounds is a contiguous bf16 tensor [B, Hkv, n_blocks, 2, d]" % where)
-    _, Hkv, n_blocks, _, _ = bounds.shape
+    Hkv, n_blocks = held[1], held[2]
     lens, keep = _lens(where, "seq_lens", seq_lens, B), _i32(keep)
     if out is None:
         out = _result_maker(stream, torch.empty)((B, Hkv, max(keep, 0)), dtype=torch.int32, device=q.device)

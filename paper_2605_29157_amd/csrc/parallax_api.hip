@@ -607,15 +607,12 @@ int32_t keys_of_lists(const plx::DecodeRowsParams &p) {
     return p.d.window > 0 && in_window < p.d.Lmax ? (int32_t)in_window : p.d.Lmax;
 }
 
-// Split count of a call over lists (bf16 rows): that of a plain one over as many keys, doubled while half of the units stay idle and
-// every wave keeps a tile (see pick_splits_rows).
+// Split count of a call over lists (bf16 rows): a workgroup for every unit, a block at least for every split. Sweeps of S over 28 calls of
+// 1 - 32 sequences x lists of 16 - 512 blocks: at most 2 % from the best (the rule for plain calls up to 24 %: 8 x 16 heads, d = 64, 64
+// blocks, S = 1 40.6 us, 2 32.7, 4 33.5; 128 pairs x 128 blocks 124, 108, 106; 192 pairs x 64 blocks 77, 86, 83).
 int32_t pick_splits_lists(const plx::DecodeRowsParams &p) {
-    const int32_t keys = keys_of_lists(p);
-    const int64_t pairs = (int64_t)p.d.B * p.d.Hkv, cus = query_num_cus();
-    const int32_t block_tiles = (keys + plx::kDecodeBlockKeys - 1) / plx::kDecodeBlockKeys;
-    int32_t s = parallax_decode_num_splits(p.d.B, p.d.Hq, p.d.Hkv, keys, p.d.d, 0);
-    while (s > 1 && 2 * pairs * s <= cus && 2 * s <= std::min(block_tiles, PLX_MAX_SPLITS)) s *= 2;
-    return s;
+    const int64_t pairs = (int64_t)p.d.B * p.d.Hkv, blocks = (keys_of_lists(p) + PLX_BLOCK_KEYS - 1) / PLX_BLOCK_KEYS;
+    return (int32_t)std::max<int64_t>(1, std::min({query_num_cus() / pairs, blocks, (int64_t)PLX_MAX_SPLITS}));
 }
 
 // ... and over 4-bit rows: the cheapest by a model of decode_q4_kernel, in us. A workgroup starts in 3; its four waves take a tile
