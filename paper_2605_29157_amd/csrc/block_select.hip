@@ -11,7 +11,6 @@
 // a block, 1 / 64 of the cache's) beside 2 D additions in 64 bits a column; the choice, one workgroup a list, latency.
 #include "plx_kernels.h"
 #include "plx_q4.h"
-#include "plx_rows.h"
 
 namespace plx {
 
@@ -150,6 +149,13 @@ struct Bounds16 {
         }
     }
 };
+// sum + 0 * x, x both bf16 halves: NaN once one of them is infinite or NaN, in one instruction (with bits and compares 128 lists of 2048
+// blocks took 34.5 us, so 32.5)
+__device__ __forceinline__ float add_zero_times(uint32_t x, float sum) {
+    typedef __bf16 bf16_pair __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16_pair, x), bf16_pair{(__bf16)0.f, (__bf16)0.f}, sum, false);
+}
+
 // The score's key of one of these blocks, the same for the four lanes from 4 n on, which share it; its number among the 16 is returned.
 // COLS columns (query rows x heads of the group) at a time.
 template <int D, int COLS>
@@ -201,10 +207,10 @@ __device__ __forceinline__ int score_blocks(const BlockSelect &p, int b, int h, 
     uint32_t odd = 0;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-        uint32_t x = 0;
+        float x = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x |= not_finite_halves(lo[s][i]) | not_finite_halves(hi[s][i]);
-        odd |= x != 0 ? 1u << s : 0u;
+        for (int i = 0; i < 4; ++i) x = add_zero_times(hi[s][i], add_zero_times(lo[s][i], x));
+        odd |= x != x ? 1u << s : 0u;
     }
     const int mine = D == 128 ? (lane & 8 ? 2 : 0) + (lane & 4 ? 1 : 0) : (lane & 4 ? 1 : 0);
     if (__builtin_expect(__any(odd != 0), 0)) {
@@ -219,10 +225,11 @@ __device__ __forceinline__ int held_blocks(const BlockSelect &p, int b) {
     return p.seq_lens == nullptr ? p.n_blocks : min((int)(((int64_t)max(p.seq_lens[b], 0) + kListBlock - 1) / kListBlock), p.n_blocks);
 }
 
-// Blocks up to which one launch does it all, a workgroup reading its list's bounds alone. Two launches / one in a replayed graph, us,
-// d = 128, two columns: 8 lists of 64 blocks 8.8 / 7.1, 128 blocks 8.2 / 7.4, 512 11.7 / 17.2; 128 lists 9.0 / 7.4, 10.1 / 9.0,
-// 16.2 / 17.9; 512 lists 13.9 / 13.3, 17.8 / 15.9, 42.5 / 39.4 (and on a stream the host saves a launch).
-constexpr int kOneLaunchBlocks = 128;
+// Blocks up to which one launch does it all, a workgroup reading its list's bounds alone, in one round of its waves. Two launches / one in a
+// replayed graph, us, d = 128, two columns: 8 lists of 64 blocks 8.2 / 6.5, 128 8.5 / 7.4, 256 8.7 / 9.2; 128 lists 8.6 / 6.8, 9.0 / 7.7,
+// 9.8 / 9.9; 512 lists 13.4 / 9.2, 17.1 / 11.5, 24.9 / 19.4 (and on a stream the host saves a launch, 2.8); 512 blocks, in two rounds:
+// 8 lists 8.9 / 13.0, 128 lists 13.8 / 14.0.
+constexpr int kOneLaunchBlocks = 256;
 constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64;
 constexpr int kPickKeys = 4096;  // that are kept in LDS
 constexpr int kDigits = 512;     // values of a digit of 9 bits
@@ -373,11 +380,13 @@ __global__ __launch_bounds__(kPickThreads) void block_pick_kernel(BlockSelect p)
 template <int D, int COLS>
 __global__ __launch_bounds__(kPickThreads) void block_select_kernel(BlockSelect p) {
     __shared__ PickScratch scratch;
-    __shared__ uint64_t keys[kPickKeys];
+    __shared__ uint64_t keys[kOneLaunchBlocks];
+    static_assert(kOneLaunchBlocks <= kPickWaves * 16, "a round of the waves");
     const int h = blockIdx.x, b = blockIdx.y, held = held_blocks(p, b);
     int32_t *out = p.block_list + ((int64_t)b * p.Hkv + h) * p.keep;
     if (all_kept(p, held, out)) return;
-    for (int j0 = (threadIdx.x >> 6) * 16; j0 < held; j0 += kPickWaves * 16) {
+    const int j0 = (threadIdx.x >> 6) * 16;
+    if (j0 < held) {
         Bounds16<D> bounds;
         bounds.load(p, b, h, j0, held);
         uint64_t key;

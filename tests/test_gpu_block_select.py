@@ -223,3 +223,21 @@ def test_steps_of_a_sequence(plx, page, four):
         ref = masked.masked_forward(host(q)[:, :, None], host(r)[:, :, None], hk, hv, d ** -0.5, mask)
         bound = rows.bf16_bound(host(q)[:, :, None], host(r)[:, :, None], hk, hv, d ** -0.5, mask)
         assert (np.abs(host(out)[:, :, None] - ref) <= bound).all(), n
+
+
+@pytest.mark.parametrize("n", [240, 255, 256, 257])
+@pytest.mark.parametrize("d", [64, 128])
+def test_select_around_one_round(plx, d, n):
+    """As many blocks as a workgroup scores at once, and one more; every place of a row holds the value that is not finite once."""
+    B, keep = 4, 9
+    a = _normal((B, 2, n, d), 7).float()
+    bounds = torch.stack([a - 1.5, a + 1.5], 3).to(torch.bfloat16)
+    for i, bad in enumerate((float("inf"), -float("inf"), float("nan"))):
+        for h in range(2):
+            bounds[i, h, 3 + 37 * h + torch.arange(4) * 50, (i + h) % 2, (torch.arange(4) * 17 + 31 * h + 5 * i) % d] = bad
+    q = _normal((B, 4, d), 8)
+    got = plx.parallax_select_blocks(q, bounds, None, keep, first=0, recent=1)
+    hq, hb = host(q).reshape(B, 2, -1, d), host(bounds)
+    for b in range(B):
+        for h in range(2):
+            assert got[b, h].tolist() == blocks.select(hq[b, h], hb[b, h, :, 0], hb[b, h, :, 1], keep, 0, 1), (b, h)
