@@ -343,9 +343,10 @@ plx_status parallax_cache_compact(const plx_cache_compact_args *args, void *hip_
  *     d / 2 bytes of K codes, d / 2 of V codes; byte i of either: dimension 2 i in its low half, 2 i + 1 in its high one
  *     d / 16 scale bytes of K, d / 16 of V; zeros up to a multiple of 16 bytes
  * A code is a sign bit over one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (e2m1); a scale byte e stands for 2^(e - 127) and serves 16
- * dimensions, 255 makes them NaN. Written rows take the power of two that brings the largest magnitude of the 16 into [3.5, 7),
+ * dimensions, 255 makes them NaN (in V infinite or NaN, where a code is not 0). Written rows take the power of two that brings the largest magnitude of the 16 into [3.5, 7),
  * e within 4 .. 252 (what is left over above saturates, below becomes 0), and round to nearest, ties to the even code; 16 dimensions
- * of which one is infinite or NaN get e = 255. Every value of such a row is exact in bf16.
+ * of which one is infinite or NaN get e = 255 and codes of 0. Every value of such a row is exact in bf16. (A decode holds weights times
+ * the scales of V in bf16: scales beyond 2^119 may overflow there, and below 2^-100 lose bits.)
  *   rows         [B, Hkv, capacity, row] (stride[0]: sequence, [1]: head, [2]: row), or with a block table pools
  *                [num_pages, Hkv, page_size, row] (stride[0]: page); strides in BYTES, multiples of 16, stride[2] >= the row
  *   block_table  [B, block_table_stride] or NULL, as in plx_decode_args; capacity <= block_table_stride * page_size
@@ -369,7 +370,7 @@ int32_t parallax_q4_row_bytes(int32_t d); /* 0: not a head dimension that such c
  *   counts   [B] or NULL. write: rows from counts[b] on are passed over (a padded batch). read: of the cache's tokens, those from
  *            counts[b] on (the sequence's length) come back as zeros.
  * Tokens outside [0, capacity), and those whose table entry is no page, are not written and come back as zeros. The pages that are
- * written must not be shared (parallax_cache_extend makes them so).
+ * written must not be shared (parallax_cache_extend makes them so); a cache of stride 0 is not written (PLX_ERR_SHAPE).
  */
 typedef struct {
     plx_q4_cache cache;
@@ -393,8 +394,8 @@ plx_status parallax_cache_read_q4(const plx_q4_rows_args *args, void *hip_stream
  *   k          a bf16 cache or pool as in plx_decode_args (element strides), d 64 or 128; or NULL: the K part of q4, whose B, Hkv,
  *              d and capacity are then the call's
  *   seq_lens   [B] or NULL (= capacity, which is Lmax of plx_decode_args)
- *   from_lens  [B] or NULL: only the blocks from that of token from_lens[b] on (what a sequence held when its bounds were last
- *              brought up to date). max_new: the most tokens that any sequence has gained since; 0 = all blocks
+ *   from_lens  [B] or NULL: only the blocks from that of token from_lens[b] on (the tokens in front of it are the same as when the bounds
+ *              were last brought up to date). max_new: the most tokens that any sequence holds behind from_lens[b]; 0 = all blocks
  * Blocks behind seq_lens, and those in front of from_lens, are left as they were.
  */
 #define PLX_BLOCK_KEYS 64

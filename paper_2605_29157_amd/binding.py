@@ -839,9 +839,9 @@ def parallax_decode_q4(q, r, cache, scale, seq_lens=None, use_r=True, num_splits
 
 def parallax_cache_bounds(k, bounds, seq_lens=None, from_lens=None, max_new=0, block_table=None, stream=None):
     """The smallest and largest key of every block of 64 tokens, by dimension, into bounds [B, Hkv, n_blocks, 2, d] (bf16), which is
-    returned. k: the bf16 keys [B, Hkv, capacity, d] or pools of a block_table, or a 4-bit cache. from_lens: what the sequences held
-    when their bounds were last brought up to date; only blocks from there on are looked at. max_new: no sequence has gained more
-    tokens since (0: not known)."""
+    returned. k: the bf16 keys [B, Hkv, capacity, d] or pools of a block_table, or a 4-bit cache. from_lens: the tokens in
+    front of these are the same as when the bounds were last brought up to date; only blocks from there on are looked at. max_new: no
+    sequence holds more tokens behind its from_lens (0: not known)."""
     where = "parallax_cache_bounds"
     _on_current_device(where, k, bounds, seq_lens, from_lens, block_table)
     if k.dim() != 4 or bounds.dim() != 5:

@@ -241,3 +241,16 @@ def test_the_binding_refuses_host_tensors(binding):  # noqa: F811
                  lambda: binding.parallax_decode(q, q, k, k, 0.1, block_list=torch.zeros(1, 1, 1, dtype=torch.int32))):
         with pytest.raises(ValueError):
             call()
+
+
+def test_one_place_for_several_rows_is_not_written(binding):  # noqa: F811
+    """A cache that sequences or heads share by a stride of 0 can be read, and is refused by a write."""
+    lib = binding.load_library()
+    for fields, status in ((dict(stride0=0), binding.PLX_ERR_SHAPE), (dict(stride1=0), binding.PLX_ERR_SHAPE),
+                           (dict(stride0=0, B=1), binding.PLX_OK), (dict(stride1=0, Hkv=1), binding.PLX_OK)):
+        a = binding.plx_q4_rows_args()
+        _q4(binding, a.cache, **fields)
+        a.k, a.v, a.T, a.dtype = 0x3000, 0x4000, 0, binding.PLX_BF16
+        a.k_stride[:] = a.v_stride[:] = (128, 128, 128)
+        assert lib.parallax_cache_write_q4(ctypes.byref(a), None) == status, fields
+        assert lib.parallax_cache_read_q4(ctypes.byref(a), None) == binding.PLX_OK, fields
