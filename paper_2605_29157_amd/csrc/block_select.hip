@@ -176,13 +176,17 @@ __device__ __forceinline__ int score_blocks(const BlockSelect &p, int b, int h, 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const double q0 = (double)bf16_lo_f32(q[i]), q1 = (double)bf16_hi_f32(q[i]);
-                // of negative q the smallest key counts
-                const uint32_t down = ((q[i] & 0x8000u) ? 0xffffu : 0u) | ((q[i] & 0x80000000u) ? 0xffff0000u : 0u);
+                // of negative q the smallest key counts: bytes 0 - 3 of the pair instead of 4 - 7
+                // of negative q the smallest key counts: a byte permutation picks the bound's half and widens it to fp32 (selected
+                // by masks and widened after: a third of the instructions more, 128 lists of 2048 blocks 32.8 us, so 30.9)
+                const uint32_t s0 = 0x05040c0cu ^ ((uint32_t)__builtin_amdgcn_sbfe((int)q[i], 15, 1) & 0x04040000u);
+                const uint32_t s1 = 0x07060c0cu ^ ((uint32_t)((int)q[i] >> 31) & 0x04040000u);
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) {
-                    const uint32_t y = (lo[s][i] & down) | (hi[s][i] & ~down);
-                    sum[c][s] = fma(q0, (double)bf16_lo_f32(y), sum[c][s]);
-                    sum[c][s] = fma(q1, (double)bf16_hi_f32(y), sum[c][s]);
+                    const float y0 = __builtin_bit_cast(float, __builtin_amdgcn_perm(hi[s][i], lo[s][i], s0));
+                    const float y1 = __builtin_bit_cast(float, __builtin_amdgcn_perm(hi[s][i], lo[s][i], s1));
+                    sum[c][s] = fma(q0, (double)y0, sum[c][s]);
+                    sum[c][s] = fma(q1, (double)y1, sum[c][s]);
                 }
             }
         }
@@ -227,7 +231,7 @@ __device__ __forceinline__ int held_blocks(const BlockSelect &p, int b) {
 
 // Blocks up to which one launch does it all, a workgroup reading its list's bounds alone, in one round of its waves. Two launches / one in a
 // replayed graph, us, d = 128, two columns: 8 lists of 64 blocks 8.2 / 6.5, 128 8.5 / 7.4, 256 8.7 / 9.2; 128 lists 8.6 / 6.8, 9.0 / 7.7,
-// 9.8 / 9.9; 512 lists 13.4 / 9.2, 17.1 / 11.5, 24.9 / 19.4 (and on a stream the host saves a launch, 2.8); 512 blocks, in two rounds:
+// 9.8 / 9.9; 512 lists 13.4 / 8.8, 17.1 / 10.9, 24.9 / 19.4 (and on a stream the host saves a launch, 2.8); 512 blocks, in two rounds:
 // 8 lists 8.9 / 13.0, 128 lists 13.8 / 14.0.
 constexpr int kOneLaunchBlocks = 256;
 constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64;
@@ -376,9 +380,10 @@ __global__ __launch_bounds__(kPickThreads) void block_pick_kernel(BlockSelect p)
     }
 }
 
-// Both in one launch, a workgroup a list, for few blocks
+// Both in one launch, a workgroup a list, for few blocks. (Two workgroups a unit: with the registers of one, 512 lists of 128 blocks 13.9
+// us, so 10.9.)
 template <int D, int COLS>
-__global__ __launch_bounds__(kPickThreads) void block_select_kernel(BlockSelect p) {
+__global__ __launch_bounds__(kPickThreads, 8) void block_select_kernel(BlockSelect p) {
     __shared__ PickScratch scratch;
     __shared__ uint64_t keys[kOneLaunchBlocks];
     static_assert(kOneLaunchBlocks <= kPickWaves * 16, "a round of the waves");
