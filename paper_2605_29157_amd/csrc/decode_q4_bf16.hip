@@ -269,7 +269,7 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
             if constexpr (D == 128) {
                 const u32x4 codes = *(const u32x4 *)(row + k_at);
                 const uint32_t scales = *(const uint16_t *)(row + k_scale_at);
-                const float lo = q4_scale(scales & 255u), hi = q4_scale(scales >> 8);
+                const float lo = q4_scale_byte(scales, 0), hi = q4_scale_byte(scales, 1);
 #pragma unroll
                 for (int s = 0; s < KSTEPS; ++s) {
                     const u32x4 kf = q4_to_bf16(codes[s], s < 2 ? lo : hi);
@@ -349,7 +349,8 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
                 for (int d = 0; d < 2; ++d) {
                     const uint32_t e4 = operand_scales<D, C, J>(scales[h][d]) & keep[h][d];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[4 * d + e] = q4_scale((e4 >> (8 * e)) & 255u);
+                    for (int e = 0; e < 4; ++e)  // (at D = 128 with more columns the compiler would make too many ahead, and spill)
+                        x[4 * d + e] = D == 64 || C <= 4 ? q4_scale_byte(e4, e) : q4_scale((e4 >> (8 * e)) & 255u);
                 }
                 float y[8];
 #pragma unroll
