@@ -348,7 +348,8 @@ plx_status parallax_cache_compact(const plx_cache_compact_args *args, void *hip_
  * of which one is infinite or NaN get e = 255 and codes of 0. Every value of such a row is exact in bf16. (A decode holds weights times
  * the scales of V in bf16: scales beyond 2^119 may overflow there, and below 2^-100 lose bits.)
  *   rows         [B, Hkv, capacity, row] (stride[0]: sequence, [1]: head, [2]: row), or with a block table pools
- *                [num_pages, Hkv, page_size, row] (stride[0]: page); strides in BYTES, multiples of 16, stride[2] >= the row
+ *                [num_pages, Hkv, page_size, row] (stride[0]: page); strides in BYTES, multiples of 16, stride[2] >= the row;
+ *                those of rows and pages below 2^36
  *   block_table  [B, block_table_stride] or NULL, as in plx_decode_args; capacity <= block_table_stride * page_size
  * The page calls take such pools as one bf16 pool (v NULL) of d = row bytes / 2.
  */

@@ -8,9 +8,10 @@
 // What bounds them: the bytes of the rows, 4 D of bf16 and 9 D / 8 of the cache; few rows: one launch. A thread has 16 bytes
 // of bf16 of each of its rows, two neighbours share a scale, and the scale bytes of eight threads are put together, so that
 // a row goes out in whole dwords. Many rows: four a thread, all on their way at once, of one sequence and head, whose numbers, first token
-// and count are the workgroup's: with divisions by T, Hkv and the page size a row (the last in 64 bits) a kernel that moves 172 MB
-// through pages of 16 took 47 us to write and 55 to read, now 37 and 27 (4.7, 6.5 TB/s). K and V pass through once and are asked for and stored
-// as such: read back 34 without, and 38 written.
+// and count are the workgroup's. What a row costs beside its bytes decides: 172 MB through pages of 16 were written in 47 us and read back
+// in 55 with divisions by T, Hkv and the page size a row (the last in 64 bits); with a workgroup's rows of one sequence 38 and 34; K and V,
+// which pass once, asked for and stored as such 37 and 27; the page by a multiplication, offsets from 32-bit factors, magnitudes and codes
+// from bf16 pairs, all lookups in front of the loads 36 and 27 (4.7, 6.5 TB/s; without pages 33 and 27; a copy of as much 35).
 #include "plx_kernels.h"
 #include "plx_q4.h"
 
@@ -19,8 +20,8 @@ namespace plx {
 namespace {
 
 // Rows from which a thread takes four: us, written / read, one a thread and four: d = 128 3200 rows 3.0 / 3.1 and 3.9 / 3.7, 16000
-// 5.0 / 4.4 and 4.9 / 4.4, 32000 7.7 / 6.2 and 6.8 / 5.6, 262144 (172 MB) 42 / 30 and 35 / 28; fp32 131072 29 / 29 and 31 / 26. And
-// tokens of a sequence from which it does, in workgroups: 33 tokens (two workgroups of 32) 8.0 / 6.4 and 8.9 / 7.2, 64 12.9 / 9.4 and 10.7 / 9.0.
+// 5.0 / 4.4 and 4.9 / 4.4, 32000 7.7 / 6.2 and 6.6 / 5.7, 262144 (172 MB) 42 / 30 and 33 / 28; fp32 131072 29 / 29 and 31 / 26. And
+// tokens of a sequence from which it does, in workgroups: 33 tokens (two workgroups of 32) 8.0 / 6.4 and 8.9 / 7.2, 64 12.9 / 9.4 and 9.9 / 9.1.
 constexpr int64_t kManyRows = 32000;
 constexpr int kManyRuns = 2;
 
@@ -48,14 +49,35 @@ struct Q4Place {
     }
     __device__ __forceinline__ int token(int i) const { return t + kRows * i; }
     __device__ __forceinline__ bool has(const Q4Rows &p, int i) const { return any && (ROWS == 1 || token(i) < p.T); }
-    // byte offset of a token's row in the cache, or -1
-    __device__ __forceinline__ int64_t row_of(const Q4Rows &p, int64_t token) const {
+    // Where a token's row is, in two steps so that no branch and no wait comes between the rows: its page (0 without a table, -1: no row), ..
+    __device__ __forceinline__ int page_of(const Q4Rows &p, int64_t token, bool wanted) const {
         const Q4Cache &c = p.cache;
-        if (token < 0 || token >= c.capacity) return -1;
-        const int64_t at = q4_token_offset(c.block_table, c.table_stride, c.page_size, c.num_pages, c.stride, b, token);
-        return at < 0 ? -1 : at + h * c.stride[1];
+        wanted = wanted && token >= 0 && token < c.capacity;
+        int page = 0;
+        if (c.block_table != nullptr) {  // (uniform)
+            const uint32_t n = wanted ? (uint32_t)token : 0;
+            page = c.block_table[b * c.table_stride + (__umulhi(2 * n, c.page_mul) >> c.page_shift)];
+            if (page >= c.num_pages) page = -1;
+        }
+        return wanted ? page : -1;
     }
-    __device__ __forceinline__ int64_t element(const int64_t (&s)[3], int i) const { return b * s[0] + h * s[1] + token(i) * s[2] + DIMS * part; }
+    // .. and its byte offset, or -1. (Pages and rows are counted in 16 bytes: with factors of 32 bits it takes four multiplications, each
+    // of the time of four other instructions.)
+    __device__ __forceinline__ int64_t row_of(const Q4Rows &p, int64_t token, int page) const {
+        const Q4Cache &c = p.cache;
+        const uint32_t row16 = (uint32_t)((uint64_t)c.stride[2] >> 4), page16 = (uint32_t)((uint64_t)c.stride[0] >> 4), n = (uint32_t)token;
+        int64_t at = h * c.stride[1];
+        if (c.block_table == nullptr) {
+            at += b * c.stride[0] + (int64_t)((uint64_t)n * row16 << 4);
+        } else {
+            const uint32_t page_no = __umulhi(2 * n, c.page_mul) >> c.page_shift;
+            at += (int64_t)((uint64_t)(uint32_t)page * page16 + (uint64_t)(n - page_no * c.page_size) * row16) << 4;
+        }
+        return page < 0 ? -1 : at;
+    }
+    __device__ __forceinline__ int64_t element(const int64_t (&s)[3], int i, int T) const {  // (behind the last token: one in front of it)
+        return b * s[0] + h * s[1] + min(t, T - 1) * s[2] + DIMS * part + (token(i) < T ? i * (kRows * s[2]) : 0);
+    }
 };
 
 }  // namespace
@@ -67,50 +89,64 @@ __global__ __launch_bounds__(256) void cache_write_q4_kernel(Q4Rows p) {
     const int64_t start = p.start != nullptr ? p.start[me.b] : 0;
     const int count = p.counts != nullptr ? p.counts[me.b] : p.T;
     const void *src = me.is_v ? p.v : p.k;
-    int64_t at[ROWS];
+    int page[ROWS];
     u32x4 raw[ROWS];
     f32x4 wide[ROWS][2];
 #pragma unroll
+    for (int i = 0; i < ROWS; ++i) page[i] = me.page_of(p, start + me.token(i), me.has(p, i) && me.token(i) < count);
+#pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-        at[i] = -1;
-        wide[i][0] = wide[i][1] = f32x4{};
-        raw[i] = u32x4{};
-        if (!me.has(p, i)) continue;
-        const int64_t e = me.element(me.is_v ? p.vs : p.ks, i);
+        const int64_t e = me.element(me.is_v ? p.vs : p.ks, i, p.T);
         if constexpr (F32) {
             wide[i][0] = *(const f32x4 *)((const float *)src + e), wide[i][1] = *(const f32x4 *)((const float *)src + e + 4);
         } else {
             raw[i] = __builtin_nontemporal_load((const u32x4 *)((const __bf16 *)src + e));
         }
-        if (me.token(i) < count) at[i] = me.row_of(p, start + me.token(i));
     }
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-        float x[8];
+        uint32_t top = 0;  // of the magnitudes' bits, as those of a float: infinities and NaN are the largest
+        if constexpr (F32) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (F32)
-                x[e] = wide[i][0][e], x[4 + e] = wide[i][1][e];
-            else
-                x[2 * e] = bf16_lo_f32(raw[i][e]), x[2 * e + 1] = bf16_hi_f32(raw[i][e]);
+            for (int e = 0; e < 8; ++e) {
+                const float x = wide[i][e / 4][e % 4];  // (a cast of the element itself is compiled as one of element 0)
+                top = max(top, __builtin_bit_cast(uint32_t, x) & 0x7fffffffu);
+            }
+        } else {
+            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 both = {0, 0};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) both = __builtin_elementwise_max(both, __builtin_bit_cast(u16x2, raw[i][e] & 0x7fff7fffu));
+            const uint32_t halves = __builtin_bit_cast(uint32_t, both);
+            top = max(halves << 16, halves & 0xffff0000u);
         }
-        uint32_t top = 0;  // of the magnitudes' bits: infinities and NaN are the largest
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, __builtin_bit_cast(uint32_t, x[e]) & 0x7fffffffu);
         top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, true));  // quad_perm [1, 0, 3, 2]
         const bool bad = top >= 0x7f800000u;
         const uint32_t e = (uint32_t)min(max((int)((top + 0x200000u) >> 23) - 2, 4), 252);
         const float scale = q4_scale(e);
         uint32_t codes = 0;
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], scale, 0);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], scale, 1);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], scale, 2);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], scale, 3);
+        if constexpr (F32) {
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, wide[i][0][0], wide[i][0][1], scale, 0);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, wide[i][0][2], wide[i][0][3], scale, 1);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, wide[i][1][0], wide[i][1][1], scale, 2);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, wide[i][1][2], wide[i][1][3], scale, 3);
+        } else {
+            typedef __bf16 bf16_pair __attribute__((ext_vector_type(2)));
+            auto pair = [&](int e) {
+                const uint32_t x = raw[i][e];  // (as above)
+                return __builtin_bit_cast(bf16_pair, x);
+            };
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, pair(0), scale, 0);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, pair(1), scale, 1);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, pair(2), scale, 2);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, pair(3), scale, 3);
+        }
         uint32_t scales = (bad ? 255u : e) << (8 * (me.part / 2 & 3));  // four scales of eight lanes
         scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x4E, 0xf, 0xf, true);   // quad_perm [2, 3, 0, 1]
         scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x141, 0xf, 0xf, true);  // row_half_mirror
-        if (at[i] < 0) continue;
-        char *row = p.cache.rows + at[i];
+        const int64_t at = me.row_of(p, start + me.token(i), page[i]);
+        if (at < 0) continue;
+        char *row = p.cache.rows + at;
         *(uint32_t *)(row + (me.is_v ? Row::kV : 0) + 4 * me.part) = bad ? 0u : codes;
         if (me.part % 8 == 0) *(uint32_t *)(row + (me.is_v ? Row::kVScale : Row::kKScale) + me.part / 2) = scales;
         if constexpr (Row::kBytes > Row::kEnd) {
@@ -130,17 +166,19 @@ __global__ __launch_bounds__(256) void cache_read_q4_kernel(Q4Rows p) {
     const int64_t count = p.counts != nullptr ? p.counts[me.b] : p.cache.capacity;
     uint32_t codes[ROWS], scales[ROWS];
     int64_t to[ROWS];
+    int page[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) page[i] = me.page_of(p, start + me.token(i), me.has(p, i) && start + me.token(i) < count);
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-        codes[i] = scales[i] = 0, to[i] = -1;
-        if (!me.has(p, i)) continue;
-        const int64_t token = start + me.token(i), at = token < count ? me.row_of(p, token) : -1;
+        const int64_t at = me.row_of(p, start + me.token(i), page[i]);
+        codes[i] = scales[i] = 0;
         if (at >= 0) {
             const char *row = p.cache.rows + at;
             codes[i] = *(const Codes *)(row + (me.is_v ? Row::kV : 0) + DIMS / 2 * me.part);
             scales[i] = *(const uint8_t *)(row + (me.is_v ? Row::kVScale : Row::kKScale) + me.part / (16 / DIMS));
         }
-        to[i] = me.element(me.is_v ? p.vs : p.ks, i);
+        to[i] = me.has(p, i) ? me.element(me.is_v ? p.vs : p.ks, i, p.T) : -1;
     }
     void *dst = me.is_v ? p.v : p.k;
 #pragma unroll

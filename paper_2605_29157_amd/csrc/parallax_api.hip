@@ -542,6 +542,8 @@ plx_status take_q4_cache(const plx_q4_cache &a, plx::Q4Cache *out) {
         if (s % 16 != 0) return PLX_ERR_ALIGN;
     }
     if (a.stride[2] < row) return PLX_ERR_SHAPE;
+    // (the kernels count both in 16 bytes, in 32 bits)
+    if (a.stride[2] >> 36 || (a.block_table && a.stride[0] >> 36)) return PLX_ERR_SHAPE;
     plx::Q4Cache c{};
     c.rows = static_cast<char *>(a.rows);
     for (int i = 0; i < 3; ++i) c.stride[i] = a.stride[i];
@@ -551,6 +553,8 @@ plx_status take_q4_cache(const plx_q4_cache &a, plx::Q4Cache *out) {
         if ((int64_t)a.block_table_stride * a.page_size < a.capacity) return PLX_ERR_SHAPE;
         c.block_table = a.block_table, c.table_stride = a.block_table_stride;
         c.page_size = a.page_size, c.num_pages = a.num_pages;
+        while (c.page_shift < 31 && (int64_t)1 << c.page_shift < a.page_size) ++c.page_shift;
+        c.page_mul = (uint32_t)((((uint64_t)1 << (31 + c.page_shift)) + a.page_size - 1) / a.page_size);
     }
     *out = c;
     return PLX_OK;

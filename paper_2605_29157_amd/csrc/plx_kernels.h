@@ -68,6 +68,10 @@ struct Q4Cache {
     const int32_t *block_table;
     int64_t table_stride;
     int32_t page_size, num_pages, B, Hkv, capacity, d;
+    // token / page_size = 2 token * page_mul / 2^(32 + page_shift): page_shift = ceil(log2 page_size), page_mul = 2^(31 + page_shift) /
+    // page_size rounded up (by less than 2^page_shift / 2^31 of a page for any token below 2^31)
+    uint32_t page_mul;
+    int32_t page_shift;
 };
 // Rows [B][Hkv][T][d] of K and V (strides in elements) that become, or come from, tokens start[b] + t
 struct Q4Rows {

@@ -74,14 +74,4 @@ __device__ __forceinline__ void each_of(F &f) {
     each_of<N>(f, std::make_integer_sequence<int, N>{});
 }
 
-// Where the row of a token (0 .. 2^31 - 1) is: byte offset of its head 0 from the pools' (or caches') base, or -1 (no page)
-__device__ __forceinline__ int64_t q4_token_offset(const int32_t *table, int64_t table_stride, int page_size, int num_pages,
-                                                   const int64_t (&stride)[3], int b, int64_t token) {
-    if (table == nullptr) return (int64_t)b * stride[0] + token * stride[2];
-    const uint32_t page_no = (uint32_t)token / (uint32_t)page_size, row = (uint32_t)token - page_no * page_size;  // (in 64 bits: 80 instructions)
-    const int page = table[(int64_t)b * table_stride + page_no];
-    if (page < 0 || page >= num_pages) return -1;
-    return (int64_t)page * stride[0] + (int64_t)row * stride[2];
-}
-
 }  // namespace plx

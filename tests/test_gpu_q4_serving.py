@@ -307,3 +307,28 @@ def test_many_rows_are_as_few(plx, d, page, dtype):  # noqa: F811
     for t in range(0, T, 50):
         part = plx.parallax_cache_read_q4(many, d, 50, start=start + t, **at)
         assert all(torch.equal(a[:, :, t: t + 50].view(torch.uint8), b.view(torch.uint8)) for a, b in zip(got, part)), t
+
+
+@pytest.mark.parametrize("page", [1, 3, 7, 1000, 65535])
+def test_pages_of_far_tokens(plx, page):  # noqa: F811
+    """Rows around the borders of pages, up to token 2^25 + 1 of a sequence, in pages of sizes that are no powers of two."""
+    d, last = 64, 2 ** 25 + 1
+    n_pages = last // page + 1
+    pool = torch.empty((n_pages, 1, page, 80), dtype=torch.uint8, device=DEV)
+    table = torch.arange(n_pages, dtype=torch.int32, device=DEV).flip(0)[None].contiguous()
+    T = 5
+    k, v = (_normal((1, 1, T, d), s) for s in (1, 2))
+    small = torch.zeros(1, 1, T, 80, dtype=torch.uint8, device=DEV)
+    plx.parallax_cache_write_q4(k, v, small)
+    for first in (0, page - 2, 1000 * page - 3, last // 2, (last // page - 1) * page - 2, last + 1 - T):
+        first = max(first, 0)
+        start = _ints([first])
+        plx.parallax_cache_write_q4(k, v, pool, start=start, block_table=table)
+        for t in range(T):
+            x = first + t
+            if x // page < n_pages:
+                assert torch.equal(pool[n_pages - 1 - x // page, 0, x % page], small[0, 0, t]), (first, t)
+        back = plx.parallax_cache_read_q4(pool, d, T, start=start, block_table=table)
+        want = plx.parallax_cache_read_q4(small, d, T)
+        there = (first + torch.arange(T, device=DEV) < n_pages * page)[None, None, :, None]  # (a token past the last page: zeros)
+        assert all(torch.equal(a, torch.where(there, b, torch.zeros_like(b))) for a, b in zip(back, want)), first

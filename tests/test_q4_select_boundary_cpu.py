@@ -254,3 +254,16 @@ def test_one_place_for_several_rows_is_not_written(binding):  # noqa: F811
         a.k_stride[:] = a.v_stride[:] = (128, 128, 128)
         assert lib.parallax_cache_write_q4(ctypes.byref(a), None) == status, fields
         assert lib.parallax_cache_read_q4(ctypes.byref(a), None) == binding.PLX_OK, fields
+
+
+def test_strides_of_rows_and_pages_have_a_limit(binding):  # noqa: F811
+    lib = binding.load_library()
+    table = dict(block_table=0x2000, page_size=16, num_pages=4, block_table_stride=4)
+    for fields, status in ((dict(stride2=1 << 36), binding.PLX_ERR_SHAPE), (dict(stride0=1 << 36, **table), binding.PLX_ERR_SHAPE),
+                           (dict(stride2=(1 << 36) - 16), binding.PLX_OK), (dict(stride0=1 << 40), binding.PLX_OK)):
+        a = binding.plx_q4_rows_args()
+        _q4(binding, a.cache, **fields)
+        a.k, a.v, a.T, a.dtype = 0x3000, 0x4000, 0, binding.PLX_BF16
+        a.k_stride[:] = a.v_stride[:] = (128, 128, 128)
+        assert lib.parallax_cache_write_q4(ctypes.byref(a), None) == status, fields
+        assert lib.parallax_cache_read_q4(ctypes.byref(a), None) == status, fields
