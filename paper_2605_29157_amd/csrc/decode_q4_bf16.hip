@@ -23,7 +23,8 @@
 //     has the scale 0, so nothing in its row can reach it.
 // Steps, us for 16 x 32768 keys, 8 key heads, d = 128, and for 1 x 65536 at 8 splits (a workgroup a unit, 64 units): tiles in registers, V as bf16
 // through LDS, 32 keys at a time 130 and 81; two tiles in LDS 117, 77; 64 keys at a time, no bank conflicts 116, 61 (now bound by
-// LDS: 16 KB of V written at 64 bytes a cycle, and every read costs 6); scales with P instead 115, 50.
+// LDS: 16 KB of V written at 64 bytes a cycle, and every read costs 6); scales with P instead 115, 50; scales out of their bytes by one instruction 111, 48.5 (the loads
+// alone, without any arithmetic, 106).
 #include "plx_lds_dma.h"
 #include "plx_q4.h"
 #include "plx_rows.h"
@@ -36,8 +37,8 @@ constexpr int kQ4Waves = 4;
 constexpr float kQ4Slack = 6.f;  // in the exponent of 2
 
 // How the rows of a tile are found: 64 that follow each other in memory, counted from the start of the cache or looked up ahead
-// (lists; pages of a multiple of 64), four runs of 16 (other pages of a multiple of 16), or row by row.
-enum Q4Form { kQ4Direct, kQ4Runs64, kQ4Runs16, kQ4Any };
+// (lists; pages of a multiple of 64), four runs of 16 (other pages of a multiple of 16), eight of 8 likewise, or row by row.
+enum Q4Form { kQ4Direct, kQ4Runs64, kQ4Runs16, kQ4Runs8, kQ4Any };
 
 // The tiles of a workgroup: those of a list's blocks, or RowsScope's
 struct Q4Scope : RowsScope<false, kQ4Tile> {
@@ -87,7 +88,9 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
     static_assert(REP <= NDB, "no more copies than groups of dimensions");
     constexpr int RPC = Row::kBytes / 16;            // 16-byte chunks of a row
     constexpr int RAW = kQ4Tile * RPC;               // ... of a tile
-    constexpr int RUNS = FORM == kQ4Runs16 ? 4 : 1, RUN = RAW / RUNS;  // of rows that follow each other; chunks of one
+    constexpr bool FOLLOWING = FORM < kQ4Runs8;  // a load's rows follow each other in memory
+    constexpr int RUNS = FORM == kQ4Runs8 ? 8 : FORM == kQ4Runs16 ? 4 : 1;  // of rows that follow each other
+    constexpr int RUN = FOLLOWING ? RAW / RUNS : RAW;                       // chunks whose loads have an address of their own
     constexpr int FULL = RUN / 64, REST = RUN % 64, LOADS = FULL + (REST != 0);  // of a run
     static_assert(REST == 0 || REST == 16, "the last load of 16 rows takes 16 lanes");
     __shared__ u32x4 lds[kQ4Waves * 2 * RAW + 48];  // two tiles a wave; at the end the states of 16 columns
@@ -125,6 +128,7 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
         scope.column(P, no_words, 0, c, t, live, col_lo, col_end, col_nodes);
     }
 
+    constexpr int ADDRESSES = FOLLOWING ? RUNS : 1;
     const char *base = (const char *)p.k + (p.block_table == nullptr ? (int64_t)b * p.ksb : 0) + (int64_t)hk * p.ksh;
     u32x4 *raw = lds + w * 2 * RAW;
     const int32_t *table = p.block_table + (int64_t)b * p.table_stride;
@@ -144,19 +148,20 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
         ahead_key = key;
         if constexpr (FORM != kQ4Any) {
             // (runs behind the last token: the one that it is in)
-            const int64_t off = offset_of(min(max(key, 0) + 16 * (lane % RUNS), (Lb - 1) & ~15));
+            constexpr int LENGTH = RUNS == 8 ? 8 : 16;
+            const int64_t off = offset_of(min(max(key, 0) + LENGTH * (lane % RUNS), (Lb - 1) & ~(LENGTH - 1)));
             ahead_off[0] = (int)off, ahead_off[1] = (int)(off >> 32);
         }
         slot = 0;
     };
     // The first tile at or behind number v: its key and the addresses of its runs (kQ4Any: the offset of this lane's row)
     int64_t row_off = 0;
-    auto next_tile = [&](int &v, int &key, const char *(&run)[RUNS]) -> bool {
+    auto next_tile = [&](int &v, int &key, const char *(&run)[ADDRESSES]) -> bool {
         for (; v < v_hi; v += kQ4Waves) {
             if constexpr (FORM != kQ4Direct) {
                 if (slot == 64) look_ahead(v);
                 key = __builtin_amdgcn_readlane(ahead_key, slot);
-                if constexpr (FORM != kQ4Any)
+                if constexpr (FOLLOWING)
 #pragma unroll
                     for (int i = 0; i < RUNS; ++i)
                         run[i] = base + (((int64_t)__builtin_amdgcn_readlane(ahead_off[1], slot + i) << 32) |
@@ -174,7 +179,7 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
     };
     // Chunk n of a run is chunk n % RPC of its row n / RPC; this lane's of load i is n = 64 i + lane
     uint32_t chunk_off[LOADS];
-    if constexpr (FORM != kQ4Any)
+    if constexpr (FOLLOWING)
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const uint32_t n = 64 * i + lane;
@@ -182,9 +187,9 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
         }
     // A tile's rows on their way into stage 0 or 1 (rows past the sequence end: its last one, masked below)
     const uint32_t raw_address = lds_byte_address(raw);
-    auto issue = [&](int key, const char *const(&run)[RUNS], int stage) {
+    auto issue = [&](int key, const char *const(&run)[ADDRESSES], int stage) {
         const uint32_t to = raw_address + 16 * RAW * stage;
-        if constexpr (FORM != kQ4Any) {
+        if constexpr (FOLLOWING) {
             const bool exists = key + kQ4Tile <= Lb;  // (uniform) all of it
 #pragma unroll
             for (int r = 0; r < RUNS; ++r) {
@@ -207,11 +212,15 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
                 }
             }
         } else {
+            const int last = FORM == kQ4Runs8 ? min(Lb - 1 - key, kQ4Tile - 1) : kQ4Tile - 1;
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {  // (from the lane that has the row's offset)
-                const int n = 64 * i + lane, row = n / RPC;
-                const int lo = __shfl((int)row_off, row, 64), hi = __shfl((int)(row_off >> 32), row, 64);
-                tile_load16<64>(base + (((int64_t)hi << 32) | (uint32_t)lo) + 16 * (n % RPC), to + 1024 * i);
+            for (int i = 0; i < LOADS; ++i) {  // (from the lane that has the offset of the row, or of its run)
+                const int n = 64 * i + lane, row = FORM == kQ4Runs8 ? min(n / RPC, last) : n / RPC;
+                const int from = FORM == kQ4Runs8 ? slot - RUNS + row / 8 : row;
+                const int lo = __shfl(FORM == kQ4Runs8 ? ahead_off[0] : (int)row_off, from, 64);
+                const int hi = __shfl(FORM == kQ4Runs8 ? ahead_off[1] : (int)(row_off >> 32), from, 64);
+                const uint32_t in_run = FORM == kQ4Runs8 ? __umul24((uint32_t)row % 8, row_bytes) : 0u;
+                tile_load16<64>(base + (((int64_t)hi << 32) | (uint32_t)lo) + in_run + 16 * (n % RPC), to + 1024 * i);
             }
         }
     };
@@ -230,7 +239,7 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
     const uint32_t v_scale_at = (uint32_t)(16 * (c >> 3) + 4 * g + ((c >> 1) & 3)) * Row::kBytes + (D == 128 ? Row::kVScale : Row::kKScale);
 
     int v = v_lo + w, key = 0, key_next = 0, stage = 0;
-    const char *run[RUNS];
+    const char *run[ADDRESSES];
     bool have = next_tile(v, key, run), have_next = false;
     if (have) {
         issue(key, run, 0);
@@ -249,7 +258,7 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
         const int tk = key;
         const bool whole = scope.whole(tk, kQ4Tile);  // (uniform) every column sees all of the keys
         if (have_next)                                // (uniform) the tile is here, the next one may not be
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(RUNS * LOADS) : "memory");
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ADDRESSES * LOADS) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         const char *tile = (const char *)(raw + stage * RAW);
@@ -435,12 +444,16 @@ static void launch_q4_form(const DecodeRowsParams &P, hipStream_t stream) {
     const DecodeParams &p = P.d;
     const dim3 grid(p.S, p.Hkv, p.B);
     const bool short_rows = p.ksl < (1 << 24);  // (24-bit products of a row number below 64 and the row stride)
+    // (pages of a multiple of 8 against row by row, us: 24 x <= 6000 keys 41.8, 44.7; d = 64, window 4096, 4 rows 21.6, 23.7; pages of 16
+    // 39.3, 20.8, of 64 37.1, 20.2, none 36.2, 19.5)
     if (short_rows && p.block_table == nullptr && P.block_list == nullptr)
         hipLaunchKernelGGL((decode_q4_kernel<D, C, USE_R, kQ4Direct>), grid, dim3(256), 0, stream, P);
     else if (short_rows && (p.block_table == nullptr || p.page_size % 64 == 0))
         hipLaunchKernelGGL((decode_q4_kernel<D, C, USE_R, kQ4Runs64>), grid, dim3(256), 0, stream, P);
     else if (short_rows && p.page_size % 16 == 0)
         hipLaunchKernelGGL((decode_q4_kernel<D, C, USE_R, kQ4Runs16>), grid, dim3(256), 0, stream, P);
+    else if (short_rows && p.page_size % 8 == 0)
+        hipLaunchKernelGGL((decode_q4_kernel<D, C, USE_R, kQ4Runs8>), grid, dim3(256), 0, stream, P);
     else
         hipLaunchKernelGGL((decode_q4_kernel<D, C, USE_R, kQ4Any>), grid, dim3(256), 0, stream, P);
 }
