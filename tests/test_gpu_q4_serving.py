@@ -332,3 +332,20 @@ def test_pages_of_far_tokens(plx, page):  # noqa: F811
         want = plx.parallax_cache_read_q4(small, d, T)
         there = (first + torch.arange(T, device=DEV) < n_pages * page)[None, None, :, None]  # (a token past the last page: zeros)
         assert all(torch.equal(a, torch.where(there, b, torch.zeros_like(b))) for a, b in zip(back, want)), first
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_same_bits_in_pages_of_any_size(plx, d):  # noqa: F811
+    """Lists, windows with sinks and whole sequences that end anywhere: pages of any size give what rows without pages give."""
+    B, L = 5, 700
+    cache = torch.from_numpy(_cache(B, 2, L, d, 8)).to(DEV)
+    lens = _ints([700, 641, 8, 65, 0])
+    q, r = (_normal((B, 8, 2, d), s) for s in (1, 2))
+    names = _ints([[[0, 2, 5, 10, -1], [1, 3, 3, 4, 9]]] * B)
+    for page in (1, 7, 8, 16, 40, 48, 64, 100, 128, 1000):
+        pool, table = _paged(cache.cpu().numpy(), page, 3)
+        for more in (dict(), dict(block_list=names), dict(window=100, sinks=70)):
+            for S in (1, 3):
+                want = plx.parallax_decode_q4(q, r, cache, 0.1, seq_lens=lens, num_splits=S, **more)
+                got = plx.parallax_decode_q4(q, r, pool, 0.1, seq_lens=lens, num_splits=S, block_table=table, max_len=L, **more)
+                assert torch.equal(got, want), (page, S, tuple(more))
