@@ -349,3 +349,46 @@ def test_the_same_bits_in_pages_of_any_size(plx, d):  # noqa: F811
                 want = plx.parallax_decode_q4(q, r, cache, 0.1, seq_lens=lens, num_splits=S, **more)
                 got = plx.parallax_decode_q4(q, r, pool, 0.1, seq_lens=lens, num_splits=S, block_table=table, max_len=L, **more)
                 assert torch.equal(got, want), (page, S, tuple(more))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_lists_over_bf16_pages_of_any_size(plx, d):  # noqa: F811
+    """... and the bf16 decode over lists, whose entries may be anything."""
+    B, L = 4, 700
+    k, v = (_normal((B, 2, L, d), s) for s in (1, 2))
+    q, r = (_normal((B, 8, 2, d), s) for s in (3, 4))
+    lens = _ints([700, 641, 65, 0])
+    top, low = 2 ** 31 - 1, -2 ** 31
+    names = _ints([[[low, 0, 2, 5, 10, top], [1, 3, 3, 4, 9, -1]], [[0, 0, 0, 0, 0, 0], [10, 9, 8, 7, 6, 5]],
+                   [[-1, 0, 1, 2, 3, 4], [top, 1, low, 0, 2, 1]], [[0, 1, 2, 3, 4, 5]] * 2])
+    kept = [[[0, 2, 5, 10], [1, 3, 4, 9]], [[0], [10]], [[0, 1], [0]], [[], []]]
+    for x in (0, 1, 2):  # what the entries come to
+        for h in (0, 1):
+            seen = np.full((1, 2, L), False)
+            before = -1
+            for e in names[x, h].tolist():
+                if 0 <= e and e > before and e * 64 < lens[x].item():
+                    seen[..., e * 64: e * 64 + 64] = True
+                before = e
+            assert [j for j in range(11) if seen[0, 0, j * 64]] == kept[x][h], (x, h)
+    want = {}
+    for page in (0, 1, 7, 8, 16, 40, 64, 100, 1000):
+        kk, vv, more = k, v, {}
+        if page:
+            per = -(-L // page)
+            order = torch.randperm(B * per, device=DEV)
+            table = order.to(torch.int32).reshape(B, per)
+            kk, vv = (torch.full((B * per, 2, page, d), float("nan"), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+            for pool, rows_of in ((kk, k), (vv, v)):
+                padded = torch.full((B, 2, per * page, d), float("nan"), dtype=torch.bfloat16, device=DEV)
+                padded[:, :, :L] = rows_of
+                pool[order] = padded.reshape(B, 2, per, page, d).transpose(1, 2).reshape(B * per, 2, page, d)
+            more = dict(block_table=table, max_len=L)
+        for S in (1, 3):
+            got = plx.parallax_decode(q, r, kk, vv, 0.1, seq_lens=lens, num_splits=S, block_list=names, **more)
+            want.setdefault(S, got)
+            assert torch.equal(got, want[S]), (page, S)
+    held = lens.tolist()
+    see = np.stack([np.stack([rows.chain(held[b], 2, L) & blocks.listed_keys(x, held[b], L) for x in kept[b]]) for b in range(B)])
+    for S in (1, 3):
+        _check(want[S], host(q), host(r), host(k), host(v), 0.1, see, (S,))
