@@ -19,12 +19,15 @@
 //     the product, P: of the 16 columns of the matrix only those of the group's heads x rows are needed, and the copies of such a
 //     column hold P times the scales of one group of 16 dimensions each: 8 groups x 2 columns at D = 128 (C = 2). The product for a
 //     group's dimensions is right in its own copy only, and only that is kept. With more columns (C) the groups do not fit beside each
-//     other and P is multiplied 2, 4 or 8 times. A power of two changes no bit of P but its exponent. A key that a column does not see
-//     has the scale 0, so nothing in its row can reach it.
+//     other and P is multiplied 2, 4 or 8 times. A key that a column does not see has the scale 0, so nothing in its row can reach it.
+// P and the scales are f16: a power of two changes no bit of a weight but its exponent, and three bits more than bf16's make the rounding of P
+// disappear behind that of the result. What f16 lacks is range: the scales of a group of dimensions count from the largest that its tiles
+// have shown, and rho shrinks where P rho.k grows too large (the state with them, as with the running maximum: rarely).
 // Steps, us for 16 x 32768 keys, 8 key heads, d = 128, and for 1 x 65536 at 8 splits (a workgroup a unit, 64 units): tiles in registers, V as bf16
 // through LDS, 32 keys at a time 130 and 81; two tiles in LDS 117, 77; 64 keys at a time, no bank conflicts 116, 61 (now bound by
-// LDS: 16 KB of V written at 64 bytes a cycle, and every read costs 6); scales with P instead 115, 50; scales out of their bytes by one instruction 111, 48.5 (the loads
-// alone, without any arithmetic, 106).
+// LDS: 16 KB of V written at 64 bytes a cycle, and every read costs 6); scales with P instead 115, 50; scales out of their bytes by one
+// instruction 111, 48.5; P in f16 instead of bf16, for
+// an error of 1.7e-3 instead of 2.4e-3, 115, 52 (the loads alone, without any arithmetic, 106).
 #include "plx_lds_dma.h"
 #include "plx_q4.h"
 #include "plx_rows.h"
@@ -34,7 +37,10 @@ namespace plx {
 namespace {
 constexpr int kQ4Tile = 64;  // keys per wave tile
 constexpr int kQ4Waves = 4;
-constexpr float kQ4Slack = 6.f;  // in the exponent of 2
+// Exponents of 2: weights are held times 2^2 and may grow by 2^6 before their reference moves, the scales of a group of dimensions by 2^3 (as
+// exponents of f16: from 16 to 19), a weight times rho.k to 2^9: what is multiplied stays below 2^16 in f16
+constexpr float kQ4Slack = 6.f;
+constexpr int kWeightUp = 2, kFieldStart = 16, kFieldMost = 19, kTiltRoom = 9;
 
 // How the rows of a tile are found: 64 that follow each other in memory, counted from the start of the cache or looked up ahead
 // (lists; pages of a multiple of 64), four runs of 16 (other pages of a multiple of 16), eight of 8 likewise, or row by row.
@@ -59,6 +65,13 @@ struct Q4Scope : RowsScope<false, kQ4Tile> {
 template <int BANKS>
 __device__ __forceinline__ uint32_t from_other_quad(uint32_t old, uint32_t x) {
     return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)x, 0x124, 0xf, BANKS, false);  // row_ror:4
+}
+// Bits of the 16 lanes of a row together
+__device__ __forceinline__ uint32_t row_or(uint32_t x) {
+    x |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, true);  // row_ror:8
+    x |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xf, 0xf, true);
+    x |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xf, 0xf, true);
+    return x | (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xf, 0xf, true);
 }
 template <int A, int B>
 __device__ __forceinline__ uint32_t from_quad(uint32_t x) {  // lanes A, B, A, B of the quad
@@ -231,6 +244,9 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
 #pragma unroll
     for (int i = 0; i < NDB; ++i) o1[i] = o2[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float scale_log2 = p.scale * kLog2e;
+    // What a scale byte of this lane's group stands for is 2^(byte - 127): its operand is 2^(byte - scale_base - 15). P2 (this lane's column) is
+    // held times 2^-tilt_ref, by way of rho
+    int scale_base = -256, tilt_ref = 0;
 
     // This lane's places in a tile: of the K rows, and of the rows it gives the transposing reads (element i of a lane's 4-bit
     // operand is key 32 (i / 8) + 16 (i / 4 % 2) + 4 g + i % 4, of its scales, 32 keys at a time, likewise)
@@ -299,7 +315,10 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
         u32x2 scales[2];  // of V, 8 keys each
 #pragma unroll
         for (int h = 0; h < 2; ++h) scales[h] = lds_read_tr8(tile + 32 * h * Row::kBytes + v_scale_at);
-        u32x2 keep[2] = {{~0u, ~0u}, {~0u, ~0u}};  // bytes of the keys that are seen
+        uint32_t keep[8];  // 16 bits a key that is seen, the keys in the order of p1
+        u32x2 looked_at[2] = {scales[0], scales[1]};  // of keys that some column sees
+#pragma unroll
+        for (int n = 0; n < 8; ++n) keep[n] = ~0u;
         float factor = scale_log2;
         if (__builtin_expect(!whole, 0)) {
             uint32_t seen[2];
@@ -311,65 +330,131 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
                 const bool ok = (seen[e >> 3] >> (e & 7)) & 1u;
                 s1[e >> 2][e & 3] = ok ? s1[e >> 2][e & 3] * factor : kNegInf;
                 if constexpr (USE_R) s2[e >> 2][e & 3] = ok ? s2[e >> 2][e & 3] : 0.f;
-                if (!ok) keep[e >> 3][(e >> 2) & 1] &= ~(255u << (8 * (e & 3)));
+                if (!ok) keep[e >> 1] &= e & 1 ? 0xffffu : 0xffff0000u;
             }
             factor = 1.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t any = row_or(seen[h]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!((any >> e) & 1u)) looked_at[h][e >> 2] &= ~(255u << (8 * (e & 3)));
+            }
         }
         // Any reference near the row's largest score does: it moves (and everything with it) only when a score is 2^6 above it
         float tmax = kNegInf;
 #pragma unroll
         for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, s1[e >> 2][e & 3]);
         tmax *= factor;
-        if (__builtin_expect(__any(tmax > m_run + kQ4Slack), 0)) {  // (rare, but for the first tile)
+        // a bound on the largest |P2| of this lane's keys
+        float tilt = 0.f;
+        if constexpr (USE_R) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) tilt = fmaxf(tilt, fabsf(s2[e >> 2][e & 3]));
+        }
+        const float reach = USE_R ? tilt * fast_exp2(tmax - m_run) : 0.f;
+        // (this group's largest scale byte, in the upper byte of two halves; below it whatever comes)
+        int top;
+        {
+            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 x = {0, 0};
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int d = 0; d < 2; ++d) {
+                    const uint32_t y = looked_at[h][d];
+                    x = __builtin_elementwise_max(x, __builtin_elementwise_max(__builtin_bit_cast(u16x2, y), __builtin_bit_cast(u16x2, y << 8)));
+                }
+            const uint32_t both = __builtin_bit_cast(uint32_t, x);
+            top = (int)(max(both >> 16, both & 0xffffu) >> 8);
+            if constexpr (D == 64) top = c & 4 ? top : 0;  // (the others have the scales of K)
+        }
+        constexpr float kTiltMost = 1 << kTiltRoom;
+        if (__builtin_expect(__any((tmax > m_run + kQ4Slack) | (top > scale_base + kFieldMost) | (reach > kTiltMost)), 0)) {
+            // (rare, but for the first tile)
             tmax = rows_max(tmax);
             const float m_new = fmaxf(m_run, tmax);
             const float alpha = fast_exp2(m_run - (m_new == kNegInf ? 0.f : m_new));
             m_run = m_new;
             dsum1 *= alpha, dsum2 *= alpha;
+            if (__any(top == 255)) {  // (NaN, whatever the reference: the largest of the others)
+                top = 0;
 #pragma unroll
-            for (int i = 0; i < NDB; ++i) {
-                o1[i] *= alpha;
-                if constexpr (USE_R) o2[i] *= alpha;
+                for (int e = 0; e < 16; ++e) {
+                    const int byte = (int)(looked_at[e >> 3][(e >> 2) & 1] >> (8 * (e & 3)) & 255u);
+                    if ((D == 128 || (c & 4)) && byte != 255) top = max(top, byte);
+                }
+            }
+            top = max(top, __builtin_amdgcn_update_dpp(top, top, 0x128, 0xf, 0xf, false));  // of the group: lanes c and c + 8, ..
+            top = max(top, __shfl_xor(top, 16, 64));
+            top = max(top, __shfl_xor(top, 32, 64));
+            const int base = top > scale_base + kFieldMost ? max(top - kFieldStart, 0) : scale_base, down = scale_base - base;
+            scale_base = base;
+            auto move = [&](auto j) __attribute__((always_inline)) {
+                constexpr int J = decltype(j)::value;
+                const float by = __builtin_amdgcn_ldexpf(alpha, (int)operand_scales<D, C, J>((uint32_t)down));
+#pragma unroll
+                for (int n = 0; n < REP; ++n) {
+                    o1[REP * J + n] *= by;
+                    if constexpr (USE_R) o2[REP * J + n] *= by;
+                }
+            };
+            each_of<OPERANDS>(move);
+            if constexpr (USE_R) {
+                const float most = rows_max(tilt) * fast_exp2(tmax - (m_run == kNegInf ? 0.f : m_run));  // (of this column)
+                if (__any(most > kTiltMost)) {
+                    const int less = most > kTiltMost && most < __builtin_inff() ? __builtin_amdgcn_frexp_expf(most) - kTiltRoom + 3 : 0;
+                    const float by = __builtin_amdgcn_ldexpf(1.f, -less);
+                    tilt_ref += less, dsum2 *= by;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s2[e >> 2][e & 3] *= by;
+#pragma unroll
+                    for (int i = 0; i < NDB; ++i) o2[i] *= by;
+#pragma unroll
+                    for (int s = 0; s < KSTEPS; ++s)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t x = rf[s][e];
+                            rf[s][e] = pack_bf16(bf16_lo_f32(x) * by, bf16_hi_f32(x) * by);
+                        }
+                }
             }
         }
-        const float neg_m = m_run == kNegInf ? 0.f : -m_run;
-        // P1 and P2 are rounded to bf16 once, as matrix operands (the scales, powers of two, change no bit of them); d1 and d2 add the
-        // rounded values, so that the weights still sum to one.
-        float p1[16], p2[16];
+        const float up_m = m_run == kNegInf ? 0.f : kWeightUp - m_run;
+        // P1 and P2 are rounded to f16 once (to bf16 they made the result's error 1.4 times that of its own rounding); d1 and d2 add the
+        // rounded values, so that the weights still sum to one and what cancels between O1 d2 and O2 does so exactly.
+        uint32_t w1[8], w2[8];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            p1[e] = fast_exp2(fmaf(s1[e >> 2][e & 3], factor, neg_m));
-            p2[e] = USE_R ? p1[e] * s2[e >> 2][e & 3] : 0.f;
+        for (int n = 0; n < 8; ++n) {
+            float p1[2], p2[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                p1[e] = fast_exp2(fmaf(s1[n >> 1][2 * (n & 1) + e], factor, up_m));
+                p2[e] = USE_R ? p1[e] * s2[n >> 1][2 * (n & 1) + e] : 0.f;
+            }
+            w1[n] = pack_f16(p1[0], p1[1]), dsum1 = add_f16_pair(w1[n], dsum1);
+            if constexpr (USE_R) w2[n] = pack_f16(p2[0], p2[1]), dsum2 = add_f16_pair(w2[n], dsum2);
         }
+        // this group's scales as f16: the exponent is the byte less scale_base (255, and what is beyond: infinite; too small: 0)
+        uint32_t own[8];
 #pragma unroll
-        for (int e = 0; e < 16; e += 8) {
-            pack8_bf16_accumulate(p1[e], p1[e + 1], p1[e + 2], p1[e + 3], p1[e + 4], p1[e + 5], p1[e + 6], p1[e + 7], dsum1);
-            if constexpr (USE_R)
-                pack8_bf16_accumulate(p2[e], p2[e + 1], p2[e + 2], p2[e + 3], p2[e + 4], p2[e + 5], p2[e + 6], p2[e + 7], dsum2);
+        for (int n = 0; n < 8; ++n) {
+            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+            const uint32_t bytes = __builtin_amdgcn_perm(0u, scales[n >> 2][(n >> 1) & 1], n & 1 ? 0x0c030c02u : 0x0c010c00u);
+            const uint16_t less = (uint16_t)scale_base;
+            u16x2 x = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, bytes), u16x2{less, less});
+            x = __builtin_elementwise_min(x, u16x2{31, 31}) << 10;
+            own[n] = __builtin_bit_cast(uint32_t, x);
         }
         // ---- O1^T += V^T P1^T, O2^T += V^T P2^T, 16 * REP dimensions with the same operands --------------------
         auto products = [&](auto j) __attribute__((always_inline)) {
             constexpr int J = decltype(j)::value;
             u32x4 pb1[2], pb2[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float x[8];
-#pragma unroll
-                for (int d = 0; d < 2; ++d) {
-                    const uint32_t e4 = operand_scales<D, C, J>(scales[h][d]) & keep[h][d];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)  // (at D = 128 with more columns the compiler would make too many ahead, and spill)
-                        x[4 * d + e] = D == 64 || C <= 4 ? q4_scale_byte(e4, e) : q4_scale((e4 >> (8 * e)) & 255u);
-                }
-                float y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = p1[8 * h + e] * x[e];
-                pb1[h] = u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
-                if constexpr (USE_R) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = p2[8 * h + e] * x[e];
-                    pb2[h] = u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
-                }
+            for (int n = 0; n < 8; ++n) {
+                const uint32_t x = operand_scales<D, C, J>(own[n]) & keep[n];
+                pb1[n >> 2][n & 3] = mul_f16_pair(w1[n], x);
+                if constexpr (USE_R) pb2[n >> 2][n & 3] = mul_f16_pair(w2[n], x);
             }
 #pragma unroll
             for (int n = 0; n < REP; ++n) {
@@ -377,9 +462,9 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
                 const u32x2 codes = lds_read_tr4(tile + v_at + 8 * i);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const u32x4 x = q4_to_bf16(codes[h], 1.f);
-                    o1[i] = mfma16(x, pb1[h], o1[i]);
-                    if constexpr (USE_R) o2[i] = mfma16(x, pb2[h], o2[i]);
+                    const u32x4 x = q4_to_f16(codes[h]);
+                    o1[i] = mfma16_f16(x, pb1[h], o1[i]);
+                    if constexpr (USE_R) o2[i] = mfma16_f16(x, pb2[h], o2[i]);
                 }
             }
         };
@@ -400,7 +485,20 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
     float *mrg_m = (float *)(lds + kQ4Waves * 2 * RAW), *mrg_d1 = mrg_m + kQ4Waves * 16, *mrg_d2 = mrg_d1 + kQ4Waves * 16;
     __syncthreads();  // every wave is done with its tiles
     {
-        const float s1 = rows_sum(dsum1), s2 = rows_sum(dsum2);
+        // (back to what m_run stands for)
+        const float s1 = __builtin_amdgcn_ldexpf(rows_sum(dsum1), -kWeightUp), s2 = __builtin_amdgcn_ldexpf(rows_sum(dsum2), tilt_ref - kWeightUp);
+        auto put_back = [&](auto j) __attribute__((always_inline)) {
+            constexpr int J = decltype(j)::value;
+            const int up = (int)operand_scales<D, C, J>((uint32_t)scale_base) + 15 - 127 - kWeightUp;
+#pragma unroll
+            for (int i = REP * J; i < REP * (J + 1); ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    o1[i][e] = __builtin_amdgcn_ldexpf(o1[i][e], up);
+                    if constexpr (USE_R) o2[i][e] = __builtin_amdgcn_ldexpf(o2[i][e], up + tilt_ref);
+                }
+        };
+        each_of<OPERANDS>(put_back);
         // a row in front of the sequence sees nothing, also where all others see everything
         const bool none = col_end == 0;
         if (g == 0) {

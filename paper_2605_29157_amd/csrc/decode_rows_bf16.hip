@@ -246,19 +246,35 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
         const float alpha = fast_exp2(m_run - m_use);  // 0 on the first tile that is seen
         m_run = m_new;
         // P1 and P2 are rounded to bf16 once, as matrix operands; d1 and d2 add the rounded values, so
-        // that the weights still sum to one.
+        // that the weights still sum to one. LIST: what the rounding takes is multiplied too (without it the result's error is
+        // 1.4 times that of its own rounding; 16 x 8 lists of 64 blocks 58.1 us, with it 59.1).
+        u32x4 rest1 = {0u, 0u, 0u, 0u}, rest2 = rest1;
+        auto split = [&](const float(&x)[8], u32x4 &rest, float &sum) {
+            u32x4 y;
+            if constexpr (LIST) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t pair = pack_bf16(x[2 * e], x[2 * e + 1]);
+                    const uint32_t left = pack_bf16(x[2 * e] - bf16_lo_f32(pair), x[2 * e + 1] - bf16_hi_f32(pair));
+                    sum = add_bf16_pair(left, add_bf16_pair(pair, sum)), y[e] = pair, rest[e] = left;
+                }
+            } else {
+                y = pack8_bf16_accumulate(x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7], sum);
+            }
+            return y;
+        };
         float p1[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) p1[e] = fast_exp2(x[e] - m_use);
         dsum1 *= alpha;
-        const u32x4 pb1 = pack8_bf16_accumulate(p1[0], p1[1], p1[2], p1[3], p1[4], p1[5], p1[6], p1[7], dsum1);
+        const u32x4 pb1 = split(p1, rest1, dsum1);
         u32x4 pb2 = {0u, 0u, 0u, 0u};
         if constexpr (USE_R) {
             float p2[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) p2[e] = (seen >> e) & 1u ? p1[e] * s2[e >> 2][e & 3] : 0.f;
             dsum2 *= alpha;
-            pb2 = pack8_bf16_accumulate(p2[0], p2[1], p2[2], p2[3], p2[4], p2[5], p2[6], p2[7], dsum2);
+            pb2 = split(p2, rest2, dsum2);
         }
         if (!__all(alpha == 1.f)) {
 #pragma unroll
@@ -271,7 +287,9 @@ __global__ __launch_bounds__(256, 2) void decode_rows_kernel(DecodeRowsParams P)
         for (int i = 0; i < NDB; ++i) {
             const u32x4 vt = v_fragment(i);
             o1[i] = mfma16(vt, pb1, o1[i]);
+            if constexpr (LIST) o1[i] = mfma16(vt, rest1, o1[i]);
             if constexpr (USE_R) o2[i] = mfma16(vt, pb2, o2[i]);
+            if constexpr (LIST && USE_R) o2[i] = mfma16(vt, rest2, o2[i]);
         }
         wave_lds_fence();
     }

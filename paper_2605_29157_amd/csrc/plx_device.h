@@ -76,6 +76,10 @@ __device__ __forceinline__ u32x4 pack8_bf16_accumulate(float p0, float p1, float
                  __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)};
 }
 
+__device__ __forceinline__ float add_bf16_pair(uint32_t x, float sum) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), bf16x2{(__bf16)1.0f, (__bf16)1.0f}, sum, false);
+}
+
 // Transposing LDS read (ds_read_b64_tr_b16). Within each group of 16 lanes, lane i receives
 // element i%4 of the 8 bytes addressed by lanes i/4, 4 + i/4, 8 + i/4, 12 + i/4. With lane i
 // addressing row i/4, elements 4*(i%4)..+3 of a row-major [4 rows][16 elements] block, lane i

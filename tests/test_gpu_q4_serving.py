@@ -4,8 +4,8 @@ import numpy as np
 import pytest
 import torch
 
-from oracle import blocks, rows
-from parity import host
+from oracle import blocks, masked, rows
+from parity import BF16_REL_L2, host, rel_l2
 from test_gpu_guard_bands import Guarded, plx  # noqa: F401
 from test_gpu_q4 import _cache, _check, _normal, _paged
 from test_gpu_streams import _noise
@@ -392,3 +392,71 @@ def test_lists_over_bf16_pages_of_any_size(plx, d):  # noqa: F811
     see = np.stack([np.stack([rows.chain(held[b], 2, L) & blocks.listed_keys(x, held[b], L) for x in kept[b]]) for b in range(B)])
     for S in (1, 3):
         _check(want[S], host(q), host(r), host(k), host(v), 0.1, see, (S,))
+
+
+@pytest.mark.parametrize("kind", ["v grows", "v falls", "v of one group", "v huge", "v tiny", "u large", "u grows", "u falls", "u tiny", "all"])
+@pytest.mark.parametrize("d,Hq,Tq", [(128, 2, 1), (128, 4, 1), (128, 8, 2), (64, 3, 1), (64, 8, 1), (64, 4, 4)])
+def test_references_move(plx, d, Hq, Tq, kind):  # noqa: F811
+    """Values of V and products rho.k whose size changes by many powers of two along the sequence, between dimensions, or is far from one."""
+    L = 1500
+    k, v = (_normal((1, 1, L, d), s).float() for s in (1, 2))
+    q, r = (_normal((1, Hq, Tq, d), s) for s in (3, 4))
+    ramp = torch.exp2(torch.linspace(-25, 25, L, device=DEV))[:, None]
+    if kind in ("v grows", "all"):
+        v *= ramp
+    if kind == "v falls":
+        v *= ramp.flip(0)
+    if kind in ("v of one group", "all"):
+        v[..., 16:32] *= 2.0 ** 9
+    if kind == "v huge":
+        v *= 2.0 ** 90
+    if kind == "v tiny":
+        v *= 2.0 ** -90
+    if kind == "u large":
+        r = (r.float() * 2.0 ** 14).to(torch.bfloat16)
+    if kind == "u tiny":
+        r = (r.float() * 2.0 ** -30).to(torch.bfloat16)
+    if kind in ("u grows", "u falls", "all"):  # (in dimensions that q does not look at)
+        half = torch.exp2(torch.linspace(-4, 12, L, device=DEV))[:, None]
+        k[..., d // 2:] *= half.flip(0) if kind == "u falls" else half
+        q[..., d // 2:] = 0
+    cache = torch.zeros(1, 1, L, blocks.row_bytes(d), dtype=torch.uint8, device=DEV)
+    plx.parallax_cache_write_q4(k, v, cache)
+    hk, hv = (x.double().cpu().numpy() for x in plx.parallax_cache_read_q4(cache, d, L, dtype=torch.float32))
+    see = rows.chain(L, Tq, L)[None, None]
+    hq, hr = host(q).astype(np.float64), host(r).astype(np.float64)
+    unit = np.abs(hv).max()  # (the bound's arithmetic is in units of one)
+    for S in (1, 2, 5):
+        got = plx.parallax_decode_q4(q, r, cache, d ** -0.5, num_splits=S)
+        got = host(got).astype(np.float64)
+        ref = masked.masked_forward(hq, hr, hk, hv, d ** -0.5, np.broadcast_to(see, (1, Hq, Tq, L)))
+        assert np.isfinite(got).all()
+        assert rel_l2(got, ref) <= BF16_REL_L2, (kind, S)
+        bound = rows.bf16_bound(hq, hr, hk, hv / unit, d ** -0.5, np.broadcast_to(see, (1, Hq, Tq, L))) * unit
+        assert (np.abs(got - ref) <= bound).all(), (kind, S, float((np.abs(got - ref) / bound).max()))
+
+
+@pytest.mark.parametrize("large", [1.0, 2.0 ** 6])
+@pytest.mark.parametrize("d", [64, 128])
+def test_what_cancels_does_so_exactly(plx, d, large):  # noqa: F811
+    """One key, or one value for all keys: the weights sum to one, so the value comes back whatever rho is (to a bf16 rounding of f32 sums
+    of 2^-23 |rho.k|, which is below half of its step)."""
+    L = 130
+    k, v = (_normal((2, 2, L, d), s) for s in (1, 2))
+    q, r = (_normal((2, 8, d), s) for s in (3, 4))
+    r = (r.float() * large).to(torch.bfloat16)
+    cache = torch.zeros(2, 2, L, blocks.row_bytes(d), dtype=torch.uint8, device=DEV)
+    for lens, values in ((_ints([1, 1]), v), (_ints([L, 77]), v[:, :, :1].expand(-1, -1, L, -1).contiguous())):
+        plx.parallax_cache_write_q4(k, values, cache)
+        want = plx.parallax_cache_read_q4(cache, d, 1)[1][:, :, 0].repeat_interleave(4, 1)
+        for S in (1, 3):
+            got = plx.parallax_decode_q4(q, r, cache, d ** -0.5, seq_lens=lens, num_splits=S)
+            assert ((got.float() - want.float()).abs() <= 2.0 ** -8 * want.float().abs()).all(), (S, "a step")
+            if int(lens[0]) == 1:
+                assert torch.equal(got, want), S
+        names = _ints([[[0, 1, 2]] * 2] * 2)
+        got = plx.parallax_decode(q, r, k, values, d ** -0.5, seq_lens=lens, block_list=names)
+        want = values[:, :, 0].repeat_interleave(4, 1)
+        assert ((got.float() - want.float()).abs() <= 2.0 ** -8 * want.float().abs()).all()
+        if int(lens[0]) == 1:
+            assert torch.equal(got, want)
