@@ -377,7 +377,8 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
             const float alpha = fast_exp2(m_run - (m_new == kNegInf ? 0.f : m_new));
             m_run = m_new;
             dsum1 *= alpha, dsum2 *= alpha;
-            if (__any(top == 255)) {  // (NaN, whatever the reference: the largest of the others)
+            const bool nan = __any(top == 255);  // (whatever the reference: the largest of the others)
+            if (nan) {
                 top = 0;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -388,8 +389,18 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
             top = max(top, __builtin_amdgcn_update_dpp(top, top, 0x128, 0xf, 0xf, false));  // of the group: lanes c and c + 8, ..
             top = max(top, __shfl_xor(top, 16, 64));
             top = max(top, __shfl_xor(top, 32, 64));
-            const int base = top > scale_base + kFieldMost ? max(top - kFieldStart, 0) : scale_base, down = scale_base - base;
+            const int base = top > scale_base + kFieldMost ? min(max(top - kFieldStart, 0), 224) : scale_base;
+            const int down = scale_base - base;
             scale_base = base;
+            if (nan) {  // (the exponent of infinity)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    uint32_t x = scales[e >> 3][(e >> 2) & 1];
+                    const int at = 8 * (e & 3);
+                    if ((x >> at & 255u) == 255u) x = (x & ~(255u << at)) | (uint32_t)(scale_base + 31) << at;
+                    scales[e >> 3][(e >> 2) & 1] = x;
+                }
+            }
             auto move = [&](auto j) __attribute__((always_inline)) {
                 constexpr int J = decltype(j)::value;
                 const float by = __builtin_amdgcn_ldexpf(alpha, (int)operand_scales<D, C, J>((uint32_t)down));
@@ -435,15 +446,14 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
             w1[n] = pack_f16(p1[0], p1[1]), dsum1 = add_f16_pair(w1[n], dsum1);
             if constexpr (USE_R) w2[n] = pack_f16(p2[0], p2[1]), dsum2 = add_f16_pair(w2[n], dsum2);
         }
-        // this group's scales as f16: the exponent is the byte less scale_base (255, and what is beyond: infinite; too small: 0)
+        // this group's scales as f16: the exponent is the byte less scale_base (too small: 0; of keys that nobody sees: whatever comes)
         uint32_t own[8];
 #pragma unroll
         for (int n = 0; n < 8; ++n) {
             typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
             const uint32_t bytes = __builtin_amdgcn_perm(0u, scales[n >> 2][(n >> 1) & 1], n & 1 ? 0x0c030c02u : 0x0c010c00u);
             const uint16_t less = (uint16_t)scale_base;
-            u16x2 x = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, bytes), u16x2{less, less});
-            x = __builtin_elementwise_min(x, u16x2{31, 31}) << 10;
+            const u16x2 x = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, bytes), u16x2{less, less}) << 10;
             own[n] = __builtin_bit_cast(uint32_t, x);
         }
         // ---- O1^T += V^T P1^T, O2^T += V^T P2^T, 16 * REP dimensions with the same operands --------------------

@@ -460,3 +460,33 @@ def test_what_cancels_does_so_exactly(plx, d, large):  # noqa: F811
         assert ((got.float() - want.float()).abs() <= 2.0 ** -8 * want.float().abs()).all()
         if int(lens[0]) == 1:
             assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("huge", [False, True])
+@pytest.mark.parametrize("d,Hq", [(128, 2), (128, 8), (64, 4)])
+def test_nan_in_a_value_stays_in_its_dimensions(plx, d, Hq, huge):  # noqa: F811
+    """16 dimensions of V of one key are NaN: those of the rows that see it are not finite, all other ones as without it (but for where
+    the references stand: both are within the rounding of the same result)."""
+    L, at = 400, 333
+    k, v = (_normal((1, 1, L, d), s).float() for s in (1, 2))
+    q, r = (_normal((1, Hq, 2, d), s) for s in (3, 4))
+    if huge:
+        v *= 2.0 ** 105
+    cache = torch.zeros(1, 1, L, blocks.row_bytes(d), dtype=torch.uint8, device=DEV)
+    plx.parallax_cache_write_q4(k, v, cache)
+    bad = v.clone()
+    bad[0, 0, at, 21] = float("nan")
+    other = cache.clone()
+    plx.parallax_cache_write_q4(k, bad, other)
+    for n, S in ((L, 1), (L, 3), (at + 1, 1), (at + 2, 2), (at, 1)):  # (the second row of two ends at n; the first one key before)
+        lens = _ints([n])
+        want = plx.parallax_decode_q4(q, r, cache, d ** -0.5, seq_lens=lens, num_splits=S)
+        got = plx.parallax_decode_q4(q, r, other, d ** -0.5, seq_lens=lens, num_splits=S)
+        assert torch.isfinite(want.float()).all()
+        for t in range(2):
+            sees = at < n - 1 + t
+            assert torch.equal(torch.isfinite(got[:, :, t, 16:32].float()), torch.full_like(got[:, :, t, 16:32], not sees, dtype=torch.bool)), (n, S, t)
+            rest = [x for x in range(d) if not 16 <= x < 32]
+            assert rel_l2(host(got)[:, :, t, rest], host(want)[:, :, t, rest]) <= BF16_REL_L2, (n, S, t)
+            if not sees:
+                assert rel_l2(host(got)[:, :, t], host(want)[:, :, t]) <= BF16_REL_L2, (n, S, t)
