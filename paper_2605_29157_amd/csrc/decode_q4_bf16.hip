@@ -27,7 +27,7 @@
 // through LDS, 32 keys at a time 130 and 81; two tiles in LDS 117, 77; 64 keys at a time, no bank conflicts 116, 61 (now bound by
 // LDS: 16 KB of V written at 64 bytes a cycle, and every read costs 6); scales with P instead 115, 50; scales out of their bytes by one
 // instruction 111, 48.5; P in f16 instead of bf16, for
-// an error of 1.7e-3 instead of 2.4e-3, 115, 52 (the loads alone, without any arithmetic, 106).
+// an error of 1.7e-3 instead of 2.4e-3, 116, 52 (the loads alone, without any arithmetic, 106).
 #include "plx_lds_dma.h"
 #include "plx_q4.h"
 #include "plx_rows.h"
@@ -552,7 +552,7 @@ static void launch_q4_form(const DecodeRowsParams &P, hipStream_t stream) {
     const DecodeParams &p = P.d;
     const dim3 grid(p.S, p.Hkv, p.B);
     const bool short_rows = p.ksl < (1 << 24);  // (24-bit products of a row number below 64 and the row stride)
-    // (pages of a multiple of 8 against row by row, us: 24 x <= 6000 keys 41.8, 44.7; d = 64, window 4096, 4 rows 21.6, 23.7; pages of 16
+    // (when P was bf16: pages of a multiple of 8 against row by row, us: 24 x <= 6000 keys 41.8, 44.7; d = 64, window 4096, 4 rows 21.6, 23.7; pages of 16
     // 39.3, 20.8, of 64 37.1, 20.2, none 36.2, 19.5)
     if (short_rows && p.block_table == nullptr && P.block_list == nullptr)
         hipLaunchKernelGGL((decode_q4_kernel<D, C, USE_R, kQ4Direct>), grid, dim3(256), 0, stream, P);
