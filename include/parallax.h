@@ -346,7 +346,8 @@ plx_status parallax_cache_compact(const plx_cache_compact_args *args, void *hip_
  * dimensions, 255 makes them NaN (in V infinite or NaN, where a code is not 0). Written rows take the power of two that brings the largest magnitude of the 16 into [3.5, 7),
  * e within 4 .. 252 (what is left over above saturates, below becomes 0), and round to nearest, ties to the even code; 16 dimensions
  * of which one is infinite or NaN get e = 255 and codes of 0. Every value of such a row is exact in bf16. (A decode multiplies weights by
- * scales of V in f16, relative to the largest of the 16 dimensions that it has come to: a key whose scale lies 2^16 below that counts as 0.)
+ * scales of V in f16, relative to the largest of the 16 dimensions that it has come to: a key whose scale lies 2^16 below that counts as 0, as does
+ * one whose weight lies 2^27 below the row's largest; scales of V beyond 2^116 may overflow.)
  *   rows         [B, Hkv, capacity, row] (stride[0]: sequence, [1]: head, [2]: row), or with a block table pools
  *                [num_pages, Hkv, page_size, row] (stride[0]: page); strides in BYTES, multiples of 16, stride[2] >= the row;
  *                those of rows and pages below 2^36
