@@ -345,9 +345,11 @@ plx_status parallax_cache_compact(const plx_cache_compact_args *args, void *hip_
  * A code is a sign bit over one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (e2m1); a scale byte e stands for 2^(e - 127) and serves 16
  * dimensions, 255 makes them NaN (in V infinite or NaN, where a code is not 0). Written rows take the power of two that brings the largest magnitude of the 16 into [3.5, 7),
  * e within 4 .. 252 (what is left over above saturates, below becomes 0), and round to nearest, ties to the even code; 16 dimensions
- * of which one is infinite or NaN get e = 255 and codes of 0. Every value of such a row is exact in bf16. (A decode multiplies weights by
- * scales of V in f16, relative to the largest of the 16 dimensions that it has come to: a key whose scale lies 2^16 below that counts as 0, as does
- * one whose weight lies 2^27 below the row's largest; scales of V beyond 2^116 may overflow.)
+ * of which one is infinite or NaN get e = 255 and codes of 0. Every value of such a row is exact in bf16. (A decode rounds a weight to 11 bits or
+ * more, however far its scales are from those of other keys: weight times value is off by at most 2^-11 of itself, or 2^-13 of the
+ * largest weight times scale of the 64 keys and 16 dimensions that it is in; weight times rho.k times value likewise, or 2^-7 of that weight
+ * times scale where the 64 keys have less than 2^-16 of the row's weight. Sums are fp32 in which the largest weight of a row counts 2^-8: values
+ * below 2^-100 lose bits.)
  *   rows         [B, Hkv, capacity, row] (stride[0]: sequence, [1]: head, [2]: row), or with a block table pools
  *                [num_pages, Hkv, page_size, row] (stride[0]: page); strides in BYTES, multiples of 16, stride[2] >= the row;
  *                those of rows and pages below 2^36

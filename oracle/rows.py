@@ -56,12 +56,14 @@ def random_tree(Tq, rng, reach=6):
     return bits
 
 
-def bf16_bound(q, r, k, v, scale, mask, eps=2.0 ** -8):
+def bf16_bound(q, r, k, v, scale, mask, eps=2.0 ** -8, eps_p=None):
     """Element-wise bound on a bf16 kernel's error that rounds P1 = p, P2 = p u and the output to bf16 (half a step is 2^-8 of
     a value) and keeps everything else in fp32: O1 and d1 hold the same rounded P1, O2 and d2 the same rounded P2, so
     with o = O1 / d1 (1 + d2 / d1) - O2 / d1
         |err| <= 2^-8 (|o| + 2 |1 + ubar| sum p |v| + sum p |u| |v| + 3 (sum p |u|) sum p |v|) + second order
-    (each quotient by d1 moves by at most 2^-8 of itself); 1.02 covers the second order and the fp32 sums."""
+    (each quotient by d1 moves by at most 2^-8 of itself); 1.02 covers the second order and the fp32 sums.
+    eps_p: what P1 and P2 are off by, relative to them, where a kernel holds them in other bits than the output."""
+    eps_p = eps if eps_p is None else eps_p
     q, r, k, v = (np.asarray(x, dtype=np.float64) for x in (q, r, k, v))
     B, Hq, Tq, d = q.shape
     G = Hq // k.shape[1]
@@ -80,7 +82,7 @@ def bf16_bound(q, r, k, v, scale, mask, eps=2.0 ** -8):
             ubar, ua = (P * U).sum(axis=1, keepdims=True), (P * np.abs(U)).sum(axis=1, keepdims=True)
             o = (P * (1 + ubar - U)) @ V
             pv = P @ np.abs(V)
-            bound[b, h] = 1.02 * eps * (np.abs(o) + 2 * np.abs(1 + ubar) * pv + (P * np.abs(U)) @ np.abs(V) + 3 * ua * pv)
+            bound[b, h] = 1.02 * (eps * np.abs(o) + eps_p * (2 * np.abs(1 + ubar) * pv + (P * np.abs(U)) @ np.abs(V) + 3 * ua * pv))
     return bound
 
 

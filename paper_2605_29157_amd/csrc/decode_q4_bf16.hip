@@ -20,14 +20,20 @@
 //     column hold P times the scales of one group of 16 dimensions each: 8 groups x 2 columns at D = 128 (C = 2). The product for a
 //     group's dimensions is right in its own copy only, and only that is kept. With more columns (C) the groups do not fit beside each
 //     other and P is multiplied 2, 4 or 8 times. A key that a column does not see has the scale 0, so nothing in its row can reach it.
-// P and the scales are f16: a power of two changes no bit of a weight but its exponent, and three bits more than bf16's make the rounding of P
-// disappear behind that of the result. What f16 lacks is range: the scales of a group of dimensions count from the largest that its tiles
-// have shown, and rho shrinks where P rho.k grows too large (the state with them, as with the running maximum: rarely).
-// Steps, us for 16 x 32768 keys, 8 key heads, d = 128, and for 1 x 65536 at 8 splits (a workgroup a unit, 64 units): tiles in registers, V as bf16
+// P. One rounding of it to bf16 makes the result's error 1.4 times that of its own rounding; f16 has the bits but not the range, and bf16 for
+// what the rounding leaves costs as many products again. So a tile is looked at first. Where f16 holds its operands (all keys seen, scales within 2^8
+// of each other, each column's largest weight not 2^16 below the row's, P rho.k not too large) they are f16, the scales as exponents,
+// and what a product loses is at most 2^-13 of the tile's largest one in that column and group. Any other tile (the ends of a
+// sequence or window, values or products rho.k of other sizes beside each other, rows with a few heavy keys, NaN) takes its P in two bf16, with
+// scales of any size. O1 and O2 count in the same unit either way, so the two kinds of tile mix.
+// us, 16 x 32768 keys, 8 key heads, d = 128, at the best split, for 2, 4, 8, 16 columns: all tiles in f16 with references that followed the largest scale
+// (and lost smaller ones) 116, 118, 119, 125; now 117, 120, 121, 132; all tiles in two bf16, as they are where scores have a standard deviation
+// of 12, 142, 164, 195, 255. (Ends of sequences in f16, too: 100 x <= 500 keys 25.4, so 23.5, but the compiler then spills registers of the second
+// way, and 16 x 64 listed blocks go from 25.0 to 26.5.)
+// Steps before that, us for 16 x 32768 keys, 8 key heads, d = 128, and for 1 x 65536 at 8 splits (a workgroup a unit, 64 units): tiles in registers, V as bf16
 // through LDS, 32 keys at a time 130 and 81; two tiles in LDS 117, 77; 64 keys at a time, no bank conflicts 116, 61 (now bound by
 // LDS: 16 KB of V written at 64 bytes a cycle, and every read costs 6); scales with P instead 115, 50; scales out of their bytes by one
-// instruction 111, 48.5; P in f16 instead of bf16, for
-// an error of 1.7e-3 instead of 2.4e-3, 116, 52 (the loads alone, without any arithmetic, 106).
+// instruction 111, 48.5 (the loads alone, without any arithmetic, 106).
 #include "plx_lds_dma.h"
 #include "plx_q4.h"
 #include "plx_rows.h"
@@ -37,10 +43,11 @@ namespace plx {
 namespace {
 constexpr int kQ4Tile = 64;  // keys per wave tile
 constexpr int kQ4Waves = 4;
-// Exponents of 2: weights are held times 2^2 and may grow by 2^6 before their reference moves, the scales of a group of dimensions by 2^3 (as
-// exponents of f16: from 16 to 19), a weight times rho.k to 2^9: what is multiplied stays below 2^16 in f16
-constexpr float kQ4Slack = 6.f;
-constexpr int kWeightUp = 2, kFieldStart = 16, kFieldMost = 19, kTiltRoom = 9;
+// Exponents of 2. Weights are held times 2^13 and may grow by 2^2 before their reference moves, P rho.k times 2^7 (rho times 2^-6). Tiles of f16:
+// scales down to 2^8 below the largest, weights whose largest is not below 2^-16, P rho.k below 2^15.
+constexpr float kQ4Slack = 2.f, kWeightFloor = 16.f;
+constexpr int kWeightUp = 13, kProbeDown = 6, kScaleRange = 8, kProbeMost = 15;
+constexpr int kRecordDown = 8;  // in a record weights are 2^8 lower: times the largest values they are finite
 
 // How the rows of a tile are found: 64 that follow each other in memory, counted from the start of the cache or looked up ahead
 // (lists; pages of a multiple of 64), four runs of 16 (other pages of a multiple of 16), eight of 8 likewise, or row by row.
@@ -66,16 +73,32 @@ template <int BANKS>
 __device__ __forceinline__ uint32_t from_other_quad(uint32_t old, uint32_t x) {
     return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)x, 0x124, 0xf, BANKS, false);  // row_ror:4
 }
-// Bits of the 16 lanes of a row together
+// Bits of the 16 lanes of a row together, and the largest number of theirs
 __device__ __forceinline__ uint32_t row_or(uint32_t x) {
     x |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, true);  // row_ror:8
     x |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xf, 0xf, true);
     x |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xf, 0xf, true);
     return x | (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xf, 0xf, true);
 }
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xf, 0xf, true));
+    return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xf, 0xf, true));
+}
 template <int A, int B>
 __device__ __forceinline__ uint32_t from_quad(uint32_t x) {  // lanes A, B, A, B of the quad
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, A | B << 2 | A << 4 | B << 6, 0xf, 0xf, true);
+}
+// A number cut to the 16 bits of mantissa that two bf16 hold
+__device__ __forceinline__ float cut(float x) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffffff00u); }
+// The upper bf16 of two such numbers, and what they leave
+__device__ __forceinline__ void halves(float a, float b, u32x4 &upper_halves, u32x4 &rest, int i) {
+    auto upper = [](float lo, float hi) {
+        return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
+    };
+    const uint32_t big = upper(a, b);
+    upper_halves[i] = big, rest[i] = upper(a - bf16_lo_f32(big), b - bf16_hi_f32(big));
 }
 // Group (16 dimensions) 16 / C * J + c % (16 / C) of the scales for operand J of C columns. own: the tr_b8 read's, D = 128: group c % 8,
 // D = 64: scales of K (c % 8 < 4) and then of V.
@@ -124,8 +147,6 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
 
     // ---- this lane's column: q and rho operands, key set ---------------------------------------------------
     u32x4 qf[KSTEPS], rf[KSTEPS];
-    int col_end, col_lo;
-    TreeRow col_nodes{};
     {
         const int col = c / REP;
         const bool live = col < n_cols;
@@ -138,8 +159,13 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
             qf[s] = live ? *(const u32x4 *)(qrow + 8 * s) : z;
             if constexpr (USE_R) rf[s] = live ? *(const u32x4 *)(rrow + 8 * s) : z;
         }
-        scope.column(P, no_words, 0, c, t, live, col_lo, col_end, col_nodes);
     }
+    TreeRow no_nodes{};
+    auto key_set = [&](int column, int &lo, int &end) {  // of matrix column `column`
+        const int col = column / REP;
+        const bool live = col < n_cols;
+        scope.column(P, no_words, 0, column, live ? col / G : 0, live, lo, end, no_nodes);
+    };
 
     constexpr int ADDRESSES = FOLLOWING ? RUNS : 1;
     const char *base = (const char *)p.k + (p.block_table == nullptr ? (int64_t)b * p.ksb : 0) + (int64_t)hk * p.ksh;
@@ -147,9 +173,11 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
     const int32_t *table = p.block_table + (int64_t)b * p.table_stride;
     auto offset_of = [&](int key) -> int64_t {
         if (FORM == kQ4Direct || p.block_table == nullptr) return (int64_t)key * p.ksl;
-        const int page_no = key / p.page_size;
+        int page_size = p.page_size;
+        if constexpr (FORM == kQ4Any && C == 16) asm volatile("" : "+s"(page_size));  // (no register to keep its reciprocal in)
+        const int page_no = key / page_size;
         const int64_t page = min(max(table[page_no], 0), p.num_pages - 1);
-        return page * p.ksb + (int64_t)(key - page_no * p.page_size) * p.ksl;
+        return page * p.ksb + (int64_t)(key - page_no * page_size) * p.ksl;
     };
     const uint32_t row_bytes = (uint32_t)p.ksl;
 
@@ -190,9 +218,11 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
         }
         return false;
     };
-    // Chunk n of a run is chunk n % RPC of its row n / RPC; this lane's of load i is n = 64 i + lane
+    // Chunk n of a run is chunk n % RPC of its row n / RPC; this lane's of load i is n = 64 i + lane. Many columns leave no registers for all of
+    // them: 16 n where rows follow each other without a gap, else worked out for every tile
+    constexpr bool KEPT = C < 8;
     uint32_t chunk_off[LOADS];
-    if constexpr (FOLLOWING)
+    if constexpr (FOLLOWING && KEPT)
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const uint32_t n = 64 * i + lane;
@@ -207,15 +237,21 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
 #pragma unroll
             for (int r = 0; r < RUNS; ++r) {
                 const uint32_t dst = to + 16 * RUN * r;
-                if (__builtin_expect(exists, 1)) {
+                if (__builtin_expect(exists && KEPT, 1)) {
 #pragma unroll
                     for (int i = 0; i < FULL; ++i) tile_load16_uniform<false>(chunk_off[i], run[r], dst + 1024 * i);
                     if constexpr (REST != 0) tile_load16_uniform<true>(chunk_off[FULL], run[r], dst + 1024 * FULL);
+                } else if (exists && row_bytes == Row::kBytes) {  // (uniform)
+#pragma unroll
+                    for (int i = 0; i < FULL; ++i) tile_load16_uniform<false>(16u * lane, run[r] + 1024 * i, dst + 1024 * i);
+                    if constexpr (REST != 0) tile_load16_uniform<true>(16u * lane, run[r] + 1024 * FULL, dst + 1024 * FULL);
                 } else {
                     const int last = Lb - 1 - min(key + 16 * r, (Lb - 1) & ~15);
+                    int l = lane;
+                    asm volatile("" : "+v"(l));  // (the offsets are worked out here: kept across the loop they would be spilled)
 #pragma unroll
                     for (int i = 0; i < LOADS; ++i) {
-                        const int n = 64 * i + lane;
+                        const int n = 64 * i + l;
                         const uint32_t off = __umul24((uint32_t)min(n / RPC, last), row_bytes) + 16u * (n % RPC);
                         if (i < FULL)
                             tile_load16_uniform<false>(off, run[r], dst + 1024 * i);
@@ -226,9 +262,11 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
             }
         } else {
             const int last = FORM == kQ4Runs8 ? min(Lb - 1 - key, kQ4Tile - 1) : kQ4Tile - 1;
+            int l = lane;
+            asm volatile("" : "+v"(l));  // (as above)
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {  // (from the lane that has the offset of the row, or of its run)
-                const int n = 64 * i + lane, row = FORM == kQ4Runs8 ? min(n / RPC, last) : n / RPC;
+                const int n = 64 * i + l, row = FORM == kQ4Runs8 ? min(n / RPC, last) : n / RPC;
                 const int from = FORM == kQ4Runs8 ? slot - RUNS + row / 8 : row;
                 const int lo = __shfl(FORM == kQ4Runs8 ? ahead_off[0] : (int)row_off, from, 64);
                 const int hi = __shfl(FORM == kQ4Runs8 ? ahead_off[1] : (int)(row_off >> 32), from, 64);
@@ -244,15 +282,18 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
 #pragma unroll
     for (int i = 0; i < NDB; ++i) o1[i] = o2[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float scale_log2 = p.scale * kLog2e;
-    // What a scale byte of this lane's group stands for is 2^(byte - 127): its operand is 2^(byte - scale_base - 15). P2 (this lane's column) is
-    // held times 2^-tilt_ref, by way of rho
-    int scale_base = -256, tilt_ref = 0;
-
-    // This lane's places in a tile: of the K rows, and of the rows it gives the transposing reads (element i of a lane's 4-bit
-    // operand is key 32 (i / 8) + 16 (i / 4 % 2) + 4 g + i % 4, of its scales, 32 keys at a time, likewise)
-    const uint32_t k_at = (uint32_t)c * Row::kBytes + (D == 128 ? 16 : 8) * g, k_scale_at = (uint32_t)c * Row::kBytes + Row::kKScale + (D == 128 ? 2 : 1) * g;
-    const uint32_t v_at = (uint32_t)(32 * (c >> 3) + 16 * ((c >> 2) & 1) + 4 * g + (c & 3)) * Row::kBytes + Row::kV;
-    const uint32_t v_scale_at = (uint32_t)(16 * (c >> 3) + 4 * g + ((c >> 1) & 3)) * Row::kBytes + (D == 128 ? Row::kVScale : Row::kKScale);
+    // (uniform) O1 and O2 count in 2^(zero - 127): a scale byte is 2^(byte - zero) to them
+    int zero = 128;
+    bool counted = false;
+    auto recount = [&](int to) {
+        const float by = __builtin_amdgcn_ldexpf(1.f, zero - to);
+        zero = to;
+#pragma unroll
+        for (int i = 0; i < NDB; ++i) {
+            o1[i] *= by;
+            if constexpr (USE_R) o2[i] *= by;
+        }
+    };
 
     int v = v_lo + w, key = 0, key_next = 0, stage = 0;
     const char *run[ADDRESSES];
@@ -268,7 +309,15 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
 #pragma unroll
     for (int s = 0; s < KSTEPS; ++s) {
         asm volatile("" : "+v"(qf[s]));
-        if constexpr (USE_R) asm volatile("" : "+v"(rf[s]));
+        if constexpr (USE_R) {
+            asm volatile("" : "+v"(rf[s]));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {  // (exact but for what is too small to count)
+                const uint32_t x = rf[s][e];
+                constexpr float by = 1.f / (1 << kProbeDown);
+                rf[s][e] = pack_bf16(bf16_lo_f32(x) * by, bf16_hi_f32(x) * by);
+            }
+        }
     }
     while (have) {
         const int tk = key;
@@ -278,6 +327,14 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
         else
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         const char *tile = (const char *)(raw + stage * RAW);
+        // This lane's places in a tile: of the K rows, and of the rows it gives the transposing reads (element i of a lane's 4-bit
+        // operand is key 32 (i / 8) + 16 (i / 4 % 2) + 4 g + i % 4, of its scales, 32 keys at a time, likewise)
+        int place = lane;
+        if constexpr (C == 16) asm volatile("" : "+v"(place));  // (no registers to keep them in across the loop)
+        const uint32_t pc = place & 15, pg = place >> 4;
+        const uint32_t k_at = pc * Row::kBytes + (D == 128 ? 16 : 8) * pg, k_scale_at = pc * Row::kBytes + Row::kKScale + (D == 128 ? 2 : 1) * pg;
+        const uint32_t v_at = (32 * (pc >> 3) + 16 * ((pc >> 2) & 1) + 4 * pg + (pc & 3)) * Row::kBytes + Row::kV;
+        const uint32_t v_scale_at = (16 * (pc >> 3) + 4 * pg + ((pc >> 1) & 3)) * Row::kBytes + (D == 128 ? Row::kVScale : Row::kKScale);
         int key_third = 0;  // the tile behind the next one is looked for here, and asked for when this one has been read
         bool have_third = false;
         if (have_next) {
@@ -315,170 +372,165 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
         u32x2 scales[2];  // of V, 8 keys each
 #pragma unroll
         for (int h = 0; h < 2; ++h) scales[h] = lds_read_tr8(tile + 32 * h * Row::kBytes + v_scale_at);
-        uint32_t keep[8];  // 16 bits a key that is seen, the keys in the order of p1
-        u32x2 looked_at[2] = {scales[0], scales[1]};  // of keys that some column sees
-#pragma unroll
-        for (int n = 0; n < 8; ++n) keep[n] = ~0u;
+        uint32_t seen[2] = {0xffu, 0xffu};
         float factor = scale_log2;
         if (__builtin_expect(!whole, 0)) {
-            uint32_t seen[2];
+            int l = lane, lo, end;
+            asm volatile("" : "+v"(l));  // (the key set is worked out here, see above)
+            key_set(l & 15, lo, end);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) seen[h] = scope.seen(P, col_nodes, col_lo, col_end, tk + 32 * h, g);
+            for (int h = 0; h < 2; ++h) seen[h] = scope.seen(P, no_nodes, lo, end, tk + 32 * h, l >> 4);
             asm volatile("" : "+v"(seen[0]), "+v"(seen[1]));  // (not to be worked out for every tile)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const bool ok = (seen[e >> 3] >> (e & 7)) & 1u;
                 s1[e >> 2][e & 3] = ok ? s1[e >> 2][e & 3] * factor : kNegInf;
                 if constexpr (USE_R) s2[e >> 2][e & 3] = ok ? s2[e >> 2][e & 3] : 0.f;
-                if (!ok) keep[e >> 1] &= e & 1 ? 0xffffu : 0xffff0000u;
             }
             factor = 1.f;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t any = row_or(seen[h]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (!((any >> e) & 1u)) looked_at[h][e >> 2] &= ~(255u << (8 * (e & 3)));
-            }
         }
-        // Any reference near the row's largest score does: it moves (and everything with it) only when a score is 2^6 above it
+        // Any reference near the row's largest score does: it moves (and everything with it) only when a weight is 2^2 above it
         float tmax = kNegInf;
 #pragma unroll
         for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, s1[e >> 2][e & 3]);
         tmax *= factor;
-        // a bound on the largest |P2| of this lane's keys
-        float tilt = 0.f;
-        if constexpr (USE_R) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) tilt = fmaxf(tilt, fabsf(s2[e >> 2][e & 3]));
-        }
-        const float reach = USE_R ? tilt * fast_exp2(tmax - m_run) : 0.f;
-        // (this group's largest scale byte, in the upper byte of two halves; below it whatever comes)
-        int top;
-        {
-            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-            u16x2 x = {0, 0};
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int d = 0; d < 2; ++d) {
-                    const uint32_t y = looked_at[h][d];
-                    x = __builtin_elementwise_max(x, __builtin_elementwise_max(__builtin_bit_cast(u16x2, y), __builtin_bit_cast(u16x2, y << 8)));
-                }
-            const uint32_t both = __builtin_bit_cast(uint32_t, x);
-            top = (int)(max(both >> 16, both & 0xffffu) >> 8);
-            if constexpr (D == 64) top = c & 4 ? top : 0;  // (the others have the scales of K)
-        }
-        constexpr float kTiltMost = 1 << kTiltRoom;
-        if (__builtin_expect(__any((tmax > m_run + kQ4Slack) | (top > scale_base + kFieldMost) | (reach > kTiltMost)), 0)) {
-            // (rare, but for the first tile)
+        if (__builtin_expect(__any(tmax > m_run + kQ4Slack), 0)) {  // (rare, but for the first tile)
             tmax = rows_max(tmax);
             const float m_new = fmaxf(m_run, tmax);
             const float alpha = fast_exp2(m_run - (m_new == kNegInf ? 0.f : m_new));
             m_run = m_new;
             dsum1 *= alpha, dsum2 *= alpha;
-            const bool nan = __any(top == 255);  // (whatever the reference: the largest of the others)
-            if (nan) {
-                top = 0;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int byte = (int)(looked_at[e >> 3][(e >> 2) & 1] >> (8 * (e & 3)) & 255u);
-                    if ((D == 128 || (c & 4)) && byte != 255) top = max(top, byte);
-                }
+            for (int i = 0; i < NDB; ++i) {
+                o1[i] *= alpha;
+                if constexpr (USE_R) o2[i] *= alpha;
             }
-            top = max(top, __builtin_amdgcn_update_dpp(top, top, 0x128, 0xf, 0xf, false));  // of the group: lanes c and c + 8, ..
-            top = max(top, __shfl_xor(top, 16, 64));
-            top = max(top, __shfl_xor(top, 32, 64));
-            const int base = top > scale_base + kFieldMost ? min(max(top - kFieldStart, 0), 224) : scale_base;
-            const int down = scale_base - base;
-            scale_base = base;
-            if (nan) {  // (the exponent of infinity)
+        }
+        float tilt = 0.f;  // of this lane's keys
+        if constexpr (USE_R) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    uint32_t x = scales[e >> 3][(e >> 2) & 1];
-                    const int at = 8 * (e & 3);
-                    if ((x >> at & 255u) == 255u) x = (x & ~(255u << at)) | (uint32_t)(scale_base + 31) << at;
-                    scales[e >> 3][(e >> 2) & 1] = x;
-                }
-            }
-            auto move = [&](auto j) __attribute__((always_inline)) {
-                constexpr int J = decltype(j)::value;
-                const float by = __builtin_amdgcn_ldexpf(alpha, (int)operand_scales<D, C, J>((uint32_t)down));
-#pragma unroll
-                for (int n = 0; n < REP; ++n) {
-                    o1[REP * J + n] *= by;
-                    if constexpr (USE_R) o2[REP * J + n] *= by;
-                }
-            };
-            each_of<OPERANDS>(move);
-            if constexpr (USE_R) {
-                const float most = rows_max(tilt) * fast_exp2(tmax - (m_run == kNegInf ? 0.f : m_run));  // (of this column)
-                if (__any(most > kTiltMost)) {
-                    const int less = most > kTiltMost && most < __builtin_inff() ? __builtin_amdgcn_frexp_expf(most) - kTiltRoom + 3 : 0;
-                    const float by = __builtin_amdgcn_ldexpf(1.f, -less);
-                    tilt_ref += less, dsum2 *= by;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s2[e >> 2][e & 3] *= by;
-#pragma unroll
-                    for (int i = 0; i < NDB; ++i) o2[i] *= by;
-#pragma unroll
-                    for (int s = 0; s < KSTEPS; ++s)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t x = rf[s][e];
-                            rf[s][e] = pack_bf16(bf16_lo_f32(x) * by, bf16_hi_f32(x) * by);
-                        }
-                }
-            }
+            for (int e = 0; e < 16; ++e) tilt = fmaxf(tilt, fabsf(s2[e >> 2][e & 3]));
         }
         const float up_m = m_run == kNegInf ? 0.f : kWeightUp - m_run;
-        // P1 and P2 are rounded to f16 once (to bf16 they made the result's error 1.4 times that of its own rounding); d1 and d2 add the
-        // rounded values, so that the weights still sum to one and what cancels between O1 d2 and O2 does so exactly.
-        uint32_t w1[8], w2[8];
-#pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            float p1[2], p2[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                p1[e] = fast_exp2(fmaf(s1[n >> 1][2 * (n & 1) + e], factor, up_m));
-                p2[e] = USE_R ? p1[e] * s2[n >> 1][2 * (n & 1) + e] : 0.f;
-            }
-            w1[n] = pack_f16(p1[0], p1[1]), dsum1 = add_f16_pair(w1[n], dsum1);
-            if constexpr (USE_R) w2[n] = pack_f16(p2[0], p2[1]), dsum2 = add_f16_pair(w2[n], dsum2);
+        auto weight = [&](int e) { return fast_exp2(fmaf(s1[e >> 2][e & 3], factor, up_m)); };
+        if (__builtin_expect(whole && !counted, 0)) {  // (once) the largest scale of the wave's first whole tile's last key, and 2^2 of room
+            int top = D == 128 || (c & 4) ? (int)(scales[1][1] >> 24) : 0;
+            top = (int)row_max((uint32_t)top);
+            top = __builtin_amdgcn_readlane(top, 48);
+            recount(min(max(top + 2, 64), 190)), counted = true;
         }
-        // this group's scales as f16: the exponent is the byte less scale_base (too small: 0; of keys that nobody sees: whatever comes)
-        uint32_t own[8];
+        // This lane's scales counted from zero - 8: 0 .. 8 if they are within reach (lower ones wrap round)
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 own[8], widest = {0, 0};
 #pragma unroll
         for (int n = 0; n < 8; ++n) {
-            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
             const uint32_t bytes = __builtin_amdgcn_perm(0u, scales[n >> 2][(n >> 1) & 1], n & 1 ? 0x0c030c02u : 0x0c010c00u);
-            const uint16_t less = (uint16_t)scale_base;
-            const u16x2 x = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, bytes), u16x2{less, less}) << 10;
-            own[n] = __builtin_bit_cast(uint32_t, x);
+            const uint16_t lowest = (uint16_t)(zero - kScaleRange);
+            own[n] = __builtin_bit_cast(u16x2, bytes) - u16x2{lowest, lowest};
+            widest = __builtin_elementwise_max(widest, own[n]);
         }
-        // ---- O1^T += V^T P1^T, O2^T += V^T P2^T, 16 * REP dimensions with the same operands --------------------
-        auto products = [&](auto j) __attribute__((always_inline)) {
-            constexpr int J = decltype(j)::value;
-            u32x4 pb1[2], pb2[2];
+        bool wild = max(widest[0], widest[1]) > kScaleRange;
+        if constexpr (D == 64) wild = wild && (c & 4);  // (the others have the scales of K)
+        if (__builtin_expect(__any(tmax < m_run - kWeightFloor), 0)) {
+            wild |= rows_max(tmax) < m_run - kWeightFloor;  // (of the tile)
+        }
+        if constexpr (USE_R) wild |= tilt * fast_exp2(tmax - m_run + kWeightUp) > 1 << kProbeMost;
+
+        if (__builtin_expect(whole && !__any(wild), 1)) {
+            // P1 and P2 in f16, once (in bf16 they made the result's error 1.4 times that of its own rounding); d1 and d2 add the rounded
+            // values, so that the weights still sum to one and what cancels between O1 d2 and O2 does so exactly.
+            uint32_t w1[8], w2[8];
 #pragma unroll
             for (int n = 0; n < 8; ++n) {
-                const uint32_t x = operand_scales<D, C, J>(own[n]) & keep[n];
-                pb1[n >> 2][n & 3] = mul_f16_pair(w1[n], x);
-                if constexpr (USE_R) pb2[n >> 2][n & 3] = mul_f16_pair(w2[n], x);
+                const float p0 = weight(2 * n), p1 = weight(2 * n + 1);
+                w1[n] = pack_f16(p0, p1), dsum1 = add_f16_pair(w1[n], dsum1);
+                if constexpr (USE_R) {
+                    w2[n] = pack_f16(p0 * s2[n >> 1][2 * (n & 1)], p1 * s2[n >> 1][2 * (n & 1) + 1]);
+                    dsum2 = add_f16_pair(w2[n], dsum2);
+                }
+                own[n] = own[n] * u16x2{1 << 10, 1 << 10} + u16x2{(15 - kScaleRange) << 10, (15 - kScaleRange) << 10};  // as f16
             }
+            if constexpr (C >= 4) __builtin_amdgcn_sched_barrier(0);
+            // ---- O1^T += V^T P1^T, O2^T += V^T P2^T, 16 * REP dimensions with the same operands --------------------
+            auto products = [&](auto j) __attribute__((always_inline)) {
+                constexpr int J = decltype(j)::value;
+                u32x4 pb1[2], pb2[2];
 #pragma unroll
-            for (int n = 0; n < REP; ++n) {
-                const int i = REP * J + n;
-                const u32x2 codes = lds_read_tr4(tile + v_at + 8 * i);
+                for (int n = 0; n < 8; ++n) {
+                    const uint32_t x = operand_scales<D, C, J>(__builtin_bit_cast(uint32_t, own[n]));
+                    pb1[n >> 2][n & 3] = mul_f16_pair(w1[n], x);
+                    if constexpr (USE_R) pb2[n >> 2][n & 3] = mul_f16_pair(w2[n], x);
+                }
+#pragma unroll
+                for (int n = 0; n < REP; ++n) {
+                    const int i = REP * J + n;
+                    const u32x2 codes = lds_read_tr4(tile + v_at + 8 * i);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const u32x4 x = q4_to_f16(codes[h]);
+                        o1[i] = mfma16_f16(x, pb1[h], o1[i]);
+                        if constexpr (USE_R) o2[i] = mfma16_f16(x, pb2[h], o2[i]);
+                    }
+                }
+                if constexpr (C >= 8) __builtin_amdgcn_sched_barrier(0);
+            };
+            each_of<OPERANDS>(products);
+        } else {
+            // Any sizes: P1 and P2 are cut to 16 bits, which two bf16 hold, times their scales. Only a scale 2^90 above what O1 and O2 count in
+            // is too large, and moves that. A scale of NaN (255, infinite here): infinity less itself.
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t byte = (scales[e >> 3][(e >> 2) & 1] >> (8 * (e & 3))) & 255u;
+                const bool some = (row_or(seen[e >> 3]) >> (e & 7)) & 1u;  // (a column that sees the key)
+                if (some && byte != 255 && (D == 128 || (c & 4))) top = max(top, byte);
+            }
+            if (__any((int)top > zero + 90)) {
+                top = row_max(top);
+                top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+                top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+                recount(min(__builtin_amdgcn_readfirstlane((int)top), 190));
+            }
+            const float unit = __builtin_amdgcn_ldexpf(1.f, 127 - zero);
+            u32x2 keep[2];  // bytes of the keys that are seen: bits 0 .. 3 of a half, to bytes
+#pragma unroll
+            for (int h = 0; h < 2; ++h) keep[h] = u32x2{((seen[h] & 15u) * 0x204081u & 0x01010101u) * 255u, ((seen[h] >> 4) * 0x204081u & 0x01010101u) * 255u};
+            float p1[16], p2[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                p1[e] = cut(weight(e)), dsum1 += p1[e];
+                if constexpr (USE_R) p2[e] = cut(p1[e] * s2[e >> 2][e & 3]), dsum2 += p2[e];
+            }
+            auto products = [&](auto j) __attribute__((always_inline)) {
+                constexpr int J = decltype(j)::value;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const u32x4 x = q4_to_f16(codes[h]);
-                    o1[i] = mfma16_f16(x, pb1[h], o1[i]);
-                    if constexpr (USE_R) o2[i] = mfma16_f16(x, pb2[h], o2[i]);
+                    u32x4 pb1, pb2, rest1, rest2;
+#pragma unroll
+                    for (int d = 0; d < 2; ++d) {
+                        const uint32_t e4 = operand_scales<D, C, J>(scales[h][d]) & keep[h][d];
+#pragma unroll
+                        for (int e = 0; e < 4; e += 2) {
+                            const float x0 = q4_scale_byte(e4, e) * unit, x1 = q4_scale_byte(e4, e + 1) * unit;
+                            const int at = 8 * h + 4 * d + e, to = 2 * d + e / 2;
+                            halves(p1[at] * x0, p1[at + 1] * x1, pb1, rest1, to);
+                            if constexpr (USE_R) halves(p2[at] * x0, p2[at + 1] * x1, pb2, rest2, to);
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < REP; ++n) {
+                        const int i = REP * J + n;
+                        const u32x4 x = q4_to_bf16(lds_read_tr4(tile + v_at + 8 * i)[h], 1.f);
+                        o1[i] = mfma16(x, pb1, o1[i]);
+                        if constexpr (USE_R) o2[i] = mfma16(x, pb2, o2[i]);
+                        o1[i] = mfma16(x, rest1, o1[i]);
+                        if constexpr (USE_R) o2[i] = mfma16(x, rest2, o2[i]);
+                    }
+                    if constexpr (D == 128) __builtin_amdgcn_sched_barrier(0);  // (step after step: together they need more registers than there are)
                 }
-            }
-        };
-        each_of<OPERANDS>(products);
+            };
+            each_of<OPERANDS>(products);
+        }
 
         if (have_third) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (read before it is written again)
@@ -494,25 +546,25 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
     f32x4 *mrg1 = (f32x4 *)lds, *mrg2 = mrg1 + kQ4Waves * QUADS;  // [wave][quad]
     float *mrg_m = (float *)(lds + kQ4Waves * 2 * RAW), *mrg_d1 = mrg_m + kQ4Waves * 16, *mrg_d2 = mrg_d1 + kQ4Waves * 16;
     __syncthreads();  // every wave is done with its tiles
+    int last = threadIdx.x;
+    asm volatile("" : "+v"(last));  // (places of threads are worked out again: kept across the loop they would be spilled)
     {
-        // (back to what m_run stands for)
-        const float s1 = __builtin_amdgcn_ldexpf(rows_sum(dsum1), -kWeightUp), s2 = __builtin_amdgcn_ldexpf(rows_sum(dsum2), tilt_ref - kWeightUp);
-        auto put_back = [&](auto j) __attribute__((always_inline)) {
-            constexpr int J = decltype(j)::value;
-            const int up = (int)operand_scales<D, C, J>((uint32_t)scale_base) + 15 - 127 - kWeightUp;
+        const int lane = last & 63, c = lane & 15, g = lane >> 4;
+        constexpr int DOWN = -kWeightUp - kRecordDown;
+        const float s1 = __builtin_amdgcn_ldexpf(rows_sum(dsum1), DOWN), s2 = __builtin_amdgcn_ldexpf(rows_sum(dsum2), DOWN + kProbeDown);
 #pragma unroll
-            for (int i = REP * J; i < REP * (J + 1); ++i)
+        for (int i = 0; i < NDB; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    o1[i][e] = __builtin_amdgcn_ldexpf(o1[i][e], up);
-                    if constexpr (USE_R) o2[i][e] = __builtin_amdgcn_ldexpf(o2[i][e], up + tilt_ref);
-                }
-        };
-        each_of<OPERANDS>(put_back);
+            for (int e = 0; e < 4; ++e) {
+                o1[i][e] = __builtin_amdgcn_ldexpf(o1[i][e], zero - 127 + DOWN);
+                if constexpr (USE_R) o2[i][e] = __builtin_amdgcn_ldexpf(o2[i][e], zero - 127 + DOWN + kProbeDown);
+            }
         // a row in front of the sequence sees nothing, also where all others see everything
-        const bool none = col_end == 0;
+        int lo, end;
+        key_set(c, lo, end);
+        const bool none = end == 0;
         if (g == 0) {
-            mrg_m[w * 16 + c] = none ? kNegInf : m_run;
+            mrg_m[w * 16 + c] = none ? kNegInf : m_run + kRecordDown;
             mrg_d1[w * 16 + c] = none ? 0.f : s1;
             mrg_d2[w * 16 + c] = none ? 0.f : s2;
         }
@@ -525,7 +577,7 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
         }
     }
     __syncthreads();
-    for (int at = tid; at < NDB * 4 * C; at += 256) {
+    for (int at = last; at < NDB * 4 * C; at += 256) {
         const int i = at / (4 * C), quarter = at / C % 4, col = at % C, x = col * REP + i % REP;  // x: matrix column
         if (col >= n_cols) continue;
         float m_star = kNegInf, wt[kQ4Waves], d1 = 0.f, d2 = 0.f;
