@@ -343,17 +343,18 @@ plx_status parallax_cache_compact(const plx_cache_compact_args *args, void *hip_
  *     d / 2 bytes of K codes, d / 2 of V codes; byte i of either: dimension 2 i in its low half, 2 i + 1 in its high one
  *     d / 16 scale bytes of K, d / 16 of V; zeros up to a multiple of 16 bytes
  * A code is a sign bit over one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (e2m1); a scale byte e stands for 2^(e - 127) and serves 16
- * dimensions, 255 makes them NaN (in V infinite or NaN, where a code is not 0). Written rows take the power of two that brings the largest magnitude of the 16 into [3.5, 7),
+ * dimensions, 255 makes them NaN whatever their codes. Written rows take the power of two that brings the largest magnitude of the 16 into [3.5, 7),
  * e within 4 .. 252 (what is left over above saturates, below becomes 0), and round to nearest, ties to the even code; 16 dimensions
  * of which one is infinite or NaN get e = 255 and codes of 0. Every value of such a row is exact in bf16. (A decode rounds a weight to 11 bits or
  * more, however far its scales are from those of other keys: weight times value is off by at most 2^-11 of itself, or 2^-13 of the
- * largest weight times scale of the 64 keys and 16 dimensions that it is in; weight times rho.k times value likewise, or 2^-7 of that weight
- * times scale where the 64 keys have less than 2^-16 of the row's weight. Sums are fp32 in which the largest weight of a row counts 2^-8: values
- * below 2^-100 lose bits.)
+ * largest weight times scale of the 64 keys and 16 dimensions that it is in; weight times rho.k times value likewise, or 2^-31 of the row's
+ * largest weight times a scale that is at most 2^8 above those of the 64 keys. Sums are fp32 in which the largest weight of a row counts 2^-8:
+ * values below 2^-100 lose bits.)
  *   rows         [B, Hkv, capacity, row] (stride[0]: sequence, [1]: head, [2]: row), or with a block table pools
  *                [num_pages, Hkv, page_size, row] (stride[0]: page); strides in BYTES, multiples of 16, stride[2] >= the row;
  *                those of rows and pages below 2^36
- *   block_table  [B, block_table_stride] or NULL, as in plx_decode_args; capacity <= block_table_stride * page_size
+ *   block_table  [B, block_table_stride] or NULL, as in plx_decode_args; capacity <= block_table_stride * page_size. An entry that is no page
+ *                stands for no rows to a write or a read back, and is clamped as there by a decode and by bounds
  * The page calls take such pools as one bf16 pool (v NULL) of d = row bytes / 2.
  */
 typedef struct {

@@ -111,3 +111,29 @@ def test_rows_with_few_heavy_keys(plx, d, Hq, Tq, large):  # noqa: F811
     q = (_normal((1, Hq, Tq, d), 9).float() * large).to(torch.bfloat16)
     v = v * torch.exp2((torch.arange(L, device=DEV) // 64 % 13 - 6).float())[:, None] * torch.exp2((torch.arange(d, device=DEV) // 16 % 5 - 2).float())
     _compare(plx, q, r, k, v)
+
+
+@pytest.mark.parametrize("codes", ["any", "zeros"])
+@pytest.mark.parametrize("at", [70, 450, 510])
+@pytest.mark.parametrize("d,Hq,Tq", SHAPES)
+def test_scale_255_is_nan_to_a_decode_too(plx, d, Hq, Tq, at, codes):  # noqa: F811
+    """Rows from elsewhere with scale byte 255 and codes that are not 0: NaN in the 16 dimensions of V for the rows that see them, whatever the
+    codes, as reading them back gives; all else as it was."""
+    L, group = 512, 1
+    q, r = _normal((1, Hq, Tq, d), 1), _normal((1, Hq, Tq, d), 2)
+    cache = torch.zeros(1, 1, L, blocks.row_bytes(d), dtype=torch.uint8, device=DEV)
+    plx.parallax_cache_write_q4(_normal((1, 1, L, d), 3), _normal((1, 1, L, d), 4), cache)
+    want = host(plx.parallax_decode_q4(q, r, cache, d ** -0.5, num_splits=1))
+    if codes == "zeros":
+        cache[0, 0, at, d // 2 + 8 * group: d // 2 + 8 * group + 8] = 0
+    cache[0, 0, at, d + d // 16 + group] = 255
+    v = host(plx.parallax_cache_read_q4(cache, d, L)[1])
+    assert np.isnan(v[0, 0, at, 16 * group: 16 * group + 16]).all() and np.isnan(v).sum() == 16
+    names = torch.arange(8, dtype=torch.int32, device=DEV).reshape(1, 1, 8)
+    for more in (dict(num_splits=1), dict(num_splits=3), dict(block_list=names)):
+        got = host(plx.parallax_decode_q4(q, r, cache, d ** -0.5, **more))
+        nan = np.zeros(got.shape, dtype=bool)
+        for t in range(Tq):
+            nan[:, :, t, 16 * group: 16 * group + 16] = at <= L - Tq + t
+        assert np.array_equal(np.isnan(got), nan), more
+        assert np.isfinite(got[~nan]).all() and np.linalg.norm((got - want)[~nan]) <= 1e-2 * np.linalg.norm(want[~nan])
