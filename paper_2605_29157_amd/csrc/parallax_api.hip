@@ -714,7 +714,8 @@ plx_status parallax_cache_write_q4(const plx_q4_rows_args *a, void *hip_stream) 
     const plx_status st = take_q4_rows(a, &p);
     if (st != PLX_OK) return st;
     // (one place for several rows)
-    if ((p.cache.B > 1 && !p.cache.block_table && p.cache.stride[0] == 0) || (p.cache.Hkv > 1 && p.cache.stride[1] == 0)) return PLX_ERR_SHAPE;
+    const int32_t slots = p.cache.block_table ? p.cache.num_pages : p.cache.B;
+    if ((slots > 1 && p.cache.stride[0] == 0) || (p.cache.Hkv > 1 && p.cache.stride[1] == 0)) return PLX_ERR_SHAPE;
     if (a->T == 0) return PLX_OK;
     return plx::launch_cache_write_q4(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PLX_OK : PLX_ERR_LAUNCH;
 }

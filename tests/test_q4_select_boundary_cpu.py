@@ -267,3 +267,18 @@ def test_strides_of_rows_and_pages_have_a_limit(binding):  # noqa: F811
         a.k_stride[:] = a.v_stride[:] = (128, 128, 128)
         assert lib.parallax_cache_write_q4(ctypes.byref(a), None) == status, fields
         assert lib.parallax_cache_read_q4(ctypes.byref(a), None) == status, fields
+
+
+def test_one_place_for_several_pages_is_not_written(binding):  # noqa: F811
+    """Pools whose pages share one place can be read, and are refused by a write, as are sequences of one place without a table."""
+    lib = binding.load_library()
+    table = dict(block_table=0x2000, page_size=16, block_table_stride=4)
+    for fields, status in ((dict(stride0=0, num_pages=4, **table), binding.PLX_ERR_SHAPE), (dict(stride0=0, num_pages=4, B=1, **table), binding.PLX_ERR_SHAPE),
+                           (dict(stride1=0, num_pages=4, **table), binding.PLX_ERR_SHAPE), (dict(stride0=0, num_pages=1, **table), binding.PLX_OK),
+                           (dict(num_pages=4, **table), binding.PLX_OK)):
+        a = binding.plx_q4_rows_args()
+        _q4(binding, a.cache, **fields)
+        a.k, a.v, a.T, a.dtype = 0x3000, 0x4000, 0, binding.PLX_BF16
+        a.k_stride[:] = a.v_stride[:] = (128, 128, 128)
+        assert lib.parallax_cache_write_q4(ctypes.byref(a), None) == status, fields
+        assert lib.parallax_cache_read_q4(ctypes.byref(a), None) == binding.PLX_OK, fields
