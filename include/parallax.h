@@ -375,7 +375,8 @@ int32_t parallax_q4_row_bytes(int32_t d); /* 0: not a head dimension that such c
  *   counts   [B] or NULL. write: rows from counts[b] on are passed over (a padded batch). read: of the cache's tokens, those from
  *            counts[b] on (the sequence's length) come back as zeros.
  * Tokens outside [0, capacity), and those whose table entry is no page, are not written and come back as zeros. The pages that are
- * written must not be shared (parallax_cache_extend makes them so); a cache whose sequences, pages or heads share a place by a stride of 0 is not written (PLX_ERR_SHAPE).
+ * written must not be shared (parallax_cache_extend makes them so); a cache whose sequences, pages or heads share a place by a stride of 0 is not written, nor are
+ * such k, v read into (PLX_ERR_SHAPE).
  */
 typedef struct {
     plx_q4_cache cache;

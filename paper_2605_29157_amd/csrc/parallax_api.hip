@@ -723,7 +723,11 @@ plx_status parallax_cache_write_q4(const plx_q4_rows_args *a, void *hip_stream) 
 plx_status parallax_cache_read_q4(const plx_q4_rows_args *a, void *hip_stream) {
     plx::Q4Rows p{};
     const plx_status st = take_q4_rows(a, &p);
-    if (st != PLX_OK || a->T == 0) return st;
+    if (st != PLX_OK) return st;
+    // (one place for several rows)
+    if (p.cache.B > 1 && (p.ks[0] == 0 || p.vs[0] == 0)) return PLX_ERR_SHAPE;
+    if (p.cache.Hkv > 1 && (p.ks[1] == 0 || p.vs[1] == 0)) return PLX_ERR_SHAPE;
+    if (a->T == 0) return PLX_OK;
     return plx::launch_cache_read_q4(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PLX_OK : PLX_ERR_LAUNCH;
 }
 

@@ -282,3 +282,18 @@ def test_one_place_for_several_pages_is_not_written(binding):  # noqa: F811
         a.k_stride[:] = a.v_stride[:] = (128, 128, 128)
         assert lib.parallax_cache_write_q4(ctypes.byref(a), None) == status, fields
         assert lib.parallax_cache_read_q4(ctypes.byref(a), None) == binding.PLX_OK, fields
+
+
+def test_one_place_for_several_rows_is_not_read_into(binding):  # noqa: F811
+    """Rows that sequences or heads share by a stride of 0 can be written from, and are refused as what a read back writes."""
+    lib = binding.load_library()
+    for tensor in ("k_stride", "v_stride"):
+        for axis, alone in ((0, dict(B=1)), (1, dict(Hkv=1))):
+            for fields, status in ((dict(), binding.PLX_ERR_SHAPE), (alone, binding.PLX_OK)):
+                a = binding.plx_q4_rows_args()
+                _q4(binding, a.cache, **fields)
+                a.k, a.v, a.T, a.dtype = 0x3000, 0x4000, 0, binding.PLX_BF16
+                a.k_stride[:] = a.v_stride[:] = (256, 128, 128)
+                getattr(a, tensor)[axis] = 0
+                assert lib.parallax_cache_read_q4(ctypes.byref(a), None) == status, (tensor, axis, fields)
+                assert lib.parallax_cache_write_q4(ctypes.byref(a), None) == binding.PLX_OK, (tensor, axis, fields)
