@@ -428,7 +428,8 @@ plx_status parallax_cache_bounds(const plx_cache_bounds_args *args, void *hip_st
  * block with a bound that is infinite or NaN counts as the highest, and so does a sum that is NaN.
  *   q          [B, Hq, Tq, d] bf16 contiguous, (Hq / Hkv) * Tq <= 16; Tq 0 = 1
  *   bounds     as above
- *   seq_lens   [B] or NULL (= 64 * n_blocks): ceil(L_b / 64) blocks, at most n_blocks
+ *   seq_lens   [B] or NULL (= 64 * n_blocks): ceil(L_b / 64) blocks, at most n_blocks (of a longer sequence the `recent` ones are the
+ *              last that have bounds)
  *   block_list [B, Hkv, keep] int32, written: ascending, -1 behind the last (a sequence with up to `keep` blocks keeps them all)
  *   keep       >= first + recent, >= 1
  *   workspace  parallax_select_blocks_workspace_bytes(B, Hkv, n_blocks), 16-byte aligned

@@ -837,11 +837,12 @@ def parallax_decode_q4(q, r, cache, scale, seq_lens=None, use_r=True, num_splits
     return out
 
 
-def parallax_cache_bounds(k, bounds, seq_lens=None, from_lens=None, max_new=0, block_table=None, stream=None):
+def parallax_cache_bounds(k, bounds, seq_lens=None, from_lens=None, max_new=0, block_table=None, stream=None, max_len=None):
     """The smallest and largest key of every block of 64 tokens, by dimension, into bounds [B, Hkv, n_blocks, 2, d] (bf16), which is
     returned. k: the bf16 keys [B, Hkv, capacity, d] or pools of a block_table, or a 4-bit cache. from_lens: the tokens in
     front of these are the same as when the bounds were last brought up to date; only blocks from there on are looked at. max_new: no
-    sequence holds more tokens behind its from_lens (0: not known)."""
+    sequence holds more tokens behind its from_lens (0: not known). max_len: no sequence of a block_table is longer (default: what its pages
+    hold, as far as that only rounds up to whole pages); bounds with fewer blocks than that takes are refused."""
     where = "parallax_cache_bounds"
     _on_current_device(where, k, bounds, seq_lens, from_lens, block_table)
     if k.dim() != 4 or bounds.dim() != 5:
@@ -850,8 +851,20 @@ def parallax_cache_bounds(k, bounds, seq_lens=None, from_lens=None, max_new=0, b
     if bounds.dtype != torch.bfloat16 or not bounds.is_contiguous() or two != 2 or k.shape[1] != Hkv:
         raise ValueError("%s: bounds is a contiguous bf16 tensor [B, Hkv, n_blocks, 2, d]" % where)
     most = min(64 * n_blocks, 0x7fffffff)
-    if block_table is None and k.shape[2] > most:
-        raise ValueError("%s: bounds for %d blocks are too few for %d tokens" % (where, n_blocks, k.shape[2]))
+    tokens = k.shape[2]  # at least
+    if max_len is not None:
+        tokens = _i32(max_len)
+        if tokens < 1:
+            raise ValueError("%s: max_len must be at least 1" % where)
+        if block_table is None and tokens > k.shape[2]:
+            raise ValueError("%s: the cache holds %d tokens" % (where, k.shape[2]))
+    elif block_table is not None:
+        tokens = (block_table.shape[-1] - 1) * k.shape[2] + 1
+    if tokens > most:
+        raise ValueError("%s: bounds for %d blocks are too few for %d tokens%s" %
+                         (where, n_blocks, tokens, "" if block_table is None or max_len is not None else " (or give max_len)"))
+    if max_len is not None:
+        most = tokens
     lens = _lens(where, "seq_lens", seq_lens, B), _lens(where, "from_lens", from_lens, B)
     tail = (bounds.data_ptr(), n_blocks, _i32(max_new), *lens)
     if k.dtype == torch.uint8:
@@ -871,7 +884,8 @@ def parallax_cache_bounds(k, bounds, seq_lens=None, from_lens=None, max_new=0, b
 def parallax_select_blocks(q, bounds, seq_lens, keep, first=1, recent=2, out=None, workspace=None, stream=None):
     """The blocks that a step with queries q [B, Hq, (Tq,) d] reads: int32 [B, Hkv, keep], ascending, -1 behind the last: the
     `first` ones, the `recent` last ones, and of the others those with the highest bound on a product with one of the queries
-    (of the rows and heads that share a key head; of equal ones the lower number)."""
+    (of the rows and heads that share a key head; of equal ones the lower number). A sequence has no more blocks than bounds: of a longer one
+    the `recent` ones are the last that have any."""
     where = "parallax_select_blocks"
     _on_current_device(where, q, bounds, seq_lens, out, workspace)
     shape = q.shape

@@ -241,3 +241,41 @@ def test_select_around_one_round(plx, d, n):
     for b in range(B):
         for h in range(2):
             assert got[b, h].tolist() == blocks.select(hq[b, h], hb[b, h, :, 0], hb[b, h, :, 1], keep, 0, 1), (b, h)
+
+
+@pytest.mark.parametrize("four", [False, True])
+def test_bounds_are_not_cut_unasked(plx, four):
+    """A block table with more pages than bounds have room for is refused like a contiguous cache of that length, unless max_len says that
+    no sequence is that long; pages that only round a length up are not."""
+    d, page, L = 64, 16, 300
+    k = _normal((1, 1, 400, d), 1)
+    if four:
+        keys = torch.zeros((1, 1, 400, blocks.row_bytes(d)), dtype=torch.uint8, device=DEV)
+        plx.parallax_cache_write_q4(k, k, keys)
+        k = plx.parallax_cache_read_q4(keys, d, 400)[0]
+    else:
+        keys = k
+    pools, table = _paged(keys, page, 2, 200 if four else float("nan"))
+    assert table.shape[1] == 25
+    few = torch.full((1, 1, 5, 2, d), 7.0, dtype=torch.bfloat16, device=DEV)
+    lens = _ints([L])
+    for more in (dict(), dict(max_len=321), dict(max_len=0), dict(max_len=-1)):
+        with pytest.raises(ValueError):
+            plx.parallax_cache_bounds(pools, few, lens, block_table=table, **more)
+    with pytest.raises(ValueError):
+        plx.parallax_cache_bounds(keys, few, lens, max_len=401)
+    assert (few == 7.0).all()
+    low, high = blocks.bounds(host(k)[0, 0], L)
+    for more in (dict(max_len=320), dict(max_len=L)):
+        few.fill_(7.0)
+        plx.parallax_cache_bounds(pools, few, lens, block_table=table, **more)
+        assert np.array_equal(host(few)[0, 0, :, 0], low) and np.array_equal(host(few)[0, 0, :, 1], high)
+    # 20 pages for 301 .. 320 tokens, 21 for the first of the sixth block
+    plx.parallax_cache_bounds(pools, few, lens, block_table=table[:, :20].contiguous())
+    assert np.array_equal(host(few)[0, 0, :, 0], low)
+    with pytest.raises(ValueError):
+        plx.parallax_cache_bounds(pools, few, lens, block_table=table[:, :21].contiguous())
+    # a contiguous cache of which a part is looked at
+    few.fill_(7.0)
+    plx.parallax_cache_bounds(keys, few, lens, max_len=320)
+    assert np.array_equal(host(few)[0, 0, :, 1], high)
