@@ -424,7 +424,7 @@ plx_status parallax_cache_bounds(const plx_cache_bounds_args *args, void *hip_st
  * of the others those with the highest score
  *     score_j = max over the query rows and the heads of the group of  sum_i max(q_i lo_ji, q_i hi_ji),
  * no less than scale^-1 times the largest score of any key in the block; of equal ones the lower number. The sums
- * are made in 64 bits (exact for any bf16 values whose products lie within 2^37 of each other, so no order of additions shows); a
+ * are made in 64 bits (exact where the products that are not 0 lie within 2^30 of each other, so no order of additions shows); a
  * block with a bound that is infinite or NaN counts as the highest, and so does a sum that is NaN.
  *   q          [B, Hq, Tq, d] bf16 contiguous, (Hq / Hkv) * Tq <= 16; Tq 0 = 1
  *   bounds     as above

@@ -4,8 +4,8 @@
 // For a block j with smallest and largest keys lo_j, hi_j (by dimension) and a query q no key of the block has a larger product than
 //     sum_i max(q_i lo_ji, q_i hi_ji) = sum_i max(q_i, 0) hi_ji + min(q_i, 0) lo_ji.
 // The score is the largest of these over the rows and heads that share the list. A list has to be the same however its sums are
-// ordered, so they are made in 64 bits: a product of two bf16 has 16 bits, so sums of 128 of them are exact unless they lie more than
-// 2^37 apart.
+// ordered, so they are made in 64 bits: a product of two bf16 has 16 bits, 128 of them add 7, which leaves 30 of 53 for their range: sums are exact
+// where the products that are not 0 lie within 2^30 of each other.
 //
 // What bounds them: bounds, the keys read once (2 D bytes a key; few blocks: one launch); scores, the bounds read once (4 D bytes
 // a block, 1 / 64 of the cache's) beside 2 D additions in 64 bits a column; the choice, one workgroup a list, latency.
@@ -176,7 +176,6 @@ __device__ __forceinline__ int score_blocks(const BlockSelect &p, int b, int h, 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const double q0 = (double)bf16_lo_f32(q[i]), q1 = (double)bf16_hi_f32(q[i]);
-                // of negative q the smallest key counts: bytes 0 - 3 of the pair instead of 4 - 7
                 // of negative q the smallest key counts: a byte permutation picks the bound's half and widens it to fp32 (selected
                 // by masks and widened after: a third of the instructions more, 128 lists of 2048 blocks 32.8 us, so 30.9)
                 const uint32_t s0 = 0x05040c0cu ^ ((uint32_t)__builtin_amdgcn_sbfe((int)q[i], 15, 1) & 0x04040000u);

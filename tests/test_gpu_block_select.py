@@ -279,3 +279,19 @@ def test_bounds_are_not_cut_unasked(plx, four):
     few.fill_(7.0)
     plx.parallax_cache_bounds(keys, few, lens, max_len=320)
     assert np.array_equal(host(few)[0, 0, :, 1], high)
+
+
+@pytest.mark.parametrize("n_blocks", [40, 300])
+@pytest.mark.parametrize("d", [64, 128])
+def test_equal_sums_in_any_order_are_equal(plx, d, n_blocks):
+    """Blocks whose bounds are the same numbers in other dimensions, with products up to 2^30 of each other: equal scores, so the lower
+    numbers are kept."""
+    rng = np.random.default_rng(d)
+    x = rng.integers(128, 256, d) * np.exp2(rng.integers(-29, 1, d).astype(np.float64)) * rng.choice([-1, 1], d)
+    x[0], x[1] = 255.0, 128.0 * 2.0 ** -29
+    q = torch.full((1, 1, d), 255.0 / 128, dtype=torch.bfloat16, device=DEV)
+    b = np.stack([rng.permutation(x) for _ in range(n_blocks)])
+    bounds = torch.tensor(np.stack([b, b], 1)[None, None], dtype=torch.bfloat16, device=DEV)
+    assert np.array_equal(host(bounds)[0, 0, :, 0], b)
+    got = plx.parallax_select_blocks(q, bounds, None, 7, first=0, recent=0)
+    assert got.flatten().tolist() == list(range(7))

@@ -1,4 +1,6 @@
 """Pins of the oracle for 4-bit rows, block bounds and selection."""
+import math
+
 import numpy as np
 import pytest
 
@@ -58,3 +60,37 @@ def test_selection():
 def test_listed_keys():
     see = blocks.listed_keys([0, 0, 2, -1, 7], 140, 200)
     assert see.sum() == 64 + 12 and see[:64].all() and see[128:140].all()
+
+
+def test_sums_of_products_within_2_to_the_30_are_exact_in_any_order():
+    """128 products of two bf16 (integers below 2^16 times powers of two): with the largest 2^30 times the smallest that is not 0, sums of 64
+    bits have no rounding; at 2^37 they have."""
+    def orders(x):
+        yield x
+        yield x[::-1]
+        rng = np.random.default_rng(1)
+        for _ in range(20):
+            yield rng.permutation(x)
+
+    def sums(x):
+        for y in orders(x):
+            total = 0.0
+            for v in y.tolist():
+                total += v
+            yield total
+            yield float(y.reshape(16, 8).sum(1).reshape(2, 8).sum(0).sum())
+
+    for small in (255 * 255, 129 * 129, 193 * 255, 2 ** 14):  # (significands of 8 bits each)
+        for sign in (1.0, -1.0):
+            high = float(255 * 255)
+            e = math.floor(math.log2(2.0 ** 30 * small / high))
+            x = np.full(128, high * 2.0 ** e)
+            assert 2.0 ** 29 < x[0] / small <= 2.0 ** 30
+            x[::3] = sign * small
+            x[1::5] *= -1.0
+            assert set(sums(x)) == {math.fsum(x)}, (small, sign)
+            x[:] = high * 2.0 ** e
+            x[77] = small  # the sum is as large as it gets
+            assert set(sums(x)) == {math.fsum(x)}
+    x = np.array([255.0 * 255 * 2.0 ** 35] * 64 + [129.0 * 129 * 2.0 ** -1] * 64)
+    assert len(set(sums(x))) > 1
