@@ -620,22 +620,22 @@ int32_t pick_splits_lists(const plx::DecodeRowsParams &p) {
 }
 
 // ... and over 4-bit rows: the cheapest by a model of decode_q4_kernel, in us. A workgroup starts in 3; its four waves take a tile
-// of 64 keys each in 1.5 where it is alone on its unit and in 2.8 where two share it (d = 64: 0.62 of both); of more than two on a unit
-// one pair follows the other; the memory gives 5.6 TB/s (5.0 where the tiles of d = 64 of one workgroup a unit are on their way: 16 x 8 heads
-// x 32768 keys at S = 2 73 us, at 4 67). The merge takes 2.5 (of more than 8 records a row 4) and 0.2 a MB of records.
-// Against sweeps of S (1 .. 64) over 36 calls of 1 - 100 sequences x 500 - 100000 keys and lists of 16 - 128 blocks its choice is on average
-// 0.5 % from the best, at worst 7 %; the rule for bf16 rows was up to 60 % (16 x 8192 keys, 128 pairs: S = 1 49 us, 2 35, 4 36).
+// of 64 keys each in 1.5 where it is alone on its unit and in 2.9 where two share it (d = 64: 0.74 and 0.62 of that); of more than two on a unit
+// one pair follows the other; the memory gives 5.6 TB/s, to one workgroup a unit 5.55. The merge takes 3.5 (of more than 8 records a row 4) and 0.6 a
+// MB of records. Against sweeps of S (1 .. 64) over 36 calls of 1 - 100 sequences x 500 - 100000 keys and lists of 16 - 128 blocks (scores of a standard
+// deviation of 1) its choice is on average 0.7 % from the best, at worst 11 % (32 x <= 16384 keys: S = 1 109 us, 2 102, 7 99); with the constants of
+// an earlier kernel it was 1.8 and 20 %, the rule for bf16 rows up to 50 % (16 x 8192 keys, 128 pairs: S = 1 55 us, 2 37, 4 38).
 int32_t pick_splits_q4(const plx::DecodeRowsParams &p) {
     const int64_t pairs = (int64_t)p.d.B * p.d.Hkv, cus = query_num_cus();
     const int64_t keys = keys_of_lists(p), tiles = (keys + PLX_BLOCK_KEYS - 1) / PLX_BLOCK_KEYS;
-    const double width = p.d.d == 128 ? 1.0 : 0.62, mb = 1e-6 * (double)pairs * (double)keys * (double)parallax_q4_row_bytes(p.d.d);
-    const double records_us = 0.2e-6 * (double)p.d.B * p.d.Hq * p.d.Tq * (2 * p.d.d + 4) * 4;
+    const double alone = p.d.d == 128 ? 1.5 : 1.5 * 0.74, shared = p.d.d == 128 ? 2.9 : 2.9 * 0.62;
+    const double mb = 1e-6 * (double)pairs * (double)keys * (double)parallax_q4_row_bytes(p.d.d);
+    const double records_us = 0.6e-6 * (double)p.d.B * p.d.Hq * p.d.Tq * (2 * p.d.d + 4) * 4;
     auto cost = [&](int64_t s) {
         const double n = (double)(((tiles + s - 1) / s + 3) / 4);
         const int64_t per_unit = (pairs * s + cus - 1) / cus;
-        const double busy = (double)(per_unit / 2) * (3.0 + 2.8 * width * n) + (double)(per_unit % 2) * (3.0 + 1.5 * width * n);
-        const double rate = p.d.d == 64 && per_unit == 1 ? 5.0 : 5.6;
-        return std::max(busy, 3.0 + mb / rate) + (s > 1 ? (s <= 8 ? 2.5 : 4.0) + records_us * (double)s : 0.0);
+        const double busy = (double)(per_unit / 2) * (3.0 + shared * n) + (double)(per_unit % 2) * (3.0 + alone * n);
+        return std::max(busy, 3.0 + mb / (per_unit == 1 ? 5.55 : 5.6)) + (s > 1 ? (s <= 8 ? 3.5 : 4.0) + records_us * (double)s : 0.0);
     };
     int64_t best = 1;
     for (int64_t s = 2; s <= std::min<int64_t>(tiles, PLX_MAX_SPLITS); ++s)
