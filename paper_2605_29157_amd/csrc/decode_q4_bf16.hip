@@ -262,16 +262,18 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
             }
         } else {
             const int last = FORM == kQ4Runs8 ? min(Lb - 1 - key, kQ4Tile - 1) : kQ4Tile - 1;
-            int l = lane;
-            asm volatile("" : "+v"(l));  // (as above)
+            int row0 = lane / RPC, chunk0 = lane % RPC;
+            if constexpr (D == 128) asm volatile("" : "+v"(row0), "+v"(chunk0));  // (what follows from them is worked out here, as above)
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {  // (from the lane that has the offset of the row, or of its run)
-                const int n = 64 * i + l, row = FORM == kQ4Runs8 ? min(n / RPC, last) : n / RPC;
+                const int more = chunk0 + 64 * i % RPC, over = more >= RPC;
+                const int at = row0 + 64 * i / RPC + over, chunk = more - RPC * over;
+                const int row = FORM == kQ4Runs8 ? min(at, last) : at;
                 const int from = FORM == kQ4Runs8 ? slot - RUNS + row / 8 : row;
                 const int lo = __shfl(FORM == kQ4Runs8 ? ahead_off[0] : (int)row_off, from, 64);
                 const int hi = __shfl(FORM == kQ4Runs8 ? ahead_off[1] : (int)(row_off >> 32), from, 64);
                 const uint32_t in_run = FORM == kQ4Runs8 ? __umul24((uint32_t)row % 8, row_bytes) : 0u;
-                tile_load16<64>(base + (((int64_t)hi << 32) | (uint32_t)lo) + in_run + 16 * (n % RPC), to + 1024 * i);
+                tile_load16<64>(base + (((int64_t)hi << 32) | (uint32_t)lo) + in_run + 16 * chunk, to + 1024 * i);
             }
         }
     };
@@ -604,8 +606,8 @@ static void launch_q4_form(const DecodeRowsParams &P, hipStream_t stream) {
     const DecodeParams &p = P.d;
     const dim3 grid(p.S, p.Hkv, p.B);
     const bool short_rows = p.ksl < (1 << 24);  // (24-bit products of a row number below 64 and the row stride)
-    // (when P was bf16: pages of a multiple of 8 against row by row, us: 24 x <= 6000 keys 41.8, 44.7; d = 64, window 4096, 4 rows 21.6, 23.7; pages of 16
-    // 39.3, 20.8, of 64 37.1, 20.2, none 36.2, 19.5)
+    // (us, pages of a multiple of 8 against row by row: 24 x <= 6000 keys 46, 50; d = 64, window 4096, 4 rows 24.3, 27.1; pages of 16 41.3,
+    // 23.5, of 64 40, 21.8, none 38.7, 21.5)
     if (short_rows && p.block_table == nullptr && P.block_list == nullptr)
         hipLaunchKernelGGL((decode_q4_kernel<D, C, USE_R, kQ4Direct>), grid, dim3(256), 0, stream, P);
     else if (short_rows && (p.block_table == nullptr || p.page_size % 64 == 0))
