@@ -21,15 +21,15 @@
 //     group's dimensions is right in its own copy only, and only that is kept. With more columns (C) the groups do not fit beside each
 //     other and P is multiplied 2, 4 or 8 times. A key that a column does not see has the scale 0, so nothing in its row can reach it.
 // P. One rounding of it to bf16 makes the result's error 1.4 times that of its own rounding; f16 has the bits but not the range, and bf16 for
-// what the rounding leaves costs as many products again. So a tile is looked at first. Where f16 holds its operands (all keys seen, scales within 2^8
+// what the rounding leaves costs as many products again. So a tile is looked at first. Where f16 holds its operands (scales within 2^8
 // of each other, each column's largest weight not 2^16 below the row's, P rho.k not too large) they are f16, the scales as exponents,
-// and what a product loses is at most 2^-13 of the tile's largest one in that column and group. Any other tile (the ends of a
-// sequence or window, values or products rho.k of other sizes beside each other, rows with a few heavy keys, NaN) takes its P in two bf16, with
-// scales of any size. O1 and O2 count in the same unit either way, so the two kinds of tile mix.
+// and what a product loses is at most 2^-13 of the tile's largest one in that column and group. Any other tile (values or
+// products rho.k of other sizes beside each other, rows with a few heavy keys, NaN; at d = 128 also the ends of a sequence or window) takes its P in
+// two bf16, with scales of any size. O1 and O2 count in the same unit either way, so the two kinds of tile mix.
 // us, 16 x 32768 keys, 8 key heads, d = 128, at the best split, for 2, 4, 8, 16 columns: all tiles in f16 with references that followed the largest scale
-// (and lost smaller ones) 116, 118, 119, 125; now 117, 120, 121, 132; all tiles in two bf16, as they are where scores have a standard deviation
-// of 12, 142, 164, 195, 255. (Ends of sequences in f16, too: 100 x <= 500 keys 25.4, so 23.5, but the compiler then spills registers of the second
-// way, and 16 x 64 listed blocks go from 25.0 to 26.5.)
+// (and lost smaller ones) 116, 118, 119, 125; now 117, 118, 121, 131; all tiles in two bf16, as they are where scores have a standard deviation
+// of 12, 142, 164, 195, 255. Ends of sequences in f16, too: d = 64, window 4096, 4 rows 22.6 us, so 21.4; at d = 128 100 x <= 500 keys 25.4 and
+// 23.5, but the compiler then spills registers of the second way, and 16 x 64 listed blocks take 26.5 instead of 25.0.
 // Steps before that, us for 16 x 32768 keys, 8 key heads, d = 128, and for 1 x 65536 at 8 splits (a workgroup a unit, 64 units): tiles in registers, V as bf16
 // through LDS, 32 keys at a time 130 and 81; two tiles in LDS 117, 77; 64 keys at a time, no bank conflicts 116, 61 (now bound by
 // LDS: 16 KB of V written at 64 bytes a cycle, and every read costs 6); scales with P instead 115, 50; scales out of their bytes by one
@@ -400,12 +400,15 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
             tmax = rows_max(tmax);
             const float m_new = fmaxf(m_run, tmax);
             const float alpha = fast_exp2(m_run - (m_new == kNegInf ? 0.f : m_new));
+            const bool any = __any(m_run > kNegInf);  // (nothing to move in front of the first tile)
             m_run = m_new;
-            dsum1 *= alpha, dsum2 *= alpha;
+            if (any) {
+                dsum1 *= alpha, dsum2 *= alpha;
 #pragma unroll
-            for (int i = 0; i < NDB; ++i) {
-                o1[i] *= alpha;
-                if constexpr (USE_R) o2[i] *= alpha;
+                for (int i = 0; i < NDB; ++i) {
+                    o1[i] *= alpha;
+                    if constexpr (USE_R) o2[i] *= alpha;
+                }
             }
         }
         float tilt = 0.f;  // of this lane's keys
@@ -415,30 +418,37 @@ __global__ __launch_bounds__(256, 2) void decode_q4_kernel(DecodeRowsParams P) {
         }
         const float up_m = m_run == kNegInf ? 0.f : kWeightUp - m_run;
         auto weight = [&](int e) { return fast_exp2(fmaf(s1[e >> 2][e & 3], factor, up_m)); };
-        if (__builtin_expect(whole && !counted, 0)) {  // (once) the largest scale of the wave's first whole tile's last key, and 2^2 of room
+        // This lane's scales counted from zero - 8: 0 .. 8 if they are within reach (lower ones wrap round)
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 own[8];
+        auto far_scales = [&]() {
+            u16x2 widest = {0, 0};
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                const uint32_t bytes = __builtin_amdgcn_perm(0u, scales[n >> 2][(n >> 1) & 1], n & 1 ? 0x0c030c02u : 0x0c010c00u);
+                const uint16_t lowest = (uint16_t)(zero - kScaleRange);
+                own[n] = __builtin_bit_cast(u16x2, bytes) - u16x2{lowest, lowest};
+                widest = __builtin_elementwise_max(widest, own[n]);
+            }
+            const bool far = max(widest[0], widest[1]) > kScaleRange;
+            return D == 64 ? far && (c & 4) : far;  // (the others have the scales of K)
+        };
+        bool wild = far_scales();
+        if (__builtin_expect(whole && !counted && __any(wild), 0)) {  // (once) the largest scale of the tile's last key, and 2^2 of room
             int top = D == 128 || (c & 4) ? (int)(scales[1][1] >> 24) : 0;
             top = (int)row_max((uint32_t)top);
             top = __builtin_amdgcn_readlane(top, 48);
             recount(min(max(top + 2, 64), 190)), counted = true;
+            wild = far_scales();
         }
-        // This lane's scales counted from zero - 8: 0 .. 8 if they are within reach (lower ones wrap round)
-        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-        u16x2 own[8], widest = {0, 0};
-#pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            const uint32_t bytes = __builtin_amdgcn_perm(0u, scales[n >> 2][(n >> 1) & 1], n & 1 ? 0x0c030c02u : 0x0c010c00u);
-            const uint16_t lowest = (uint16_t)(zero - kScaleRange);
-            own[n] = __builtin_bit_cast(u16x2, bytes) - u16x2{lowest, lowest};
-            widest = __builtin_elementwise_max(widest, own[n]);
-        }
-        bool wild = max(widest[0], widest[1]) > kScaleRange;
-        if constexpr (D == 64) wild = wild && (c & 4);  // (the others have the scales of K)
         if (__builtin_expect(__any(tmax < m_run - kWeightFloor), 0)) {
-            wild |= rows_max(tmax) < m_run - kWeightFloor;  // (of the tile)
+            const float most = rows_max(tmax);  // (of the tile; -infinity: nothing to lose)
+            wild |= most < m_run - kWeightFloor && most > kNegInf;
         }
         if constexpr (USE_R) wild |= tilt * fast_exp2(tmax - m_run + kWeightUp) > 1 << kProbeMost;
 
-        if (__builtin_expect(whole && !__any(wild), 1)) {
+        // (a key that a column does not see has a weight of 0, and here a scale within reach)
+        if (__builtin_expect((whole || D == 64) && !__any(wild), 1)) {
             // P1 and P2 in f16, once (in bf16 they made the result's error 1.4 times that of its own rounding); d1 and d2 add the rounded
             // values, so that the weights still sum to one and what cancels between O1 d2 and O2 does so exactly.
             uint32_t w1[8], w2[8];

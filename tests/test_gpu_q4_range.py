@@ -4,7 +4,7 @@ large weight with values of zero, values near the ends of bf16's range.
 Weights are rounded to the 11 bits of f16 (off by at most 2^-11 of themselves) or cut to 16. Where they are f16 the largest of 64 neighbours
 is at least 2^-12 of the row's largest in all tiles that a sum here comes from. It counts 2^13 (P rho.k: 2^7) times that, times a scale of
 at least 2^-7, and products are multiples of 2^-24: off by at most 2^-12 of that largest weight times scale. Scores (sums of d products in fp32,
-magnitudes up to 40, errors of 2^-24 of that for each of a few steps) and the exponentials add less than 2^-15: 2^-11 + 2^-12 + 2^-15 < 2^-10.
+magnitudes up to 120, errors of 2^-24 of that for each of a few steps) and the exponentials add less than 2^-15: 2^-11 + 2^-12 + 2^-15 < 2^-10.
 """
 import numpy as np
 import pytest
@@ -93,6 +93,16 @@ def test_a_large_probe_product_of_no_weight(plx, d, Hq, Tq, power):  # noqa: F81
     k[0, 0, 3] = _against(q, d ** -0.5, -60.0)
     k[0, 0, 3, d // 2:] = r[0, 0, 0, d // 2:].float() * 2.0 ** power
     _compare(plx, q, r, k, v)
+
+
+@pytest.mark.parametrize("score", [-120.0, 120.0])
+@pytest.mark.parametrize("d,Hq,Tq", SHAPES)
+def test_scores_that_jump(plx, d, Hq, Tq, score):  # noqa: F811
+    """The first 320 keys' scores are 2^173 times smaller or larger than all that follow: nothing, or all, of the result is theirs."""
+    q, r, k, v = _inputs(d, Hq, Tq, 700)
+    k[0, 0, :320] = _against(q, d ** -0.5, score) + k[0, 0, :320] / 64
+    v[0, 0, :320] *= 4.0
+    _compare(plx, q, (r.float() / 16).to(torch.bfloat16), k, v)
 
 
 @pytest.mark.parametrize("power", [-98, 118, 122])
