@@ -451,7 +451,8 @@ plx_status parallax_select_blocks(const plx_select_blocks_args *args, void *hip_
  * a row sees of its keys those in listed blocks only. bf16, (Hq / Hkv) * Tq <= 16, no window, prep all zero (PLX_ERR_SHAPE).
  *   block_list  [B, Hkv, n_list] int32 on the device, ascending. An entry that is no block of the sequence (-1), or not above the one in
  *               front of it, is passed over. (So repeated entries count once; out of order a block may count more often.)
- * What lies in other blocks reaches no output. *_call_splits: as parallax_decode_call_splits.
+ * What lies in other blocks reaches no output. (Weights are multiplied in two parts: an infinite value that is seen may come out as NaN.)
+ * *_call_splits: as parallax_decode_call_splits.
  */
 typedef struct {
     plx_decode_args decode;

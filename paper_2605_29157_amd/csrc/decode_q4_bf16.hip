@@ -27,7 +27,7 @@
 // products rho.k of other sizes beside each other, rows with a few heavy keys, NaN; at d = 128 also the ends of a sequence or window) takes its P in
 // two bf16, with scales of any size. O1 and O2 count in the same unit either way, so the two kinds of tile mix.
 // us, 16 x 32768 keys, 8 key heads, d = 128, at the best split, for 2, 4, 8, 16 columns: all tiles in f16 with references that followed the largest scale
-// (and lost smaller ones) 116, 118, 119, 125; now 117, 118, 121, 131; all tiles in two bf16, as they are where scores have a standard deviation
+// (and lost smaller ones) 116, 117, 120, 124; now 117, 119, 122, 131; all tiles in two bf16, as they are where scores have a standard deviation
 // of 12, 142, 164, 195, 255. Ends of sequences in f16, too: d = 64, window 4096, 4 rows 22.6 us, so 21.4; at d = 128 100 x <= 500 keys 25.4 and
 // 23.5, but the compiler then spills registers of the second way, and 16 x 64 listed blocks take 26.5 instead of 25.0.
 // Steps before that, us for 16 x 32768 keys, 8 key heads, d = 128, and for 1 x 65536 at 8 splits (a workgroup a unit, 64 units): tiles in registers, V as bf16
