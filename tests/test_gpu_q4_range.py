@@ -49,13 +49,13 @@ def _against(q, scale, score):
     return score / scale * x / (x * x).sum()
 
 
-@pytest.mark.parametrize("power", [14, 17, 30, 50])
-@pytest.mark.parametrize("place", ["first", "middle", "last"])
+@pytest.mark.parametrize("power", [14, 17, 30, 50, 100])
+@pytest.mark.parametrize("place", ["first", "64th", "middle", "last"])
 @pytest.mark.parametrize("d,Hq,Tq", SHAPES)
 def test_a_large_value_of_no_weight(plx, d, Hq, Tq, place, power):  # noqa: F811
     """One key's values are 2^power larger than the others', its score 60 below theirs (a weight of 2^-86)."""
     L = 1500
-    at = {"first": 0, "middle": L // 2, "last": L - Tq}[place]
+    at = {"first": 0, "64th": 63, "middle": L // 2, "last": L - Tq}[place]
     q, r, k, v = _inputs(d, Hq, Tq, L)
     k[0, 0, at] = _against(q, d ** -0.5, -60.0)
     v[0, 0, at] *= 2.0 ** power
@@ -105,7 +105,7 @@ def test_scores_that_jump(plx, d, Hq, Tq, score):  # noqa: F811
     _compare(plx, q, (r.float() / 16).to(torch.bfloat16), k, v)
 
 
-@pytest.mark.parametrize("power", [-98, 118, 122])
+@pytest.mark.parametrize("power", [-98, 118, 122, 124])
 @pytest.mark.parametrize("d,Hq,Tq", SHAPES)
 def test_values_near_the_ends_of_the_range(plx, d, Hq, Tq, power):  # noqa: F811
     q, r, k, v = _inputs(d, Hq, Tq, 130)
